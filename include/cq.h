@@ -275,6 +275,92 @@ int cq_stage_fault(unsigned int* fault_host);
  * are the same.  Pass NULL, NULL to switch it off (the default).  Setting and reading the pair is thread-safe. */
 int cq_set_timing_events(void* before_quantize_pass, void* after_quantize_pass);
 
+/* ------------------------------------------------------------------------------------------------
+ * Serving a quantized model: a linear layer on 8-bit floats, and a quantized key/value cache with the
+ * attention that reads it.  (The paper stops at quantized operands; these consume them.)
+ * ------------------------------------------------------------------------------------------------
+ *
+ * Block quantization to e4m3 (the 8-bit float with 4 exponent and 3 fraction bits, largest value 448):
+ *     s = fl32(max |x| / 448) over a block,  code = e4m3(fl32(x / s)), nearest even;  s == 0 -> code 0.
+ * A block of activations is 128 consecutive elements of a row, a block of weights 128 x 128; the last
+ * ones may be smaller.  A block with an infinity or NaN gets a scale that is one: what is computed from it is NaN.
+ *   X, W      device [T x ld] / [N x ld] 16-bit, any 2-byte alignment (16-byte aligned with K and ld multiples of 8: fast)
+ *   codes     out device uint8 [T x ldc] / [N x ldc], ldc >= K; bytes beyond column K are not written
+ *   scale     out activations: device float, block b of row i at scale[b * lds + i], lds >= T;
+ *             weights: dense device float [ceil(N / 128)][ceil(K / 128)]
+ */
+int cq_fp8_quantize_act(const void* X, int dtype, int64_t T, int64_t K, int64_t ld, void* codes, int64_t ldc,
+                        float* scale, int64_t lds, void* stream);
+int cq_fp8_quantize_weight(const void* W, int dtype, int64_t N, int64_t K, int64_t ld, void* codes, int64_t ldc,
+                           float* scale, void* stream);
+
+/*
+ * out[m, n] = sum over blocks b of  a_scale[b, m] * w_scale[n / 128, b] * sum_{k in b} A[m, k] W[n, k]
+ * of operands as written above (W is stored [output channels x input channels]); fp32 sums, rounded once.
+ *   A [M x lda], W [N x ldw]  device codes, 16-byte aligned, lda and ldw multiples of 16 (bytes beyond K are not used)
+ *   a_scale                   16-byte aligned, lds a multiple of 4, >= M
+ *   out                       device [M x ldo] of out_dtype (CQ_F16, CQ_BF16, CQ_F32); ldo >= N
+ * K == 0 writes zeros.  CQ_ERR_ALIGN for operands that are not laid out so.
+ */
+int cq_fp8_matmul(const void* A, int64_t lda, const float* a_scale, int64_t lds, const void* W, int64_t ldw,
+                  const float* w_scale, int64_t M, int64_t N, int64_t K, void* out, int out_dtype, int64_t ldo, void* stream);
+
+/* cq_fp8_quantize_act of X [M x ldx] followed by cq_fp8_matmul, the codes kept in the workspace
+ * (256-byte aligned, >= cq_fp8_linear_workspace_bytes(M, K); contents undefined after). */
+size_t cq_fp8_linear_workspace_bytes(int64_t M, int64_t K);
+int cq_fp8_linear(const void* X, int dtype, int64_t M, int64_t K, int64_t ldx, const void* W, int64_t ldw, const float* w_scale,
+                  int64_t N, void* out, int out_dtype, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The key/value cache.  Keys and values each:
+ *   codes  device int8 [pages][H][page_size][D] (bits = 8) or uint8 [pages][H][page_size][D / 2] (bits = 4, nibbles as in
+ *          cq_quantize_act), 16-byte aligned
+ *   scale  device float [pages][H][page_size], 16-byte aligned
+ *   col    device float [H][D], 16-byte aligned: channel factors b shared by all tokens (the column factors of the
+ *          CrossQuant scale, c_j^(1 - alpha) of a calibration run); null for keys and values both: ones
+ * An element stands for code * fl32(scale * b).  D is 64 or 128, page_size a multiple of 16 up to 4096,
+ * pages * H * page_size < 2^31 - 4096.  Token slot n lies in page n / page_size at offset n % page_size.
+ *
+ * cq_kv_write quantizes T tokens (K, V: 16-bit, element (t, h, d) at t * token_stride + h * head_stride + d) into their slots:
+ *   u = fl32(x * fl32(1 / b)), scale = fl32(max_d |u| / qmax), code = round-half-even(fl32(u / scale)); a head whose u are all 0,
+ *   and a channel whose factor is not above 0, gets codes 0.  A head with an infinity or NaN gets such a scale and codes 0.
+ *   Slots below 0 or beyond the cache are skipped.  Two tokens with one slot leave one of them there, or a mixture.
+ * cq_kv_read writes what L slots stand for to k_out, v_out (dense [L][H][D], 16-byte aligned, CQ_F16, CQ_BF16 or CQ_F32);
+ *   slots below 0 or beyond the cache read as zeros.
+ * slots: device int64.
+ */
+int cq_kv_write(const void* K, int64_t k_token_stride, int64_t k_head_stride, const void* V, int64_t v_token_stride,
+                int64_t v_head_stride, int dtype, int64_t T, const int64_t* slots, void* k_codes, void* v_codes,
+                float* k_scale, float* v_scale, const float* k_col, const float* v_col, int bits, int64_t pages,
+                int64_t page_size, int64_t H, int64_t D, void* stream);
+int cq_kv_read(const void* k_codes, const void* v_codes, const float* k_scale, const float* v_scale, const float* k_col,
+               const float* v_col, int bits, int64_t pages, int64_t page_size, int64_t H, int64_t D, int64_t L,
+               const int64_t* slots, void* k_out, void* v_out, int out_dtype, void* stream);
+
+/*
+ * Attention over the cache: for sequence b with n = lens[b] tokens, whose token j lies in page
+ * page_table[b * table_stride + j / page_size], query token i of Lq (the sequence's last Lq tokens) sees the
+ * tokens j <= n - Lq + i; query heads h * Hq / H .. share key/value head h:
+ *   out[b, i, h'] = softmax_j(softmax_scale * q . k_j) v_j
+ *   Q     16-bit, element (b, i, h', d) at b * q_batch_stride + i * q_token_stride + h' * q_head_stride + d
+ *   out   dense [B][Lq][Hq][D] of Q's dtype;  lse  float [B][Lq][Hq], the logarithm of the softmax's sum; nullable
+ * A query that sees no token gets zeros (lse: -infinity).  Tokens of a page number outside the cache are not
+ * seen; lens beyond table_width * page_size are cut to it, below 0 they count as 0.  Whatever lies in slots behind a
+ * sequence's end has no effect.  softmax_scale lies above 0 (CQ_ERR_ALPHA otherwise).  The result does not depend on what other
+ * sequences hold, but its last bits may depend on all lengths (they set where the work is cut); equal calls give equal bits.
+ * workspace: device, 256-byte aligned, >= cq_kv_attention_workspace_bytes(D); contents undefined after.
+ */
+size_t cq_kv_attention_workspace_bytes(int64_t D);
+int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_token_stride, int64_t q_head_stride, int64_t B,
+                    int64_t Lq, int64_t Hq, const void* k_codes, const void* v_codes, const float* k_scale, const float* v_scale,
+                    const float* k_col, const float* v_col, int bits, int64_t pages, int64_t page_size, int64_t H, int64_t D,
+                    const int* page_table, int64_t table_width, int64_t table_stride, const int* lens, double softmax_scale,
+                    void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Health check of the product and the attention, as cq_stage_fault is of the quantizers: 1 if a bounded wait in one of their
+ * kernels ever gave up on the current device.  Synchronises the device. */
+int cq_serve_fault(unsigned int* fault_host);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -25,7 +26,10 @@ EXPORTS = (
     "cq_set_tuning", "cq_set_timing_events", "cq_quantize_act_noalloc",
     "cq_quantize_weight_groupwise", "cq_case_indicators", "cq_remove_kernel", "cq_stage_fault",
     "cq_vector_max", "cq_quantize_act_given",
+    "cq_fp8_quantize_act", "cq_fp8_quantize_weight", "cq_fp8_matmul", "cq_fp8_linear_workspace_bytes", "cq_fp8_linear",
+    "cq_kv_write", "cq_kv_read", "cq_kv_attention_workspace_bytes", "cq_kv_attention", "cq_serve_fault",
 )
+_SIZES = ("cq_workspace_bytes", "cq_host_scratch_bytes", "cq_fp8_linear_workspace_bytes", "cq_kv_attention_workspace_bytes")
 
 
 class CQError(RuntimeError):
@@ -72,10 +76,24 @@ def lib() -> C.CDLL:
         L.cq_case_indicators.argtypes = [vp, vp, vp, vp, i64, i64, ci, vp, vp]
         L.cq_remove_kernel.argtypes = [vp, ci, i64, i64, i64, dbl, ci, C.c_float, vp, vp, vp, C.c_size_t, vp]
         L.cq_stage_fault.argtypes = [vp]
+        sz = C.c_size_t
+        L.cq_fp8_quantize_act.argtypes = [vp, ci, i64, i64, i64, vp, i64, vp, i64, vp]
+        L.cq_fp8_quantize_weight.argtypes = [vp, ci, i64, i64, i64, vp, i64, vp, vp]
+        L.cq_fp8_matmul.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, vp, ci, i64, vp]
+        L.cq_fp8_linear_workspace_bytes.restype = sz
+        L.cq_fp8_linear_workspace_bytes.argtypes = [i64, i64]
+        L.cq_fp8_linear.argtypes = [vp, ci, i64, i64, i64, vp, i64, vp, i64, vp, ci, i64, vp, sz, vp]
+        L.cq_kv_write.argtypes = [vp, i64, i64, vp, i64, i64, ci, i64, vp, vp, vp, vp, vp, vp, vp, ci, i64, i64, i64, i64, vp]
+        L.cq_kv_read.argtypes = [vp, vp, vp, vp, vp, vp, ci, i64, i64, i64, i64, i64, vp, vp, vp, ci, vp]
+        L.cq_kv_attention_workspace_bytes.restype = sz
+        L.cq_kv_attention_workspace_bytes.argtypes = [i64]
+        L.cq_kv_attention.argtypes = [vp, ci, i64, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, ci, i64, i64, i64, i64,
+                                      vp, i64, i64, vp, dbl, vp, vp, vp, sz, vp]
+        L.cq_serve_fault.argtypes = [vp]
         L.cq_set_tuning.argtypes = [C.c_char_p, ci]
         L.cq_set_timing_events.argtypes = [vp, vp]
         for name in EXPORTS:
-            if name not in ("cq_status_string", "cq_workspace_bytes", "cq_host_scratch_bytes"):
+            if name != "cq_status_string" and name not in _SIZES:
                 getattr(L, name).restype = ci
         _lib = L
     return _lib
@@ -496,4 +514,271 @@ def stage_fault() -> int:
     """1 if a bounded wait on a staged row copy ever gave up on the current device, else 0."""
     flag = C.c_uint(0)
     _check(lib().cq_stage_fault(C.byref(flag)), "cq_stage_fault")
+    return int(flag.value)
+
+
+# ----------------------------------------------------------------------------- 8-bit float linear layer
+BLOCK = 128                   # elements under one scale: along a row of activations, along both axes of a weight
+
+
+class Fp8Act(NamedTuple):
+    """Block-quantized activations: e4m3 codes [T, K] (row pitch a multiple of 16) and their scales [ceil(K / 128), T]
+    (row pitch a multiple of 4)."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+
+
+class Fp8Weight(NamedTuple):
+    """Block-quantized weights [out channels, in channels]: e4m3 codes [N, K] (row pitch a multiple of 16) and one scale for
+    each 128 x 128 block [ceil(N / 128), ceil(K / 128)]."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+
+
+def _up(v: int, m: int) -> int:
+    return -(-v // m) * m
+
+
+def _addr(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _raw() -> int:
+    return _raw_stream(torch.cuda.current_device()) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _fp8_codes(rows: int, K: int, device) -> torch.Tensor:
+    return torch.empty((rows, _up(K, 16)), dtype=torch.float8_e4m3fn, device=device)[:, :K]
+
+
+def _pitch(x: torch.Tensor, what: str) -> int:
+    """Row pitch of a 2-D tensor with contiguous columns."""
+    rows, cols = x.shape
+    if rows > 0 and cols > 1 and x.stride(1) != 1:
+        raise ValueError(f"{what}: columns must be contiguous")
+    return x.stride(0) if rows > 1 else max(x.stride(0), _up(cols, 16))
+
+
+def _check_fp8(pair, rows: int | None, K: int, scale_shape, device, what: str) -> None:
+    codes, scale = pair
+    if codes.dim() != 2 or codes.dtype != torch.float8_e4m3fn or codes.device != device or codes.shape[1] != K or \
+            (rows is not None and codes.shape[0] != rows):
+        raise ValueError(f"{what}.codes must be float8_e4m3fn [{'rows' if rows is None else rows}, {K}] on {device}")
+    if scale.dtype != torch.float32 or tuple(scale.shape) != tuple(scale_shape) or scale.device != device:
+        raise ValueError(f"{what}.scale must be float32 {tuple(scale_shape)} on {device}")
+
+
+def fp8_quantize_act(X: torch.Tensor, *, out: Fp8Act | None = None) -> Fp8Act:
+    """e4m3 codes of activations [T, K], one scale for each run of 128 elements of a row."""
+    T, K, ld = _matrix_args(X)
+    nb = -(-K // BLOCK)
+    if out is None:
+        out = Fp8Act(_fp8_codes(T, K, X.device), torch.empty((nb, _up(T, 4)), dtype=torch.float32, device=X.device)[:, :T])
+    else:
+        _check_fp8(out, T, K, (nb, T), X.device, "out")
+    _check(lib().cq_fp8_quantize_act(_addr(X), _DT[X.dtype], T, K, ld, _addr(out.codes), _pitch(out.codes, "out.codes"), _addr(out.scale),
+                                     _scale_pitch(out.scale), _raw()), "cq_fp8_quantize_act")
+    return out
+
+
+def _scale_pitch(scale: torch.Tensor) -> int:
+    nb, T = scale.shape
+    if nb > 0 and T > 1 and scale.stride(1) != 1:
+        raise ValueError("scales of a block must be contiguous along the rows")
+    return scale.stride(0) if nb > 1 else max(scale.stride(0), _up(T, 4))
+
+
+def fp8_quantize_weight(W: torch.Tensor, *, out: Fp8Weight | None = None) -> Fp8Weight:
+    """e4m3 codes of a weight matrix [out channels, in channels], one scale for each block of 128 x 128."""
+    N, K, ld = _matrix_args(W)
+    shape = (-(-N // BLOCK), -(-K // BLOCK))
+    if out is None:
+        out = Fp8Weight(_fp8_codes(N, K, W.device), torch.empty(shape, dtype=torch.float32, device=W.device))
+    else:
+        _check_fp8(out, N, K, shape, W.device, "out")
+        if not out.scale.is_contiguous():
+            raise ValueError("out.scale must be contiguous")
+    _check(lib().cq_fp8_quantize_weight(_addr(W), _DT[W.dtype], N, K, ld, _addr(out.codes), _pitch(out.codes, "out.codes"), _addr(out.scale),
+                                        _raw()), "cq_fp8_quantize_weight")
+    return out
+
+
+def _product_out(out, M: int, N: int, dtype, device):
+    if out is None:
+        return torch.empty((M, N), dtype=dtype, device=device)
+    if tuple(out.shape) != (M, N) or out.dtype != dtype or out.device != device or (M > 0 and N > 1 and out.stride(1) != 1):
+        raise ValueError(f"out must be a [{M}, {N}] tensor of {dtype} on {device} with contiguous columns")
+    return out
+
+
+def _out_pitch(out: torch.Tensor) -> int:
+    return out.stride(0) if out.shape[0] > 1 else max(out.shape[1], 1)
+
+
+def fp8_matmul(a: Fp8Act, w: Fp8Weight, out_dtype: torch.dtype = torch.bfloat16, *, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The product [T, N] of block-quantized activations and weights (fp32 sums, rounded once to out_dtype)."""
+    T, K = a.codes.shape
+    N, nb = w.codes.shape[0], -(-K // BLOCK)
+    dev = a.codes.device
+    if not a.codes.is_cuda or out_dtype not in _DT:
+        raise TypeError("expected CUDA tensors and a float16, bfloat16 or float32 result")
+    _check_fp8(a, T, K, (nb, T), dev, "a")
+    _check_fp8(w, N, K, (-(-N // BLOCK), nb), dev, "w")
+    if not w.scale.is_contiguous():
+        raise ValueError("w.scale must be contiguous")
+    out = _product_out(out, T, N, out_dtype, dev)
+    _check(lib().cq_fp8_matmul(_addr(a.codes), _pitch(a.codes, "a.codes"), _addr(a.scale), _scale_pitch(a.scale), _addr(w.codes),
+                               _pitch(w.codes, "w.codes"), _addr(w.scale), T, N, K, _addr(out), _DT[out_dtype], _out_pitch(out), _raw()),
+           "cq_fp8_matmul")
+    return out
+
+
+def fp8_linear(X: torch.Tensor, w: Fp8Weight, out_dtype: torch.dtype | None = None, *, out: torch.Tensor | None = None,
+               workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """X [T, K] through a block-quantized weight: fp8_quantize_act and fp8_matmul in one call."""
+    T, K, ld = _matrix_args(X)
+    codes, scale = w
+    N = codes.shape[0]
+    dt = out_dtype or X.dtype
+    if dt not in _DT:
+        raise TypeError("expected a float16, bfloat16 or float32 result")
+    _check_fp8(w, N, K, (-(-N // BLOCK), -(-K // BLOCK)), X.device, "w")
+    if not scale.is_contiguous():
+        raise ValueError("w.scale must be contiguous")
+    out = _product_out(out, T, N, dt, X.device)
+    L = lib()
+    if workspace is None:
+        workspace = torch.empty(L.cq_fp8_linear_workspace_bytes(T, K), dtype=torch.uint8, device=X.device)
+    _check(L.cq_fp8_linear(X.data_ptr(), _DT[X.dtype], T, K, ld, codes.data_ptr(), _pitch(codes, "w.codes"), scale.data_ptr(), N,
+                           out.data_ptr(), _DT[dt], _out_pitch(out), workspace.data_ptr(), workspace.numel(), _raw()), "cq_fp8_linear")
+    return out
+
+
+# ----------------------------------------------------------------------------- key/value cache
+class KVCache:
+    """A paged cache of quantized keys and values (layout in include/cq.h); checks its tensors once, when it is made.
+
+    k_codes, v_codes   int8 [pages, H, page_size, D] (bits = 8) or uint8 [pages, H, page_size, D / 2] (bits = 4)
+    k_scale, v_scale   float32 [pages, H, page_size]
+    k_col, v_col       float32 [H, D] channel factors, both or neither
+    """
+    __slots__ = ("k_codes", "v_codes", "k_scale", "v_scale", "bits", "k_col", "v_col", "pages", "page_size", "heads", "head_dim",
+                 "device", "_args")
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, bits: int = 8, k_col=None, v_col=None):
+        if bits not in (4, 8):
+            raise CQError(4, "KVCache")
+        if k_codes.dim() != 4:
+            raise ValueError("codes must be [pages, heads, page_size, head_dim]")
+        pages, H, page, width = k_codes.shape
+        D = width if bits == 8 else 2 * width
+        dev = k_codes.device
+        want = torch.int8 if bits == 8 else torch.uint8
+        for t in (k_codes, v_codes):
+            if t.shape != k_codes.shape or t.dtype != want or t.device != dev or not t.is_contiguous():
+                raise ValueError(f"codes of keys and values must be contiguous {want} tensors of one shape on one device")
+        for t in (k_scale, v_scale):
+            if t.shape != (pages, H, page) or t.dtype != torch.float32 or t.device != dev or not t.is_contiguous():
+                raise ValueError(f"scales must be contiguous float32 [{pages}, {H}, {page}] on {dev}")
+        if (k_col is None) != (v_col is None):
+            raise ValueError("channel factors are given for keys and values or for neither")
+        if k_col is not None:
+            for t in (k_col, v_col):
+                if t.shape != (H, D) or t.dtype != torch.float32 or t.device != dev or not t.is_contiguous():
+                    raise ValueError(f"channel factors must be contiguous float32 [{H}, {D}] on {dev}")
+        if not k_codes.is_cuda:
+            raise TypeError("expected CUDA tensors")
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.bits = k_codes, v_codes, k_scale, v_scale, bits
+        self.k_col, self.v_col, self.device = k_col, v_col, dev
+        self.pages, self.heads, self.page_size, self.head_dim = pages, H, page, D
+        self._args = (k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _addr(k_col), _addr(v_col),
+                      bits, pages, page, H, D)
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, heads: int, head_dim: int, bits: int = 8, *, k_col=None, v_col=None, device="cuda"):
+        """A cache of zeros."""
+        if bits not in (4, 8):
+            raise CQError(4, "KVCache.empty")
+        width, dt = (head_dim, torch.int8) if bits == 8 else (head_dim // 2, torch.uint8)
+        codes = [torch.zeros((pages, heads, page_size, width), dtype=dt, device=device) for _ in range(2)]
+        scale = [torch.zeros((pages, heads, page_size), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(*codes, *scale, bits, k_col, v_col)
+
+
+def _slots(slots: torch.Tensor, device) -> int:
+    if slots.dim() != 1 or slots.dtype != torch.int64 or slots.device != device or not slots.is_contiguous():
+        raise ValueError(f"slots must be a contiguous int64 vector on {device}")
+    return slots.numel()
+
+
+def kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """Quantize keys and values [T, H, D] (float16 / bfloat16; any strides of tokens and heads) into their slots of the cache."""
+    T = _slots(slots, cache.device)
+    shape = (T, cache.heads, cache.head_dim)
+    for t in (k, v):
+        if t.shape != shape or t.dtype != k.dtype or t.dtype not in (torch.float16, torch.bfloat16) or t.device != cache.device:
+            raise ValueError(f"keys and values must be float16 / bfloat16 {shape} on {cache.device}")
+        if T > 0 and t.stride(2) != 1:
+            raise ValueError("head elements must be contiguous")
+    _check(lib().cq_kv_write(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), _DT[k.dtype], T,
+                             slots.data_ptr(), *cache._args, _raw()), "cq_kv_write")
+
+
+def kv_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, *, out=None):
+    """(keys, values) [L, H, D] that the slots stand for; `out` = a pair of tensors to fill."""
+    n = _slots(slots, cache.device)
+    shape = (n, cache.heads, cache.head_dim)
+    if dtype not in _DT:
+        raise TypeError("expected a float16, bfloat16 or float32 result")
+    if out is None:
+        out = (torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device))
+    for t in out:
+        if t.shape != shape or t.dtype != dtype or t.device != cache.device or not t.is_contiguous():
+            raise ValueError(f"out must be two contiguous {dtype} tensors {shape} on {cache.device}")
+    _check(lib().cq_kv_read(*cache._args, n, slots.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), _DT[dtype], _raw()), "cq_kv_read")
+    return out
+
+
+def kv_attention_workspace_bytes(head_dim: int) -> int:
+    return int(lib().cq_kv_attention_workspace_bytes(head_dim))
+
+
+def kv_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, lens: torch.Tensor, *, scale: float | None = None,
+                 out: torch.Tensor | None = None, lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of the last Lq tokens of each sequence, q [B, Lq, Hq, D], over the cache.
+
+    page_table int32 [B, pages], lens int32 [B] (tokens of each sequence, those of q included).  `scale` multiplies the
+    logits (default 1 / sqrt(D)); `lse` float32 [B, Lq, Hq] receives the logarithm of the softmax's sum."""
+    dev, D = cache.device, cache.head_dim
+    if q.dim() != 4 or q.dtype not in (torch.float16, torch.bfloat16) or q.device != dev or q.shape[3] != D:
+        raise ValueError(f"q must be float16 / bfloat16 [B, Lq, Hq, {D}] on {dev}")
+    B, Lq, Hq, _ = q.shape
+    if q.numel() > 0 and q.stride(3) != 1:
+        raise ValueError("head elements must be contiguous")
+    if page_table.dim() != 2 or page_table.shape[0] != B or page_table.dtype != torch.int32 or page_table.device != dev or \
+            (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError(f"page_table must be int32 [{B}, pages] on {dev} with contiguous rows")
+    if lens.dim() != 1 or lens.shape[0] != B or lens.dtype != torch.int32 or lens.device != dev or not lens.is_contiguous():
+        raise ValueError(f"lens must be a contiguous int32 vector of {B} on {dev}")
+    if out is None:
+        out = torch.empty((B, Lq, Hq, D), dtype=q.dtype, device=dev)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape and dtype")
+    if lse is not None and (lse.shape != q.shape[:3] or lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous float32 [B, Lq, Hq] tensor")
+    L = lib()
+    if workspace is None:
+        workspace = torch.empty(L.cq_kv_attention_workspace_bytes(D), dtype=torch.uint8, device=dev)
+    width = page_table.shape[1]
+    _check(L.cq_kv_attention(q.data_ptr(), _DT[q.dtype], q.stride(0), q.stride(1), q.stride(2), B, Lq, Hq, *cache._args,
+                             page_table.data_ptr(), width, page_table.stride(0) if B > 1 else width, lens.data_ptr(),
+                             D ** -0.5 if scale is None else float(scale), out.data_ptr(), _addr(lse), workspace.data_ptr(),
+                             workspace.numel(), _raw()), "cq_kv_attention")
+    return out
+
+
+def serve_fault() -> int:
+    """1 if a bounded wait of fp8_matmul, fp8_linear or kv_attention ever gave up on the current device, else 0."""
+    flag = C.c_uint(0)
+    _check(lib().cq_serve_fault(C.byref(flag)), "cq_serve_fault")
     return int(flag.value)

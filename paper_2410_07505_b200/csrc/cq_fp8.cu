@@ -1,0 +1,238 @@
+// Block quantization to 8-bit floats (e4m3): activations with one scale for each run of 128 elements of a row,
+// weights with one scale for each 128 x 128 block.
+//
+//   s = fl32(max |x| / 448),  code = e4m3(fl32(x / s)),  s == 0 -> code 0
+//
+// 448 is e4m3's largest value.  448 = 7 * 2^6, so s has the mantissa of the INT4 scales fl32(max / 7), and the
+// division-free exact quotient that the integer weight quantizers use for 16-bit elements holds here as it stands.
+// A block with an infinity or NaN gets a scale that is one (the maximum is taken over the bit patterns, where NaN is
+// largest), so that everything computed from the block is NaN rather than a wrong number.
+//
+// Both are bound by HBM: 2 bytes read and 1 byte written for an element, the block's maximum found in registers.
+#include "cq_serve.cuh"
+
+namespace cq {
+
+constexpr float kE4m3Max = 448.0f;
+constexpr int kBlk = 128;
+
+__device__ __forceinline__ uint32_t absmax8(const uint4& w) {
+    const uint32_t m = max_u16x2(max_u16x2(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu), max_u16x2(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu));
+    return max(m & 0xFFFFu, m >> 16);
+}
+
+__device__ __forceinline__ float e4m3_quotient_slow(float x, float s) {
+    if (s == 0.0f) return 0.0f;
+    const float u = __fdiv_rn(x, s);
+    return u > kE4m3Max ? kE4m3Max : (u < -kE4m3Max ? -kE4m3Max : u);      // NaN stays NaN
+}
+
+// Eight elements under one scale -> eight codes.  rs = guarded_rcp(s): NaN where the short form does not hold.
+template <int DT>
+__device__ __forceinline__ uint2 e4m3_row8(const uint4& w, float s, float rs) {
+    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+    uint32_t h[4];
+    if (rs == rs) {
+        const float2 rs2 = make_float2(rs, rs), ns2 = make_float2(-s, -s);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 x = unpack16x2<DT>(words[k]);
+            const float2 q0 = __fmul2_rn(x, rs2);
+            const float2 u = __ffma2_rn(__ffma2_rn(q0, ns2, x), rs2, q0);
+            h[k] = pack_e4m3x2(u.x, u.y);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 x = unpack16x2<DT>(words[k]);
+            h[k] = pack_e4m3x2(e4m3_quotient_slow(x.x, s), e4m3_quotient_slow(x.y, s));
+        }
+    }
+    return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+}
+
+// ---- activations --------------------------------------------------------------------------------
+// A warp takes one row x 1024 columns (four 16-byte loads a lane, all issued first; 16 lanes hold a block), a CTA
+// eight consecutive rows, whose scales leave as whole 32-byte sectors of the block-major scale matrix.
+constexpr int kActVec = 4;
+constexpr int kActRows = 8;
+constexpr int kActCols = 256 * kActVec;
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads)
+k10_fp8_act(const uint4* __restrict__ X, int64_t T, int K8, int64_t ld8, uint8_t* __restrict__ codes, int64_t ldc,
+            float* __restrict__ scale, int64_t lds, unsigned col_chunks) {
+    __shared__ float s_scale[2 * kActVec][kActRows];
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const unsigned chunk = blockIdx.x % col_chunks;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x / col_chunks) * kActRows;
+    const int64_t row = row0 + warp;
+    const int v0 = static_cast<int>(chunk) * (kActCols / 8) + lane;
+    uint4 w[kActVec];
+#pragma unroll
+    for (int k = 0; k < kActVec; ++k) {
+        const int v = v0 + 32 * k;
+        w[k] = make_uint4(0, 0, 0, 0);
+        if (row < T && v < K8) w[k] = ld_stream(X + row * ld8 + v);
+    }
+#pragma unroll
+    for (int k = 0; k < kActVec; ++k) {
+        uint32_t m = absmax8(w[k]);
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
+        const float s = __fdiv_rn(cvt16<DT>(static_cast<uint16_t>(m)), kE4m3Max);
+        const uint2 c = e4m3_row8<DT>(w[k], s, guarded_rcp(s));
+        const int v = v0 + 32 * k;
+        if (row < T && v < K8) *reinterpret_cast<uint2*>(codes + row * ldc + static_cast<int64_t>(v) * 8) = c;
+        if ((lane & 15) == 0) s_scale[2 * k + (lane >> 4)][warp] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2 * kActVec * kActRows) {
+        const int b = threadIdx.x / kActRows, r = threadIdx.x % kActRows;
+        const int64_t blk = static_cast<int64_t>(chunk) * (2 * kActVec) + b;
+        if (blk * (kBlk / 8) < K8 && row0 + r < T) scale[blk * lds + row0 + r] = s_scale[b][r];
+    }
+}
+
+// Any alignment, pitch and number of columns: a warp per row and block, 2-byte loads and 1-byte stores.
+template <int DT>
+__global__ void __launch_bounds__(kThreads)
+g10_fp8_act(const uint16_t* __restrict__ X, int64_t T, int64_t K, int64_t ld, uint8_t* __restrict__ codes, int64_t ldc,
+            float* __restrict__ scale, int64_t lds, int64_t nblk) {
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int lane = threadIdx.x & 31;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+    if (item >= T * nblk) return;                       // whole warps
+    const int64_t row = item / nblk, blk = item % nblk;
+    uint16_t x[4];
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t col = blk * kBlk + lane + 32 * k;
+        x[k] = col < K ? X[row * ld + col] : uint16_t(0);
+        m = max(m, static_cast<uint32_t>(x[k] & 0x7FFFu));
+    }
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
+    const float s = __fdiv_rn(cvt16<DT>(static_cast<uint16_t>(m)), kE4m3Max);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t col = blk * kBlk + lane + 32 * k;
+        if (col < K) codes[row * ldc + col] = static_cast<uint8_t>(pack_e4m3x2(e4m3_quotient_slow(cvt16<DT>(x[k]), s), 0.0f));
+    }
+    if (lane == 0) scale[blk * lds + row] = s;
+}
+
+// ---- weights --------------------------------------------------------------------------------------
+// One CTA per 128 x 128 block, held in registers between the maximum and the codes (eight 16-byte loads a thread).
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kThreads)
+k11_fp8_weight(const uint16_t* __restrict__ W, int64_t N, int64_t K, int64_t ld, uint8_t* __restrict__ codes, int64_t ldc,
+               float* __restrict__ scale, int64_t kblocks) {
+    __shared__ uint32_t s_max[kThreads / 32];
+    const int64_t nb = blockIdx.x / kblocks, kb = blockIdx.x % kblocks;
+    const int64_t col = kb * kBlk + (threadIdx.x & 15) * 8;
+    const int64_t row0 = nb * kBlk + (threadIdx.x >> 4);
+    uint4 w[8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t row = row0 + 16 * i;
+        w[i] = make_uint4(0, 0, 0, 0);
+        if constexpr (VEC) {
+            if (row < N && col < K) w[i] = ld_stream(reinterpret_cast<const uint4*>(W + row * ld + col));
+        } else {
+            uint32_t h[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] = (row < N && col + e < K) ? W[row * ld + col + e] : 0u;
+            w[i] = make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, absmax8(w[i]));
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
+    if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; ++i) m = max(m, s_max[i]);
+    const float s = __fdiv_rn(cvt16<DT>(static_cast<uint16_t>(m)), kE4m3Max);
+    const float rs = guarded_rcp(s);
+    if (threadIdx.x == 0) scale[nb * kblocks + kb] = s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t row = row0 + 16 * i;
+        if (row >= N || col >= K) continue;
+        const uint2 c = e4m3_row8<DT>(w[i], s, rs);
+        uint8_t* out = codes + row * ldc + col;
+        if constexpr (VEC) {
+            st_stream(reinterpret_cast<uint2*>(out), c);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < K) out[e] = static_cast<uint8_t>((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
+        }
+    }
+}
+
+static int check_codes(const void* codes, int64_t rows, int64_t K, int64_t ldc, const float* scale) {
+    if (ldc < K) return CQ_ERR_SHAPE;
+    if (rows > 0 && K > 0) {
+        if (codes == nullptr || scale == nullptr) return CQ_ERR_NULL;
+        if (!ptr_aligned(scale, 4)) return CQ_ERR_ALIGN;
+    }
+    return CQ_OK;
+}
+
+int fp8_quantize_act_impl(const void* X, int dtype, int64_t T, int64_t K, int64_t ld, void* codes, int64_t ldc,
+                          float* scale, int64_t lds, cudaStream_t st) {
+    int rc = check_matrix(X, dtype, T, K, ld);
+    if (rc == CQ_OK) rc = check_codes(codes, T, K, ldc, scale);
+    if (rc != CQ_OK) return rc;
+    if (lds < T) return CQ_ERR_SHAPE;
+    if (T == 0 || K == 0) return CQ_OK;
+    const bool fast = K % 8 == 0 && ld % 8 == 0 && ldc % 8 == 0 && ptr_aligned(X, 16) && ptr_aligned(codes, 8);
+    uint8_t* c = static_cast<uint8_t*>(codes);
+    if (fast) {
+        const int64_t chunks = (K + kActCols - 1) / kActCols;
+        const int64_t blocks = chunks * ((T + kActRows - 1) / kActRows);
+        if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
+        auto kern = dtype == CQ_F16 ? k10_fp8_act<CQ_F16> : k10_fp8_act<CQ_BF16>;
+        kern<<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(static_cast<const uint4*>(X), T, static_cast<int>(K / 8), ld / 8, c, ldc,
+                                                                 scale, lds, static_cast<unsigned>(chunks));
+    } else {
+        const int64_t nblk = (K + kBlk - 1) / kBlk;
+        const int64_t blocks = (T * nblk + kThreads / 32 - 1) / (kThreads / 32);
+        if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
+        auto kern = dtype == CQ_F16 ? g10_fp8_act<CQ_F16> : g10_fp8_act<CQ_BF16>;
+        kern<<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(static_cast<const uint16_t*>(X), T, K, ld, c, ldc, scale, lds, nblk);
+    }
+    return launch_status();
+}
+
+}  // namespace cq
+
+extern "C" {
+
+int cq_fp8_quantize_act(const void* X, int dtype, int64_t T, int64_t K, int64_t ld, void* codes, int64_t ldc,
+                        float* scale, int64_t lds, void* stream) {
+    return cq::fp8_quantize_act_impl(X, dtype, T, K, ld, codes, ldc, scale, lds, static_cast<cudaStream_t>(stream));
+}
+
+int cq_fp8_quantize_weight(const void* W, int dtype, int64_t N, int64_t K, int64_t ld, void* codes, int64_t ldc,
+                           float* scale, void* stream) {
+    using namespace cq;
+    int rc = check_matrix(W, dtype, N, K, ld);
+    if (rc == CQ_OK) rc = check_codes(codes, N, K, ldc, scale);
+    if (rc != CQ_OK) return rc;
+    if (N == 0 || K == 0) return CQ_OK;
+    const int64_t kblocks = (K + kBlk - 1) / kBlk, blocks = kblocks * ((N + kBlk - 1) / kBlk);
+    if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
+    const bool vec = K % 8 == 0 && ld % 8 == 0 && ldc % 8 == 0 && ptr_aligned(W, 16) && ptr_aligned(codes, 8);
+    auto kern = dtype == CQ_F16 ? (vec ? k11_fp8_weight<CQ_F16, true> : k11_fp8_weight<CQ_F16, false>)
+                                : (vec ? k11_fp8_weight<CQ_BF16, true> : k11_fp8_weight<CQ_BF16, false>);
+    kern<<<static_cast<unsigned>(blocks), kThreads, 0, static_cast<cudaStream_t>(stream)>>>(
+        static_cast<const uint16_t*>(W), N, K, ld, static_cast<uint8_t*>(codes), ldc, scale, kblocks);
+    return launch_status();
+}
+
+}  // extern "C"
