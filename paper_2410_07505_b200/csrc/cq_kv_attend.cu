@@ -3,38 +3,45 @@
 // With l_j = scale * sum_d q_d kf_d kc_jd * ka_j (codes kc, token scales ka, channel factors kf; likewise vc, va, vf):
 //   out_d = vf_d * sum_j softmax(l)_j va_j vc_jd
 // Neither factor has to be applied to a cached element: kf goes into the query, ka onto the logit, va onto the
-// probability, vf onto the result.  The cache is read once and its codes meet the tensor cores as fp16 integers (exact).
+// probability, vf onto the result.  The cache is read once and its codes meet the tensor cores as they are.
 //
-// Bound by HBM: 2 (D bits / 8 + 4) bytes for a token and key/value head, and a few query rows (the G heads that share
-// it x the query tokens) to use them for, so the products run on mma.sync (m16n8k16, fp32 sums) straight from registers
-// while the loads set the pace.
+// Bound by HBM: 2 (D bits / 8 + 4) bytes for a token and key/value head, and few query rows (the G heads that share it
+// times the query tokens) to use them for, so the products run on mma.sync (m16n8k16, fp32 sums) from registers while
+// the loads set the pace.  Tokens (and, for the result, channels) are the 16-row side and query rows the 8-column side,
+// so that up to 8 query rows cost one product where the other way round would pad them to 16.
 //
 // Work: every (sequence, head, tile of rows) is a group of 64-token units; all units in a row are cut into equal parts,
-// one for each resident CTA, whatever the lengths are.  A CTA's four warps take 16 tokens of a unit each and keep
-// running maxima, sums and results of their own (no barrier between units); they are joined in warp order at the end of
-// a group.  A group that ends in another CTA leaves its sums in the workspace and a second kernel joins those in the
-// order of the tokens: the same bits every time.
-// Each warp feeds itself through a ring of asynchronous copies (tensor-map boxes of 16 tokens, swizzled so that the
-// fragments' reads meet no bank conflicts, and the tokens' scales), running ahead across groups.  Waits are bounded.
+// one for each resident CTA, whatever the lengths are.  A CTA's four computing warps take 16 tokens of a unit each and
+// keep running maxima, sums and results of their own (no barrier between units); they are joined in a fixed order at the
+// end of a group.  A group that ends in another CTA leaves its sums in the workspace and a second kernel joins those in
+// the order of the tokens: the same bits every time.
+// A fifth warp keeps a ring of units filled by asynchronous copies (tensor-map boxes, swizzled so that the fragments'
+// reads meet no bank conflicts, and the tokens' scales), running ahead across groups.  Waits are bounded.
 //
-// fp16 operands: a query row (times kf) is scaled by a power of two into [2^14, 2^15) before it is rounded, so its
-// rounding is 2^-12 of each element; probabilities times va are scaled by 2^15 over a power of two above the largest va
-// seen, so small ones keep 11 bits down to 2^-29 of the largest.  Logits, maxima, sums and results are fp32.
+// fp16 operands.  A key's code goes in as the subnormal (code + bias) * 2^-24, bias 128 or 8: its bits are the biased code,
+// no arithmetic needed.  The bias is taken out of a logit by starting its sum at -bias * sum_d q_d.  (The other nibble of a
+// byte comes in as 16 times its value; the query holds a sixteenth there.)  The tensor cores align a subnormal by its
+// nominal exponent, which costs a sum about 2^-13 of one code: nothing beside a logit's other terms, but too much for a
+// result whose likely tokens hold code 0, so a value's code goes in exactly, as fp16 1024 + code + bias minus 1024 + bias.
+// A query row (times kf) is scaled by a power of two into [2^14, 2^15) before it is rounded, so its rounding is 2^-12 of
+// each element; probabilities times va are scaled by 2^15 over a power of two above the largest va seen, so small ones
+// keep 11 bits down to 2^-29 of the largest.  Logits, maxima, sums and results are fp32.
 #include "cq_kv.cuh"
 
 namespace cq {
 
 __device__ unsigned int g_attn_fault = 0;      // set if a bounded wait ever gave up
 
-constexpr int kUnit = 64;                       // tokens of a unit: 16 for each warp
+constexpr int kUnit = 64;                       // tokens of a unit: 16 for each computing warp
 constexpr int kAttWarps = 4;
-constexpr int kAttThreads = 32 * kAttWarps;
+constexpr int kAttThreads = 32 * (kAttWarps + 1);
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct AttendArgs {
     const void* q; int64_t qb, ql, qh;          // strides of sequences, tokens and heads, in elements
     int q_vec;                                  // rows of q may be read four elements at a time
+    int bf16;                                   // type of q and out
     const int* table; int64_t table_stride;     // [B][table_stride] page numbers
     const int* lens;                            // [B]
     const float* scale[2];                      // token scales of keys and values
@@ -45,6 +52,7 @@ struct AttendArgs {
     float softmax_scale;
     int64_t pages;
     int B, Lq, Hq, H, G, page_size, row_tiles;
+    int box;                                    // tokens of a copy: 16, 32 or 64, a divisor of the page size
     int64_t capacity;                           // tokens a row of the table can name
 };
 
@@ -122,34 +130,38 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 __device__ __forceinline__ float pow2i(int e) { return e < -126 ? 0.0f : __int_as_float((e + 127) << 23); }
-__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-    return r;
-}
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b)[2]) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
 // (code + bias) in the low bits of fp16 1024, minus 1024 and the bias: exact
-constexpr uint32_t kH1152 = 0x64806480u;        // 1024 + 128, twice
-constexpr uint32_t kH1032 = 0x64086408u;        // 1024 + 8
-constexpr uint32_t kHSixteenth = 0x2C002C00u;   // 1 / 16
-constexpr uint32_t kHm72 = 0xD480D480u;         // -(1024 / 16 + 8)
-__device__ __forceinline__ uint32_t byte_pair(uint32_t w, uint32_t sel) { return hsub2(__byte_perm(w, 0x64646464u, sel), kH1152); }
-__device__ __forceinline__ uint32_t nib_low(uint32_t w) { return hsub2((w & 0x000F000Fu) | 0x64006400u, kH1032); }
-__device__ __forceinline__ uint32_t nib_high(uint32_t w) { return hfma2((w & 0x00F000F0u) | 0x64006400u, kHSixteenth, kHm72); }
+__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t byte_pair(uint32_t w, uint32_t sel) { return hsub2(__byte_perm(w, 0x64646464u, sel), 0x64806480u); }
+__device__ __forceinline__ uint32_t nib_low(uint32_t w) { return hsub2((w & 0x000F000Fu) | 0x64006400u, 0x64086408u); }
+__device__ __forceinline__ uint32_t nib_high(uint32_t w) {          // 16 (code + 8) in those bits: times 1 / 16, minus 1024 / 16 + 8
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"((w & 0x00F000F0u) | 0x64006400u), "r"(0x2C002C00u), "r"(0xD480D480u));
+    return r;
+}
+__device__ __forceinline__ float unpack_half_lo(uint32_t h) { return __half2float(__ushort_as_half(static_cast<uint16_t>(h & 0xFFFFu))); }
+__device__ __forceinline__ float unpack_half_hi(uint32_t h) { return __half2float(__ushort_as_half(static_cast<uint16_t>(h >> 16))); }
+__device__ __forceinline__ float2 unpack16x2_rt(uint32_t w, int bf16) { return bf16 ? unpack16x2<CQ_BF16>(w) : unpack16x2<CQ_F16>(w); }
+__device__ __forceinline__ uint16_t pack16_rt(float v, int bf16) { return bf16 ? pack16<CQ_BF16>(v) : pack16<CQ_F16>(v); }
+__device__ __forceinline__ void warps_barrier() { asm volatile("bar.sync 1, %0;" :: "n"(32 * kAttWarps) : "memory"); }   // computing warps
 
 // 16-byte piece `c` of row `r` in a box of rows of RB bytes under the tensor map's swizzle of that width
 template <int RB>
@@ -159,449 +171,439 @@ __device__ __forceinline__ uint32_t box_at(int r, int c) {
     else return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
 }
 
-// The place along D of element e (0..3: the fragment's k = 2r, 2r+1, 2r+8, 2r+9) of contraction step kk for lane r of
-// a quad: any assignment serves as long as queries and keys share it; this one lets a lane read 16 bytes at a time.
-template <int D, int BITS>
-__device__ __forceinline__ int place(int r, int kk, int e) {
-    if constexpr (BITS == 8) return r * (D / 4) + kk * 4 + e;
-    else return r * (D / 4) + (kk >> 1) * 8 + (kk & 1) * 2 + (e >> 1) + (e & 1) * 4;
-}
-
-template <int D, int BITS, int MT>
+template <int D, int BITS, int NT>
 struct AttendShape {
     static constexpr int kRow = D * BITS / 8;                   // bytes of a token's codes
-    static constexpr int kBox = 16 * kRow;
-    static constexpr int kStages = BITS == 8 && D == 128 ? 3 : 4;
-    static constexpr int kRows = 16 * MT;
-    static constexpr size_t kSmem = 1024 + size_t(kAttWarps) * kStages * (2 * kBox + 128) + size_t(kRows) * D * 4;
+    static constexpr int kTile = kUnit * kRow;                  // of a unit's keys or values
+    static constexpr int kRows = 8 * NT;
+    static constexpr int kPerSm = NT == 1 ? 3 : NT == 2 ? 2 : 1;
+    static constexpr int kStages = kPerSm == 3 ? (D * BITS == 1024 ? 3 : 6) : kPerSm == 2 ? (D * BITS == 1024 ? 5 : 8) : 8;
+    static constexpr int kPitch = D + 2;                        // floats of a joined row: pairs of lanes' stores meet two to a bank
+    static constexpr size_t kSmem = 1024 + size_t(kStages) * (2 * kTile + 2 * kUnit * 4) + size_t(2) * kRows * kPitch * 4;
 };
 
 // ---- units of a CTA -------------------------------------------------------------------------------
-template <int DT, int D, int BITS, int MT>
-__global__ void __launch_bounds__(kAttThreads, MT == 1 ? 3 : 2)
+template <int D, int BITS, int NT>
+__global__ void __launch_bounds__(kAttThreads, AttendShape<D, BITS, NT>::kPerSm)
 k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const AttendArgs p) {
-    using S = AttendShape<D, BITS, MT>;
-    constexpr int RB = S::kRow, ST = S::kStages, KK = D / 16, NT = D / 8, ROWS = S::kRows;
+    using S = AttendShape<D, BITS, NT>;
+    constexpr int RB = S::kRow, ST = S::kStages, KK = D / 16, MT = D / 16, ROWS = S::kRows, PITCH = S::kPitch;
+    constexpr float kBias = BITS == 8 ? 128.0f : 8.0f;
+    constexpr uint32_t kFlip = BITS == 8 ? 0x80808080u : 0x88888888u;          // two's complement -> biased
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    __shared__ uint64_t full[kAttWarps][ST];
-    __shared__ int s_valid[kAttWarps][ST];
-    __shared__ float s_m[kAttWarps][ROWS], s_l[kAttWarps][ROWS];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, r4 = lane & 3;
-    uint8_t* s_box = smem + warp * ST * 2 * S::kBox;                                       // [stage][keys, values][16][RB]
-    float* s_scale = reinterpret_cast<float*>(smem + kAttWarps * ST * 2 * S::kBox) + warp * ST * 32;   // [stage][keys, values][16]
-    float* s_o = reinterpret_cast<float*>(smem + kAttWarps * ST * (2 * S::kBox + 128));    // [ROWS][D]
+    float* s_scale = reinterpret_cast<float*>(smem + ST * 2 * S::kTile);       // [stage][keys, values][64]
+    float* s_o = s_scale + ST * 2 * kUnit;                                     // [2][ROWS][PITCH]
+    __shared__ uint64_t full[ST], empty[ST];
+    __shared__ int s_valid[ST][kAttWarps];                                      // tokens of each 16 that are there
+    __shared__ float s_m[kAttWarps][ROWS], s_l[kAttWarps][ROWS], s_top[ROWS], s_sum[ROWS];
+    __shared__ volatile uint32_t s_dead;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, r4 = lane & 3;
 
     asm volatile("griddepcontrol.launch_dependents;");
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < ST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], kAttWarps); }
+        mbar_init_fence();
+        s_dead = 0;
+    }
     const int64_t units = tiles_before(p, p.B) * p.H * p.row_tiles;
     const int64_t parts = min(units, static_cast<int64_t>(gridDim.x));          // so that none is empty
     if (blockIdx.x >= parts) return;
     const int64_t u0 = part_start(units, blockIdx.x, parts), u1 = part_start(units, blockIdx.x + 1, parts);
-    if (lane == 0)
-        for (int i = 0; i < ST; ++i) mbar_init(&full[warp][i], 1);
-    mbar_init_fence();
-    __syncwarp();
+    Cursor at;
+    at.seek(p, u0);
+    __syncthreads();
 
-    // -- the loading side: units ahead of the computing side
-    Cursor ahead;
-    ahead.seek(p, u0);
-    Cursor now = ahead;
-    int64_t to_load = u1 - u0;
-    int known_b = -1, known_tile = 0, known_page = -1;         // lane i: the page of this warp's tokens in tile known_tile + i
-    auto load = [&](int stage) {                               // the next unit's 16 tokens of this warp
-        const int tok = ahead.tile * kUnit + warp * 16;
-        const int valid = min(16, ahead.len - tok);
-        if (known_b != ahead.b || ahead.tile < known_tile || ahead.tile >= known_tile + 32) {
-            known_b = ahead.b;
-            known_tile = ahead.tile;
-            const int mine = (known_tile + lane) * kUnit + warp * 16;
-            known_page = mine < ahead.len ? __ldg(p.table + ahead.b * p.table_stride + mine / p.page_size) : -1;
-        }
-        const int page = __shfl_sync(0xFFFFFFFFu, known_page, ahead.tile - known_tile);
-        const bool there = valid > 0 && page >= 0 && page < p.pages;
-        if (lane == 0) {
-            s_valid[warp][stage] = there ? valid : 0;
-            if (there) {
-                const int head = ahead.group / p.row_tiles;
-                const int64_t row = (static_cast<int64_t>(page) * p.H + head) * p.page_size + tok % p.page_size;
-                uint8_t* box = s_box + stage * 2 * S::kBox;
-                mbar_expect_tx(&full[warp][stage], 2 * S::kBox + 128);
-                tile_load(box, &mapK, 0, static_cast<int32_t>(row), &full[warp][stage]);
-                tile_load(box + S::kBox, &mapV, 0, static_cast<int32_t>(row), &full[warp][stage]);
-                bulk_load(s_scale + stage * 32, p.scale[0] + row, 64, &full[warp][stage]);
-                bulk_load(s_scale + stage * 32 + 16, p.scale[1] + row, 64, &full[warp][stage]);
+    if (warp == kAttWarps) {
+        // -- the loading warp: lane i takes the i-th box of a unit
+        const int nbox = kUnit / p.box;
+        int known_b = -1, known_first = 0, known_page = -1;    // lane i: page number known_first + i of the sequence
+        bool ok = true;
+        int64_t n = 0;
+        for (; n < u1 - u0; ++n) {
+            const int stage = static_cast<int>(n % ST);
+            const int tok0 = at.tile * kUnit, tok = tok0 + (lane & (nbox - 1)) * p.box;
+            const int first = tok0 / p.page_size, mine = tok / p.page_size;
+            if (known_b != at.b || first < known_first || first + nbox > known_first + 32) {
+                known_b = at.b;
+                known_first = first;
+                known_page = static_cast<int64_t>(first + lane) * p.page_size < at.len ? __ldg(p.table + at.b * p.table_stride + first + lane) : -1;
             }
+            const int page = __shfl_sync(0xFFFFFFFFu, known_page, mine - known_first);
+            const bool there = tok < at.len && page >= 0 && page < p.pages;
+            const unsigned boxes = __ballot_sync(0xFFFFFFFFu, there && lane < nbox);
+            if (!(ok = role_wait(&empty[stage], (static_cast<uint32_t>(n / ST) & 1u) ^ 1u, &s_dead))) break;
+            if (lane < kAttWarps)
+                s_valid[stage][lane] = ((boxes >> (lane * 16 / p.box)) & 1u) ? max(0, min(16, at.len - tok0 - lane * 16)) : 0;
+            __syncwarp();
+            if (lane == 0) mbar_expect_tx(&full[stage], __popc(boxes) * static_cast<uint32_t>(p.box) * (2 * RB + 8));
+            __syncwarp();
+            if (there && lane < nbox) {
+                const int head = at.group / p.row_tiles;
+                const int64_t row = (static_cast<int64_t>(page) * p.H + head) * p.page_size + tok % p.page_size;
+                uint8_t* box = smem + stage * 2 * S::kTile + lane * p.box * RB;
+                float* sc = s_scale + stage * 2 * kUnit + lane * p.box;
+                tile_load(box, &mapK, 0, static_cast<int32_t>(row), &full[stage]);
+                bulk_load(sc, p.scale[0] + row, p.box * 4, &full[stage]);
+                tile_load(box + S::kTile, &mapV, 0, static_cast<int32_t>(row), &full[stage]);
+                bulk_load(sc + kUnit, p.scale[1] + row, p.box * 4, &full[stage]);
+            }
+            at.next(p);
         }
-        --to_load;
-        ahead.next(p);
-    };
-    for (int i = 0; i < ST && to_load > 0; ++i) load(i);
-    __syncwarp();
+        if (!ok)                                                // copies still in flight land before the CTA leaves
+            for (int64_t j = n > ST ? n - ST : 0; j < n; ++j)
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&full[j % ST], static_cast<uint32_t>(j / ST) & 1u); ++polls) {}
+        return;
+    }
 
-    uint32_t phases = 0;                                       // parity of each stage's barrier
-    int stage = 0;
+    // -- the computing warps
+    const uint8_t* k_row = smem + warp * 16 * RB;               // this warp's tokens in a stage
+    int64_t n_at = 0;
     bool dead = false;
     for (int64_t u = u0; u < u1;) {
-        // -- one group, or the part of it that lies in this CTA
-        const int head = now.group / p.row_tiles, rt = now.group % p.row_tiles;
-        const int first_tile = now.tile, tiles = now.tiles, len = now.len, b = now.b;
+        // one group, or the part of it that lies in this CTA
+        const int head = at.group / p.row_tiles, rt = at.group - head * p.row_tiles;
+        const int first_tile = at.tile, tiles = at.tiles, len = at.len, b = at.b;
         const int n_units = static_cast<int>(min(u1 - u, static_cast<int64_t>(tiles - first_tile)));
         const int R = p.G * p.Lq;
-        uint32_t qf[MT][KK][4];
-        float fac[MT][2];                                      // logits of row quad, quad + 8: product * fac * ka
-        int last[MT][2];                                       // last token that the row sees
+        uint32_t qf[NT][KK][2];
+        float fac[NT][2], start[NT][2];                         // of rows 2 r4, 2 r4 + 1: factor of logits, start of their sums
+        int last[NT][2];                                        // and the last token that they see
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            float2 x[2][KK][2];
-            float top[2] = {0.0f, 0.0f};
+        for (int nt = 0; nt < NT; ++nt) {
+            // this lane: a quarter of row g8, the elements that it meets in the keys
+            const int row = rt * ROWS + nt * 8 + g8;
+            const int i = row / p.G, g = row - i * p.G;
+            const bool there = row < R;
+            const uint16_t* src = static_cast<const uint16_t*>(p.q) + b * p.qb + i * p.ql + static_cast<int64_t>(head * p.G + g) * p.qh + r4 * (D / 4);
+            const float* kcol = p.col[0] != nullptr ? p.col[0] + static_cast<int64_t>(head) * D + r4 * (D / 4) : nullptr;
+            float v[D / 4];
+            float top = 0.0f;
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                const int row = rt * ROWS + mt * 16 + hf * 8 + quad;
-                const int i = row / p.G, g = row - i * p.G;
-                const bool there = row < R;
-                last[mt][hf] = there ? len - p.Lq + i : -1;
-                const uint16_t* src = static_cast<const uint16_t*>(p.q) + b * p.qb + i * p.ql + static_cast<int64_t>(head * p.G + g) * p.qh;
-#pragma unroll
-                for (int kk = 0; kk < KK; kk += (BITS == 8 ? 1 : 2)) {
-                    // the four (INT4: eight) neighbours along D of this step (these two steps)
-                    constexpr int kN = BITS == 8 ? 4 : 8;
-                    const int d0 = place<D, BITS>(r4, kk, 0);
-                    float v[kN];
-#pragma unroll
-                    for (int e = 0; e < kN; e += 4) {
-                        uint2 w = make_uint2(0, 0);
-                        if (there) {
-                            if (p.q_vec) {
-                                w = __ldg(reinterpret_cast<const uint2*>(src + d0 + e));
-                            } else {
-                                w.x = src[d0 + e] | (static_cast<uint32_t>(src[d0 + e + 1]) << 16);
-                                w.y = src[d0 + e + 2] | (static_cast<uint32_t>(src[d0 + e + 3]) << 16);
-                            }
-                        }
-                        const float2 lo = unpack16x2<DT>(w.x), hi = unpack16x2<DT>(w.y);
-                        v[e] = lo.x; v[e + 1] = lo.y; v[e + 2] = hi.x; v[e + 3] = hi.y;
-                        if (p.col[0] != nullptr) {
-                            const float4 c = __ldg(reinterpret_cast<const float4*>(p.col[0] + static_cast<int64_t>(head) * D + d0 + e));
-                            v[e] *= c.x; v[e + 1] *= c.y; v[e + 2] *= c.z; v[e + 3] *= c.w;
-                        }
-                    }
-                    if constexpr (BITS == 8) {
-                        x[hf][kk][0] = make_float2(v[0], v[1]);
-                        x[hf][kk][1] = make_float2(v[2], v[3]);
+            for (int e = 0; e < D / 4; e += 4) {
+                uint2 w = make_uint2(0, 0);
+                if (there) {
+                    if (p.q_vec) {
+                        w = __ldg(reinterpret_cast<const uint2*>(src + e));
                     } else {
-                        x[hf][kk][0] = make_float2(v[0], v[4]);
-                        x[hf][kk][1] = make_float2(v[1], v[5]);
-                        x[hf][kk + 1][0] = make_float2(v[2], v[6]);
-                        x[hf][kk + 1][1] = make_float2(v[3], v[7]);
+                        w.x = src[e] | (static_cast<uint32_t>(src[e + 1]) << 16);
+                        w.y = src[e + 2] | (static_cast<uint32_t>(src[e + 3]) << 16);
                     }
-#pragma unroll
-                    for (int e = 0; e < kN; ++e) top[hf] = fmaxf(top[hf], fabsf(v[e]));
                 }
-                top[hf] = fmaxf(top[hf], __shfl_xor_sync(0xFFFFFFFFu, top[hf], 1));
-                top[hf] = fmaxf(top[hf], __shfl_xor_sync(0xFFFFFFFFu, top[hf], 2));
-                // power of two that brings the largest element into [2^14, 2^15); within the range of a float both ways
-                const int e = top[hf] > 0.0f ? max(-100, min(100, 14 - (static_cast<int>(__float_as_uint(top[hf]) >> 23) - 127))) : 0;
-                const float up = pow2i(e);
-                fac[mt][hf] = pow2i(-e) * p.softmax_scale * kLog2e;
+                const float2 lo = unpack16x2_rt(w.x, p.bf16), hi = unpack16x2_rt(w.y, p.bf16);
+                v[e] = lo.x; v[e + 1] = lo.y; v[e + 2] = hi.x; v[e + 3] = hi.y;
+                if (kcol != nullptr) {
+                    const float4 c = __ldg(reinterpret_cast<const float4*>(kcol + e));
+                    v[e] *= c.x; v[e + 1] *= c.y; v[e + 2] *= c.z; v[e + 3] *= c.w;
+                }
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk) {
-                    qf[mt][kk][hf] = pack_half2(x[hf][kk][0].x * up, x[hf][kk][0].y * up);
-                    qf[mt][kk][2 + hf] = pack_half2(x[hf][kk][1].x * up, x[hf][kk][1].y * up);
+                for (int k = 0; k < 4; ++k) top = fmaxf(top, fabsf(v[e + k]));
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            // power of two that brings the largest element into [2^14, 2^15); within the range of a float both ways
+            const int up_exp = top > 0.0f ? max(-100, min(100, 14 - (static_cast<int>(__float_as_uint(top) >> 23) - 127))) : 0;
+            const float up = pow2i(up_exp);
+            float sum = 0.0f;                                   // of the rounded elements, whichever units they are held in
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                if constexpr (BITS == 8) {
+                    qf[nt][kk][0] = pack_half2(v[4 * kk] * up, v[4 * kk + 1] * up);
+                    qf[nt][kk][1] = pack_half2(v[4 * kk + 2] * up, v[4 * kk + 3] * up);
+                    sum += unpack_half_lo(qf[nt][kk][0]) + unpack_half_hi(qf[nt][kk][0]) + unpack_half_lo(qf[nt][kk][1]) + unpack_half_hi(qf[nt][kk][1]);
+                } else {
+                    // nibbles (0, 4 | 1, 5) of a word in even steps, (2, 6 | 3, 7) in odd ones; the second pair comes in sixteenfold
+                    const int e = (kk >> 1) * 8 + (kk & 1) * 2;
+                    qf[nt][kk][0] = pack_half2(v[e] * up, v[e + 4] * up);
+                    qf[nt][kk][1] = pack_half2(v[e + 1] * up * 0.0625f, v[e + 5] * up * 0.0625f);
+                    sum += unpack_half_lo(qf[nt][kk][0]) + unpack_half_hi(qf[nt][kk][0]) + 16.0f * (unpack_half_lo(qf[nt][kk][1]) + unpack_half_hi(qf[nt][kk][1]));
                 }
             }
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+            const float my_fac = pow2i(-up_exp) * p.softmax_scale * (kLog2e * 16777216.0f);       // codes come in as 2^-24
+            const float my_start = -sum * (kBias / 16777216.0f);
+            const int my_last = there ? len - p.Lq + i : -1;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int from = (2 * r4 + e) * 4;
+                fac[nt][e] = __shfl_sync(0xFFFFFFFFu, my_fac, from);
+                start[nt][e] = __shfl_sync(0xFFFFFFFFu, my_start, from);
+                last[nt][e] = __shfl_sync(0xFFFFFFFFu, my_last, from);
+            }
         }
-        float o[MT][NT][4], m[MT][2], l[MT][2];
+        // results of channels g8 * D/8 + 2 t, + 1 (elements 0 1 | 2 3) and rows 2 r4, 2 r4 + 1
+        float o[NT][MT][4], m[NT][2], l[NT][2];
         int va_exp = -126;                                     // results are held in units of 2^(va_exp - 15)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            m[mt][0] = m[mt][1] = -INFINITY;
-            l[mt][0] = l[mt][1] = 0.0f;
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.0f;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) o[mt][t][0] = o[mt][t][1] = o[mt][t][2] = o[mt][t][3] = 0.0f;
+            for (int t = 0; t < MT; ++t) o[nt][t][0] = o[nt][t][1] = o[nt][t][2] = o[nt][t][3] = 0.0f;
         }
 
-        for (int n = 0; n < n_units; ++n) {
-            const int valid = dead ? 0 : s_valid[warp][stage];
-            if (valid > 0) {
-                if (!mbar_wait(&full[warp][stage], (phases >> stage) & 1u)) {
-                    dead = true;                               // nothing is loaded or computed from here on
-                    if (lane == 0) atomicExch(&g_attn_fault, 1u);
-                }
-                phases ^= 1u << stage;
+        for (int n = 0; n < n_units; ++n, ++n_at) {
+            const int stage = static_cast<int>(n_at % ST);
+            if (!dead && !role_wait(&full[stage], static_cast<uint32_t>(n_at / ST) & 1u, &s_dead)) {
+                dead = true;                                   // nothing is computed from here on
+                if (lane == 0) atomicExch(&g_attn_fault, 1u);
             }
-            if (valid > 0 && !dead) {
+            const int valid = dead ? 0 : s_valid[stage][warp];
+            if (valid > 0) {
                 const int tok0 = (first_tile + n) * kUnit + warp * 16;
-                const uint8_t* kbox = s_box + stage * 2 * S::kBox;
-                const uint8_t* vbox = kbox + S::kBox;
-                const float* sc = s_scale + stage * 32;
-                // -- logits: 16 rows x 16 tokens for each tile of rows
-                float s[MT][2][4];
+                const uint8_t* kbox = k_row + stage * 2 * S::kTile;
+                const uint8_t* vbox = kbox + S::kTile;
+                const float* sc = s_scale + stage * 2 * kUnit + warp * 16;
+                // -- logits of tokens g8 (elements 0 1) and g8 + 8 (2 3), rows 2 r4, 2 r4 + 1
+                float s[NT][4];
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    constexpr int kWords = RB / 16;            // words of a lane: a quarter of the row
-                    uint32_t w[kWords];
-                    const int row = nt * 8 + quad;
+                for (int nt = 0; nt < NT; ++nt) {
+                    s[nt][0] = s[nt][2] = start[nt][0];
+                    s[nt][1] = s[nt][3] = start[nt][1];
+                }
+                constexpr int kWords = RB / 16;                // words of a lane and token: a quarter of the row
+                uint32_t w[2][kWords];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
                     if constexpr (kWords >= 4) {
 #pragma unroll
                         for (int c = 0; c < kWords / 4; ++c) {
-                            const uint4 t = *reinterpret_cast<const uint4*>(kbox + box_at<RB>(row, r4 * (kWords / 4) + c));
-                            w[4 * c] = t.x; w[4 * c + 1] = t.y; w[4 * c + 2] = t.z; w[4 * c + 3] = t.w;
+                            const uint4 t = *reinterpret_cast<const uint4*>(kbox + box_at<RB>(h * 8 + g8, r4 * (kWords / 4) + c));
+                            w[h][4 * c] = t.x; w[h][4 * c + 1] = t.y; w[h][4 * c + 2] = t.z; w[h][4 * c + 3] = t.w;
                         }
                     } else {
-                        const uint2 t = *reinterpret_cast<const uint2*>(kbox + box_at<RB>(row, r4 >> 1) + (r4 & 1) * 8);
-                        w[0] = t.x; w[1] = t.y;
+                        const uint2 t = *reinterpret_cast<const uint2*>(kbox + box_at<RB>(h * 8 + g8, r4 >> 1) + (r4 & 1) * 8);
+                        w[h][0] = t.x; w[h][1] = t.y;
                     }
+                }
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) s[mt][nt][0] = s[mt][nt][1] = s[mt][nt][2] = s[mt][nt][3] = 0.0f;
+                for (int j = 0; j < kWords; ++j) {
+                    const uint32_t x0 = w[0][j] ^ kFlip, x1 = w[1][j] ^ kFlip;
+                    if constexpr (BITS == 8) {
+                        const uint32_t a0 = __byte_perm(x0, 0, 0x4140), a1 = __byte_perm(x1, 0, 0x4140);
+                        const uint32_t a2 = __byte_perm(x0, 0, 0x4342), a3 = __byte_perm(x1, 0, 0x4342);
 #pragma unroll
-                    for (int j = 0; j < kWords; ++j) {
-                        if constexpr (BITS == 8) {
-                            const uint32_t x = w[j] ^ 0x80808080u;
-                            const uint32_t b0 = byte_pair(x, 0x4140u), b1 = byte_pair(x, 0x4342u);
+                        for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][j]);
+                    } else {
+                        const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
 #pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) mma16816(s[mt][nt], qf[mt][j], b0, b1);
-                        } else {
-                            const uint32_t x = w[j] ^ 0x88888888u, y = x >> 8;
-                            const uint32_t b0 = nib_low(x), b1 = nib_high(x), b2 = nib_low(y), b3 = nib_high(y);
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) {
-                                mma16816(s[mt][nt], qf[mt][2 * j], b0, b1);
-                                mma16816(s[mt][nt], qf[mt][2 * j + 1], b2, b3);
-                            }
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma16816(s[nt], x0 & 0x000F000Fu, x1 & 0x000F000Fu, x0 & 0x00F000F0u, x1 & 0x00F000F0u, qf[nt][2 * j]);
+                            mma16816(s[nt], y0 & 0x000F000Fu, y1 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x00F000F0u, qf[nt][2 * j + 1]);
                         }
                     }
                 }
-                // -- probabilities; this lane's tokens are 2 r4, 2 r4 + 1 (nt = 0) and those + 8 (nt = 1)
-                const float2 ka[2] = {*reinterpret_cast<const float2*>(sc + 2 * r4), *reinterpret_cast<const float2*>(sc + 8 + 2 * r4)};
-                float2 va[2] = {*reinterpret_cast<const float2*>(sc + 16 + 2 * r4), *reinterpret_cast<const float2*>(sc + 24 + 2 * r4)};
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {               // what lies past the end may be anything
-                    if (nt * 8 + 2 * r4 >= valid) va[nt].x = 0.0f;
-                    if (nt * 8 + 2 * r4 + 1 >= valid) va[nt].y = 0.0f;
-                }
-                const uint32_t vtop = __reduce_max_sync(0xFFFFFFFFu, max(max(__float_as_uint(va[0].x) & 0x7FFFFFFFu, __float_as_uint(va[0].y) & 0x7FFFFFFFu),
-                                                                         max(__float_as_uint(va[1].x) & 0x7FFFFFFFu, __float_as_uint(va[1].y) & 0x7FFFFFFFu)));
+                // -- probabilities
+                const float ka[2] = {sc[g8], sc[g8 + 8]};
+                float va[2] = {sc[kUnit + g8], sc[kUnit + g8 + 8]};
+                if (g8 >= valid) va[0] = 0.0f;                 // what lies past the end may be anything
+                if (g8 + 8 >= valid) va[1] = 0.0f;
+                const uint32_t vtop = __reduce_max_sync(0xFFFFFFFFu, max(__float_as_uint(va[0]) & 0x7FFFFFFFu, __float_as_uint(va[1]) & 0x7FFFFFFFu));
                 const int vexp = max(va_exp, min(126, static_cast<int>(vtop >> 23) - 126));        // 2^vexp > every va
                 const float vshift = pow2i(max(va_exp - vexp, -127));
                 va_exp = vexp;
                 const float vinv = pow2i(-vexp);
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    va[nt].x = va[nt].x * vinv * 32768.0f;
-                    va[nt].y = va[nt].y * vinv * 32768.0f;
-                }
+                va[0] = va[0] * vinv * 32768.0f;
+                va[1] = va[1] * vinv * 32768.0f;
                 const bool edge = tok0 + 15 > len - p.Lq || valid < 16;       // some row does not see some token
-                uint32_t pf[MT][4];
-                float shrink[MT][2];
-                bool any = false;
+                uint32_t pf[NT][2];
+                float shrink[NT][2];
+                bool grown = vshift != 1.0f;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
+                for (int nt = 0; nt < NT; ++nt) {
+                    float pr[2][2];
 #pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
-                        float e[2][2];
-#pragma unroll
-                        for (int nt = 0; nt < 2; ++nt) {
-                            e[nt][0] = s[mt][nt][2 * hf] * (fac[mt][hf] * ka[nt].x);
-                            e[nt][1] = s[mt][nt][2 * hf + 1] * (fac[mt][hf] * ka[nt].y);
-                            if (edge) {
-                                const int t = tok0 + nt * 8 + 2 * r4;
-                                if (t > last[mt][hf]) e[nt][0] = -INFINITY;
-                                if (t + 1 > last[mt][hf]) e[nt][1] = -INFINITY;
-                            }
+                    for (int e = 0; e < 2; ++e) {
+                        float x0 = s[nt][e] * ka[0], x1 = s[nt][2 + e] * ka[1];
+                        if (edge) {
+                            if (tok0 + g8 > last[nt][e]) x0 = -INFINITY;
+                            if (tok0 + g8 + 8 > last[nt][e]) x1 = -INFINITY;
                         }
-                        float top = fmaxf(fmaxf(e[0][0], e[0][1]), fmaxf(e[1][0], e[1][1]));
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                        const float was = m[mt][hf], is = fmaxf(was, top);
+                        float top = fmaxf(x0, x1);             // in units of fac, which is above 0
+                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+                        const float was = m[nt][e], is = fmaxf(was, top);
                         const float ref = is == -INFINITY ? 0.0f : is;
-                        const float keep = ex2(was - ref);
-                        m[mt][hf] = is;
-                        float sum = 0.0f;
+                        m[nt][e] = is;
+                        // differences first: a product with fac that is rounded before the subtraction would lose the small ones
+                        pr[0][e] = ex2((x0 - ref) * fac[nt][e]);
+                        pr[1][e] = ex2((x1 - ref) * fac[nt][e]);
+                        const float keep = ex2((was - ref) * fac[nt][e]);
+                        l[nt][e] = __fmaf_rn(l[nt][e], keep, pr[0][e] + pr[1][e]);
+                        shrink[nt][e] = keep * vshift;
+                        grown = grown || is != was;
+                    }
+                    pf[nt][0] = transpose8x8(pack_half2(pr[0][0] * va[0], pr[0][1] * va[0]));
+                    pf[nt][1] = transpose8x8(pack_half2(pr[1][0] * va[1], pr[1][1] * va[1]));
+                }
+                if (__any_sync(0xFFFFFFFFu, grown)) {
 #pragma unroll
-                        for (int nt = 0; nt < 2; ++nt) {
-                            const float p0 = ex2(e[nt][0] - ref), p1 = ex2(e[nt][1] - ref);
-                            sum += p0 + p1;
-                            pf[mt][2 * nt + hf] = pack_half2(p0 * va[nt].x, p1 * va[nt].y);
+                    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                        for (int t = 0; t < MT; ++t) {
+                            o[nt][t][0] *= shrink[nt][0]; o[nt][t][1] *= shrink[nt][1];
+                            o[nt][t][2] *= shrink[nt][0]; o[nt][t][3] *= shrink[nt][1];
                         }
-                        l[mt][hf] = __fmaf_rn(l[mt][hf], keep, sum);
-                        shrink[mt][hf] = keep * vshift;
-                        any = any || is != was;
                     }
                 }
-                if (__any_sync(0xFFFFFFFFu, any) || vshift != 1.0f) {
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            o[mt][t][0] *= shrink[mt][0]; o[mt][t][1] *= shrink[mt][0];
-                            o[mt][t][2] *= shrink[mt][1]; o[mt][t][3] *= shrink[mt][1];
-                        }
-                }
-                // -- results: tile t of eight columns holds element t of every lane group's share of the row
+                // -- results
                 constexpr int kVWords = RB / 32;               // words of a lane and token: an eighth of the row
-                uint32_t w[4][kVWords];
+                uint32_t z[4][kVWords];                        // tokens 2 r4, 2 r4 + 1, 2 r4 + 8, 2 r4 + 9
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int row = 2 * r4 + (k & 1) + (k >> 1) * 8;
                     if constexpr (kVWords == 4) {
-                        const uint4 t = *reinterpret_cast<const uint4*>(vbox + box_at<RB>(row, quad));
-                        w[k][0] = t.x; w[k][1] = t.y; w[k][2] = t.z; w[k][3] = t.w;
+                        const uint4 t = *reinterpret_cast<const uint4*>(vbox + box_at<RB>(row, g8));
+                        z[k][0] = t.x; z[k][1] = t.y; z[k][2] = t.z; z[k][3] = t.w;
                     } else if constexpr (kVWords == 2) {
-                        const uint2 t = *reinterpret_cast<const uint2*>(vbox + box_at<RB>(row, quad >> 1) + (quad & 1) * 8);
-                        w[k][0] = t.x; w[k][1] = t.y;
+                        const uint2 t = *reinterpret_cast<const uint2*>(vbox + box_at<RB>(row, g8 >> 1) + (g8 & 1) * 8);
+                        z[k][0] = t.x; z[k][1] = t.y;
                     } else {
-                        w[k][0] = *reinterpret_cast<const uint32_t*>(vbox + box_at<RB>(row, quad >> 2) + (quad & 3) * 4);
+                        z[k][0] = *reinterpret_cast<const uint32_t*>(vbox + box_at<RB>(row, g8 >> 2) + (g8 & 3) * 4);
                     }
                 }
 #pragma unroll
                 for (int j = 0; j < kVWords; ++j) {
+                    uint32_t x[2][2];                          // [tokens +0, +8][half of the word]: the two tokens' bytes side by side
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint32_t a = z[2 * k][j] ^ kFlip, c = z[2 * k + 1][j] ^ kFlip;
+                        x[k][0] = __byte_perm(a, c, BITS == 8 ? 0x5140 : 0x5410);
+                        x[k][1] = __byte_perm(a, c, BITS == 8 ? 0x7362 : 0x7632);
+                    }
                     if constexpr (BITS == 8) {
-                        uint32_t x[2][2];
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const uint32_t a = w[2 * k][j] ^ 0x80808080u, c = w[2 * k + 1][j] ^ 0x80808080u;
-                            x[k][0] = __byte_perm(a, c, 0x5140u);
-                            x[k][1] = __byte_perm(a, c, 0x7362u);
-                        }
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t a0 = byte_pair(x[0][e], 0x4140), a1 = byte_pair(x[0][e], 0x4342);
+                            const uint32_t a2 = byte_pair(x[1][e], 0x4140), a3 = byte_pair(x[1][e], 0x4342);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t sel = (e & 1) ? 0x4342u : 0x4140u;
-                            const uint32_t b0 = byte_pair(x[0][e >> 1], sel), b1 = byte_pair(x[1][e >> 1], sel);
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) mma16816(o[mt][4 * j + e], pf[mt], b0, b1);
+                            for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][2 * j + e], a0, a1, a2, a3, pf[nt]);
                         }
                     } else {
-                        uint32_t x[2][2];
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const uint32_t a = w[2 * k][j] ^ 0x88888888u, c = w[2 * k + 1][j] ^ 0x88888888u;
-                            x[k][0] = __byte_perm(a, c, 0x5410u);
-                            x[k][1] = __byte_perm(a, c, 0x7632u);
-                        }
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t lo = (e & 1) ? x[0][e >> 1] >> 8 : x[0][e >> 1], hi = (e & 1) ? x[1][e >> 1] >> 8 : x[1][e >> 1];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            uint32_t b[2];
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                const uint32_t y = (e & 2) ? x[k][e >> 2] >> 8 : x[k][e >> 2];
-                                b[k] = (e & 1) ? nib_high(y) : nib_low(y);
-                            }
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) mma16816(o[mt][8 * j + e], pf[mt], b[0], b[1]);
+                            for (int nt = 0; nt < NT; ++nt)
+                                mma16816(o[nt][4 * j + e], nib_low(lo), nib_high(lo), nib_low(hi), nib_high(hi), pf[nt]);
                         }
                     }
                 }
             }
             __syncwarp();                                      // the stage has been read by every lane
-            if (to_load > 0 && !dead) load(stage);
-            __syncwarp();
-            stage = stage + 1 == ST ? 0 : stage + 1;
-            now.next(p);
+            if (lane == 0) mbar_arrive(&empty[stage]);
         }
+        // the cursor moves on to the unit behind this part of the group
+        at.tile = first_tile + n_units - 1;
+        at.next(p);
 
-        // -- join the four warps
+        // -- join the four warps: maxima and sums first, then results (warps 0 and 1 store, 2 and 3 add to them)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                l[mt][hf] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][hf], 1);
-                l[mt][hf] += __shfl_xor_sync(0xFFFFFFFFu, l[mt][hf], 2);
-                if (r4 == 0) {
-                    s_m[warp][mt * 16 + hf * 8 + quad] = m[mt][hf];
-                    s_l[warp][mt * 16 + hf * 8 + quad] = l[mt][hf];
+            for (int e = 0; e < 2; ++e) {
+                l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], 4);
+                l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], 8);
+                l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], 16);
+                m[nt][e] = m[nt][e] == -INFINITY ? -INFINITY : m[nt][e] * fac[nt][e];
+                if (g8 == 0) {
+                    s_m[warp][nt * 8 + 2 * r4 + e] = m[nt][e];
+                    s_l[warp][nt * 8 + 2 * r4 + e] = l[nt][e];
                 }
             }
-        __syncthreads();
-        float f[MT][2];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                const int row = mt * 16 + hf * 8 + quad;
-                float top = s_m[0][row];
-#pragma unroll
-                for (int w = 1; w < kAttWarps; ++w) top = fmaxf(top, s_m[w][row]);
-                f[mt][hf] = ex2(m[mt][hf] - (top == -INFINITY ? 0.0f : top)) * pow2i(va_exp) * (1.0f / 32768.0f);
-            }
-        for (int w = 0; w < kAttWarps; ++w) {
-            if (warp == w) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            // columns 2 r4, 2 r4 + 1 of tile t are element t of the shares of lane groups 2 r4, 2 r4 + 1
-                            float* at = s_o + (mt * 16 + (e >> 1) * 8 + quad) * D + (2 * r4 + (e & 1)) * (D / 8) + t;
-                            const float v = o[mt][t][e] * f[mt][e >> 1];
-                            *at = w == 0 ? v : *at + v;
-                        }
-            }
-            __syncthreads();
-        }
-        const bool begins = first_tile == 0, ends = first_tile + n_units == tiles;
-        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (begins ? 1 : 0);
+        warps_barrier();
         const int rows = min(ROWS, R - rt * ROWS);
-        for (int idx = threadIdx.x; idx < rows * D; idx += kAttThreads) {
-            const int row = idx / D, d = idx % D;
-            float top = s_m[0][row];
-#pragma unroll
-            for (int w = 1; w < kAttWarps; ++w) top = fmaxf(top, s_m[w][row]);
+        if (threadIdx.x < ROWS) {
+            const int row = threadIdx.x;
+            const float top = fmaxf(fmaxf(s_m[0][row], s_m[1][row]), fmaxf(s_m[2][row], s_m[3][row]));
             const float ref = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
 #pragma unroll
             for (int w = 0; w < kAttWarps; ++w) sum += s_l[w][row] * ex2(s_m[w][row] - ref);
-            const float v = s_o[idx];
-            if (begins && ends) {
+            s_top[row] = top;
+            s_sum[row] = sum;
+        }
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass) {
+            if ((warp >> 1) == pass) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int row = nt * 8 + 2 * r4 + e;
+                        if (row < rows) {
+                            const float top = fmaxf(fmaxf(s_m[0][row], s_m[1][row]), fmaxf(s_m[2][row], s_m[3][row]));
+                            const float f = ex2(m[nt][e] - (top == -INFINITY ? 0.0f : top)) * pow2i(va_exp) * (1.0f / 32768.0f);
+                            float* dst = s_o + (warp & 1) * ROWS * PITCH + row * PITCH + g8 * (D / 8);
+#pragma unroll
+                            for (int t = 0; t < MT; ++t) {
+                                float2 v = make_float2(o[nt][t][e] * f, o[nt][t][2 + e] * f);
+                                float2* at2 = reinterpret_cast<float2*>(dst + 2 * t);
+                                if (pass == 1) { const float2 w2 = *at2; v.x += w2.x; v.y += w2.y; }
+                                *at2 = v;
+                            }
+                        }
+                    }
+            }
+            warps_barrier();
+        }
+        const bool whole = first_tile == 0 && first_tile + n_units == tiles;
+        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (first_tile == 0 ? 1 : 0);
+        for (int idx = threadIdx.x; idx < rows * D; idx += 32 * kAttWarps) {
+            const int row = idx / D, d = idx % D;
+            const float top = s_top[row], sum = s_sum[row];
+            const float v = s_o[row * PITCH + d] + s_o[(ROWS + row) * PITCH + d];
+            if (whole) {
                 const int rr = rt * ROWS + row, i = rr / p.G, g = rr - i * p.G;
-                const int64_t at = (static_cast<int64_t>(b) * p.Lq + i) * p.Hq + head * p.G + g;
+                const int64_t dst = (static_cast<int64_t>(b) * p.Lq + i) * p.Hq + head * p.G + g;
                 float res = sum == 0.0f ? 0.0f : __fdiv_rn(v, sum);
                 if (p.col[1] != nullptr) res *= __ldg(p.col[1] + static_cast<int64_t>(head) * D + d);
-                static_cast<uint16_t*>(p.out)[at * D + d] = pack16<DT>(res);
-                if (p.lse != nullptr && d == 0) p.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+                static_cast<uint16_t*>(p.out)[dst * D + d] = pack16_rt(res, p.bf16);
+                if (p.lse != nullptr && d == 0) p.lse[dst] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
             } else {
                 p.part[(slot * ROWS + row) * D + d] = v;
                 if (d < 2) p.part[2 * static_cast<int64_t>(gridDim.x) * ROWS * D + (slot * ROWS + row) * 2 + d] = d == 0 ? top : sum;
             }
         }
-        __syncthreads();
+        warps_barrier();
         u += n_units;
-    }
-    if (dead) {                                                // copies still in flight land before the CTA leaves
-        for (int i = 0; i < ST; ++i)
-            if (s_valid[warp][i] > 0) mbar_wait(&full[warp][i], (phases >> i) & 1u);
     }
 }
 
 // ---- join of groups that lie in several CTAs: one block for each query row ---------------------------
-template <int DT, int D>
+template <int D>
 __global__ void __launch_bounds__(D)
-k17_kv_join(const AttendArgs p, int64_t ctas, int rows_per_tile) {
-    const int64_t row_id = blockIdx.x;                          // (b * Lq + i) * Hq + head * G + g
-    const int hq = static_cast<int>(row_id % p.Hq);
-    const int i = static_cast<int>(row_id / p.Hq % p.Lq), b = static_cast<int>(row_id / p.Hq / p.Lq);
-    const int head = hq / p.G, r = i * p.G + hq % p.G;
-    const int rt = r / rows_per_tile, row = r % rows_per_tile;
+k17_kv_join(const AttendArgs p, int ctas, int rows_per_tile) {
+    const int row_id = blockIdx.x;                              // (b * Lq + i) * Hq + head * G + g
+    const int bi = row_id / p.Hq, hq = row_id - bi * p.Hq, b = bi / p.Lq, i = bi - b * p.Lq;
+    const int head = hq / p.G, r = i * p.G + hq - head * p.G;
+    const int rt = r / rows_per_tile, row = r - rt * rows_per_tile;
     const int d = threadIdx.x;
     const int len = seq_len(p, b);
-    const int64_t at = row_id * D + d;
+    const int64_t at = static_cast<int64_t>(row_id) * D + d;
+    int64_t c0 = 0, c1 = 0;
+    if (len > 0) {
+        const int64_t per = static_cast<int64_t>(p.H) * p.row_tiles;
+        const int64_t before = tiles_before(p, b), units = tiles_before(p, p.B) * per;
+        const int tiles = tiles_of(len);
+        const int64_t g0 = before * per + (static_cast<int64_t>(head) * p.row_tiles + rt) * tiles;
+        const int64_t parts = min(units, static_cast<int64_t>(ctas));
+        c0 = part_of(units, g0, parts);
+        c1 = part_of(units, g0 + tiles - 1, parts);
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (len == 0) {                                             // nothing to attend to
-        asm volatile("griddepcontrol.wait;" ::: "memory");      // (the memory may still be read by work before the call)
         static_cast<uint16_t*>(p.out)[at] = 0;
         if (p.lse != nullptr && d == 0) p.lse[row_id] = -INFINITY;
         return;
     }
-    const int64_t per = static_cast<int64_t>(p.H) * p.row_tiles;
-    const int64_t before = tiles_before(p, b), units = tiles_before(p, p.B) * per;
-    const int tiles = tiles_of(len);
-    const int64_t g0 = before * per + (static_cast<int64_t>(head) * p.row_tiles + rt) * tiles;
-    const int64_t parts = min(units, ctas);
-    const int64_t c0 = part_of(units, g0, parts), c1 = part_of(units, g0 + tiles - 1, parts);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (c0 == c1) return;                                       // that CTA has written the result
-    const float* stats = p.part + 2 * ctas * rows_per_tile * D;
+    const float* stats = p.part + 2 * static_cast<int64_t>(ctas) * rows_per_tile * D;
     auto slot = [&](int64_t c) { return ((2 * c + (c == c0 ? 1 : 0)) * rows_per_tile + row); };
     float top = -INFINITY;
+#pragma unroll 4
     for (int64_t c = c0; c <= c1; ++c) top = fmaxf(top, stats[slot(c) * 2]);
     const float ref = top == -INFINITY ? 0.0f : top;
     float sum = 0.0f, v = 0.0f;
@@ -613,7 +615,7 @@ k17_kv_join(const AttendArgs p, int64_t ctas, int rows_per_tile) {
     }
     float res = sum == 0.0f ? 0.0f : __fdiv_rn(v, sum);
     if (p.col[1] != nullptr) res *= __ldg(p.col[1] + static_cast<int64_t>(head) * D + d);
-    static_cast<uint16_t*>(p.out)[at] = pack16<DT>(res);
+    static_cast<uint16_t*>(p.out)[at] = pack16_rt(res, p.bf16);
     if (p.lse != nullptr && d == 0) p.lse[row_id] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
@@ -628,31 +630,34 @@ static size_t attend_workspace(int64_t D) {
     return static_cast<size_t>(sm_count()) * kMaxPerSm * 2 * 32 * (D + 2) * sizeof(float);
 }
 
-template <int DT, int D, int BITS, int MT>
-static int launch_attend(const AttendArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t st) {
-    using S = AttendShape<D, BITS, MT>;
+template <int D>
+static int launch_join(const AttendArgs& p, int64_t ctas, int rows_per_tile, bool dependent, cudaStream_t st) {
+    const int64_t rows = static_cast<int64_t>(p.B) * p.Lq * p.Hq;
+    return launch_ex(k17_kv_join<D>, dim3(static_cast<unsigned>(rows)), D, 0, st, 1, dependent, p, static_cast<int>(ctas), rows_per_tile);
+}
+
+template <int D, int BITS, int NT>
+static int launch_attend(AttendArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t st) {
+    using S = AttendShape<D, BITS, NT>;
     static thread_local LaunchMemo memo;
-    int per_sm = resident_ctas(k16_kv_attend<DT, D, BITS, MT>, kAttThreads, S::kSmem, S::kSmem, memo);
+    int per_sm = resident_ctas(k16_kv_attend<D, BITS, NT>, kAttThreads, S::kSmem, S::kSmem, memo);
     if (per_sm < 1) return CQ_ERR_CUDA;
     if (per_sm > kMaxPerSm) per_sm = kMaxPerSm;
+    p.row_tiles = (p.G * p.Lq + S::kRows - 1) / S::kRows;
     int64_t ctas = static_cast<int64_t>(sm_count()) * per_sm;
     const int64_t most = static_cast<int64_t>(p.B) * p.H * p.row_tiles * ((p.capacity + kUnit - 1) / kUnit);
     if (ctas > most) ctas = most;
-    const int rc = launch_ex(k16_kv_attend<DT, D, BITS, MT>, dim3(static_cast<unsigned>(ctas)), kAttThreads, S::kSmem, st, 1, false, mapK, mapV, p);
-    if (rc != CQ_OK) return rc;
-    const int64_t rows = static_cast<int64_t>(p.B) * p.Lq * p.Hq;
-    return launch_ex(k17_kv_join<DT, D>, dim3(static_cast<unsigned>(rows)), D, 0, st, 1, !tuning_no_pdl(), p, ctas, S::kRows);
+    const int rc = launch_ex(k16_kv_attend<D, BITS, NT>, dim3(static_cast<unsigned>(ctas)), kAttThreads, S::kSmem, st, 1, false, mapK, mapV, p);
+    return rc != CQ_OK ? rc : launch_join<D>(p, ctas, S::kRows, !tuning_no_pdl(), st);
 }
 
-template <int DT, int D, int BITS>
+template <int D, int BITS>
 static int launch_attend_rows(AttendArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t st) {
-    const int64_t R = static_cast<int64_t>(p.G) * p.Lq;
-    if (R <= 16) {
-        p.row_tiles = 1;
-        return launch_attend<DT, D, BITS, 1>(p, mapK, mapV, st);
-    }
-    p.row_tiles = static_cast<int>((R + 31) / 32);
-    return launch_attend<DT, D, BITS, 2>(p, mapK, mapV, st);
+    const int R = p.G * p.Lq;
+    if (R <= 8) return launch_attend<D, BITS, 1>(p, mapK, mapV, st);
+    if (R <= 16) return launch_attend<D, BITS, 2>(p, mapK, mapV, st);
+    if (R <= 24) return launch_attend<D, BITS, 3>(p, mapK, mapV, st);
+    return launch_attend<D, BITS, 4>(p, mapK, mapV, st);
 }
 
 }  // namespace cq
@@ -687,6 +692,8 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
     p.q_vec = ptr_aligned(Q, 8) && ((q_batch_stride | q_token_stride | q_head_stride) & 3) == 0;
     p.table = page_table; p.table_stride = table_stride; p.lens = lens;
     p.scale[0] = k_scale; p.scale[1] = v_scale; p.col[0] = k_col; p.col[1] = v_col;
+    p.bf16 = dtype == CQ_BF16;
+    p.box = page_size % 64 == 0 ? 64 : page_size % 32 == 0 ? 32 : 16;
     p.out = out; p.lse = lse; p.part = static_cast<float*>(workspace);
     p.softmax_scale = static_cast<float>(softmax_scale);
     p.pages = pages; p.B = static_cast<int>(B); p.Lq = static_cast<int>(Lq); p.Hq = static_cast<int>(Hq); p.H = static_cast<int>(H);
@@ -694,24 +701,16 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
     p.row_tiles = 1;
     p.capacity = pages > 0 ? table_width * page_size : 0;
     if (p.capacity == 0) {                                      // no token can be named: every row is empty
-        const int64_t rows = B * Lq * Hq;
-        if (D == 64) return dtype == CQ_F16 ? launch_ex(k17_kv_join<CQ_F16, 64>, dim3(static_cast<unsigned>(rows)), 64, 0, st, 1, false, p, 1, 16)
-                                            : launch_ex(k17_kv_join<CQ_BF16, 64>, dim3(static_cast<unsigned>(rows)), 64, 0, st, 1, false, p, 1, 16);
-        return dtype == CQ_F16 ? launch_ex(k17_kv_join<CQ_F16, 128>, dim3(static_cast<unsigned>(rows)), 128, 0, st, 1, false, p, 1, 16)
-                               : launch_ex(k17_kv_join<CQ_BF16, 128>, dim3(static_cast<unsigned>(rows)), 128, 0, st, 1, false, p, 1, 16);
+        return D == 64 ? launch_join<64>(p, 1, 8, false, st) : launch_join<128>(p, 1, 8, false, st);
     }
     const uint32_t row_bytes = static_cast<uint32_t>(D * bits / 8);
     const CUtensorMapSwizzle swizzle = row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
     const uint64_t rows = static_cast<uint64_t>(pages) * H * page_size;
     CUtensorMap mapK, mapV;
-    if (!make_byte_map(&mapK, k_codes, row_bytes, rows, row_bytes, row_bytes, 16, swizzle) ||
-        !make_byte_map(&mapV, v_codes, row_bytes, rows, row_bytes, row_bytes, 16, swizzle)) return CQ_ERR_CUDA;
-    if (dtype == CQ_F16) {
-        if (D == 128) return bits == 8 ? launch_attend_rows<CQ_F16, 128, 8>(p, mapK, mapV, st) : launch_attend_rows<CQ_F16, 128, 4>(p, mapK, mapV, st);
-        return bits == 8 ? launch_attend_rows<CQ_F16, 64, 8>(p, mapK, mapV, st) : launch_attend_rows<CQ_F16, 64, 4>(p, mapK, mapV, st);
-    }
-    if (D == 128) return bits == 8 ? launch_attend_rows<CQ_BF16, 128, 8>(p, mapK, mapV, st) : launch_attend_rows<CQ_BF16, 128, 4>(p, mapK, mapV, st);
-    return bits == 8 ? launch_attend_rows<CQ_BF16, 64, 8>(p, mapK, mapV, st) : launch_attend_rows<CQ_BF16, 64, 4>(p, mapK, mapV, st);
+    if (!make_byte_map(&mapK, k_codes, row_bytes, rows, row_bytes, row_bytes, p.box, swizzle) ||
+        !make_byte_map(&mapV, v_codes, row_bytes, rows, row_bytes, row_bytes, p.box, swizzle)) return CQ_ERR_CUDA;
+    if (D == 128) return bits == 8 ? launch_attend_rows<128, 8>(p, mapK, mapV, st) : launch_attend_rows<128, 4>(p, mapK, mapV, st);
+    return bits == 8 ? launch_attend_rows<64, 8>(p, mapK, mapV, st) : launch_attend_rows<64, 4>(p, mapK, mapV, st);
 }
 
 int cq_serve_fault(unsigned int* fault_host) {
