@@ -11,7 +11,8 @@
 // so that up to 8 query rows cost one product where the other way round would pad them to 16.
 //
 // Work: every (sequence, head, tile of rows) is a group of 64-token units; all units in a row are cut into equal parts,
-// one for each resident CTA, whatever the lengths are.  A CTA's four computing warps take 16 tokens of a unit each and
+// one for each resident CTA, whatever the lengths are.  (A group counts kLead units more than it has, which is what its
+// beginning and end cost, so that a part of many short groups is no longer than one of a few long ones.)  A CTA's four computing warps take 16 tokens of a unit each and
 // keep running maxima, sums and results of their own (no barrier between units); they are joined in a fixed order at the
 // end of a group.  A group that ends in another CTA leaves its sums in the workspace and a second kernel joins those in
 // the order of the tokens: the same bits every time.
@@ -24,8 +25,10 @@
 // nominal exponent, which costs a sum about 2^-13 of one code: nothing beside a logit's other terms, but too much for a
 // result whose likely tokens hold code 0, so a value's code goes in exactly, as fp16 1024 + code + bias minus 1024 + bias.
 // A query row (times kf) is scaled by a power of two into [2^14, 2^15) before it is rounded, so its rounding is 2^-12 of
-// each element; probabilities times va are scaled by 2^15 over a power of two above the largest va seen, so small ones
-// keep 11 bits down to 2^-29 of the largest.  Logits, maxima, sums and results are fp32.
+// each element; probabilities times va are scaled by 2^10 over a power of two above the largest va seen, so small ones
+// keep 11 bits down to 2^-24 of the reference.  Logits, maxima, sums and results are fp32.
+// The running reference of a row is a logit that was the largest when it was taken; it is only renewed, with all sums and
+// results rescaled, when some logit exceeds it by more than 5 in base 2, which probabilities up to 2^5 times 2^10 allow.
 #include "cq_kv.cuh"
 
 namespace cq {
@@ -53,6 +56,7 @@ struct AttendArgs {
     int64_t pages;
     int B, Lq, Hq, H, G, page_size, row_tiles;
     int box;                                    // tokens of a copy: 16, 32 or 64, a divisor of the page size
+    int unit_pages, unit_rest;                  // whole pages in a unit of tokens, and what is left
     int64_t capacity;                           // tokens a row of the table can name
 };
 
@@ -63,11 +67,13 @@ __device__ __forceinline__ int seq_len(const AttendArgs& p, int b) {
 }
 __device__ __forceinline__ int tiles_of(int len) { return (len + kUnit - 1) / kUnit; }
 
-// Units before sequence `upto` (in tiles of one row group), computed by a whole warp.
-__device__ __forceinline__ int64_t tiles_before(const AttendArgs& p, int upto) {
+// Units before sequence `upto` for one head and tile of rows, the groups' leads included; by a whole warp.
+constexpr int kLead = 4;
+__device__ __forceinline__ int span_of(int len) { return len > 0 ? tiles_of(len) + kLead : 0; }
+__device__ __forceinline__ int64_t spans_before(const AttendArgs& p, int upto) {
     const int lane = threadIdx.x & 31;
     int64_t sum = 0;
-    for (int b = lane; b < upto; b += 32) sum += tiles_of(seq_len(p, b));
+    for (int b = lane; b < upto; b += 32) sum += span_of(seq_len(p, b));
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
     return sum;
@@ -85,20 +91,20 @@ struct Cursor {
         group = 0;
         tile = 0;
     }
-    __device__ __forceinline__ void next(const AttendArgs& p) {
-        if (++tile < tiles) return;
+    __device__ __forceinline__ void next_group(const AttendArgs& p) {
         tile = 0;
         if (++group < p.H * p.row_tiles) return;
         enter(p, b + 1);
     }
-    // the unit with number u, by a whole warp
+    __device__ __forceinline__ bool same_group(const Cursor& o) const { return b == o.b && group == o.group; }
+    // the first real unit at or behind place u, by a whole warp
     __device__ __forceinline__ void seek(const AttendArgs& p, int64_t u) {
         const int lane = threadIdx.x & 31;
         const int64_t per = static_cast<int64_t>(p.H) * p.row_tiles;
         int64_t base = 0;
         for (int b0 = 0; b0 < p.B; b0 += 32) {
             const int mine = b0 + lane < p.B ? seq_len(p, b0 + lane) : 0;
-            const int64_t n = tiles_of(mine);
+            const int64_t n = span_of(mine);
             int64_t incl = n;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
@@ -111,10 +117,10 @@ struct Cursor {
                 b = b0 + l;
                 len = __shfl_sync(0xFFFFFFFFu, mine, l);
                 tiles = tiles_of(len);
-                const int64_t before = base + __shfl_sync(0xFFFFFFFFu, incl, l) - tiles;
+                const int64_t span = tiles + kLead, before = base + __shfl_sync(0xFFFFFFFFu, incl, l) - span;
                 const int64_t r = u - before * per;
-                group = static_cast<int>(r / tiles);
-                tile = static_cast<int>(r - static_cast<int64_t>(group) * tiles);
+                group = static_cast<int>(r / span);
+                tile = max(0, static_cast<int>(r - group * span) - kLead);
                 return;
             }
             base += __shfl_sync(0xFFFFFFFFu, incl, 31);
@@ -151,10 +157,16 @@ __device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
     return r;
 }
 __device__ __forceinline__ uint32_t byte_pair(uint32_t w, uint32_t sel) { return hsub2(__byte_perm(w, 0x64646464u, sel), 0x64806480u); }
-__device__ __forceinline__ uint32_t nib_low(uint32_t w) { return hsub2((w & 0x000F000Fu) | 0x64006400u, 0x64086408u); }
+// (a & mask) ^ bits in one instruction, with both in registers
+__device__ __forceinline__ uint32_t and_xor(uint32_t a, uint32_t mask, uint32_t bits) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
+    return r;
+}
+__device__ __forceinline__ uint32_t nib_low(uint32_t w) { return hsub2(and_xor(w, 0x000F000Fu, 0x64086408u), 0x64086408u); }      // the flip of the sign bit included
 __device__ __forceinline__ uint32_t nib_high(uint32_t w) {          // 16 (code + 8) in those bits: times 1 / 16, minus 1024 / 16 + 8
     uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"((w & 0x00F000F0u) | 0x64006400u), "r"(0x2C002C00u), "r"(0xD480D480u));
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(and_xor(w, 0x00F000F0u, 0x64806480u)), "r"(0x2C002C00u), "r"(0xD480D480u));
     return r;
 }
 __device__ __forceinline__ float unpack_half_lo(uint32_t h) { return __half2float(__ushort_as_half(static_cast<uint16_t>(h & 0xFFFFu))); }
@@ -189,13 +201,12 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     using S = AttendShape<D, BITS, NT>;
     constexpr int RB = S::kRow, ST = S::kStages, KK = D / 16, MT = D / 16, ROWS = S::kRows, PITCH = S::kPitch;
     constexpr float kBias = BITS == 8 ? 128.0f : 8.0f;
-    constexpr uint32_t kFlip = BITS == 8 ? 0x80808080u : 0x88888888u;          // two's complement -> biased
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     float* s_scale = reinterpret_cast<float*>(smem + ST * 2 * S::kTile);       // [stage][keys, values][64]
     float* s_o = s_scale + ST * 2 * kUnit;                                     // [2][ROWS][PITCH]
     __shared__ uint64_t full[ST], empty[ST];
-    __shared__ int s_valid[ST][kAttWarps];                                      // tokens of each 16 that are there
+    __shared__ unsigned s_boxes[ST];                                            // boxes of the unit that are there
     __shared__ float s_m[kAttWarps][ROWS], s_l[kAttWarps][ROWS], s_top[ROWS], s_sum[ROWS];
     __shared__ volatile uint32_t s_dead;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, r4 = lane & 3;
@@ -206,65 +217,84 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         mbar_init_fence();
         s_dead = 0;
     }
-    const int64_t units = tiles_before(p, p.B) * p.H * p.row_tiles;
-    const int64_t parts = min(units, static_cast<int64_t>(gridDim.x));          // so that none is empty
+    const int64_t units = spans_before(p, p.B) * p.H * p.row_tiles;
+    const int64_t parts = min(units, static_cast<int64_t>(gridDim.x));
     if (blockIdx.x >= parts) return;
-    const int64_t u0 = part_start(units, blockIdx.x, parts), u1 = part_start(units, blockIdx.x + 1, parts);
-    Cursor at;
-    at.seek(p, u0);
+    Cursor at, end;
+    at.seek(p, part_start(units, blockIdx.x, parts));
+    end.seek(p, part_start(units, blockIdx.x + 1, parts));
     __syncthreads();
 
     if (warp == kAttWarps) {
-        // -- the loading warp: lane i takes the i-th box of a unit
+        // -- the loading warp: lane i takes the i-th box of a unit.  One warp's chain of dependent instructions for each unit is what
+        //    it costs, so everything that a group shares is kept, and places advance by additions.
         const int nbox = kUnit / p.box;
-        int known_b = -1, known_first = 0, known_page = -1;    // lane i: page number known_first + i of the sequence
+        const int box_row = lane * p.box;
+        const bool mine = lane < nbox;
+        const uint32_t box_bytes = static_cast<uint32_t>(p.box) * (2 * RB + 8);
         bool ok = true;
-        int64_t n = 0;
-        for (; n < u1 - u0; ++n) {
-            const int stage = static_cast<int>(n % ST);
-            const int tok0 = at.tile * kUnit, tok = tok0 + (lane & (nbox - 1)) * p.box;
-            const int first = tok0 / p.page_size, mine = tok / p.page_size;
-            if (known_b != at.b || first < known_first || first + nbox > known_first + 32) {
-                known_b = at.b;
-                known_first = first;
-                known_page = static_cast<int64_t>(first + lane) * p.page_size < at.len ? __ldg(p.table + at.b * p.table_stride + first + lane) : -1;
+        int stage = 0, issued = 0;
+        uint32_t round = 0;                                    // parity of the stage's turn
+        while (ok && at.b < p.B && !(at.same_group(end) && at.tile >= end.tile)) {
+            const int n_units = (at.same_group(end) ? end.tile : at.tiles) - at.tile;
+            const int* table = p.table + at.b * p.table_stride;
+            const int head_row = (at.group / p.row_tiles) * p.page_size, page_rows = p.H * p.page_size;
+            int tok = at.tile * kUnit + (mine ? box_row : 0);
+            int idx = tok / p.page_size, off = tok - idx * p.page_size;
+            int known_first = idx - 32, known_page = -1;       // lane i: page number known_first + i of the sequence
+            for (int n = 0; n < n_units; ++n) {
+                const int first = __shfl_sync(0xFFFFFFFFu, idx, 0);
+                if (first + nbox > known_first + 32) {
+                    known_first = first;
+                    known_page = static_cast<int64_t>(first + lane) * p.page_size < at.len ? __ldg(table + first + lane) : -1;
+                }
+                const int page = __shfl_sync(0xFFFFFFFFu, known_page, idx - known_first);
+                const bool there = mine && tok < at.len && page >= 0 && page < p.pages;
+                const unsigned boxes = __ballot_sync(0xFFFFFFFFu, there);
+                if (!(ok = role_wait(&empty[stage], round ^ 1u, &s_dead))) break;
+                if (lane == 0) {
+                    s_boxes[stage] = boxes;
+                    mbar_expect_tx(&full[stage], __popc(boxes) * box_bytes);
+                }
+                __syncwarp();
+                if (there) {
+                    const int row = page * page_rows + head_row + off;          // below 2^31
+                    uint8_t* box = smem + stage * 2 * S::kTile + box_row * RB;
+                    float* sc = s_scale + stage * 2 * kUnit + box_row;
+                    tile_load(box, &mapK, 0, row, &full[stage]);
+                    bulk_load(sc, p.scale[0] + row, p.box * 4, &full[stage]);
+                    tile_load(box + S::kTile, &mapV, 0, row, &full[stage]);
+                    bulk_load(sc + kUnit, p.scale[1] + row, p.box * 4, &full[stage]);
+                }
+                tok += kUnit;
+                idx += p.unit_pages;
+                off += p.unit_rest;
+                if (off >= p.page_size) { off -= p.page_size; ++idx; }
+                issued = min(issued + 1, ST);
+                if (++stage == ST) { stage = 0; round ^= 1u; }
             }
-            const int page = __shfl_sync(0xFFFFFFFFu, known_page, mine - known_first);
-            const bool there = tok < at.len && page >= 0 && page < p.pages;
-            const unsigned boxes = __ballot_sync(0xFFFFFFFFu, there && lane < nbox);
-            if (!(ok = role_wait(&empty[stage], (static_cast<uint32_t>(n / ST) & 1u) ^ 1u, &s_dead))) break;
-            if (lane < kAttWarps)
-                s_valid[stage][lane] = ((boxes >> (lane * 16 / p.box)) & 1u) ? max(0, min(16, at.len - tok0 - lane * 16)) : 0;
-            __syncwarp();
-            if (lane == 0) mbar_expect_tx(&full[stage], __popc(boxes) * static_cast<uint32_t>(p.box) * (2 * RB + 8));
-            __syncwarp();
-            if (there && lane < nbox) {
-                const int head = at.group / p.row_tiles;
-                const int64_t row = (static_cast<int64_t>(page) * p.H + head) * p.page_size + tok % p.page_size;
-                uint8_t* box = smem + stage * 2 * S::kTile + lane * p.box * RB;
-                float* sc = s_scale + stage * 2 * kUnit + lane * p.box;
-                tile_load(box, &mapK, 0, static_cast<int32_t>(row), &full[stage]);
-                bulk_load(sc, p.scale[0] + row, p.box * 4, &full[stage]);
-                tile_load(box + S::kTile, &mapV, 0, static_cast<int32_t>(row), &full[stage]);
-                bulk_load(sc + kUnit, p.scale[1] + row, p.box * 4, &full[stage]);
-            }
-            at.next(p);
+            at.tile += n_units;
+            if (at.tile >= at.tiles) at.next_group(p);
         }
         if (!ok)                                                // copies still in flight land before the CTA leaves
-            for (int64_t j = n > ST ? n - ST : 0; j < n; ++j)
-                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&full[j % ST], static_cast<uint32_t>(j / ST) & 1u); ++polls) {}
+            for (; issued > 0; --issued) {
+                if (--stage < 0) { stage = ST - 1; round ^= 1u; }
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&full[stage], round); ++polls) {}
+            }
         return;
     }
 
     // -- the computing warps
     const uint8_t* k_row = smem + warp * 16 * RB;               // this warp's tokens in a stage
-    int64_t n_at = 0;
+    const int my_box = warp * 16 / p.box;
+    int stage = 0;
+    uint32_t round = 0;
     bool dead = false;
-    for (int64_t u = u0; u < u1;) {
+    while (at.b < p.B && !(at.same_group(end) && at.tile >= end.tile)) {
         // one group, or the part of it that lies in this CTA
         const int head = at.group / p.row_tiles, rt = at.group - head * p.row_tiles;
         const int first_tile = at.tile, tiles = at.tiles, len = at.len, b = at.b;
-        const int n_units = static_cast<int>(min(u1 - u, static_cast<int64_t>(tiles - first_tile)));
+        const int n_units = (at.same_group(end) ? end.tile : tiles) - first_tile;
         const int R = p.G * p.Lq;
         uint32_t qf[NT][KK][2];
         float fac[NT][2], start[NT][2];                         // of rows 2 r4, 2 r4 + 1: factor of logits, start of their sums
@@ -333,25 +363,26 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             }
         }
         // results of channels g8 * D/8 + 2 t, + 1 (elements 0 1 | 2 3) and rows 2 r4, 2 r4 + 1
-        float o[NT][MT][4], m[NT][2], l[NT][2];
-        int va_exp = -126;                                     // results are held in units of 2^(va_exp - 15)
+        float o[NT][MT][4], ref[NT][2], l[NT][2];               // ref: references, in base 2
+        bool fresh = true;                                     // no token yet (a row that does not see the first will see none)
+        int va_exp = -100;                                     // results are held in units of 2^(va_exp - 10)
+        float va_unit = pow2i(10 - va_exp), va_top = pow2i(va_exp);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            m[nt][0] = m[nt][1] = -INFINITY;
+            ref[nt][0] = ref[nt][1] = 0.0f;
             l[nt][0] = l[nt][1] = 0.0f;
 #pragma unroll
             for (int t = 0; t < MT; ++t) o[nt][t][0] = o[nt][t][1] = o[nt][t][2] = o[nt][t][3] = 0.0f;
         }
 
-        for (int n = 0; n < n_units; ++n, ++n_at) {
-            const int stage = static_cast<int>(n_at % ST);
-            if (!dead && !role_wait(&full[stage], static_cast<uint32_t>(n_at / ST) & 1u, &s_dead)) {
+        for (int n = 0; n < n_units; ++n) {
+            if (!dead && !role_wait(&full[stage], round, &s_dead)) {
                 dead = true;                                   // nothing is computed from here on
                 if (lane == 0) atomicExch(&g_attn_fault, 1u);
             }
-            const int valid = dead ? 0 : s_valid[stage][warp];
-            if (valid > 0) {
-                const int tok0 = (first_tile + n) * kUnit + warp * 16;
+            const int tok0 = (first_tile + n) * kUnit + warp * 16;
+            const int valid = len - tok0;                      // tokens from here to the end
+            if (valid > 0 && !dead && ((s_boxes[stage] >> my_box) & 1u) != 0u) {
                 const uint8_t* kbox = k_row + stage * 2 * S::kTile;
                 const uint8_t* vbox = kbox + S::kTile;
                 const float* sc = s_scale + stage * 2 * kUnit + warp * 16;
@@ -379,18 +410,20 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 }
 #pragma unroll
                 for (int j = 0; j < kWords; ++j) {
-                    const uint32_t x0 = w[0][j] ^ kFlip, x1 = w[1][j] ^ kFlip;
                     if constexpr (BITS == 8) {
+                        const uint32_t x0 = w[0][j] ^ 0x80808080u, x1 = w[1][j] ^ 0x80808080u;         // two's complement -> biased
                         const uint32_t a0 = __byte_perm(x0, 0, 0x4140), a1 = __byte_perm(x1, 0, 0x4140);
                         const uint32_t a2 = __byte_perm(x0, 0, 0x4342), a3 = __byte_perm(x1, 0, 0x4342);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][j]);
                     } else {
-                        const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            mma16816(s[nt], x0 & 0x000F000Fu, x1 & 0x000F000Fu, x0 & 0x00F000F0u, x1 & 0x00F000F0u, qf[nt][2 * j]);
-                            mma16816(s[nt], y0 & 0x000F000Fu, y1 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x00F000F0u, qf[nt][2 * j + 1]);
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t y0 = w[0][j] >> (8 * h), y1 = w[1][j] >> (8 * h);
+                            const uint32_t a0 = and_xor(y0, 0x000F000Fu, 0x00080008u), a1 = and_xor(y1, 0x000F000Fu, 0x00080008u);
+                            const uint32_t a2 = and_xor(y0, 0x00F000F0u, 0x00800080u), a3 = and_xor(y1, 0x00F000F0u, 0x00800080u);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][2 * j + h]);
                         }
                     }
                 }
@@ -399,54 +432,77 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 float va[2] = {sc[kUnit + g8], sc[kUnit + g8 + 8]};
                 if (g8 >= valid) va[0] = 0.0f;                 // what lies past the end may be anything
                 if (g8 + 8 >= valid) va[1] = 0.0f;
-                const uint32_t vtop = __reduce_max_sync(0xFFFFFFFFu, max(__float_as_uint(va[0]) & 0x7FFFFFFFu, __float_as_uint(va[1]) & 0x7FFFFFFFu));
-                const int vexp = max(va_exp, min(126, static_cast<int>(vtop >> 23) - 126));        // 2^vexp > every va
-                const float vshift = pow2i(max(va_exp - vexp, -127));
-                va_exp = vexp;
-                const float vinv = pow2i(-vexp);
-                va[0] = va[0] * vinv * 32768.0f;
-                va[1] = va[1] * vinv * 32768.0f;
-                const bool edge = tok0 + 15 > len - p.Lq || valid < 16;       // some row does not see some token
-                uint32_t pf[NT][2];
-                float shrink[NT][2];
-                bool grown = vshift != 1.0f;
+                const bool edge = tok0 + 15 > len - p.Lq;      // some row does not see some token
+                float x[NT][2][2], pr[NT][2][2];               // [row][token]: logits in units of fac, probabilities
+                float most = 0.0f;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float pr[2][2];
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float x0 = s[nt][e] * ka[0], x1 = s[nt][2 + e] * ka[1];
-                        if (edge) {
-                            if (tok0 + g8 > last[nt][e]) x0 = -INFINITY;
-                            if (tok0 + g8 + 8 > last[nt][e]) x1 = -INFINITY;
-                        }
-                        float top = fmaxf(x0, x1);             // in units of fac, which is above 0
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
-                        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-                        const float was = m[nt][e], is = fmaxf(was, top);
-                        const float ref = is == -INFINITY ? 0.0f : is;
-                        m[nt][e] = is;
-                        // differences first: a product with fac that is rounded before the subtraction would lose the small ones
-                        pr[0][e] = ex2((x0 - ref) * fac[nt][e]);
-                        pr[1][e] = ex2((x1 - ref) * fac[nt][e]);
-                        const float keep = ex2((was - ref) * fac[nt][e]);
-                        l[nt][e] = __fmaf_rn(l[nt][e], keep, pr[0][e] + pr[1][e]);
-                        shrink[nt][e] = keep * vshift;
-                        grown = grown || is != was;
+                        x[nt][e][0] = s[nt][e] * ka[0];
+                        x[nt][e][1] = s[nt][2 + e] * ka[1];
                     }
-                    pf[nt][0] = transpose8x8(pack_half2(pr[0][0] * va[0], pr[0][1] * va[0]));
-                    pf[nt][1] = transpose8x8(pack_half2(pr[1][0] * va[1], pr[1][1] * va[1]));
+                if (edge) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            if (tok0 + g8 > last[nt][e]) x[nt][e][0] = -INFINITY;
+                            if (tok0 + g8 + 8 > last[nt][e]) x[nt][e][1] = -INFINITY;
+                        }
                 }
-                if (__any_sync(0xFFFFFFFFu, grown)) {
+                // a product with fac is rounded once, as the reference, and used for all that refers to it: its rounding cancels
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        pr[nt][e][0] = ex2(__fmaf_rn(x[nt][e][0], fac[nt][e], -ref[nt][e]));
+                        pr[nt][e][1] = ex2(__fmaf_rn(x[nt][e][1], fac[nt][e], -ref[nt][e]));
+                        most = fmaxf(most, fmaxf(pr[nt][e][0], pr[nt][e][1]));
+                    }
+                if (__any_sync(0xFFFFFFFFu, most > 32.0f || fmaxf(va[0], va[1]) >= va_top) || fresh) {    // new references and units
+                    const uint32_t vtop = __reduce_max_sync(0xFFFFFFFFu, max(__float_as_uint(va[0]) & 0x7FFFFFFFu, __float_as_uint(va[1]) & 0x7FFFFFFFu));
+                    const int new_exp = max(va_exp, min(126, static_cast<int>(vtop >> 23) - 126));        // 2^new_exp > every va
+                    const float vshift = pow2i(max(va_exp - new_exp, -127));
+                    va_exp = new_exp;
+                    va_unit = pow2i(10 - va_exp);
+                    va_top = pow2i(va_exp);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
+                        float shrink[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float top = fmaxf(x[nt][e][0], x[nt][e][1]);
+                            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+                            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+                            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+                            top = __fmul_rn(top, fac[nt][e]);
+                            float next = fresh ? top : fmaxf(ref[nt][e], top);
+                            if (next == -INFINITY) next = 0.0f;
+                            const float keep = fresh ? 0.0f : ex2(ref[nt][e] - next);
+                            ref[nt][e] = next;
+                            l[nt][e] *= keep;
+                            shrink[e] = keep * vshift;
+                            pr[nt][e][0] = ex2(__fmaf_rn(x[nt][e][0], fac[nt][e], -next));
+                            pr[nt][e][1] = ex2(__fmaf_rn(x[nt][e][1], fac[nt][e], -next));
+                        }
 #pragma unroll
                         for (int t = 0; t < MT; ++t) {
-                            o[nt][t][0] *= shrink[nt][0]; o[nt][t][1] *= shrink[nt][1];
-                            o[nt][t][2] *= shrink[nt][0]; o[nt][t][3] *= shrink[nt][1];
+                            o[nt][t][0] *= shrink[0]; o[nt][t][1] *= shrink[1];
+                            o[nt][t][2] *= shrink[0]; o[nt][t][3] *= shrink[1];
                         }
                     }
+                    fresh = false;
+                }
+                va[0] *= va_unit;
+                va[1] *= va_unit;
+                uint32_t pf[NT][2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    l[nt][0] += pr[nt][0][0] + pr[nt][0][1];
+                    l[nt][1] += pr[nt][1][0] + pr[nt][1][1];
+                    pf[nt][0] = transpose8x8(pack_half2(pr[nt][0][0] * va[0], pr[nt][1][0] * va[0]));
+                    pf[nt][1] = transpose8x8(pack_half2(pr[nt][0][1] * va[1], pr[nt][1][1] * va[1]));
                 }
                 // -- results
                 constexpr int kVWords = RB / 32;               // words of a lane and token: an eighth of the row
@@ -469,7 +525,8 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                     uint32_t x[2][2];                          // [tokens +0, +8][half of the word]: the two tokens' bytes side by side
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const uint32_t a = z[2 * k][j] ^ kFlip, c = z[2 * k + 1][j] ^ kFlip;
+                        const uint32_t flip = BITS == 8 ? 0x80808080u : 0u;
+                        const uint32_t a = z[2 * k][j] ^ flip, c = z[2 * k + 1][j] ^ flip;
                         x[k][0] = __byte_perm(a, c, BITS == 8 ? 0x5140 : 0x5410);
                         x[k][1] = __byte_perm(a, c, BITS == 8 ? 0x7362 : 0x7632);
                     }
@@ -485,19 +542,20 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const uint32_t lo = (e & 1) ? x[0][e >> 1] >> 8 : x[0][e >> 1], hi = (e & 1) ? x[1][e >> 1] >> 8 : x[1][e >> 1];
+                            const uint32_t a0 = nib_low(lo), a1 = nib_high(lo), a2 = nib_low(hi), a3 = nib_high(hi);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-                                mma16816(o[nt][4 * j + e], nib_low(lo), nib_high(lo), nib_low(hi), nib_high(hi), pf[nt]);
+                            for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * j + e], a0, a1, a2, a3, pf[nt]);
                         }
                     }
                 }
             }
             __syncwarp();                                      // the stage has been read by every lane
             if (lane == 0) mbar_arrive(&empty[stage]);
+            if (++stage == ST) { stage = 0; round ^= 1u; }
         }
-        // the cursor moves on to the unit behind this part of the group
-        at.tile = first_tile + n_units - 1;
-        at.next(p);
+        const bool here_ends = first_tile + n_units == tiles;
+        if (here_ends) at.next_group(p);
+        else at.tile = first_tile + n_units;
 
         // -- join the four warps: maxima and sums first, then results (warps 0 and 1 store, 2 and 3 add to them)
 #pragma unroll
@@ -507,9 +565,9 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], 4);
                 l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], 8);
                 l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], 16);
-                m[nt][e] = m[nt][e] == -INFINITY ? -INFINITY : m[nt][e] * fac[nt][e];
+                if (l[nt][e] == 0.0f) ref[nt][e] = -INFINITY;   // has seen nothing
                 if (g8 == 0) {
-                    s_m[warp][nt * 8 + 2 * r4 + e] = m[nt][e];
+                    s_m[warp][nt * 8 + 2 * r4 + e] = ref[nt][e];
                     s_l[warp][nt * 8 + 2 * r4 + e] = l[nt][e];
                 }
             }
@@ -535,7 +593,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                         const int row = nt * 8 + 2 * r4 + e;
                         if (row < rows) {
                             const float top = fmaxf(fmaxf(s_m[0][row], s_m[1][row]), fmaxf(s_m[2][row], s_m[3][row]));
-                            const float f = ex2(m[nt][e] - (top == -INFINITY ? 0.0f : top)) * pow2i(va_exp) * (1.0f / 32768.0f);
+                            const float f = ex2(ref[nt][e] - (top == -INFINITY ? 0.0f : top)) * pow2i(va_exp) * (1.0f / 1024.0f);
                             float* dst = s_o + (warp & 1) * ROWS * PITCH + row * PITCH + g8 * (D / 8);
 #pragma unroll
                             for (int t = 0; t < MT; ++t) {
@@ -549,7 +607,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             }
             warps_barrier();
         }
-        const bool whole = first_tile == 0 && first_tile + n_units == tiles;
+        const bool whole = first_tile == 0 && here_ends;
         const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (first_tile == 0 ? 1 : 0);
         for (int idx = threadIdx.x; idx < rows * D; idx += 32 * kAttWarps) {
             const int row = idx / D, d = idx % D;
@@ -568,7 +626,6 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             }
         }
         warps_barrier();
-        u += n_units;
     }
 }
 
@@ -586,9 +643,9 @@ k17_kv_join(const AttendArgs p, int ctas, int rows_per_tile) {
     int64_t c0 = 0, c1 = 0;
     if (len > 0) {
         const int64_t per = static_cast<int64_t>(p.H) * p.row_tiles;
-        const int64_t before = tiles_before(p, b), units = tiles_before(p, p.B) * per;
+        const int64_t before = spans_before(p, b), units = spans_before(p, p.B) * per;
         const int tiles = tiles_of(len);
-        const int64_t g0 = before * per + (static_cast<int64_t>(head) * p.row_tiles + rt) * tiles;
+        const int64_t g0 = before * per + (static_cast<int64_t>(head) * p.row_tiles + rt) * (tiles + kLead) + kLead;
         const int64_t parts = min(units, static_cast<int64_t>(ctas));
         c0 = part_of(units, g0, parts);
         c1 = part_of(units, g0 + tiles - 1, parts);
@@ -645,7 +702,7 @@ static int launch_attend(AttendArgs& p, const CUtensorMap& mapK, const CUtensorM
     if (per_sm > kMaxPerSm) per_sm = kMaxPerSm;
     p.row_tiles = (p.G * p.Lq + S::kRows - 1) / S::kRows;
     int64_t ctas = static_cast<int64_t>(sm_count()) * per_sm;
-    const int64_t most = static_cast<int64_t>(p.B) * p.H * p.row_tiles * ((p.capacity + kUnit - 1) / kUnit);
+    const int64_t most = static_cast<int64_t>(p.B) * p.H * p.row_tiles * ((p.capacity + kUnit - 1) / kUnit);       // real units
     if (ctas > most) ctas = most;
     const int rc = launch_ex(k16_kv_attend<D, BITS, NT>, dim3(static_cast<unsigned>(ctas)), kAttThreads, S::kSmem, st, 1, false, mapK, mapV, p);
     return rc != CQ_OK ? rc : launch_join<D>(p, ctas, S::kRows, !tuning_no_pdl(), st);
@@ -694,6 +751,8 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
     p.scale[0] = k_scale; p.scale[1] = v_scale; p.col[0] = k_col; p.col[1] = v_col;
     p.bf16 = dtype == CQ_BF16;
     p.box = page_size % 64 == 0 ? 64 : page_size % 32 == 0 ? 32 : 16;
+    p.unit_pages = static_cast<int>(kUnit / page_size);
+    p.unit_rest = static_cast<int>(kUnit % page_size);
     p.out = out; p.lse = lse; p.part = static_cast<float*>(workspace);
     p.softmax_scale = static_cast<float>(softmax_scale);
     p.pages = pages; p.B = static_cast<int>(B); p.Lq = static_cast<int>(Lq); p.Hq = static_cast<int>(Hq); p.H = static_cast<int>(H);
