@@ -543,114 +543,124 @@ def _addr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
-def _raw() -> int:
-    return _raw_stream(torch.cuda.current_device()) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+def _raw(device: int) -> int:
+    """The current stream of the tensors' device, which has to be the current one."""
+    if device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+_DT16 = {torch.float16: CQ_F16, torch.bfloat16: CQ_BF16}
+_F32, _E4M3, _I32, _I64 = torch.float32, torch.float8_e4m3fn, torch.int32, torch.int64
+
+
+def _matrix16(X: torch.Tensor):
+    """(rows, columns, pitch, dtype code, device index) of a 16-bit CUDA matrix."""
+    dt = _DT16.get(X.dtype)
+    if dt is None or X.dim() != 2:
+        raise TypeError("expected a 2-D float16 / bfloat16 tensor")
+    dev = X.get_device()
+    if dev < 0:
+        raise TypeError("expected a CUDA tensor")
+    (T, K), (ld, inner) = X.shape, X.stride()
+    if inner != 1 and K > 1 and T > 0:
+        raise ValueError("columns must be contiguous")
+    return T, K, ld if T > 1 else max(K, 1), dt, dev
 
 
 def _fp8_codes(rows: int, K: int, device) -> torch.Tensor:
-    return torch.empty((rows, _up(K, 16)), dtype=torch.float8_e4m3fn, device=device)[:, :K]
+    return torch.empty_strided((rows, K), (_up(K, 16), 1), dtype=_E4M3, device=device)
 
 
-def _pitch(x: torch.Tensor, what: str) -> int:
-    """Row pitch of a 2-D tensor with contiguous columns."""
-    rows, cols = x.shape
-    if rows > 0 and cols > 1 and x.stride(1) != 1:
-        raise ValueError(f"{what}: columns must be contiguous")
-    return x.stride(0) if rows > 1 else max(x.stride(0), _up(cols, 16))
+def _codes_pitch(codes: torch.Tensor, rows: int, K: int, dev: int, what: str) -> int:
+    if codes.dtype != _E4M3 or codes.shape != (rows, K) or codes.get_device() != dev:
+        raise ValueError(f"{what}.codes must be float8_e4m3fn [{rows}, {K}] on cuda:{dev}")
+    pitch, inner = codes.stride()
+    if inner != 1 and K > 1 and rows > 0:
+        raise ValueError(f"{what}.codes: columns must be contiguous")
+    return pitch if rows > 1 else max(pitch, _up(K, 16))
 
 
-def _check_fp8(pair, rows: int | None, K: int, scale_shape, device, what: str) -> None:
-    codes, scale = pair
-    if codes.dim() != 2 or codes.dtype != torch.float8_e4m3fn or codes.device != device or codes.shape[1] != K or \
-            (rows is not None and codes.shape[0] != rows):
-        raise ValueError(f"{what}.codes must be float8_e4m3fn [{'rows' if rows is None else rows}, {K}] on {device}")
-    if scale.dtype != torch.float32 or tuple(scale.shape) != tuple(scale_shape) or scale.device != device:
-        raise ValueError(f"{what}.scale must be float32 {tuple(scale_shape)} on {device}")
+def _act_scale_pitch(scale: torch.Tensor, nb: int, T: int, dev: int, what: str) -> int:
+    if scale.dtype != _F32 or scale.shape != (nb, T) or scale.get_device() != dev:
+        raise ValueError(f"{what}.scale must be float32 [{nb}, {T}] on cuda:{dev}")
+    pitch, inner = scale.stride()
+    if inner != 1 and T > 1 and nb > 0:
+        raise ValueError(f"{what}.scale: a block's scales must be contiguous")
+    return pitch if nb > 1 else max(pitch, _up(T, 4))
+
+
+def _check_weight_scale(scale: torch.Tensor, N: int, K: int, dev: int, what: str) -> None:
+    shape = ((N + 127) // 128, (K + 127) // 128)
+    if scale.dtype != _F32 or scale.shape != shape or scale.get_device() != dev or not scale.is_contiguous():
+        raise ValueError(f"{what}.scale must be contiguous float32 {shape} on cuda:{dev}")
 
 
 def fp8_quantize_act(X: torch.Tensor, *, out: Fp8Act | None = None) -> Fp8Act:
     """e4m3 codes of activations [T, K], one scale for each run of 128 elements of a row."""
-    T, K, ld = _matrix_args(X)
+    T, K, ld, dt, dev = _matrix16(X)
     nb = -(-K // BLOCK)
     if out is None:
-        out = Fp8Act(_fp8_codes(T, K, X.device), torch.empty((nb, _up(T, 4)), dtype=torch.float32, device=X.device)[:, :T])
-    else:
-        _check_fp8(out, T, K, (nb, T), X.device, "out")
-    _check(lib().cq_fp8_quantize_act(_addr(X), _DT[X.dtype], T, K, ld, _addr(out.codes), _pitch(out.codes, "out.codes"), _addr(out.scale),
-                                     _scale_pitch(out.scale), _raw()), "cq_fp8_quantize_act")
+        out = Fp8Act(_fp8_codes(T, K, X.device), torch.empty_strided((nb, T), (_up(T, 4), 1), dtype=_F32, device=X.device))
+    codes, scale = out
+    _check(lib().cq_fp8_quantize_act(X.data_ptr(), dt, T, K, ld, codes.data_ptr(), _codes_pitch(codes, T, K, dev, "out"), scale.data_ptr(),
+                                     _act_scale_pitch(scale, nb, T, dev, "out"), _raw(dev)), "cq_fp8_quantize_act")
     return out
-
-
-def _scale_pitch(scale: torch.Tensor) -> int:
-    nb, T = scale.shape
-    if nb > 0 and T > 1 and scale.stride(1) != 1:
-        raise ValueError("scales of a block must be contiguous along the rows")
-    return scale.stride(0) if nb > 1 else max(scale.stride(0), _up(T, 4))
 
 
 def fp8_quantize_weight(W: torch.Tensor, *, out: Fp8Weight | None = None) -> Fp8Weight:
     """e4m3 codes of a weight matrix [out channels, in channels], one scale for each block of 128 x 128."""
-    N, K, ld = _matrix_args(W)
-    shape = (-(-N // BLOCK), -(-K // BLOCK))
+    N, K, ld, dt, dev = _matrix16(W)
     if out is None:
-        out = Fp8Weight(_fp8_codes(N, K, W.device), torch.empty(shape, dtype=torch.float32, device=W.device))
-    else:
-        _check_fp8(out, N, K, shape, W.device, "out")
-        if not out.scale.is_contiguous():
-            raise ValueError("out.scale must be contiguous")
-    _check(lib().cq_fp8_quantize_weight(_addr(W), _DT[W.dtype], N, K, ld, _addr(out.codes), _pitch(out.codes, "out.codes"), _addr(out.scale),
-                                        _raw()), "cq_fp8_quantize_weight")
+        out = Fp8Weight(_fp8_codes(N, K, W.device), torch.empty((-(-N // BLOCK), -(-K // BLOCK)), dtype=_F32, device=W.device))
+    codes, scale = out
+    _check_weight_scale(scale, N, K, dev, "out")
+    _check(lib().cq_fp8_quantize_weight(W.data_ptr(), dt, N, K, ld, codes.data_ptr(), _codes_pitch(codes, N, K, dev, "out"), scale.data_ptr(),
+                                        _raw(dev)), "cq_fp8_quantize_weight")
     return out
 
 
-def _product_out(out, M: int, N: int, dtype, device):
+def _product_out(out, M: int, N: int, dtype, like: torch.Tensor):
+    """(result tensor, dtype code, pitch)"""
+    dt = _DT.get(dtype)
+    if dt is None:
+        raise TypeError("expected a float16, bfloat16 or float32 result")
     if out is None:
-        return torch.empty((M, N), dtype=dtype, device=device)
-    if tuple(out.shape) != (M, N) or out.dtype != dtype or out.device != device or (M > 0 and N > 1 and out.stride(1) != 1):
-        raise ValueError(f"out must be a [{M}, {N}] tensor of {dtype} on {device} with contiguous columns")
-    return out
-
-
-def _out_pitch(out: torch.Tensor) -> int:
-    return out.stride(0) if out.shape[0] > 1 else max(out.shape[1], 1)
+        return like.new_empty((M, N), dtype=dtype), dt, max(N, 1)
+    if out.shape != (M, N) or out.dtype != dtype or out.get_device() != like.get_device() or (M > 0 and N > 1 and out.stride(1) != 1):
+        raise ValueError(f"out must be a [{M}, {N}] tensor of {dtype} on {like.device} with contiguous columns")
+    return out, dt, out.stride(0) if M > 1 else max(N, 1)
 
 
 def fp8_matmul(a: Fp8Act, w: Fp8Weight, out_dtype: torch.dtype = torch.bfloat16, *, out: torch.Tensor | None = None) -> torch.Tensor:
     """The product [T, N] of block-quantized activations and weights (fp32 sums, rounded once to out_dtype)."""
     T, K = a.codes.shape
-    N, nb = w.codes.shape[0], -(-K // BLOCK)
-    dev = a.codes.device
-    if not a.codes.is_cuda or out_dtype not in _DT:
-        raise TypeError("expected CUDA tensors and a float16, bfloat16 or float32 result")
-    _check_fp8(a, T, K, (nb, T), dev, "a")
-    _check_fp8(w, N, K, (-(-N // BLOCK), nb), dev, "w")
-    if not w.scale.is_contiguous():
-        raise ValueError("w.scale must be contiguous")
-    out = _product_out(out, T, N, out_dtype, dev)
-    _check(lib().cq_fp8_matmul(_addr(a.codes), _pitch(a.codes, "a.codes"), _addr(a.scale), _scale_pitch(a.scale), _addr(w.codes),
-                               _pitch(w.codes, "w.codes"), _addr(w.scale), T, N, K, _addr(out), _DT[out_dtype], _out_pitch(out), _raw()),
-           "cq_fp8_matmul")
+    N, dev = w.codes.shape[0], a.codes.get_device()
+    if dev < 0:
+        raise TypeError("expected CUDA tensors")
+    lda, ldw = _codes_pitch(a.codes, T, K, dev, "a"), _codes_pitch(w.codes, N, K, dev, "w")
+    lds = _act_scale_pitch(a.scale, -(-K // BLOCK), T, dev, "a")
+    _check_weight_scale(w.scale, N, K, dev, "w")
+    out, dt, ldo = _product_out(out, T, N, out_dtype, a.codes)
+    _check(lib().cq_fp8_matmul(a.codes.data_ptr(), lda, a.scale.data_ptr(), lds, w.codes.data_ptr(), ldw, w.scale.data_ptr(), T, N, K,
+                               out.data_ptr(), dt, ldo, _raw(dev)), "cq_fp8_matmul")
     return out
 
 
 def fp8_linear(X: torch.Tensor, w: Fp8Weight, out_dtype: torch.dtype | None = None, *, out: torch.Tensor | None = None,
                workspace: torch.Tensor | None = None) -> torch.Tensor:
     """X [T, K] through a block-quantized weight: fp8_quantize_act and fp8_matmul in one call."""
-    T, K, ld = _matrix_args(X)
+    T, K, ld, dt, dev = _matrix16(X)
     codes, scale = w
     N = codes.shape[0]
-    dt = out_dtype or X.dtype
-    if dt not in _DT:
-        raise TypeError("expected a float16, bfloat16 or float32 result")
-    _check_fp8(w, N, K, (-(-N // BLOCK), -(-K // BLOCK)), X.device, "w")
-    if not scale.is_contiguous():
-        raise ValueError("w.scale must be contiguous")
-    out = _product_out(out, T, N, dt, X.device)
+    ldw = _codes_pitch(codes, N, K, dev, "w")
+    _check_weight_scale(scale, N, K, dev, "w")
+    out, odt, ldo = _product_out(out, T, N, out_dtype or X.dtype, X)
     L = lib()
     if workspace is None:
-        workspace = torch.empty(L.cq_fp8_linear_workspace_bytes(T, K), dtype=torch.uint8, device=X.device)
-    _check(L.cq_fp8_linear(X.data_ptr(), _DT[X.dtype], T, K, ld, codes.data_ptr(), _pitch(codes, "w.codes"), scale.data_ptr(), N,
-                           out.data_ptr(), _DT[dt], _out_pitch(out), workspace.data_ptr(), workspace.numel(), _raw()), "cq_fp8_linear")
+        workspace = X.new_empty(L.cq_fp8_linear_workspace_bytes(T, K), dtype=torch.uint8)
+    _check(L.cq_fp8_linear(X.data_ptr(), dt, T, K, ld, codes.data_ptr(), ldw, scale.data_ptr(), N, out.data_ptr(), odt, ldo,
+                           workspace.data_ptr(), workspace.numel(), _raw(dev)), "cq_fp8_linear")
     return out
 
 
@@ -663,33 +673,34 @@ class KVCache:
     k_col, v_col       float32 [H, D] channel factors, both or neither
     """
     __slots__ = ("k_codes", "v_codes", "k_scale", "v_scale", "bits", "k_col", "v_col", "pages", "page_size", "heads", "head_dim",
-                 "device", "_args")
+                 "device", "_index", "_args")
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, bits: int = 8, k_col=None, v_col=None):
         if bits not in (4, 8):
             raise CQError(4, "KVCache")
-        if k_codes.dim() != 4:
+        shape = k_codes.shape
+        if len(shape) != 4:
             raise ValueError("codes must be [pages, heads, page_size, head_dim]")
-        pages, H, page, width = k_codes.shape
-        D = width if bits == 8 else 2 * width
-        dev = k_codes.device
-        want = torch.int8 if bits == 8 else torch.uint8
+        pages, H, page, width = shape
+        D, want = (width, torch.int8) if bits == 8 else (2 * width, torch.uint8)
+        dev = k_codes.get_device()
         for t in (k_codes, v_codes):
-            if t.shape != k_codes.shape or t.dtype != want or t.device != dev or not t.is_contiguous():
+            if t.dtype != want or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
                 raise ValueError(f"codes of keys and values must be contiguous {want} tensors of one shape on one device")
+        shape = shape[:3]
         for t in (k_scale, v_scale):
-            if t.shape != (pages, H, page) or t.dtype != torch.float32 or t.device != dev or not t.is_contiguous():
-                raise ValueError(f"scales must be contiguous float32 [{pages}, {H}, {page}] on {dev}")
-        if (k_col is None) != (v_col is None):
-            raise ValueError("channel factors are given for keys and values or for neither")
-        if k_col is not None:
+            if t.dtype != _F32 or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+                raise ValueError(f"scales must be contiguous float32 [{pages}, {H}, {page}] on cuda:{dev}")
+        if k_col is not None or v_col is not None:
+            if k_col is None or v_col is None:
+                raise ValueError("channel factors are given for keys and values or for neither")
             for t in (k_col, v_col):
-                if t.shape != (H, D) or t.dtype != torch.float32 or t.device != dev or not t.is_contiguous():
-                    raise ValueError(f"channel factors must be contiguous float32 [{H}, {D}] on {dev}")
-        if not k_codes.is_cuda:
+                if t.dtype != _F32 or t.shape != (H, D) or not t.is_contiguous() or t.get_device() != dev:
+                    raise ValueError(f"channel factors must be contiguous float32 [{H}, {D}] on cuda:{dev}")
+        if dev < 0:
             raise TypeError("expected CUDA tensors")
         self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.bits = k_codes, v_codes, k_scale, v_scale, bits
-        self.k_col, self.v_col, self.device = k_col, v_col, dev
+        self.k_col, self.v_col, self.device, self._index = k_col, v_col, k_codes.device, dev
         self.pages, self.heads, self.page_size, self.head_dim = pages, H, page, D
         self._args = (k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _addr(k_col), _addr(v_col),
                       bits, pages, page, H, D)
@@ -705,38 +716,42 @@ class KVCache:
         return cls(*codes, *scale, bits, k_col, v_col)
 
 
-def _slots(slots: torch.Tensor, device) -> int:
-    if slots.dim() != 1 or slots.dtype != torch.int64 or slots.device != device or not slots.is_contiguous():
-        raise ValueError(f"slots must be a contiguous int64 vector on {device}")
-    return slots.numel()
+def _slots(slots: torch.Tensor, dev: int) -> int:
+    if slots.dtype != _I64 or slots.dim() != 1 or not slots.is_contiguous() or slots.get_device() != dev:
+        raise ValueError(f"slots must be a contiguous int64 vector on cuda:{dev}")
+    return slots.shape[0]
 
 
 def kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """Quantize keys and values [T, H, D] (float16 / bfloat16; any strides of tokens and heads) into their slots of the cache."""
-    T = _slots(slots, cache.device)
-    shape = (T, cache.heads, cache.head_dim)
-    for t in (k, v):
-        if t.shape != shape or t.dtype != k.dtype or t.dtype not in (torch.float16, torch.bfloat16) or t.device != cache.device:
-            raise ValueError(f"keys and values must be float16 / bfloat16 {shape} on {cache.device}")
-        if T > 0 and t.stride(2) != 1:
-            raise ValueError("head elements must be contiguous")
-    _check(lib().cq_kv_write(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), _DT[k.dtype], T,
-                             slots.data_ptr(), *cache._args, _raw()), "cq_kv_write")
+    dev = cache._index
+    T = _slots(slots, dev)
+    shape, dt = (T, cache.heads, cache.head_dim), _DT16.get(k.dtype)
+    if dt is None or k.shape != shape or v.shape != shape or v.dtype != k.dtype or k.get_device() != dev or v.get_device() != dev:
+        raise ValueError(f"keys and values must be float16 / bfloat16 {shape} on cuda:{dev}")
+    ks, vs = k.stride(), v.stride()
+    if T > 0 and (ks[2] != 1 or vs[2] != 1):
+        raise ValueError("head elements must be contiguous")
+    _check(lib().cq_kv_write(k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], dt, T, slots.data_ptr(), *cache._args, _raw(dev)),
+           "cq_kv_write")
 
 
 def kv_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, *, out=None):
     """(keys, values) [L, H, D] that the slots stand for; `out` = a pair of tensors to fill."""
-    n = _slots(slots, cache.device)
-    shape = (n, cache.heads, cache.head_dim)
-    if dtype not in _DT:
+    dev = cache._index
+    n = _slots(slots, dev)
+    shape, dt = (n, cache.heads, cache.head_dim), _DT.get(dtype)
+    if dt is None:
         raise TypeError("expected a float16, bfloat16 or float32 result")
     if out is None:
-        out = (torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device))
-    for t in out:
-        if t.shape != shape or t.dtype != dtype or t.device != cache.device or not t.is_contiguous():
-            raise ValueError(f"out must be two contiguous {dtype} tensors {shape} on {cache.device}")
-    _check(lib().cq_kv_read(*cache._args, n, slots.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), _DT[dtype], _raw()), "cq_kv_read")
-    return out
+        k, v = cache.k_scale.new_empty(shape, dtype=dtype), cache.k_scale.new_empty(shape, dtype=dtype)
+    else:
+        k, v = out
+        for t in out:
+            if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+                raise ValueError(f"out must be two contiguous {dtype} tensors {shape} on cuda:{dev}")
+    _check(lib().cq_kv_read(*cache._args, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), dt, _raw(dev)), "cq_kv_read")
+    return k, v
 
 
 def kv_attention_workspace_bytes(head_dim: int) -> int:
@@ -749,31 +764,32 @@ def kv_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, lens
 
     page_table int32 [B, pages], lens int32 [B] (tokens of each sequence, those of q included).  `scale` multiplies the
     logits (default 1 / sqrt(D)); `lse` float32 [B, Lq, Hq] receives the logarithm of the softmax's sum."""
-    dev, D = cache.device, cache.head_dim
-    if q.dim() != 4 or q.dtype not in (torch.float16, torch.bfloat16) or q.device != dev or q.shape[3] != D:
-        raise ValueError(f"q must be float16 / bfloat16 [B, Lq, Hq, {D}] on {dev}")
-    B, Lq, Hq, _ = q.shape
-    if q.numel() > 0 and q.stride(3) != 1:
+    dev, D, dt, shape = cache._index, cache.head_dim, _DT16.get(q.dtype), q.shape
+    if dt is None or len(shape) != 4 or shape[3] != D or q.get_device() != dev:
+        raise ValueError(f"q must be float16 / bfloat16 [B, Lq, Hq, {D}] on cuda:{dev}")
+    B, Lq, Hq, _ = shape
+    qs = q.stride()
+    if qs[3] != 1 and B * Lq * Hq > 0:
         raise ValueError("head elements must be contiguous")
-    if page_table.dim() != 2 or page_table.shape[0] != B or page_table.dtype != torch.int32 or page_table.device != dev or \
-            (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-        raise ValueError(f"page_table must be int32 [{B}, pages] on {dev} with contiguous rows")
-    if lens.dim() != 1 or lens.shape[0] != B or lens.dtype != torch.int32 or lens.device != dev or not lens.is_contiguous():
-        raise ValueError(f"lens must be a contiguous int32 vector of {B} on {dev}")
+    if page_table.dtype != _I32 or page_table.dim() != 2 or page_table.shape[0] != B or page_table.get_device() != dev:
+        raise ValueError(f"page_table must be int32 [{B}, pages] on cuda:{dev}")
+    width, (row, inner) = page_table.shape[1], page_table.stride()
+    if inner != 1 and width > 1:
+        raise ValueError("rows of page_table must be contiguous")
+    if lens.dtype != _I32 or lens.shape != (B,) or not lens.is_contiguous() or lens.get_device() != dev:
+        raise ValueError(f"lens must be a contiguous int32 vector of {B} on cuda:{dev}")
     if out is None:
-        out = torch.empty((B, Lq, Hq, D), dtype=q.dtype, device=dev)
-    elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or not out.is_contiguous():
+        out = q.new_empty(shape)
+    elif out.shape != shape or out.dtype != q.dtype or out.get_device() != dev or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's shape and dtype")
-    if lse is not None and (lse.shape != q.shape[:3] or lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous()):
+    if lse is not None and (lse.shape != shape[:3] or lse.dtype != _F32 or lse.get_device() != dev or not lse.is_contiguous()):
         raise ValueError("lse must be a contiguous float32 [B, Lq, Hq] tensor")
     L = lib()
     if workspace is None:
-        workspace = torch.empty(L.cq_kv_attention_workspace_bytes(D), dtype=torch.uint8, device=dev)
-    width = page_table.shape[1]
-    _check(L.cq_kv_attention(q.data_ptr(), _DT[q.dtype], q.stride(0), q.stride(1), q.stride(2), B, Lq, Hq, *cache._args,
-                             page_table.data_ptr(), width, page_table.stride(0) if B > 1 else width, lens.data_ptr(),
-                             D ** -0.5 if scale is None else float(scale), out.data_ptr(), _addr(lse), workspace.data_ptr(),
-                             workspace.numel(), _raw()), "cq_kv_attention")
+        workspace = q.new_empty(L.cq_kv_attention_workspace_bytes(D), dtype=torch.uint8)
+    _check(L.cq_kv_attention(q.data_ptr(), dt, qs[0], qs[1], qs[2], B, Lq, Hq, *cache._args, page_table.data_ptr(), width,
+                             row if B > 1 else width, lens.data_ptr(), D ** -0.5 if scale is None else float(scale), out.data_ptr(), _addr(lse),
+                             workspace.data_ptr(), workspace.numel(), _raw(dev)), "cq_kv_attention")
     return out
 
 

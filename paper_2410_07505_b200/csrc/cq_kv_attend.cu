@@ -188,10 +188,10 @@ struct AttendShape {
     static constexpr int kRow = D * BITS / 8;                   // bytes of a token's codes
     static constexpr int kTile = kUnit * kRow;                  // of a unit's keys or values
     static constexpr int kRows = 8 * NT;
-    static constexpr int kPerSm = NT == 1 ? 3 : NT == 2 ? 2 : 1;
-    static constexpr int kStages = kPerSm == 3 ? (D * BITS == 1024 ? 3 : 6) : kPerSm == 2 ? (D * BITS == 1024 ? 5 : 8) : 8;
+    static constexpr int kPerSm = NT == 1 ? 3 : NT <= 3 ? 2 : 1;
+    static constexpr int kStages = D * BITS == 1024 ? (kPerSm == 1 ? 6 : kPerSm == 2 ? 4 : 3) : (kPerSm == 3 ? 5 : 8);
     static constexpr int kPitch = D + 2;                        // floats of a joined row: pairs of lanes' stores meet two to a bank
-    static constexpr size_t kSmem = 1024 + size_t(kStages) * (2 * kTile + 2 * kUnit * 4) + size_t(2) * kRows * kPitch * 4;
+    static constexpr size_t kSmem = 1024 + size_t(kStages) * (2 * kTile + 2 * kUnit * 4) + size_t(kRows) * D * 2 + size_t(2) * kRows * kPitch * 4;
 };
 
 // ---- units of a CTA -------------------------------------------------------------------------------
@@ -204,9 +204,13 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     float* s_scale = reinterpret_cast<float*>(smem + ST * 2 * S::kTile);       // [stage][keys, values][64]
-    float* s_o = s_scale + ST * 2 * kUnit;                                     // [2][ROWS][PITCH]
+    uint4* s_q = reinterpret_cast<uint4*>(s_scale + ST * 2 * kUnit);           // [tile of rows][two steps][lane]
+    float* s_o = reinterpret_cast<float*>(s_q + NT * (KK / 2) * 32);           // [2][ROWS][PITCH]
     __shared__ uint64_t full[ST], empty[ST];
     __shared__ unsigned s_boxes[ST];                                            // boxes of the unit that are there
+    __shared__ __align__(16) float s_start[ROWS];                               // of the group's rows: start of logits' sums,
+    __shared__ float s_fac[ROWS];                                               // their factor
+    __shared__ int s_last[ROWS];                                                // and the last token that the row sees
     __shared__ float s_m[kAttWarps][ROWS], s_l[kAttWarps][ROWS], s_top[ROWS], s_sum[ROWS];
     __shared__ volatile uint32_t s_dead;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, r4 = lane & 3;
@@ -296,13 +300,11 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         const int first_tile = at.tile, tiles = at.tiles, len = at.len, b = at.b;
         const int n_units = (at.same_group(end) ? end.tile : tiles) - first_tile;
         const int R = p.G * p.Lq;
-        uint32_t qf[NT][KK][2];
-        float fac[NT][2], start[NT][2];                         // of rows 2 r4, 2 r4 + 1: factor of logits, start of their sums
-        int last[NT][2];                                        // and the last token that they see
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        // The queries as the products want them, once for all warps: tile nt of eight rows is warp nt's.  They stay in shared
+        // memory (two steps of a lane in 16 bytes): registers for them would cost a resident CTA.
+        if (warp < NT) {
             // this lane: a quarter of row g8, the elements that it meets in the keys
-            const int row = rt * ROWS + nt * 8 + g8;
+            const int row = rt * ROWS + warp * 8 + g8;
             const int i = row / p.G, g = row - i * p.G;
             const bool there = row < R;
             const uint16_t* src = static_cast<const uint16_t*>(p.q) + b * p.qb + i * p.ql + static_cast<int64_t>(head * p.G + g) * p.qh + r4 * (D / 4);
@@ -336,31 +338,39 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             const float up = pow2i(up_exp);
             float sum = 0.0f;                                   // of the rounded elements, whichever units they are held in
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                if constexpr (BITS == 8) {
-                    qf[nt][kk][0] = pack_half2(v[4 * kk] * up, v[4 * kk + 1] * up);
-                    qf[nt][kk][1] = pack_half2(v[4 * kk + 2] * up, v[4 * kk + 3] * up);
-                    sum += unpack_half_lo(qf[nt][kk][0]) + unpack_half_hi(qf[nt][kk][0]) + unpack_half_lo(qf[nt][kk][1]) + unpack_half_hi(qf[nt][kk][1]);
-                } else {
-                    // nibbles (0, 4 | 1, 5) of a word in even steps, (2, 6 | 3, 7) in odd ones; the second pair comes in sixteenfold
-                    const int e = (kk >> 1) * 8 + (kk & 1) * 2;
-                    qf[nt][kk][0] = pack_half2(v[e] * up, v[e + 4] * up);
-                    qf[nt][kk][1] = pack_half2(v[e + 1] * up * 0.0625f, v[e + 5] * up * 0.0625f);
-                    sum += unpack_half_lo(qf[nt][kk][0]) + unpack_half_hi(qf[nt][kk][0]) + 16.0f * (unpack_half_lo(qf[nt][kk][1]) + unpack_half_hi(qf[nt][kk][1]));
+            for (int k2 = 0; k2 < KK / 2; ++k2) {
+                uint32_t f[4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int kk = 2 * k2 + h;
+                    if constexpr (BITS == 8) {
+                        f[2 * h] = pack_half2(v[4 * kk] * up, v[4 * kk + 1] * up);
+                        f[2 * h + 1] = pack_half2(v[4 * kk + 2] * up, v[4 * kk + 3] * up);
+                        sum += unpack_half_lo(f[2 * h]) + unpack_half_hi(f[2 * h]) + unpack_half_lo(f[2 * h + 1]) + unpack_half_hi(f[2 * h + 1]);
+                    } else {
+                        // nibbles (0, 4 | 1, 5) of a word in even steps, (2, 6 | 3, 7) in odd ones; the second pair comes in sixteenfold
+                        const int e = k2 * 8 + h * 2;
+                        f[2 * h] = pack_half2(v[e] * up, v[e + 4] * up);
+                        f[2 * h + 1] = pack_half2(v[e + 1] * up * 0.0625f, v[e + 5] * up * 0.0625f);
+                        sum += unpack_half_lo(f[2 * h]) + unpack_half_hi(f[2 * h]) + 16.0f * (unpack_half_lo(f[2 * h + 1]) + unpack_half_hi(f[2 * h + 1]));
+                    }
                 }
+                s_q[(warp * (KK / 2) + k2) * 32 + lane] = make_uint4(f[0], f[1], f[2], f[3]);
             }
             sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
             sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-            const float my_fac = pow2i(-up_exp) * p.softmax_scale * (kLog2e * 16777216.0f);       // codes come in as 2^-24
-            const float my_start = -sum * (kBias / 16777216.0f);
-            const int my_last = there ? len - p.Lq + i : -1;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int from = (2 * r4 + e) * 4;
-                fac[nt][e] = __shfl_sync(0xFFFFFFFFu, my_fac, from);
-                start[nt][e] = __shfl_sync(0xFFFFFFFFu, my_start, from);
-                last[nt][e] = __shfl_sync(0xFFFFFFFFu, my_last, from);
+            if (r4 == 0) {
+                s_fac[warp * 8 + g8] = pow2i(-up_exp) * p.softmax_scale * (kLog2e * 16777216.0f);       // codes come in as 2^-24
+                s_start[warp * 8 + g8] = -sum * (kBias / 16777216.0f);
+                s_last[warp * 8 + g8] = there ? len - p.Lq + i : -1;
             }
+        }
+        warps_barrier();
+        float fac[NT][2];                                       // of rows 2 r4, 2 r4 + 1: factor of logits
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            fac[nt][0] = s_fac[nt * 8 + 2 * r4];
+            fac[nt][1] = s_fac[nt * 8 + 2 * r4 + 1];
         }
         // results of channels g8 * D/8 + 2 t, + 1 (elements 0 1 | 2 3) and rows 2 r4, 2 r4 + 1
         float o[NT][MT][4], ref[NT][2], l[NT][2];               // ref: references, in base 2
@@ -390,11 +400,12 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 float s[NT][4];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    s[nt][0] = s[nt][2] = start[nt][0];
-                    s[nt][1] = s[nt][3] = start[nt][1];
+                    const float2 first = *reinterpret_cast<const float2*>(s_start + nt * 8 + 2 * r4);
+                    s[nt][0] = s[nt][2] = first.x;
+                    s[nt][1] = s[nt][3] = first.y;
                 }
                 constexpr int kWords = RB / 16;                // words of a lane and token: a quarter of the row
-                uint32_t w[2][kWords];
+                uint32_t w[2][kWords], qf[NT][2][2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if constexpr (kWords >= 4) {
@@ -411,19 +422,31 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
 #pragma unroll
                 for (int j = 0; j < kWords; ++j) {
                     if constexpr (BITS == 8) {
+                        if ((j & 1) == 0) {
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                const uint4 t = s_q[(nt * (KK / 2) + j / 2) * 32 + lane];
+                                qf[nt][0][0] = t.x; qf[nt][0][1] = t.y; qf[nt][1][0] = t.z; qf[nt][1][1] = t.w;
+                            }
+                        }
                         const uint32_t x0 = w[0][j] ^ 0x80808080u, x1 = w[1][j] ^ 0x80808080u;         // two's complement -> biased
                         const uint32_t a0 = __byte_perm(x0, 0, 0x4140), a1 = __byte_perm(x1, 0, 0x4140);
                         const uint32_t a2 = __byte_perm(x0, 0, 0x4342), a3 = __byte_perm(x1, 0, 0x4342);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][j]);
+                        for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][j & 1]);
                     } else {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint4 t = s_q[(nt * (KK / 2) + j) * 32 + lane];
+                            qf[nt][0][0] = t.x; qf[nt][0][1] = t.y; qf[nt][1][0] = t.z; qf[nt][1][1] = t.w;
+                        }
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const uint32_t y0 = w[0][j] >> (8 * h), y1 = w[1][j] >> (8 * h);
                             const uint32_t a0 = and_xor(y0, 0x000F000Fu, 0x00080008u), a1 = and_xor(y1, 0x000F000Fu, 0x00080008u);
                             const uint32_t a2 = and_xor(y0, 0x00F000F0u, 0x00800080u), a3 = and_xor(y1, 0x00F000F0u, 0x00800080u);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][2 * j + h]);
+                            for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][h]);
                         }
                     }
                 }
@@ -447,8 +470,9 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            if (tok0 + g8 > last[nt][e]) x[nt][e][0] = -INFINITY;
-                            if (tok0 + g8 + 8 > last[nt][e]) x[nt][e][1] = -INFINITY;
+                            const int last = s_last[nt * 8 + 2 * r4 + e];
+                            if (tok0 + g8 > last) x[nt][e][0] = -INFINITY;
+                            if (tok0 + g8 + 8 > last) x[nt][e][1] = -INFINITY;
                         }
                 }
                 // a product with fac is rounded once, as the reference, and used for all that refers to it: its rounding cancels
@@ -697,7 +721,8 @@ template <int D, int BITS, int NT>
 static int launch_attend(AttendArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t st) {
     using S = AttendShape<D, BITS, NT>;
     static thread_local LaunchMemo memo;
-    int per_sm = resident_ctas(k16_kv_attend<D, BITS, NT>, kAttThreads, S::kSmem, S::kSmem, memo);
+    // (the static shared memory counts towards the 48 KB that need no leave, so leave is asked for in any case)
+    int per_sm = resident_ctas(k16_kv_attend<D, BITS, NT>, kAttThreads, S::kSmem, S::kSmem > 50000 ? S::kSmem : 50000, memo);
     if (per_sm < 1) return CQ_ERR_CUDA;
     if (per_sm > kMaxPerSm) per_sm = kMaxPerSm;
     p.row_tiles = (p.G * p.Lq + S::kRows - 1) / S::kRows;
