@@ -8,9 +8,9 @@
 // cores form the next block while the epilogue warps read the last one.  Tiles arrive by TMA (128-byte swizzle, zero
 // fill past the edges, so odd sizes need no other path); every wait is bounded.
 //
-// Two kernels, chosen by rows of A:
-//   k12_product      tiles of 128 rows of A x 256 rows of W, one persistent CTA an SM; bound by the tensor cores
-//   k13_product_few  the operands swapped (128 rows of W x 16..128 rows of A) and the contraction split over a
+// Two kernels, chosen by the number of rows of A:
+//   k12_product      tiles of 128 rows of A x 256 (or 128) rows of W, one persistent CTA an SM
+//   k13_product_few  the operands swapped (128 rows of W x 16..64 rows of A) and the contraction split over a
 //                    thread-block cluster, joined through distributed shared memory in rank order (no atomics: the
 //                    same bits every time); few rows of A leave the read of W as the bound
 #include "cq_serve.cuh"
@@ -36,13 +36,16 @@ __device__ __forceinline__ void mma_block(uint32_t d, uint64_t a, uint64_t b, ui
 }
 
 // ---- many rows ------------------------------------------------------------------------------------
-constexpr int kTileM = 128, kTileN = 256;
-constexpr int kStages = 4;
+constexpr int kTileM = 128;
 constexpr int kGroupM = 32;                   // tiles of A that share a sweep over W, so that both sides come from L2
 constexpr int kMainThreads = 384;             // warp 0: loads, warp 1: products, warps 4..11: running sums and stores
-constexpr size_t kStageA = kTileM * kBlkK, kStageB = kTileN * kBlkK;
 constexpr size_t kPatch = 4096;               // staging of one warp's 32 rows x 128 bytes of output
-constexpr size_t kMainSmem = kStages * (kStageA + kStageB) + 8 * kPatch + kStages * kTileM * 4 + 128;   // all but 0.9 KB of what a CTA can have
+
+template <int BN> __host__ __device__ constexpr int main_stages() { return BN == 256 ? 4 : 5; }
+template <int BN> __host__ __device__ constexpr size_t main_stage_bytes() { return (size_t(128) + BN) * kBlkK; }
+template <int BN> __host__ __device__ constexpr size_t main_smem() {
+    return main_stages<BN>() * (main_stage_bytes<BN>() + 128 * 4) + 8 * kPatch + 256;
+}
 
 struct MainArgs {
     const float* sa; int64_t lds;             // scales of A, [K blocks][lds]
@@ -61,31 +64,33 @@ __device__ __forceinline__ TilePos tile_at(int64_t t, int mtiles, int ntiles) {
     return {g * kGroupM + static_cast<int>(r % rows), static_cast<int>(r / rows)};
 }
 
-template <int OUT>
+template <int BN, int OUT>
 __global__ void __launch_bounds__(kMainThreads, 1)
 k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapW, const MainArgs p) {
+    constexpr int ST = main_stages<BN>();
+    constexpr size_t kA = size_t(128) * kBlkK, kB = size_t(BN) * kBlkK;
+    constexpr int TB = 512 / BN;              // accumulator buffers in tensor memory
+    constexpr int kCols = BN / 2;             // columns of the tile for each epilogue warp
     // No static shared memory, so that the dynamic part starts on the 1024-byte boundary that the swizzle wants.
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* s_a = smem;
-    uint8_t* s_b = s_a + kStages * kStageA;
-    uint8_t* s_patch = s_b + kStages * kStageB;
+    uint8_t* s_b = s_a + ST * kA;
+    uint8_t* s_patch = s_b + ST * kB;
     float* s_scale = reinterpret_cast<float*>(s_patch + 8 * kPatch);
-    uint64_t* full = reinterpret_cast<uint64_t*>(s_scale + kStages * kTileM);
-    uint64_t* empty = full + kStages;
-    uint64_t* tfull = empty + kStages;
-    uint64_t* tempty = tfull + 2;
-    uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(tempty + 2);
-    volatile uint32_t& s_dead = *(reinterpret_cast<volatile uint32_t*>(tempty + 2) + 1);
-    static_assert((2 * kStages + 4) * 8 + 8 <= 128, "barriers");
-    if ((smem_u32(smem) & 1023u) != 0u) {
-        if (threadIdx.x == 0) atomicExch(&g_fp8_fault, 1u);
-        return;
-    }
+    uint64_t* full = reinterpret_cast<uint64_t*>(s_scale + ST * 128);
+    uint64_t* empty = full + ST;
+    uint64_t* tfull = empty + ST;
+    uint64_t* tempty = tfull + TB;
+    uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(tempty + TB);
+    volatile uint32_t& s_dead = *(reinterpret_cast<volatile uint32_t*>(tempty + TB) + 1);
+    static_assert((2 * ST + 2 * TB) * 8 + 8 <= 256, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+    asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1 + 8); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 8); }
+        if ((smem_u32(smem) & 1023u) != 0u) atomicExch(&g_fp8_fault, 1u);      // cannot be: see above
+        for (int i = 0; i < ST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 8); }
+        for (int i = 0; i < TB; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 8); }
         mbar_init_fence();
         s_dead = 0;
         prefetch_map(&mapA);
@@ -100,85 +105,102 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (warp == 0 && lane == 0) {
-            uint32_t it = 0;
+        if (warp == 0) {
+            int s = 0;
+            uint32_t round = 0, issued = 0;
             bool ok = true;
             asm volatile("griddepcontrol.wait;" ::: "memory");
             for (int64_t t = blockIdx.x; ok && t < ntotal; t += gridDim.x) {
                 const TilePos pos = tile_at(t, p.mtiles, p.ntiles);
                 const int64_t m0 = static_cast<int64_t>(pos.m) * kTileM;
-                const uint32_t sbytes = static_cast<uint32_t>(min(static_cast<int64_t>(kTileM), (p.M - m0 + 3) & ~int64_t(3))) * 4;
-                for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-                    const int s = it % kStages;
-                    if (!(ok = role_wait(&empty[s], ((it / kStages) & 1) ^ 1, &s_dead))) break;
-                    mbar_expect_tx(&full[s], static_cast<uint32_t>(kStageA + kStageB) + sbytes);
-                    tile_load(s_a + s * kStageA, &mapA, kb * kBlkK, static_cast<int32_t>(m0), &full[s]);
-                    tile_load(s_b + s * kStageB, &mapW, kb * kBlkK, pos.n * kTileN, &full[s]);
-                    bulk_load(s_scale + s * kTileM, p.sa + kb * p.lds + m0, sbytes, &full[s]);
+                const uint32_t sbytes = static_cast<uint32_t>(min(int64_t(128), (p.M - m0 + 3) & ~int64_t(3))) * 4;
+                for (int kb = 0; kb < p.kblocks; ++kb) {
+                    if (!(ok = role_wait(&empty[s], round ^ 1u, &s_dead))) break;
+                    if (elect_one()) {
+                        mbar_expect_tx(&full[s], static_cast<uint32_t>(kA + kB) + sbytes);
+                        tile_load(s_a + s * kA, &mapA, kb * kBlkK, static_cast<int32_t>(m0), &full[s]);
+                        tile_load(s_b + s * kB, &mapW, kb * kBlkK, pos.n * BN, &full[s]);
+                        bulk_load(s_scale + s * 128, p.sa + kb * p.lds + m0, sbytes, &full[s]);
+                    }
+                    issued = min(issued + 1, uint32_t(ST));
+                    if (++s == ST) { s = 0; round ^= 1u; }
                 }
             }
             if (!ok)                          // copies still in flight land before the CTA leaves
-                for (uint32_t j = it > kStages ? it - kStages : 0; j < it; ++j)
-                    for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&full[j % kStages], (j / kStages) & 1); ++polls) {}
-        } else if (warp == 1 && lane == 0) {
-            const uint32_t idesc = idesc_fp8(kTileM, kTileN);
-            uint32_t it = 0;
+                for (; issued > 0; --issued) {
+                    if (--s < 0) { s = ST - 1; round ^= 1u; }
+                    for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&full[s], round); ++polls) {}
+                }
+        } else if (warp == 1) {
+            const uint32_t idesc = idesc_fp8(kTileM, BN);
+            const uint64_t desc_a = smem_desc_k128(s_a), desc_b = smem_desc_k128(s_b);
+            int s = 0, b = 0, pending = 0;
+            uint32_t round = 0, turn = 0;
             bool ok = true;
             for (int64_t t = blockIdx.x; ok && t < ntotal; t += gridDim.x) {
-                for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-                    const int s = it % kStages, b = it & 1;
-                    if (!(ok = role_wait(&full[s], (it / kStages) & 1, &s_dead) && role_wait(&tempty[b], ((it / 2) & 1) ^ 1, &s_dead))) break;
+                for (int kb = 0; kb < p.kblocks; ++kb) {
+                    if (!(ok = role_wait(&full[s], round, &s_dead) && role_wait(&tempty[b], turn ^ 1u, &s_dead))) break;
                     tc_fence_after();
-                    mma_block(tmem + b * kTileN, smem_desc_k128(s_a + s * kStageA), smem_desc_k128(s_b + s * kStageB), idesc);
-                    tc_commit(&empty[s]);
-                    tc_commit(&tfull[b]);
+                    if (elect_one()) {
+                        mma_block(tmem + b * BN, desc_a + s * (kA >> 4), desc_b + s * (kB >> 4), idesc);
+                        tc_commit(&tfull[b]);             // (the stage is released by the epilogue, which waits for this)
+                    }
+                    pending = min(pending + 1, TB);
+                    if (++s == ST) { s = 0; round ^= 1u; }
+                    if (++b == TB) { b = 0; turn ^= 1u; }
                 }
             }
-            // the last products of either buffer are waited for by the epilogue; after a wait that gave up, here
+            // the last products of each buffer are waited for by the epilogue; after a wait that gave up, here
             if (!ok)
-                for (uint32_t j = it > 2 ? it - 2 : 0; j < it; ++j)
-                    for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&tfull[j & 1], (j / 2) & 1); ++polls) {}
+                for (; pending > 0; --pending) {
+                    if (--b < 0) { b = TB - 1; turn ^= 1u; }
+                    for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&tfull[b], turn); ++polls) {}
+                }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-        const int ew = warp - 4, half = ew >> 2, q = ew & 3;      // 128 columns and 32 rows of the tile for each warp
+        const int ew = warp - 4, half = ew >> 2, q = ew & 3;      // half of the columns and 32 rows of the CTA's tile for each warp
         const int row = q * 32 + lane;
-        const uint32_t taddr = tmem + (static_cast<uint32_t>(q * 32) << 16) + half * 128;
+        const uint32_t taddr = tmem + (static_cast<uint32_t>(q * 32) << 16) + half * kCols;
         uint8_t* patch = s_patch + ew * kPatch;
         const int64_t nblocks = (p.N + 127) / 128;
-        uint32_t it = 0;
+        int s = 0, b = 0;
+        uint32_t round = 0, turn = 0;
         bool ok = true;
         for (int64_t t = blockIdx.x; ok && t < ntotal; t += gridDim.x) {
             const TilePos pos = tile_at(t, p.mtiles, p.ntiles);
-            const int64_t nb = min(static_cast<int64_t>(pos.n) * 2 + half, nblocks - 1);
+            const int64_t nb = min((static_cast<int64_t>(pos.n) * BN + half * kCols) / 128, nblocks - 1);
             const float* sw = p.sw + nb * p.kblocks;
-            float2 acc[64];
+            float acc[kCols];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.0f, 0.0f);
+            for (int i = 0; i < kCols; ++i) acc[i] = 0.0f;
             float w = __ldg(sw);
-            for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-                const int s = it % kStages, b = it & 1;
+            for (int kb = 0; kb < p.kblocks; ++kb) {
                 const float w_next = __ldg(sw + min(kb + 1, p.kblocks - 1));
-                if (!(ok = role_wait(&tfull[b], (it / 2) & 1, &s_dead) && role_wait(&full[s], (it / kStages) & 1, &s_dead))) break;
+                if (!(ok = role_wait(&tfull[b], turn, &s_dead) && role_wait(&full[s], round, &s_dead))) break;
                 tc_fence_after();
-                const float f = __fmul_rn(s_scale[s * kTileM + row], w);
-                const float2 f2 = make_float2(f, f);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&empty[s]);
                 float v[2][32];
-                tmem_ld32(taddr + b * kTileN, v[0]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    tmem_ld_wait(v[c & 1]);
-                    if (c < 3) tmem_ld32(taddr + b * kTileN + (c + 1) * 32, v[(c + 1) & 1]);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        acc[c * 16 + i] = __ffma2_rn(make_float2(v[c & 1][2 * i], v[c & 1][2 * i + 1]), f2, acc[c * 16 + i]);
-                }
-                tc_fence_before();
+                tmem_ld32(taddr + b * BN, v[0]);
+                const float f = __fmul_rn(s_scale[s * 128 + row], w);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&tempty[b]);
+                if (lane == 0) mbar_arrive(&empty[s]);    // the products have read the stage, and this warp its scales
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) {
+                    tmem_ld_wait(v[c & 1]);
+                    if (c + 1 < kCols / 32) {
+                        tmem_ld32(taddr + b * BN + (c + 1) * 32, v[(c + 1) & 1]);
+                    } else {                  // everything is in registers: the buffer is free
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&tempty[b]);
+                    }
+                    // (scalar multiply-adds: the packed ones run at 0.37 an SM partition and cycle here, these at 0.93)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) acc[c * 32 + i] = __fmaf_rn(v[c & 1][i], f, acc[c * 32 + i]);
+                }
                 w = w_next;
+                if (++s == ST) { s = 0; round ^= 1u; }
+                if (++b == TB) { b = 0; turn ^= 1u; }
             }
             if (!ok) break;
             // through a 4 KB patch of shared memory (a row of 128 bytes for each lane, 16-byte pieces rotated by the row)
@@ -186,22 +208,21 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             constexpr int kElem = OUT == CQ_F32 ? 4 : 2;
             constexpr int kPer = 128 / kElem;                     // columns of one patch
             const int64_t m0 = static_cast<int64_t>(pos.m) * kTileM + q * 32;
-            const int64_t n0 = static_cast<int64_t>(pos.n) * kTileN + half * 128;
+            const int64_t n0 = static_cast<int64_t>(pos.n) * BN + half * kCols;
             uint8_t* out = static_cast<uint8_t*>(p.out);
             const bool whole = (p.ldo * kElem) % 16 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
 #pragma unroll
-            for (int c = 0; c < 128 / kPer; ++c) {
+            for (int c = 0; c < kCols / kPer; ++c) {
                 __syncwarp();
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint4 o;
                     if constexpr (OUT == CQ_F32) {
-                        const float2 a = acc[c * 16 + j * 2], e = acc[c * 16 + j * 2 + 1];
-                        o = make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(e.x), __float_as_uint(e.y));
+                        const float* a = &acc[c * 32 + j * 4];
+                        o = make_uint4(__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(a[2]), __float_as_uint(a[3]));
                     } else {
-                        const float2* a = &acc[c * 32 + j * 4];
-                        o = make_uint4(pack16x2<OUT>(a[0].x, a[0].y), pack16x2<OUT>(a[1].x, a[1].y),
-                                       pack16x2<OUT>(a[2].x, a[2].y), pack16x2<OUT>(a[3].x, a[3].y));
+                        const float* a = &acc[c * 64 + j * 8];
+                        o = make_uint4(pack16x2<OUT>(a[0], a[1]), pack16x2<OUT>(a[2], a[3]), pack16x2<OUT>(a[4], a[5]), pack16x2<OUT>(a[6], a[7]));
                     }
                     *reinterpret_cast<uint4*>(patch + lane * 128 + ((j + lane) & 7) * 16) = o;
                 }
@@ -452,24 +473,35 @@ static int launch_few(const CUtensorMap& a, const CUtensorMap& w, const FewArgs&
     return launch_ex(k13_product_few<BN, OUT>, dim3(grid), kFewThreads, few_smem<BN>(), st, p.split, dependent, a, w, p);
 }
 
+template <int BN, int OUT>
+static int launch_main(const CUtensorMap& a, const CUtensorMap& w, const MainArgs& p, bool dependent, cudaStream_t st) {
+    static thread_local LaunchMemo memo;
+    if (resident_ctas(k12_product<BN, OUT>, kMainThreads, main_smem<BN>(), main_smem<BN>(), memo) < 1) return CQ_ERR_CUDA;
+    const int64_t tiles = static_cast<int64_t>(p.mtiles) * p.ntiles;
+    const int sms = sm_count();
+    const unsigned grid = static_cast<unsigned>(tiles < sms ? tiles : sms);
+    return launch_ex(k12_product<BN, OUT>, dim3(grid), kMainThreads, main_smem<BN>(), st, 1, dependent, a, w, p);
+}
+
 template <int OUT>
 static int launch_product(const void* A, int64_t lda, const float* sa, int64_t lds, const void* W, int64_t ldw, const float* sw,
                           int64_t M, int64_t N, int64_t K, void* out, int64_t ldo, bool dependent, cudaStream_t st) {
     const int kblocks = static_cast<int>((K + kBlkK - 1) / kBlkK);
     const int sms = sm_count();
-    const int64_t main_tiles = ((M + kTileM - 1) / kTileM) * ((N + kTileN - 1) / kTileN);
     CUtensorMap mapA, mapW;
-    if (M > 128 && main_tiles * 2 > sms) {
-        if (!make_byte_map(&mapA, A, K, M, lda, kBlkK, kTileM, CU_TENSOR_MAP_SWIZZLE_128B) ||
-            !make_byte_map(&mapW, W, K, N, ldw, kBlkK, kTileN, CU_TENSOR_MAP_SWIZZLE_128B)) return CQ_ERR_CUDA;
-        static thread_local LaunchMemo memo;
-        if (resident_ctas(k12_product<OUT>, kMainThreads, kMainSmem, kMainSmem, memo) < 1) return CQ_ERR_CUDA;
-        const MainArgs p{sa, lds, sw, out, ldo, M, N, kblocks, static_cast<int>((M + kTileM - 1) / kTileM),
-                         static_cast<int>((N + kTileN - 1) / kTileN)};
-        const unsigned grid = static_cast<unsigned>(main_tiles < sms ? main_tiles : sms);
-        return launch_ex(k12_product<OUT>, dim3(grid), kMainThreads, kMainSmem, st, 1, dependent, mapA, mapW, p);
+    if (M > 64) {
+        const int64_t mt = (M + kTileM - 1) / kTileM, wide = mt * ((N + 255) / 256), narrow = mt * ((N + 127) / 128);
+        // rounds of all SMs times the cost of a block in a tile of either width
+        const bool use_wide = ((wide + sms - 1) / sms) * 3 < ((narrow + sms - 1) / sms) * 2;
+        const int bn = use_wide ? 256 : 128;
+        if (mt * ((N + bn - 1) / bn) > (int64_t(1) << 40)) return CQ_ERR_SHAPE;
+        if (!make_byte_map(&mapA, A, K, M, lda, kBlkK, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+            !make_byte_map(&mapW, W, K, N, ldw, kBlkK, bn, CU_TENSOR_MAP_SWIZZLE_128B)) return CQ_ERR_CUDA;
+        const MainArgs p{sa, lds, sw, out, ldo, M, N, kblocks, static_cast<int>(mt), static_cast<int>((N + bn - 1) / bn)};
+        return use_wide ? launch_main<256, OUT>(mapA, mapW, p, dependent, st)
+                        : launch_main<128, OUT>(mapA, mapW, p, dependent, st);
     }
-    const int bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const int bn = M <= 16 ? 16 : M <= 32 ? 32 : 64;
     const int mtiles = static_cast<int>((M + bn - 1) / bn);
     const int64_t ntiles = (N + kFewW - 1) / kFewW;
     if (ntiles * mtiles > (1 << 26)) return CQ_ERR_SHAPE;
@@ -482,8 +514,7 @@ static int launch_product(const void* A, int64_t lda, const float* sa, int64_t l
     switch (bn) {
         case 16: return launch_few<16, OUT>(mapA, mapW, p, nt, dependent, st);
         case 32: return launch_few<32, OUT>(mapA, mapW, p, nt, dependent, st);
-        case 64: return launch_few<64, OUT>(mapA, mapW, p, nt, dependent, st);
-        default: return launch_few<128, OUT>(mapA, mapW, p, nt, dependent, st);
+        default: return launch_few<64, OUT>(mapA, mapW, p, nt, dependent, st);
     }
 }
 

@@ -60,14 +60,23 @@ __device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
     return done != 0;
 }
 // Bounded wait of one role of a CTA whose roles wait for one another: gives up after ~2^21 polls (about a second),
-// or as soon as another role has given up (*dead), and then marks the CTA dead.
-__device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* dead) {
+// or as soon as another role has given up (*dead), and then marks the CTA dead.  The first poll, which usually succeeds,
+// stands by itself: the roles that feed the tensor cores count their instructions.
+__device__ __forceinline__ bool role_wait_long(uint64_t* bar, uint32_t parity, volatile uint32_t* dead) {
     for (uint32_t polls = 0; polls < (1u << 21); ++polls) {
         if (mbar_try(bar, parity)) return true;
         if ((polls & 255u) == 255u && *dead != 0u) return false;
     }
     *dead = 1u;
     return false;
+}
+__device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* dead) {
+    return mbar_try(bar, parity) || role_wait_long(bar, parity, dead);
+}
+__device__ __forceinline__ bool elect_one() {                  // one lane of a converged warp
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0u;
 }
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(bar)) : "memory");
@@ -102,6 +111,7 @@ __device__ __forceinline__ void tc_mma_fp8(uint32_t d, uint64_t a, uint64_t b, u
                  "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
                  :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u) : "memory");
 }
+
 // Operand tile of rows of 128 bytes along the contraction, 128-byte swizzle, eight rows (1024 bytes) per group.
 __device__ __forceinline__ uint64_t smem_desc_k128(const void* tile) {
     const uint64_t addr = smem_u32(tile);
