@@ -63,6 +63,9 @@ __global__ void __launch_bounds__(kThreads)
 k10_fp8_act(const uint4* __restrict__ X, int64_t T, int K8, int64_t ld8, uint8_t* __restrict__ codes, int64_t ldc,
             float* __restrict__ scale, int64_t lds, unsigned col_chunks) {
     __shared__ float s_scale[2 * kActVec][kActRows];
+    // Launched while the kernel before it may still run: everything waits for that one's end.  Only then may the product
+    // be launched, which loads weights ahead of its own wait: whatever wrote them is done by then.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const unsigned chunk = blockIdx.x % col_chunks;
@@ -100,6 +103,7 @@ template <int DT>
 __global__ void __launch_bounds__(kThreads)
 g10_fp8_act(const uint16_t* __restrict__ X, int64_t T, int64_t K, int64_t ld, uint8_t* __restrict__ codes, int64_t ldc,
             float* __restrict__ scale, int64_t lds, int64_t nblk) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");            // as above
     asm volatile("griddepcontrol.launch_dependents;");
     const int lane = threadIdx.x & 31;
     const int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
@@ -197,16 +201,16 @@ int fp8_quantize_act_impl(const void* X, int dtype, int64_t T, int64_t K, int64_
         const int64_t blocks = chunks * ((T + kActRows - 1) / kActRows);
         if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
         auto kern = dtype == CQ_F16 ? k10_fp8_act<CQ_F16> : k10_fp8_act<CQ_BF16>;
-        kern<<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(static_cast<const uint4*>(X), T, static_cast<int>(K / 8), ld / 8, c, ldc,
-                                                                 scale, lds, static_cast<unsigned>(chunks));
+        return launch_ex(kern, dim3(static_cast<unsigned>(blocks)), kThreads, 0, st, 1, !tuning_no_pdl(), static_cast<const uint4*>(X), T,
+                         static_cast<int>(K / 8), ld / 8, c, ldc, scale, lds, static_cast<unsigned>(chunks));
     } else {
         const int64_t nblk = (K + kBlk - 1) / kBlk;
         const int64_t blocks = (T * nblk + kThreads / 32 - 1) / (kThreads / 32);
         if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
         auto kern = dtype == CQ_F16 ? g10_fp8_act<CQ_F16> : g10_fp8_act<CQ_BF16>;
-        kern<<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(static_cast<const uint16_t*>(X), T, K, ld, c, ldc, scale, lds, nblk);
+        return launch_ex(kern, dim3(static_cast<unsigned>(blocks)), kThreads, 0, st, 1, !tuning_no_pdl(), static_cast<const uint16_t*>(X), T, K,
+                         ld, c, ldc, scale, lds, nblk);
     }
-    return launch_status();
 }
 
 }  // namespace cq

@@ -261,15 +261,19 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 }
 
 // ---- few rows -------------------------------------------------------------------------------------
-constexpr int kFewThreads = 192;              // warps 0..3: running sums, warp 4: loads, warp 5: products
+// first warps: running sums (four, or eight that halve 64 columns between them); then one for loads, one for products
+template <int BN> __host__ __device__ constexpr int few_sum_warps() { return BN == 64 ? 8 : 4; }
+template <int BN> __host__ __device__ constexpr int few_threads() { return 32 * (few_sum_warps<BN>() + 2); }
+template <int BN> __host__ __device__ constexpr int few_per_sm() { return BN == 64 ? 2 : 3; }
 constexpr int kFewW = 128;                    // rows of W in a tile
+template <int BN> __host__ __device__ constexpr int few_buffers() { return 4; }    // accumulators: all CTAs of an SM stay within 512 columns
 
-template <int BN> __host__ __device__ constexpr int few_stages() { return BN <= 64 ? (BN <= 32 ? 5 : 4) : 3; }
+template <int BN> __host__ __device__ constexpr int few_stages() { return BN == 32 ? 3 : 4; }
 template <int BN> __host__ __device__ constexpr size_t few_stage_bytes() { return size_t(kFewW) * kBlkK + size_t(BN) * kBlkK; }
 template <int BN> __host__ __device__ constexpr size_t few_smem() {
     return 1024 + few_stages<BN>() * (few_stage_bytes<BN>() + BN * 4);
 }
-template <int BN> __host__ __device__ constexpr uint32_t few_cols() { return 2 * BN < 32 ? 32 : 2 * BN; }
+template <int BN> __host__ __device__ constexpr uint32_t few_cols() { return few_buffers<BN>() * BN; }
 
 struct FewArgs {
     const float* sa; int64_t lds;
@@ -292,9 +296,11 @@ __device__ __forceinline__ void cluster_sync_all() {
 }
 
 template <int BN, int OUT>
-__global__ void __launch_bounds__(kFewThreads)
+__global__ void __launch_bounds__(few_threads<BN>(), few_per_sm<BN>())
 k13_product_few(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapW, const FewArgs p) {
-    constexpr int kSt = few_stages<BN>();
+    constexpr int kSt = few_stages<BN>(), kFewBuffers = few_buffers<BN>(), EW = few_sum_warps<BN>(), kThr = few_threads<BN>();
+    constexpr int kCols = BN * 4 / EW;                             // columns of each summing warp
+    static_assert(few_per_sm<BN>() * few_cols<BN>() <= 512, "tensor memory");
     constexpr size_t kB = size_t(BN) * kBlkK;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -302,7 +308,7 @@ k13_product_few(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     uint8_t* s_x = s_w + kSt * size_t(kFewW) * kBlkK;              // [stage][BN][128]
     float* s_scale = reinterpret_cast<float*>(s_x + kSt * kB);     // [stage][BN]
     float* s_part = reinterpret_cast<float*>(smem);                // [BN][128], over the stages once they are done with
-    __shared__ uint64_t full[kSt], empty[kSt], tfull[2], tempty[2];
+    __shared__ uint64_t full[kSt], empty[kSt], tfull[kFewBuffers], tempty[kFewBuffers];
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_dead;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -315,96 +321,110 @@ k13_product_few(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     const int kb1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (rank + 1) / p.split);
     const int count = kb1 - kb0;
 
+    asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kSt; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1 + 4); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
+        for (int i = 0; i < kSt; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], EW); }
+        for (int i = 0; i < kFewBuffers; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], EW); }
         mbar_init_fence();
         s_dead = 0;
     }
-    if (warp == 5) tmem_alloc(&s_tmem, few_cols<BN>());
+    if (warp == EW + 1) tmem_alloc(&s_tmem, few_cols<BN>());
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
 
-    float acc[BN];
-    if (warp == 4) {
-        if (lane == 0) {
-            const uint32_t sbytes = static_cast<uint32_t>(min(static_cast<int64_t>(BN), (p.M - m0 + 3) & ~int64_t(3))) * 4;
-            bool ok = true;
-            // the weights do not depend on the kernel before this one: their first tiles are on the way before its end
-            const int head = min(kSt, count);
+    float acc[kCols];
+    if (warp == EW) {
+        const uint32_t sbytes = static_cast<uint32_t>(min(static_cast<int64_t>(BN), (p.M - m0 + 3) & ~int64_t(3))) * 4;
+        bool ok = true;
+        // the weights do not depend on the kernel before this one: their first tiles are on the way before its end
+        const int head = min(kSt, count);
+        if (elect_one())
             for (int i = 0; i < head; ++i) {
                 mbar_expect_tx(&full[i], static_cast<uint32_t>(few_stage_bytes<BN>()) + sbytes);
                 tile_load(s_w + i * size_t(kFewW) * kBlkK, &mapW, (kb0 + i) * kBlkK, static_cast<int32_t>(n0), &full[i]);
             }
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            int it = 0;
-            for (; it < count; ++it) {
-                const int s = it % kSt, kb = kb0 + it;
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        int it = 0, s = 0;
+        uint32_t round = 0;
+        for (; it < count; ++it) {
+            const int kb = kb0 + it;
+            if (it >= head && !(ok = role_wait(&empty[s], round ^ 1u, &s_dead))) break;
+            if (elect_one()) {
                 if (it >= head) {
-                    if (!(ok = role_wait(&empty[s], ((it / kSt) & 1) ^ 1, &s_dead))) break;
                     mbar_expect_tx(&full[s], static_cast<uint32_t>(few_stage_bytes<BN>()) + sbytes);
                     tile_load(s_w + s * size_t(kFewW) * kBlkK, &mapW, kb * kBlkK, static_cast<int32_t>(n0), &full[s]);
                 }
                 tile_load(s_x + s * kB, &mapA, kb * kBlkK, static_cast<int32_t>(m0), &full[s]);
                 bulk_load(s_scale + s * BN, p.sa + kb * p.lds + m0, sbytes, &full[s]);
             }
-            if (!ok)
-                for (int j = it > kSt ? it - kSt : 0; j < it; ++j)
-                    for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&full[j % kSt], (j / kSt) & 1); ++polls) {}
+            if (++s == kSt) { s = 0; round ^= 1u; }
         }
-    } else if (warp == 5) {
-        if (lane == 0) {
-            const uint32_t idesc = idesc_fp8(kFewW, BN);
-            bool ok = true;
-            int it = 0;
-            for (; it < count; ++it) {
-                const int s = it % kSt, b = it & 1;
-                if (!(ok = role_wait(&full[s], (it / kSt) & 1, &s_dead) && role_wait(&tempty[b], ((it / 2) & 1) ^ 1, &s_dead))) break;
-                tc_fence_after();
-                mma_block(tmem + b * BN, smem_desc_k128(s_w + s * size_t(kFewW) * kBlkK), smem_desc_k128(s_x + s * kB), idesc);
-                tc_commit(&empty[s]);
-                tc_commit(&tfull[b]);
+        if (!ok)                              // copies still in flight land before the CTA leaves
+            for (int j = it > kSt ? it - kSt : 0; j < it; ++j)
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&full[j % kSt], (j / kSt) & 1); ++polls) {}
+    } else if (warp == EW + 1) {
+        const uint32_t idesc = idesc_fp8(kFewW, BN);
+        const uint64_t desc_w = smem_desc_k128(s_w), desc_x = smem_desc_k128(s_x);
+        bool ok = true;
+        int it = 0, s = 0, b = 0;
+        uint32_t round = 0, turn = 0;
+        for (; it < count; ++it) {
+            if (!(ok = role_wait(&full[s], round, &s_dead) && role_wait(&tempty[b], turn ^ 1u, &s_dead))) break;
+            tc_fence_after();
+            if (elect_one()) {
+                mma_block(tmem + b * BN, desc_w + s * ((kFewW * kBlkK) >> 4), desc_x + s * (kB >> 4), idesc);
+                tc_commit(&tfull[b]);         // (the stage is released by the epilogue, which waits for this)
             }
-            if (!ok)
-                for (int j = it > 2 ? it - 2 : 0; j < it; ++j)
-                    for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&tfull[j & 1], (j / 2) & 1); ++polls) {}
+            if (++s == kSt) { s = 0; round ^= 1u; }
+            if (++b == kFewBuffers) { b = 0; turn ^= 1u; }
         }
+        if (!ok)
+            for (int j = it > kFewBuffers ? it - kFewBuffers : 0; j < it; ++j)
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&tfull[j % kFewBuffers], (j / kFewBuffers) & 1); ++polls) {}
     } else {
-        const uint32_t taddr = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+        const int c0 = (warp >> 2) * kCols;
+        const uint32_t taddr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + c0;
         const float* sw = p.sw + nb * p.kblocks;
 #pragma unroll
-        for (int i = 0; i < BN; ++i) acc[i] = 0.0f;
+        for (int i = 0; i < kCols; ++i) acc[i] = 0.0f;
         bool ok = true;
         float w = __ldg(sw + min(kb0, p.kblocks - 1));
+        int s = 0, b = 0;
+        uint32_t round = 0, turn = 0;
         for (int it = 0; it < count; ++it) {
-            const int s = it % kSt, b = it & 1;
             const float w_next = __ldg(sw + min(kb0 + it + 1, p.kblocks - 1));
-            if (!(ok = role_wait(&tfull[b], (it / 2) & 1, &s_dead) && role_wait(&full[s], (it / kSt) & 1, &s_dead))) break;
-            tc_fence_after();
-            const float4* sc = reinterpret_cast<const float4*>(s_scale + s * BN);
-            constexpr int kW = BN < 32 ? 16 : 32;
+            // the block's factors are ready before its product, so that little is left to do between that and the next
+            if (!(ok = role_wait(&full[s], round, &s_dead))) break;
+            const float4* sc = reinterpret_cast<const float4*>(s_scale + s * BN + c0);
+            float f[kCols];
 #pragma unroll
-            for (int c = 0; c < BN / kW; ++c) {
-                float v[kW];
-                if constexpr (kW == 32) tmem_ld32(taddr + b * BN + c * kW, v);
-                else tmem_ld16(taddr + b * BN + c * kW, v);
-                tmem_ld_wait(v);
-#pragma unroll
-                for (int i = 0; i < kW / 4; ++i) {
-                    const float4 f = sc[c * (kW / 4) + i];
-                    const int e = c * kW + 4 * i;
-                    acc[e] = __fmaf_rn(v[4 * i], __fmul_rn(f.x, w), acc[e]);
-                    acc[e + 1] = __fmaf_rn(v[4 * i + 1], __fmul_rn(f.y, w), acc[e + 1]);
-                    acc[e + 2] = __fmaf_rn(v[4 * i + 2], __fmul_rn(f.z, w), acc[e + 2]);
-                    acc[e + 3] = __fmaf_rn(v[4 * i + 3], __fmul_rn(f.w, w), acc[e + 3]);
-                }
+            for (int i = 0; i < kCols / 4; ++i) {
+                const float4 t = sc[i];
+                f[4 * i] = __fmul_rn(t.x, w); f[4 * i + 1] = __fmul_rn(t.y, w);
+                f[4 * i + 2] = __fmul_rn(t.z, w); f[4 * i + 3] = __fmul_rn(t.w, w);
             }
-            tc_fence_before();
+            if (!(ok = role_wait(&tfull[b], turn, &s_dead))) break;
+            tc_fence_after();
             __syncwarp();
-            if (lane == 0) { mbar_arrive(&tempty[b]); mbar_arrive(&empty[s]); }
+            if (lane == 0) mbar_arrive(&empty[s]);    // the products have read the stage, and this warp its scales
+#pragma unroll
+            for (int c = 0; c < kCols / 16; ++c) {
+                float v[16];
+                tmem_ld16(taddr + b * BN + c * 16, v);
+                tmem_ld_wait(v);
+                if (c + 1 == kCols / 16) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&tempty[b]);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[c * 16 + i] = __fmaf_rn(v[i], f[c * 16 + i], acc[c * 16 + i]);
+            }
             w = w_next;
+            if (++s == kSt) { s = 0; round ^= 1u; }
+            if (++b == kFewBuffers) { b = 0; turn ^= 1u; }
         }
     }
     // every product of this CTA has completed (the last buffers were waited for), so the stages may be written over
@@ -412,15 +432,15 @@ k13_product_few(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     __syncthreads();
     tc_fence_after();
     __syncwarp();
-    if (warp == 5) tmem_free(tmem, few_cols<BN>());
-    if (warp < 4) {
+    if (warp == EW + 1) tmem_free(tmem, few_cols<BN>());
+    if (warp < EW) {
 #pragma unroll
-        for (int j = 0; j < BN; ++j) s_part[j * kFewW + threadIdx.x] = acc[j];
+        for (int j = 0; j < kCols; ++j) s_part[((warp >> 2) * kCols + j) * kFewW + (threadIdx.x & 127)] = acc[j];
     }
     cluster_sync_all();
     const int rows = static_cast<int>(min(static_cast<int64_t>(BN), p.M - m0));
     const int j0 = rows * rank / p.split, j1 = rows * (rank + 1) / p.split;
-    for (int idx = threadIdx.x; idx < (j1 - j0) * kFewW; idx += kFewThreads) {
+    for (int idx = threadIdx.x; idx < (j1 - j0) * kFewW; idx += kThr) {
         const int j = j0 + idx / kFewW, n = idx % kFewW;
         const uint32_t at = smem_u32(s_part + j * kFewW + n);
         float sum = 0.0f;
@@ -466,11 +486,19 @@ int fp8_stage_fault(unsigned int* fault_host) {
 }
 
 template <int BN, int OUT>
-static int launch_few(const CUtensorMap& a, const CUtensorMap& w, const FewArgs& p, int ntiles, bool dependent, cudaStream_t st) {
+static int launch_few(const CUtensorMap& a, const CUtensorMap& w, FewArgs p, int64_t ntiles, bool dependent, cudaStream_t st) {
     static thread_local LaunchMemo memo;
-    if (resident_ctas(k13_product_few<BN, OUT>, kFewThreads, few_smem<BN>(), few_smem<BN>(), memo) < 1) return CQ_ERR_CUDA;
-    const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(p.mtiles) * ntiles * p.split);
-    return launch_ex(k13_product_few<BN, OUT>, dim3(grid), kFewThreads, few_smem<BN>(), st, p.split, dependent, a, w, p);
+    if (resident_ctas(k13_product_few<BN, OUT>, few_threads<BN>(), few_smem<BN>(), few_smem<BN>(), memo) < 1) return CQ_ERR_CUDA;
+    // As many parts of the contraction (up to a portable cluster's eight CTAs, two blocks each at least) as one round of
+    // resident CTAs takes, an eighth left for what clusters cannot fill: a second, partial round costs as much as the first
+    // (1 x 8192 x 8192, 64 tiles: 27.4 us with 1 part, 16.4 with 4, 15.2 with 5 or 6, 18.7 with 8).
+    const int64_t tiles = p.mtiles * ntiles;
+    int64_t split = int64_t(few_per_sm<BN>()) * sm_count() * 7 / 8 / tiles;
+    split = split > 8 ? 8 : split;
+    split = split > p.kblocks / 2 ? p.kblocks / 2 : split;
+    p.split = static_cast<int>(split < 1 ? 1 : split);
+    return launch_ex(k13_product_few<BN, OUT>, dim3(static_cast<unsigned>(tiles * p.split)), few_threads<BN>(), few_smem<BN>(), st, p.split,
+                     dependent, a, w, p);
 }
 
 template <int BN, int OUT>
@@ -505,16 +533,13 @@ static int launch_product(const void* A, int64_t lda, const float* sa, int64_t l
     const int mtiles = static_cast<int>((M + bn - 1) / bn);
     const int64_t ntiles = (N + kFewW - 1) / kFewW;
     if (ntiles * mtiles > (1 << 26)) return CQ_ERR_SHAPE;
-    int split = 1;
-    while (split < 8 && ntiles * mtiles * split * 2 <= 2 * sms && kblocks >= split * 2 * 2) split *= 2;
     if (!make_byte_map(&mapA, A, K, M, lda, kBlkK, bn, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_byte_map(&mapW, W, K, N, ldw, kBlkK, kFewW, CU_TENSOR_MAP_SWIZZLE_128B)) return CQ_ERR_CUDA;
-    const FewArgs p{sa, lds, sw, out, ldo, M, N, kblocks, mtiles, split};
-    const int nt = static_cast<int>(ntiles);
+    const FewArgs p{sa, lds, sw, out, ldo, M, N, kblocks, mtiles, 1};
     switch (bn) {
-        case 16: return launch_few<16, OUT>(mapA, mapW, p, nt, dependent, st);
-        case 32: return launch_few<32, OUT>(mapA, mapW, p, nt, dependent, st);
-        default: return launch_few<64, OUT>(mapA, mapW, p, nt, dependent, st);
+        case 16: return launch_few<16, OUT>(mapA, mapW, p, ntiles, dependent, st);
+        case 32: return launch_few<32, OUT>(mapA, mapW, p, ntiles, dependent, st);
+        default: return launch_few<64, OUT>(mapA, mapW, p, ntiles, dependent, st);
     }
 }
 

@@ -11,10 +11,22 @@
 // takes several tokens, so that channel factors are loaded (and inverted) once and all loads are issued first.
 #include "cq_kv.cuh"
 
+#include <type_traits>
+
 namespace cq {
 
-constexpr int kWriteTokens = 2;     // tokens of one thread: write (8 elements of each)
-constexpr int kReadTokens = 4;      // and read (16 elements of each)
+constexpr int kWriteTokens = 2;     // tokens of one thread: write (16 elements of each)
+constexpr int kReadTokens = 4;      // and read (8 elements of each, so that neighbours' stores are neighbours)
+
+// Slots, rows and threads all stay below 2^31, so that divisions are 32-bit (the 64-bit ones took most of the write's time:
+// 64 us for 4096 tokens of 40 heads, against 127 MB); a page size that is a power of two needs none.
+struct PageMap {
+    int size, shift;                // shift < 0: not a power of two
+    __device__ __forceinline__ uint32_t row(uint32_t slot, int H, int h) const {
+        const uint32_t page = shift >= 0 ? slot >> shift : slot / static_cast<uint32_t>(size);
+        return (page * H + h) * size + (slot - page * size);
+    }
+};
 
 struct WriteArgs {
     const uint16_t* x[2];            // keys, values [T][H][D]
@@ -24,8 +36,13 @@ struct WriteArgs {
     const float* col[2];
     const int64_t* slots;
     int64_t T, nslots;
-    int page_size, H, D;
+    PageMap pages;
+    int H;
 };
+
+// (a parameter indexed by a run-time number would be copied to local memory first)
+template <typename P>
+__device__ __forceinline__ P pick(const P (&two)[2], int kv) { return kv != 0 ? two[1] : two[0]; }
 
 // eight elements in the order of memory, as floats would need them, from any 2-byte aligned place
 template <bool VEC>
@@ -64,80 +81,92 @@ __device__ __forceinline__ void codes_of_floats(const float2 (&u)[4], float a, f
     }
 }
 
-template <int DT, int BITS, bool VEC, bool COL>
+template <int D, int DT, int BITS, bool VEC, bool COL>
 __global__ void __launch_bounds__(kThreads)
 k14_kv_write(const WriteArgs p) {
     constexpr float qmaxf = static_cast<float>((1 << (BITS - 1)) - 1);
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int kv = blockIdx.y;
-    const int lanes = p.D >> 3;                               // threads of a row: 8 or 16, an aligned part of a warp
-    const int hv = p.H * lanes;
-    const int64_t gid = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t group = gid / hv;
-    const int at = static_cast<int>(gid - group * hv);
+    constexpr uint32_t lanes = D / 16;                         // threads of a row: 4 or 8, an aligned part of a warp
+    const uint32_t hv = p.H * lanes;
+    const uint32_t gid = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t group = gid / hv, at = gid - group * hv;
     const int h = at / lanes, v = at % lanes;
-    const uint16_t* src = p.x[kv] + h * p.hs[kv] + v * 8;
-    uint4 w[kWriteTokens];
+    const uint16_t* src = pick(p.x, kv) + h * pick(p.hs, kv) + v * 16;
+    uint4 w[kWriteTokens][2];
     int64_t slot[kWriteTokens];
 #pragma unroll
     for (int i = 0; i < kWriteTokens; ++i) {
-        const int64_t t = group * kWriteTokens + i;
-        w[i] = make_uint4(0, 0, 0, 0);
+        const int64_t t = static_cast<int64_t>(group) * kWriteTokens + i;
+        w[i][0] = w[i][1] = make_uint4(0, 0, 0, 0);
         slot[i] = -1;
         if (t < p.T) {
             slot[i] = __ldg(p.slots + t);
-            w[i] = load_row8<VEC>(src + t * p.ts[kv]);
+            w[i][0] = load_row8<VEC>(src + t * pick(p.ts, kv));
+            w[i][1] = load_row8<VEC>(src + t * pick(p.ts, kv) + 8);
         }
     }
-    float2 r[4];
+    float2 r[8];
     if constexpr (COL) {
-        const float4* c = reinterpret_cast<const float4*>(p.col[kv] + static_cast<int64_t>(h) * p.D + v * 8);
-        const float4 c0 = __ldg(c), c1 = __ldg(c + 1);
-        const float cs[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+        const float4* c = reinterpret_cast<const float4*>(pick(p.col, kv) + h * D + v * 16);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            r[k] = make_float2(cs[2 * k] > 0.0f ? __fdiv_rn(1.0f, cs[2 * k]) : 0.0f, cs[2 * k + 1] > 0.0f ? __fdiv_rn(1.0f, cs[2 * k + 1]) : 0.0f);
+        for (int k = 0; k < 4; ++k) {
+            const float4 f = __ldg(c + k);
+            r[2 * k] = make_float2(f.x > 0.0f ? __frcp_rn(f.x) : 0.0f, f.y > 0.0f ? __frcp_rn(f.y) : 0.0f);
+            r[2 * k + 1] = make_float2(f.z > 0.0f ? __frcp_rn(f.z) : 0.0f, f.w > 0.0f ? __frcp_rn(f.w) : 0.0f);
+        }
     }
 #pragma unroll
     for (int i = 0; i < kWriteTokens; ++i) {
-        float2 u[4], y[4];
+        float2 u[2][4], y[2][4];
         float a;
-        const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        uint32_t m = 0;                                       // over bit patterns: NaN is largest
         if constexpr (COL) {
-            uint32_t m = 0;                                   // over bit patterns: NaN is largest
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                u[k] = __fmul2_rn(unpack16x2<DT>(words[k]), r[k]);
-                m = max(m, max(__float_as_uint(u[k].x) & 0x7FFFFFFFu, __float_as_uint(u[k].y) & 0x7FFFFFFFu));
+            for (int q = 0; q < 2; ++q) {
+                const uint32_t words[4] = {w[i][q].x, w[i][q].y, w[i][q].z, w[i][q].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    u[q][k] = __fmul2_rn(unpack16x2<DT>(words[k]), r[4 * q + k]);
+                    m = max(m, max(__float_as_uint(u[q][k].x) & 0x7FFFFFFFu, __float_as_uint(u[q][k].y) & 0x7FFFFFFFu));
+                }
             }
-            for (int off = lanes >> 1; off > 0; off >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
-            a = __fdiv_rn(__uint_as_float(m), qmaxf);
         } else {
-            const uint32_t mm = max_u16x2(max_u16x2(words[0] & 0x7FFF7FFFu, words[1] & 0x7FFF7FFFu),
-                                          max_u16x2(words[2] & 0x7FFF7FFFu, words[3] & 0x7FFF7FFFu));
-            uint32_t m = max(mm & 0xFFFFu, mm >> 16);
-            for (int off = lanes >> 1; off > 0; off >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
-            a = __fdiv_rn(cvt16<DT>(static_cast<uint16_t>(m)), qmaxf);
-        }
-        const float ra = guarded_rcp(a);
-        if (!(a <= 3.402823466e38f)) {
+            uint32_t mm = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = make_float2(kMagic, kMagic);
-        } else if constexpr (COL) {
-            codes_of_floats<BITS>(u, a, ra, y);
-        } else if (ra == ra) {
-            exact_codes_uniform_row8<DT>(w[i], a, ra, y);
-        } else {
-            exact_codes_uniform_slow<DT, BITS>(w[i], a, y);
+            for (int q = 0; q < 2; ++q)
+                mm = max_u16x2(mm, max_u16x2(max_u16x2(w[i][q].x & 0x7FFF7FFFu, w[i][q].y & 0x7FFF7FFFu),
+                                             max_u16x2(w[i][q].z & 0x7FFF7FFFu, w[i][q].w & 0x7FFF7FFFu)));
+            m = max(mm & 0xFFFFu, mm >> 16);
+        }
+        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+        if constexpr (lanes == 8) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
+        a = __fdiv_rn(COL ? __uint_as_float(m) : cvt16<DT>(static_cast<uint16_t>(m)), qmaxf);
+        const float ra = guarded_rcp(a);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            if (!(a <= 3.402823466e38f)) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[q][k] = make_float2(kMagic, kMagic);
+            } else if constexpr (COL) {
+                codes_of_floats<BITS>(u[q], a, ra, y[q]);
+            } else if (ra == ra) {
+                exact_codes_uniform_row8<DT>(w[i][q], a, ra, y[q]);
+            } else {
+                exact_codes_uniform_slow<DT, BITS>(w[i][q], a, y[q]);
+            }
         }
         if (slot[i] < 0 || slot[i] >= p.nslots) continue;
-        const int64_t page = slot[i] / p.page_size;
-        const int64_t row = (page * p.H + h) * p.page_size + (slot[i] - page * p.page_size);
-        if (v == 0) p.scale[kv][row] = a;
+        const uint64_t row = p.pages.row(static_cast<uint32_t>(slot[i]), p.H, h);
+        if (v == 0) pick(p.scale, kv)[row] = a;
         if constexpr (BITS == 8)
-            *reinterpret_cast<uint2*>(p.codes[kv] + row * p.D + v * 8) =
-                make_uint2(pack_int8x4(y[0].x, y[0].y, y[1].x, y[1].y), pack_int8x4(y[2].x, y[2].y, y[3].x, y[3].y));
+            *reinterpret_cast<uint4*>(pick(p.codes, kv) + row * D + v * 16) =
+                make_uint4(pack_int8x4(y[0][0].x, y[0][0].y, y[0][1].x, y[0][1].y), pack_int8x4(y[0][2].x, y[0][2].y, y[0][3].x, y[0][3].y),
+                           pack_int8x4(y[1][0].x, y[1][0].y, y[1][1].x, y[1][1].y), pack_int8x4(y[1][2].x, y[1][2].y, y[1][3].x, y[1][3].y));
         else
-            *reinterpret_cast<uint32_t*>(p.codes[kv] + row * (p.D / 2) + v * 4) = pack_int4x8(y);
+            *reinterpret_cast<uint2*>(pick(p.codes, kv) + row * (D / 2) + v * 8) = make_uint2(pack_int4x8(y[0]), pack_int4x8(y[1]));
     }
 }
 
@@ -146,6 +175,7 @@ struct ReadArgs {
     void* out[2];                    // [L][H][D], dense
     const int64_t* slots;
     int64_t L, nslots;
+    PageMap pages;
 };
 
 // four int8 codes / eight nibbles of a word as floats: the biased code in the low bits of 2^23, minus 2^23 and the bias
@@ -160,91 +190,73 @@ __device__ __forceinline__ void nibbles_to_float8(uint32_t w, float (&f)[8]) {
     for (int e = 0; e < 8; ++e) f[e] = __fadd_rn(__uint_as_float(((b >> (4 * e)) & 0xFu) | 0x4B000000u), -8388616.0f);
 }
 
-template <int OUT, int BITS, bool COL>
+template <int D, int OUT, int BITS, bool COL>
 __global__ void __launch_bounds__(kThreads)
 k15_kv_read(const ReadArgs p) {
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int kv = blockIdx.y;
-    const int lanes = p.c.D >> 4;
-    const int hv = p.c.H * lanes;
-    const int64_t gid = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t group = gid / hv;
-    const int at = static_cast<int>(gid - group * hv);
+    constexpr uint32_t lanes = D / 8;
+    const uint32_t hv = p.c.H * lanes;
+    const uint32_t gid = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t group = gid / hv, at = gid - group * hv;
     const int h = at / lanes, v = at % lanes;
-    if (group * kReadTokens >= p.L) return;
-    uint4 w[kReadTokens];
+    const int64_t t0 = static_cast<int64_t>(group) * kReadTokens;
+    if (t0 >= p.L) return;
+    const int64_t o0 = (t0 * p.c.H + h) * D + v * 8;
+    uint2 w[kReadTokens];
     float a[kReadTokens];
-    bool there[kReadTokens];
     int64_t slot[kReadTokens];
 #pragma unroll
-    for (int i = 0; i < kReadTokens; ++i) slot[i] = group * kReadTokens + i < p.L ? __ldg(p.slots + group * kReadTokens + i) : -1;
+    for (int i = 0; i < kReadTokens; ++i) slot[i] = t0 + i < p.L ? __ldg(p.slots + t0 + i) : -1;
 #pragma unroll
     for (int i = 0; i < kReadTokens; ++i) {
-        there[i] = slot[i] >= 0 && slot[i] < p.nslots;
-        w[i] = make_uint4(0, 0, 0, 0);
+        w[i] = make_uint2(0, 0);
         a[i] = 0.0f;
-        if (there[i]) {
-            const int64_t page = slot[i] / p.c.page_size;
-            const int64_t row = (page * p.c.H + h) * p.c.page_size + (slot[i] - page * p.c.page_size);
-            a[i] = __ldg(p.c.scale[kv] + row);
-            if constexpr (BITS == 8) {
-                w[i] = ld_stream(reinterpret_cast<const uint4*>(p.c.codes[kv] + row * p.c.D + v * 16));
-            } else {
-                const uint2 n = __ldcs(reinterpret_cast<const uint2*>(p.c.codes[kv] + row * (p.c.D / 2) + v * 8));
-                w[i].x = n.x;
-                w[i].y = n.y;
-            }
+        if (slot[i] >= 0 && slot[i] < p.nslots) {
+            const uint64_t row = p.pages.row(static_cast<uint32_t>(slot[i]), p.c.H, h);
+            a[i] = __ldg(pick(p.c.scale, kv) + row);
+            if constexpr (BITS == 8) w[i] = __ldcs(reinterpret_cast<const uint2*>(pick(p.c.codes, kv) + row * D + v * 8));
+            else w[i].x = __ldcs(reinterpret_cast<const uint32_t*>(pick(p.c.codes, kv) + row * (D / 2) + v * 4));
         }
     }
-    float col[16];
+    float col[8];
     if constexpr (COL) {
-        const float4* c = reinterpret_cast<const float4*>(p.c.col[kv] + static_cast<int64_t>(h) * p.c.D + v * 16);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float4 f = __ldg(c + k);
-            col[4 * k] = f.x; col[4 * k + 1] = f.y; col[4 * k + 2] = f.z; col[4 * k + 3] = f.w;
-        }
+        const float4* c = reinterpret_cast<const float4*>(pick(p.c.col, kv) + h * D + v * 8);
+        const float4 f0 = __ldg(c), f1 = __ldg(c + 1);
+        col[0] = f0.x; col[1] = f0.y; col[2] = f0.z; col[3] = f0.w;
+        col[4] = f1.x; col[5] = f1.y; col[6] = f1.z; col[7] = f1.w;
     }
 #pragma unroll
     for (int i = 0; i < kReadTokens; ++i) {
-        const int64_t t = group * kReadTokens + i;
+        const int64_t t = t0 + i;
         if (t >= p.L) break;
-        float x[16];
+        float x[8];
         if constexpr (BITS == 8) {
-            const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+            float f[4];
+            codes_to_float4(w[i].x, f);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float f[4];
-                codes_to_float4(words[k], f);
+            for (int e = 0; e < 4; ++e) x[e] = f[e];
+            codes_to_float4(w[i].y, f);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[4 * k + e] = f[e];
-            }
+            for (int e = 0; e < 4; ++e) x[4 + e] = f[e];
         } else {
-            const uint32_t words[2] = {w[i].x, w[i].y};
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                float f[8];
-                nibbles_to_float8(words[k], f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[8 * k + e] = f[e];
-            }
+            nibbles_to_float8(w[i].x, x);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < 8; ++e) {
             float s = a[i];
             if constexpr (COL) s = __fmul_rn(s, col[e]);
             x[e] = __fmul_rn(x[e], s);
         }
-        const int64_t o = (t * p.c.H + h) * p.c.D + v * 16;
+        const int64_t o = o0 + static_cast<int64_t>(i) * p.c.H * D;
         if constexpr (OUT == CQ_F32) {
-            float4* out = reinterpret_cast<float4*>(static_cast<float*>(p.out[kv]) + o);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) st_stream(out + k, make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]));
+            float4* out = reinterpret_cast<float4*>(static_cast<float*>(pick(p.out, kv)) + o);
+            st_stream(out, make_float4(x[0], x[1], x[2], x[3]));
+            st_stream(out + 1, make_float4(x[4], x[5], x[6], x[7]));
         } else {
-            uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out[kv]) + o);
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-                st_stream(out + k, make_uint4(pack16x2<OUT>(x[8 * k], x[8 * k + 1]), pack16x2<OUT>(x[8 * k + 2], x[8 * k + 3]),
-                                              pack16x2<OUT>(x[8 * k + 4], x[8 * k + 5]), pack16x2<OUT>(x[8 * k + 6], x[8 * k + 7])));
+            st_stream(reinterpret_cast<uint4*>(static_cast<uint16_t*>(pick(p.out, kv)) + o),
+                      make_uint4(pack16x2<OUT>(x[0], x[1]), pack16x2<OUT>(x[2], x[3]), pack16x2<OUT>(x[4], x[5]), pack16x2<OUT>(x[6], x[7])));
         }
     }
 }
@@ -262,26 +274,32 @@ int check_cache(const void* k_codes, const void* v_codes, const void* k_scale, c
     return CQ_OK;
 }
 
-template <int DT, int BITS>
-static void launch_write(const WriteArgs& p, bool vec, dim3 grid, cudaStream_t st) {
+static PageMap page_map(int64_t page_size) {
+    int shift = 0;
+    while ((int64_t(1) << shift) < page_size) ++shift;
+    return {static_cast<int>(page_size), (int64_t(1) << shift) == page_size ? shift : -1};
+}
+
+template <int D, int DT, int BITS>
+static int launch_write(const WriteArgs& p, bool vec, dim3 grid, cudaStream_t st) {
     if (p.col[0] != nullptr) {
-        if (vec) k14_kv_write<DT, BITS, true, true><<<grid, kThreads, 0, st>>>(p);
-        else k14_kv_write<DT, BITS, false, true><<<grid, kThreads, 0, st>>>(p);
+        if (vec) return launch_ex(k14_kv_write<D, DT, BITS, true, true>, grid, kThreads, 0, st, 1, !tuning_no_pdl(), p);
+        else return launch_ex(k14_kv_write<D, DT, BITS, false, true>, grid, kThreads, 0, st, 1, !tuning_no_pdl(), p);
     } else {
-        if (vec) k14_kv_write<DT, BITS, true, false><<<grid, kThreads, 0, st>>>(p);
-        else k14_kv_write<DT, BITS, false, false><<<grid, kThreads, 0, st>>>(p);
+        if (vec) return launch_ex(k14_kv_write<D, DT, BITS, true, false>, grid, kThreads, 0, st, 1, !tuning_no_pdl(), p);
+        else return launch_ex(k14_kv_write<D, DT, BITS, false, false>, grid, kThreads, 0, st, 1, !tuning_no_pdl(), p);
     }
 }
 
-template <int OUT>
-static void launch_read(const ReadArgs& p, int bits, dim3 grid, cudaStream_t st) {
+template <int D, int OUT>
+static int launch_read(const ReadArgs& p, int bits, dim3 grid, cudaStream_t st) {
     const bool col = p.c.col[0] != nullptr;
     if (bits == 8) {
-        if (col) k15_kv_read<OUT, 8, true><<<grid, kThreads, 0, st>>>(p);
-        else k15_kv_read<OUT, 8, false><<<grid, kThreads, 0, st>>>(p);
+        if (col) return launch_ex(k15_kv_read<D, OUT, 8, true>, grid, kThreads, 0, st, 1, !tuning_no_pdl(), p);
+        else return launch_ex(k15_kv_read<D, OUT, 8, false>, grid, kThreads, 0, st, 1, !tuning_no_pdl(), p);
     } else {
-        if (col) k15_kv_read<OUT, 4, true><<<grid, kThreads, 0, st>>>(p);
-        else k15_kv_read<OUT, 4, false><<<grid, kThreads, 0, st>>>(p);
+        if (col) return launch_ex(k15_kv_read<D, OUT, 4, true>, grid, kThreads, 0, st, 1, !tuning_no_pdl(), p);
+        else return launch_ex(k15_kv_read<D, OUT, 4, false>, grid, kThreads, 0, st, 1, !tuning_no_pdl(), p);
     }
 }
 
@@ -307,20 +325,20 @@ int cq_kv_write(const void* K, int64_t k_token_stride, int64_t k_head_stride, co
     p.codes[0] = static_cast<uint8_t*>(k_codes); p.codes[1] = static_cast<uint8_t*>(v_codes);
     p.scale[0] = k_scale; p.scale[1] = v_scale; p.col[0] = k_col; p.col[1] = v_col;
     p.slots = slots; p.T = T; p.nslots = pages * page_size;
-    p.page_size = static_cast<int>(page_size); p.H = static_cast<int>(H); p.D = static_cast<int>(D);
-    const int64_t threads = ((T + kWriteTokens - 1) / kWriteTokens) * H * (D / 8);
+    p.pages = page_map(page_size); p.H = static_cast<int>(H);
+    const int64_t threads = ((T + kWriteTokens - 1) / kWriteTokens) * H * (D / 16);
     const int64_t blocks = (threads + kThreads - 1) / kThreads;
-    if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
+    if (blocks * kThreads > 0x7FFFFFFF) return CQ_ERR_SHAPE;
     const bool vec = ptr_aligned(K, 16) && ptr_aligned(V, 16) &&
                      ((k_token_stride | k_head_stride | v_token_stride | v_head_stride) & 7) == 0;
     const dim3 grid(static_cast<unsigned>(blocks), 2);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == CQ_F16) {
-        if (bits == 8) launch_write<CQ_F16, 8>(p, vec, grid, st); else launch_write<CQ_F16, 4>(p, vec, grid, st);
-    } else {
-        if (bits == 8) launch_write<CQ_BF16, 8>(p, vec, grid, st); else launch_write<CQ_BF16, 4>(p, vec, grid, st);
-    }
-    return launch_status();
+    auto go = [&](auto d, auto dt) {
+        return bits == 8 ? launch_write<d.value, dt.value, 8>(p, vec, grid, st) : launch_write<d.value, dt.value, 4>(p, vec, grid, st);
+    };
+    using std::integral_constant;
+    if (D == 128) return dtype == CQ_F16 ? go(integral_constant<int, 128>{}, integral_constant<int, CQ_F16>{}) : go(integral_constant<int, 128>{}, integral_constant<int, CQ_BF16>{});
+    return dtype == CQ_F16 ? go(integral_constant<int, 64>{}, integral_constant<int, CQ_F16>{}) : go(integral_constant<int, 64>{}, integral_constant<int, CQ_BF16>{});
 }
 
 int cq_kv_read(const void* k_codes, const void* v_codes, const float* k_scale, const float* v_scale, const float* k_col,
@@ -338,15 +356,16 @@ int cq_kv_read(const void* k_codes, const void* v_codes, const float* k_scale, c
     p.c = KvCache{{static_cast<const int8_t*>(k_codes), static_cast<const int8_t*>(v_codes)}, {k_scale, v_scale}, {k_col, v_col},
                   pages, static_cast<int>(page_size), static_cast<int>(H), static_cast<int>(D)};
     p.out[0] = k_out; p.out[1] = v_out; p.slots = slots; p.L = L; p.nslots = pages * page_size;
-    const int64_t threads = ((L + kReadTokens - 1) / kReadTokens) * H * (D / 16);
+    p.pages = page_map(page_size);
+    const int64_t threads = ((L + kReadTokens - 1) / kReadTokens) * H * (D / 8);
     const int64_t blocks = (threads + kThreads - 1) / kThreads;
-    if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
+    if (blocks * kThreads > 0x7FFFFFFF) return CQ_ERR_SHAPE;
     const dim3 grid(static_cast<unsigned>(blocks), 2);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (out_dtype == CQ_F32) launch_read<CQ_F32>(p, bits, grid, st);
-    else if (out_dtype == CQ_F16) launch_read<CQ_F16>(p, bits, grid, st);
-    else launch_read<CQ_BF16>(p, bits, grid, st);
-    return launch_status();
+    if (D == 128) return out_dtype == CQ_F32 ? launch_read<128, CQ_F32>(p, bits, grid, st)
+                       : out_dtype == CQ_F16 ? launch_read<128, CQ_F16>(p, bits, grid, st) : launch_read<128, CQ_BF16>(p, bits, grid, st);
+    return out_dtype == CQ_F32 ? launch_read<64, CQ_F32>(p, bits, grid, st)
+         : out_dtype == CQ_F16 ? launch_read<64, CQ_F16>(p, bits, grid, st) : launch_read<64, CQ_BF16>(p, bits, grid, st);
 }
 
 }  // extern "C"
