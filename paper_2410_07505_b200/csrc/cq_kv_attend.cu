@@ -27,6 +27,8 @@
 // A query row (times kf) is scaled by a power of two into [2^14, 2^15) before it is rounded, so its rounding is 2^-12 of
 // each element; probabilities times va are scaled by 2^10 over a power of two above the largest va seen, so small ones
 // keep 11 bits down to 2^-24 of the reference.  Logits, maxima, sums and results are fp32.
+// A bf16 result hides these roundings (2^-12 and 2^-12 beside 2^-9); an fp16 result does not, so for fp16 (FINE) queries
+// and probabilities go in as two halves each, the second what the first leaves, at twice the products.
 // The running reference of a row is a logit that was the largest when it was taken; it is only renewed, with all sums and
 // results rescaled, when some logit exceeds it by more than 5 in base 2, which probabilities up to 2^5 times 2^10 allow.
 #include "cq_kv.cuh"
@@ -44,14 +46,13 @@ constexpr float kLn2 = 0.6931471805599453f;
 struct AttendArgs {
     const void* q; int64_t qb, ql, qh;          // strides of sequences, tokens and heads, in elements
     int q_vec;                                  // rows of q may be read four elements at a time
-    int bf16;                                   // type of q and out
     const int* table; int64_t table_stride;     // [B][table_stride] page numbers
     const int* lens;                            // [B]
     const float* scale[2];                      // token scales of keys and values
     const float* col[2];
     void* out;                                  // [B][Lq][Hq][D], dense
     float* lse;                                 // [B][Lq][Hq] or null
-    float* part;                                // [2 * CTAs][rows of a tile][D], then [..][2] maxima and sums
+    float* part;                                // [2 * CTAs][rows of a tile][D], then [..][2] maxima and sums, then Split[CTAs]
     float softmax_scale;
     int64_t pages;
     int B, Lq, Hq, H, G, page_size, row_tiles;
@@ -59,6 +60,12 @@ struct AttendArgs {
     int unit_pages, unit_rest;                  // whole pages in a unit of tokens, and what is left
     int64_t capacity;                           // tokens a row of the table can name
 };
+
+// A group that begins in a CTA and ends in a later one: where its sums are to be joined.  parts: 0: there is none.
+struct Split { int b, group, parts, unused; };
+__device__ __forceinline__ Split* splits_of(const AttendArgs& p, int64_t ctas, int rows, int D) {
+    return reinterpret_cast<Split*>(p.part + 2 * ctas * rows * (D + 2));
+}
 
 // ---- the sequence of units ------------------------------------------------------------------------
 __device__ __forceinline__ int seq_len(const AttendArgs& p, int b) {
@@ -69,6 +76,9 @@ __device__ __forceinline__ int tiles_of(int len) { return (len + kUnit - 1) / kU
 
 // Units before sequence `upto` for one head and tile of rows, the groups' leads included; by a whole warp.
 constexpr int kLead = 4;
+// A part has this many places at least: more parts of less than a tile or two would only make more to join (one sequence of
+// 4096 tokens, 8 heads: 19.1 us with 1, 15.4 with 4, 16.9 with 9; 32 heads of 513 tokens: 11.2, 12.0, 15.8).
+constexpr int kLeast = 4;
 __device__ __forceinline__ int span_of(int len) { return len > 0 ? tiles_of(len) + kLead : 0; }
 __device__ __forceinline__ int64_t spans_before(const AttendArgs& p, int upto) {
     const int lane = threadIdx.x & 31;
@@ -171,8 +181,13 @@ __device__ __forceinline__ uint32_t nib_high(uint32_t w) {          // 16 (code 
 }
 __device__ __forceinline__ float unpack_half_lo(uint32_t h) { return __half2float(__ushort_as_half(static_cast<uint16_t>(h & 0xFFFFu))); }
 __device__ __forceinline__ float unpack_half_hi(uint32_t h) { return __half2float(__ushort_as_half(static_cast<uint16_t>(h >> 16))); }
-__device__ __forceinline__ float2 unpack16x2_rt(uint32_t w, int bf16) { return bf16 ? unpack16x2<CQ_BF16>(w) : unpack16x2<CQ_F16>(w); }
-__device__ __forceinline__ uint16_t pack16_rt(float v, int bf16) { return bf16 ? pack16<CQ_BF16>(v) : pack16<CQ_F16>(v); }
+// two floats as fp16, and what that leaves of them
+__device__ __forceinline__ uint32_t split_half2(float& lo, float& hi) {
+    const uint32_t h = pack_half2(lo, hi);
+    lo -= unpack_half_lo(h);
+    hi -= unpack_half_hi(h);
+    return h;
+}
 __device__ __forceinline__ void warps_barrier() { asm volatile("bar.sync 1, %0;" :: "n"(32 * kAttWarps) : "memory"); }   // computing warps
 
 // 16-byte piece `c` of row `r` in a box of rows of RB bytes under the tensor map's swizzle of that width
@@ -183,29 +198,29 @@ __device__ __forceinline__ uint32_t box_at(int r, int c) {
     else return r * 32 + ((c ^ ((r >> 2) & 1)) << 4);
 }
 
-template <int D, int BITS, int NT>
+template <int D, int BITS, int NT, bool FINE>
 struct AttendShape {
     static constexpr int kRow = D * BITS / 8;                   // bytes of a token's codes
     static constexpr int kTile = kUnit * kRow;                  // of a unit's keys or values
     static constexpr int kRows = 8 * NT;
-    static constexpr int kPerSm = NT == 1 ? 3 : NT <= 3 ? 2 : 1;
-    static constexpr int kStages = D * BITS == 1024 ? (kPerSm == 1 ? 6 : kPerSm == 2 ? 4 : 3) : (kPerSm == 3 ? 5 : 8);
+    static constexpr int kPerSm = NT * D <= 128 ? 3 : 2;         // by the registers that results take
+    static constexpr int kStages = D * BITS == 1024 ? (kPerSm == 2 ? 4 : 3) : (kPerSm == 3 ? 5 : 8);
     static constexpr int kPitch = D + 2;                        // floats of a joined row: pairs of lanes' stores meet two to a bank
-    static constexpr size_t kSmem = 1024 + size_t(kStages) * (2 * kTile + 2 * kUnit * 4) + size_t(kRows) * D * 2 + size_t(2) * kRows * kPitch * 4;
+    static constexpr size_t kSmem = 1024 + size_t(kStages) * (2 * kTile + 2 * kUnit * 4) + size_t(kRows) * D * (FINE ? 4 : 2) + size_t(2) * kRows * kPitch * 4;
 };
 
 // ---- units of a CTA -------------------------------------------------------------------------------
-template <int D, int BITS, int NT>
-__global__ void __launch_bounds__(kAttThreads, AttendShape<D, BITS, NT>::kPerSm)
+template <int D, int BITS, int NT, bool FINE>
+__global__ void __launch_bounds__(kAttThreads, AttendShape<D, BITS, NT, FINE>::kPerSm)
 k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const AttendArgs p) {
-    using S = AttendShape<D, BITS, NT>;
+    using S = AttendShape<D, BITS, NT, FINE>;
     constexpr int RB = S::kRow, ST = S::kStages, KK = D / 16, MT = D / 16, ROWS = S::kRows, PITCH = S::kPitch;
     constexpr float kBias = BITS == 8 ? 128.0f : 8.0f;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     float* s_scale = reinterpret_cast<float*>(smem + ST * 2 * S::kTile);       // [stage][keys, values][64]
-    uint4* s_q = reinterpret_cast<uint4*>(s_scale + ST * 2 * kUnit);           // [tile of rows][two steps][lane]
-    float* s_o = reinterpret_cast<float*>(s_q + NT * (KK / 2) * 32);           // [2][ROWS][PITCH]
+    uint4* s_q = reinterpret_cast<uint4*>(s_scale + ST * 2 * kUnit);           // [FINE: whole, rest][tile of rows][two steps][lane]
+    float* s_o = reinterpret_cast<float*>(s_q + (FINE ? 2 : 1) * NT * (KK / 2) * 32);           // [2][ROWS][PITCH]
     __shared__ uint64_t full[ST], empty[ST];
     __shared__ unsigned s_boxes[ST];                                            // boxes of the unit that are there
     __shared__ __align__(16) float s_start[ROWS];                               // of the group's rows: start of logits' sums,
@@ -220,9 +235,21 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         for (int i = 0; i < ST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], kAttWarps); }
         mbar_init_fence();
         s_dead = 0;
+        prefetch_map(&mapK);
+        prefetch_map(&mapV);
     }
+    asm volatile("griddepcontrol.wait;" ::: "memory");         // launched while the kernel before it may still run
     const int64_t units = spans_before(p, p.B) * p.H * p.row_tiles;
-    const int64_t parts = min(units, static_cast<int64_t>(gridDim.x));
+    const int64_t parts = max(min((units + kLeast - 1) / kLeast, static_cast<int64_t>(gridDim.x)), int64_t(units > 0));
+    Split* split = splits_of(p, gridDim.x, ROWS, D) + blockIdx.x;
+    if (threadIdx.x == 0) *split = Split{0, 0, 0, 0};
+    for (int b = blockIdx.x; b < p.B; b += gridDim.x) {        // sequences with nothing to attend to
+        if (seq_len(p, b) > 0) continue;
+        const int64_t row0 = static_cast<int64_t>(b) * p.Lq * p.Hq, rows = static_cast<int64_t>(p.Lq) * p.Hq;
+        for (int64_t i = threadIdx.x; i < rows * D; i += kAttThreads) static_cast<uint16_t*>(p.out)[row0 * D + i] = 0;
+        if (p.lse != nullptr)
+            for (int64_t i = threadIdx.x; i < rows; i += kAttThreads) p.lse[row0 + i] = -INFINITY;
+    }
     if (blockIdx.x >= parts) return;
     Cursor at, end;
     at.seek(p, part_start(units, blockIdx.x, parts));
@@ -322,7 +349,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                         w.y = src[e + 2] | (static_cast<uint32_t>(src[e + 3]) << 16);
                     }
                 }
-                const float2 lo = unpack16x2_rt(w.x, p.bf16), hi = unpack16x2_rt(w.y, p.bf16);
+                const float2 lo = unpack16x2<FINE ? CQ_F16 : CQ_BF16>(w.x), hi = unpack16x2<FINE ? CQ_F16 : CQ_BF16>(w.y);
                 v[e] = lo.x; v[e + 1] = lo.y; v[e + 2] = hi.x; v[e + 3] = hi.y;
                 if (kcol != nullptr) {
                     const float4 c = __ldg(reinterpret_cast<const float4*>(kcol + e));
@@ -339,23 +366,28 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             float sum = 0.0f;                                   // of the rounded elements, whichever units they are held in
 #pragma unroll
             for (int k2 = 0; k2 < KK / 2; ++k2) {
-                uint32_t f[4];
+                uint32_t f[4], rest[4];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int kk = 2 * k2 + h;
-                    if constexpr (BITS == 8) {
-                        f[2 * h] = pack_half2(v[4 * kk] * up, v[4 * kk + 1] * up);
-                        f[2 * h + 1] = pack_half2(v[4 * kk + 2] * up, v[4 * kk + 3] * up);
-                        sum += unpack_half_lo(f[2 * h]) + unpack_half_hi(f[2 * h]) + unpack_half_lo(f[2 * h + 1]) + unpack_half_hi(f[2 * h + 1]);
-                    } else {
-                        // nibbles (0, 4 | 1, 5) of a word in even steps, (2, 6 | 3, 7) in odd ones; the second pair comes in sixteenfold
-                        const int e = k2 * 8 + h * 2;
-                        f[2 * h] = pack_half2(v[e] * up, v[e + 4] * up);
-                        f[2 * h + 1] = pack_half2(v[e + 1] * up * 0.0625f, v[e + 5] * up * 0.0625f);
-                        sum += unpack_half_lo(f[2 * h]) + unpack_half_hi(f[2 * h]) + 16.0f * (unpack_half_lo(f[2 * h + 1]) + unpack_half_hi(f[2 * h + 1]));
+                    // INT4: nibbles (0, 4 | 1, 5) of a word in even steps, (2, 6 | 3, 7) in odd ones; the second pair comes in sixteenfold
+                    const int kk = 2 * k2 + h, e = BITS == 8 ? 4 * kk : k2 * 8 + h * 2;
+                    float x[4] = {v[e], BITS == 8 ? v[e + 1] : v[e + 4], BITS == 8 ? v[e + 2] : v[e + 1], BITS == 8 ? v[e + 3] : v[e + 5]};
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const float unit = BITS == 4 && q == 1 ? 0.0625f : 1.0f;
+                        float lo = x[2 * q] * up * unit, hi = x[2 * q + 1] * up * unit;
+                        const uint32_t w = split_half2(lo, hi);
+                        float both = unpack_half_lo(w) + unpack_half_hi(w);
+                        f[2 * h + q] = w;
+                        if constexpr (FINE) {
+                            rest[2 * h + q] = pack_half2(lo, hi);
+                            both += unpack_half_lo(rest[2 * h + q]) + unpack_half_hi(rest[2 * h + q]);
+                        }
+                        sum = __fmaf_rn(both, 1.0f / unit, sum);
                     }
                 }
                 s_q[(warp * (KK / 2) + k2) * 32 + lane] = make_uint4(f[0], f[1], f[2], f[3]);
+                if constexpr (FINE) s_q[((NT + warp) * (KK / 2) + k2) * 32 + lane] = make_uint4(rest[0], rest[1], rest[2], rest[3]);
             }
             sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
             sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
@@ -405,7 +437,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                     s[nt][1] = s[nt][3] = first.y;
                 }
                 constexpr int kWords = RB / 16;                // words of a lane and token: a quarter of the row
-                uint32_t w[2][kWords], qf[NT][2][2];
+                uint32_t w[2][kWords], qf[(FINE ? 2 : 1) * NT][2][2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if constexpr (kWords >= 4) {
@@ -424,7 +456,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                     if constexpr (BITS == 8) {
                         if ((j & 1) == 0) {
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
+                            for (int nt = 0; nt < (FINE ? 2 : 1) * NT; ++nt) {
                                 const uint4 t = s_q[(nt * (KK / 2) + j / 2) * 32 + lane];
                                 qf[nt][0][0] = t.x; qf[nt][0][1] = t.y; qf[nt][1][0] = t.z; qf[nt][1][1] = t.w;
                             }
@@ -433,10 +465,10 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                         const uint32_t a0 = __byte_perm(x0, 0, 0x4140), a1 = __byte_perm(x1, 0, 0x4140);
                         const uint32_t a2 = __byte_perm(x0, 0, 0x4342), a3 = __byte_perm(x1, 0, 0x4342);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][j & 1]);
+                        for (int nt = 0; nt < (FINE ? 2 : 1) * NT; ++nt) mma16816(s[nt % NT], a0, a1, a2, a3, qf[nt][j & 1]);
                     } else {
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
+                        for (int nt = 0; nt < (FINE ? 2 : 1) * NT; ++nt) {
                             const uint4 t = s_q[(nt * (KK / 2) + j) * 32 + lane];
                             qf[nt][0][0] = t.x; qf[nt][0][1] = t.y; qf[nt][1][0] = t.z; qf[nt][1][1] = t.w;
                         }
@@ -446,7 +478,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                             const uint32_t a0 = and_xor(y0, 0x000F000Fu, 0x00080008u), a1 = and_xor(y1, 0x000F000Fu, 0x00080008u);
                             const uint32_t a2 = and_xor(y0, 0x00F000F0u, 0x00800080u), a3 = and_xor(y1, 0x00F000F0u, 0x00800080u);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma16816(s[nt], a0, a1, a2, a3, qf[nt][h]);
+                            for (int nt = 0; nt < (FINE ? 2 : 1) * NT; ++nt) mma16816(s[nt % NT], a0, a1, a2, a3, qf[nt][h]);
                         }
                     }
                 }
@@ -520,13 +552,21 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 }
                 va[0] *= va_unit;
                 va[1] *= va_unit;
-                uint32_t pf[NT][2];
+                uint32_t pf[(FINE ? 2 : 1) * NT][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     l[nt][0] += pr[nt][0][0] + pr[nt][0][1];
                     l[nt][1] += pr[nt][1][0] + pr[nt][1][1];
-                    pf[nt][0] = transpose8x8(pack_half2(pr[nt][0][0] * va[0], pr[nt][1][0] * va[0]));
-                    pf[nt][1] = transpose8x8(pack_half2(pr[nt][0][1] * va[1], pr[nt][1][1] * va[1]));
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float lo = pr[nt][0][k] * va[k], hi = pr[nt][1][k] * va[k];
+                        if constexpr (FINE) {
+                            pf[nt][k] = transpose8x8(split_half2(lo, hi));
+                            pf[NT + nt][k] = transpose8x8(pack_half2(lo, hi));
+                        } else {
+                            pf[nt][k] = transpose8x8(pack_half2(lo, hi));
+                        }
+                    }
                 }
                 // -- results
                 constexpr int kVWords = RB / 32;               // words of a lane and token: an eighth of the row
@@ -560,7 +600,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                             const uint32_t a0 = byte_pair(x[0][e], 0x4140), a1 = byte_pair(x[0][e], 0x4342);
                             const uint32_t a2 = byte_pair(x[1][e], 0x4140), a3 = byte_pair(x[1][e], 0x4342);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][2 * j + e], a0, a1, a2, a3, pf[nt]);
+                            for (int nt = 0; nt < (FINE ? 2 : 1) * NT; ++nt) mma16816(o[nt % NT][2 * j + e], a0, a1, a2, a3, pf[nt]);
                         }
                     } else {
 #pragma unroll
@@ -568,7 +608,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                             const uint32_t lo = (e & 1) ? x[0][e >> 1] >> 8 : x[0][e >> 1], hi = (e & 1) ? x[1][e >> 1] >> 8 : x[1][e >> 1];
                             const uint32_t a0 = nib_low(lo), a1 = nib_high(lo), a2 = nib_low(hi), a3 = nib_high(hi);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * j + e], a0, a1, a2, a3, pf[nt]);
+                            for (int nt = 0; nt < (FINE ? 2 : 1) * NT; ++nt) mma16816(o[nt % NT][4 * j + e], a0, a1, a2, a3, pf[nt]);
                         }
                     }
                 }
@@ -633,6 +673,12 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
         }
         const bool whole = first_tile == 0 && here_ends;
         const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (first_tile == 0 ? 1 : 0);
+        if (first_tile == 0 && !here_ends && threadIdx.x == 0) {               // begins here: at most one group does, the last
+            const int64_t place = part_start(units, blockIdx.x + 1, parts);
+            // the group's last place is as far behind this part's end as its tiles that are left
+            const int64_t last = place + (tiles - (first_tile + n_units)) - 1;
+            *split = Split{b, head * p.row_tiles + rt, static_cast<int>(part_of(units, last, parts) - blockIdx.x) + 1, 0};
+        }
         for (int idx = threadIdx.x; idx < rows * D; idx += 32 * kAttWarps) {
             const int row = idx / D, d = idx % D;
             const float top = s_top[row], sum = s_sum[row];
@@ -642,7 +688,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 const int64_t dst = (static_cast<int64_t>(b) * p.Lq + i) * p.Hq + head * p.G + g;
                 float res = sum == 0.0f ? 0.0f : __fdiv_rn(v, sum);
                 if (p.col[1] != nullptr) res *= __ldg(p.col[1] + static_cast<int64_t>(head) * D + d);
-                static_cast<uint16_t*>(p.out)[dst * D + d] = pack16_rt(res, p.bf16);
+                static_cast<uint16_t*>(p.out)[dst * D + d] = pack16<FINE ? CQ_F16 : CQ_BF16>(res);
                 if (p.lse != nullptr && d == 0) p.lse[dst] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
             } else {
                 p.part[(slot * ROWS + row) * D + d] = v;
@@ -653,50 +699,69 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
     }
 }
 
-// ---- join of groups that lie in several CTAs: one block for each query row ---------------------------
-template <int D>
-__global__ void __launch_bounds__(D)
+// ---- join of groups that lie in several CTAs: one block for a CTA's split group and one of its rows ----------
+// Maxima and weights of all parts first, then the parts' results, dealt out to the block's D-wide teams and added in a
+// fixed order.  (A loop over the parts in one team took 20 us for one sequence of 4096 tokens, cut into 55 parts a head.)
+constexpr int kJoinThreads = 256;
+constexpr int kJoinParts = 1024;                                // more than CTAs that can be resident
+
+template <int D, int DT>
+__global__ void __launch_bounds__(kJoinThreads)
 k17_kv_join(const AttendArgs p, int ctas, int rows_per_tile) {
-    const int row_id = blockIdx.x;                              // (b * Lq + i) * Hq + head * G + g
-    const int bi = row_id / p.Hq, hq = row_id - bi * p.Hq, b = bi / p.Lq, i = bi - b * p.Lq;
-    const int head = hq / p.G, r = i * p.G + hq - head * p.G;
-    const int rt = r / rows_per_tile, row = r - rt * rows_per_tile;
-    const int d = threadIdx.x;
-    const int len = seq_len(p, b);
-    const int64_t at = static_cast<int64_t>(row_id) * D + d;
-    int64_t c0 = 0, c1 = 0;
-    if (len > 0) {
-        const int64_t per = static_cast<int64_t>(p.H) * p.row_tiles;
-        const int64_t before = spans_before(p, b), units = spans_before(p, p.B) * per;
-        const int tiles = tiles_of(len);
-        const int64_t g0 = before * per + (static_cast<int64_t>(head) * p.row_tiles + rt) * (tiles + kLead) + kLead;
-        const int64_t parts = min(units, static_cast<int64_t>(ctas));
-        c0 = part_of(units, g0, parts);
-        c1 = part_of(units, g0 + tiles - 1, parts);
-    }
+    constexpr int kTeams = kJoinThreads / D;
+    __shared__ float s_w[kJoinParts], s_red[kJoinThreads / 32], s_v[kTeams][D];
+    asm volatile("griddepcontrol.launch_dependents;");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (len == 0) {                                             // nothing to attend to
-        static_cast<uint16_t*>(p.out)[at] = 0;
-        if (p.lse != nullptr && d == 0) p.lse[row_id] = -INFINITY;
-        return;
-    }
-    if (c0 == c1) return;                                       // that CTA has written the result
+    const Split sp = splits_of(p, ctas, rows_per_tile, D)[blockIdx.x];
+    const int head = sp.group / p.row_tiles, rt = sp.group - head * p.row_tiles;
+    const int row = blockIdx.y, r = rt * rows_per_tile + row;
+    if (sp.parts == 0 || r >= p.G * p.Lq) return;
+    const int n = min(sp.parts, kJoinParts), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float* stats = p.part + 2 * static_cast<int64_t>(ctas) * rows_per_tile * D;
-    auto slot = [&](int64_t c) { return ((2 * c + (c == c0 ? 1 : 0)) * rows_per_tile + row); };
+    auto slot = [&](int k) { return (2 * (static_cast<int64_t>(blockIdx.x) + k) + (k == 0 ? 1 : 0)) * rows_per_tile + row; };
+    auto over_block = [&](float v, bool sum) {                  // maximum or sum over the block, in a fixed order
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+            const float o = __shfl_xor_sync(0xFFFFFFFFu, v, off);
+            v = sum ? v + o : fmaxf(v, o);
+        }
+        __syncthreads();
+        if (lane == 0) s_red[warp] = v;
+        __syncthreads();
+        v = s_red[0];
+#pragma unroll
+        for (int w = 1; w < kJoinThreads / 32; ++w) v = sum ? v + s_red[w] : fmaxf(v, s_red[w]);
+        return v;
+    };
     float top = -INFINITY;
-#pragma unroll 4
-    for (int64_t c = c0; c <= c1; ++c) top = fmaxf(top, stats[slot(c) * 2]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, v = 0.0f;
-#pragma unroll 4
-    for (int64_t c = c0; c <= c1; ++c) {
-        const float f = ex2(stats[slot(c) * 2] - ref);
-        sum = __fmaf_rn(stats[slot(c) * 2 + 1], f, sum);
-        v = __fmaf_rn(p.part[slot(c) * D + d], f, v);
+    for (int k = threadIdx.x; k < n; k += kJoinThreads) {
+        const float m = stats[slot(k) * 2];
+        s_w[k] = m;
+        top = fmaxf(top, m);
     }
+    top = over_block(top, false);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+    for (int k = threadIdx.x; k < n; k += kJoinThreads) {
+        const float f = ex2(s_w[k] - ref);
+        s_w[k] = f;
+        sum = __fmaf_rn(stats[slot(k) * 2 + 1], f, sum);
+    }
+    sum = over_block(sum, true);                                // (its barriers also publish the weights)
+    const int d = threadIdx.x % D, team = threadIdx.x / D;
+    float v = 0.0f;
+#pragma unroll 8
+    for (int k = team; k < n; k += kTeams) v = __fmaf_rn(p.part[slot(k) * D + d], s_w[k], v);
+    s_v[team][d] = v;
+    __syncthreads();
+    if (team != 0) return;
+#pragma unroll
+    for (int t = 1; t < kTeams; ++t) v += s_v[t][d];
+    const int i = r / p.G, g = r - i * p.G;
+    const int64_t row_id = (static_cast<int64_t>(sp.b) * p.Lq + i) * p.Hq + head * p.G + g;
     float res = sum == 0.0f ? 0.0f : __fdiv_rn(v, sum);
     if (p.col[1] != nullptr) res *= __ldg(p.col[1] + static_cast<int64_t>(head) * D + d);
-    static_cast<uint16_t*>(p.out)[at] = pack16_rt(res, p.bf16);
+    static_cast<uint16_t*>(p.out)[row_id * D + d] = pack16<DT>(res);
     if (p.lse != nullptr && d == 0) p.lse[row_id] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
@@ -708,38 +773,48 @@ int attn_stage_fault(unsigned int* fault_host) {
 }
 
 static size_t attend_workspace(int64_t D) {
-    return static_cast<size_t>(sm_count()) * kMaxPerSm * 2 * 32 * (D + 2) * sizeof(float);
+    return static_cast<size_t>(sm_count()) * kMaxPerSm * (2 * 32 * (D + 2) * sizeof(float) + sizeof(Split));
 }
 
-template <int D>
-static int launch_join(const AttendArgs& p, int64_t ctas, int rows_per_tile, bool dependent, cudaStream_t st) {
-    const int64_t rows = static_cast<int64_t>(p.B) * p.Lq * p.Hq;
-    return launch_ex(k17_kv_join<D>, dim3(static_cast<unsigned>(rows)), D, 0, st, 1, dependent, p, static_cast<int>(ctas), rows_per_tile);
-}
-
-template <int D, int BITS, int NT>
+template <int D, int BITS, int NT, bool FINE>
 static int launch_attend(AttendArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t st) {
-    using S = AttendShape<D, BITS, NT>;
+    using S = AttendShape<D, BITS, NT, FINE>;
     static thread_local LaunchMemo memo;
     // (the static shared memory counts towards the 48 KB that need no leave, so leave is asked for in any case)
-    int per_sm = resident_ctas(k16_kv_attend<D, BITS, NT>, kAttThreads, S::kSmem, S::kSmem > 50000 ? S::kSmem : 50000, memo);
+    int per_sm = resident_ctas(k16_kv_attend<D, BITS, NT, FINE>, kAttThreads, S::kSmem, S::kSmem > 50000 ? S::kSmem : 50000, memo);
     if (per_sm < 1) return CQ_ERR_CUDA;
     if (per_sm > kMaxPerSm) per_sm = kMaxPerSm;
     p.row_tiles = (p.G * p.Lq + S::kRows - 1) / S::kRows;
     int64_t ctas = static_cast<int64_t>(sm_count()) * per_sm;
     const int64_t most = static_cast<int64_t>(p.B) * p.H * p.row_tiles * ((p.capacity + kUnit - 1) / kUnit);       // real units
     if (ctas > most) ctas = most;
-    const int rc = launch_ex(k16_kv_attend<D, BITS, NT>, dim3(static_cast<unsigned>(ctas)), kAttThreads, S::kSmem, st, 1, false, mapK, mapV, p);
-    return rc != CQ_OK ? rc : launch_join<D>(p, ctas, S::kRows, !tuning_no_pdl(), st);
+    const int rc = launch_ex(k16_kv_attend<D, BITS, NT, FINE>, dim3(static_cast<unsigned>(ctas)), kAttThreads, S::kSmem, st, 1, !tuning_no_pdl(), mapK, mapV, p);
+    if (rc != CQ_OK) return rc;
+    const int rows = p.G * p.Lq < S::kRows ? p.G * p.Lq : S::kRows;
+    return launch_ex(k17_kv_join<D, FINE ? CQ_F16 : CQ_BF16>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(rows)), kJoinThreads, 0, st, 1, !tuning_no_pdl(),
+                     p, static_cast<int>(ctas), S::kRows);
 }
 
-template <int D, int BITS>
+// Rows beyond 16 of 128 channels go into further tiles of 16: registers for 32 would leave one CTA an SM (16 sequences of
+// 4000 tokens, 32 rows a head: 84 us with one tile of 32).
+template <int D, int BITS, bool FINE>
 static int launch_attend_rows(AttendArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t st) {
     const int R = p.G * p.Lq;
-    if (R <= 8) return launch_attend<D, BITS, 1>(p, mapK, mapV, st);
-    if (R <= 16) return launch_attend<D, BITS, 2>(p, mapK, mapV, st);
-    if (R <= 24) return launch_attend<D, BITS, 3>(p, mapK, mapV, st);
-    return launch_attend<D, BITS, 4>(p, mapK, mapV, st);
+    if (R <= 8) return launch_attend<D, BITS, 1, FINE>(p, mapK, mapV, st);
+    if (R <= 16 || D == 128) return launch_attend<D, BITS, 2, FINE>(p, mapK, mapV, st);
+    if constexpr (D == 64) {
+        if (R <= 24) return launch_attend<D, BITS, 3, FINE>(p, mapK, mapV, st);
+        return launch_attend<D, BITS, 4, FINE>(p, mapK, mapV, st);
+    }
+    return CQ_ERR_SHAPE;
+}
+
+// Every row empty, when no token can be named.
+__global__ void k18_no_tokens(uint16_t* out, float* lse, int64_t rows, int D) {
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < rows * D; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        out[i] = 0;
+        if (lse != nullptr && i < rows) lse[i] = -INFINITY;
+    }
 }
 
 }  // namespace cq
@@ -774,7 +849,6 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
     p.q_vec = ptr_aligned(Q, 8) && ((q_batch_stride | q_token_stride | q_head_stride) & 3) == 0;
     p.table = page_table; p.table_stride = table_stride; p.lens = lens;
     p.scale[0] = k_scale; p.scale[1] = v_scale; p.col[0] = k_col; p.col[1] = v_col;
-    p.bf16 = dtype == CQ_BF16;
     p.box = page_size % 64 == 0 ? 64 : page_size % 32 == 0 ? 32 : 16;
     p.unit_pages = static_cast<int>(kUnit / page_size);
     p.unit_rest = static_cast<int>(kUnit % page_size);
@@ -785,7 +859,9 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
     p.row_tiles = 1;
     p.capacity = pages > 0 ? table_width * page_size : 0;
     if (p.capacity == 0) {                                      // no token can be named: every row is empty
-        return D == 64 ? launch_join<64>(p, 1, 8, false, st) : launch_join<128>(p, 1, 8, false, st);
+        const int64_t rows = B * Lq * Hq;
+        k18_no_tokens<<<static_cast<unsigned>(rows < 4096 ? rows : 4096), 128, 0, st>>>(static_cast<uint16_t*>(out), lse, rows, static_cast<int>(D));
+        return launch_status();
     }
     const uint32_t row_bytes = static_cast<uint32_t>(D * bits / 8);
     const CUtensorMapSwizzle swizzle = row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
@@ -793,8 +869,13 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
     CUtensorMap mapK, mapV;
     if (!make_byte_map(&mapK, k_codes, row_bytes, rows, row_bytes, row_bytes, p.box, swizzle) ||
         !make_byte_map(&mapV, v_codes, row_bytes, rows, row_bytes, row_bytes, p.box, swizzle)) return CQ_ERR_CUDA;
-    if (D == 128) return bits == 8 ? launch_attend_rows<128, 8>(p, mapK, mapV, st) : launch_attend_rows<128, 4>(p, mapK, mapV, st);
-    return bits == 8 ? launch_attend_rows<64, 8>(p, mapK, mapV, st) : launch_attend_rows<64, 4>(p, mapK, mapV, st);
+    const bool fine = dtype == CQ_F16;
+    if (D == 128) {
+        if (bits == 8) return fine ? launch_attend_rows<128, 8, true>(p, mapK, mapV, st) : launch_attend_rows<128, 8, false>(p, mapK, mapV, st);
+        return fine ? launch_attend_rows<128, 4, true>(p, mapK, mapV, st) : launch_attend_rows<128, 4, false>(p, mapK, mapV, st);
+    }
+    if (bits == 8) return fine ? launch_attend_rows<64, 8, true>(p, mapK, mapV, st) : launch_attend_rows<64, 8, false>(p, mapK, mapV, st);
+    return fine ? launch_attend_rows<64, 4, true>(p, mapK, mapV, st) : launch_attend_rows<64, 4, false>(p, mapK, mapV, st);
 }
 
 int cq_serve_fault(unsigned int* fault_host) {
