@@ -16,6 +16,36 @@ namespace cq {
 constexpr float kE4m3Max = 448.0f;
 constexpr int kBlk = 128;
 
+// Eight neighbouring elements from any 2-byte aligned place, of which the first n are inside the row (the others read as
+// zeros): whole words as far as the address allows, never a byte outside the row.
+__device__ __forceinline__ uint4 load8_any(const uint16_t* p, int64_t n) {
+    if (n >= 8) {
+        const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p));
+        if ((at & 15u) == 0u) return ld_stream(reinterpret_cast<const uint4*>(p));
+        if ((at & 3u) == 0u) {
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
+            return make_uint4(__ldg(w), __ldg(w + 1), __ldg(w + 2), __ldg(w + 3));
+        }
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(p + 1);
+        const uint32_t a = __ldg(p), b = __ldg(w), c = __ldg(w + 1), d = __ldg(w + 2), e = __ldg(p + 7);
+        return make_uint4(a | (b << 16), __funnelshift_l(b, c, 16), __funnelshift_l(c, d, 16), (d >> 16) | (e << 16));
+    }
+    uint32_t h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = e < n ? __ldg(p + e) : 0u;
+    return make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
+}
+// The first n of eight codes to any place.
+__device__ __forceinline__ void store8_any(uint8_t* p, uint2 c, int64_t n) {
+    if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 7u) == 0u) {
+        *reinterpret_cast<uint2*>(p) = c;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < n) p[e] = static_cast<uint8_t>((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
+}
+
 __device__ __forceinline__ uint32_t absmax8(const uint4& w) {
     const uint32_t m = max_u16x2(max_u16x2(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu), max_u16x2(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu));
     return max(m & 0xFFFFu, m >> 16);
@@ -58,9 +88,10 @@ constexpr int kActVec = 4;
 constexpr int kActRows = 8;
 constexpr int kActCols = 256 * kActVec;
 
-template <int DT>
+// VEC: all rows and codes are aligned and K is a multiple of 8; otherwise each warp goes by its row's address.
+template <int DT, bool VEC>
 __global__ void __launch_bounds__(kThreads)
-k10_fp8_act(const uint4* __restrict__ X, int64_t T, int K8, int64_t ld8, uint8_t* __restrict__ codes, int64_t ldc,
+k10_fp8_act(const uint16_t* __restrict__ X, int64_t T, int64_t K, int64_t ld, uint8_t* __restrict__ codes, int64_t ldc,
             float* __restrict__ scale, int64_t lds, unsigned col_chunks) {
     __shared__ float s_scale[2 * kActVec][kActRows];
     // Launched while the kernel before it may still run: everything waits for that one's end.  Only then may the product
@@ -71,13 +102,16 @@ k10_fp8_act(const uint4* __restrict__ X, int64_t T, int K8, int64_t ld8, uint8_t
     const unsigned chunk = blockIdx.x % col_chunks;
     const int64_t row0 = static_cast<int64_t>(blockIdx.x / col_chunks) * kActRows;
     const int64_t row = row0 + warp;
-    const int v0 = static_cast<int>(chunk) * (kActCols / 8) + lane;
+    const int64_t col0 = static_cast<int64_t>(chunk) * kActCols + lane * 8;
     uint4 w[kActVec];
 #pragma unroll
     for (int k = 0; k < kActVec; ++k) {
-        const int v = v0 + 32 * k;
+        const int64_t col = col0 + 256 * k;
         w[k] = make_uint4(0, 0, 0, 0);
-        if (row < T && v < K8) w[k] = ld_stream(X + row * ld8 + v);
+        if (row < T && col < K) {
+            if constexpr (VEC) w[k] = ld_stream(reinterpret_cast<const uint4*>(X + row * ld + col));
+            else w[k] = load8_any(X + row * ld + col, K - col);
+        }
     }
 #pragma unroll
     for (int k = 0; k < kActVec; ++k) {
@@ -86,45 +120,19 @@ k10_fp8_act(const uint4* __restrict__ X, int64_t T, int K8, int64_t ld8, uint8_t
         for (int off = 8; off > 0; off >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
         const float s = __fdiv_rn(cvt16<DT>(static_cast<uint16_t>(m)), kE4m3Max);
         const uint2 c = e4m3_row8<DT>(w[k], s, guarded_rcp(s));
-        const int v = v0 + 32 * k;
-        if (row < T && v < K8) *reinterpret_cast<uint2*>(codes + row * ldc + static_cast<int64_t>(v) * 8) = c;
+        const int64_t col = col0 + 256 * k;
+        if (row < T && col < K) {
+            if constexpr (VEC) *reinterpret_cast<uint2*>(codes + row * ldc + col) = c;
+            else store8_any(codes + row * ldc + col, c, K - col);
+        }
         if ((lane & 15) == 0) s_scale[2 * k + (lane >> 4)][warp] = s;
     }
     __syncthreads();
     if (threadIdx.x < 2 * kActVec * kActRows) {
         const int b = threadIdx.x / kActRows, r = threadIdx.x % kActRows;
         const int64_t blk = static_cast<int64_t>(chunk) * (2 * kActVec) + b;
-        if (blk * (kBlk / 8) < K8 && row0 + r < T) scale[blk * lds + row0 + r] = s_scale[b][r];
+        if (blk * kBlk < K && row0 + r < T) scale[blk * lds + row0 + r] = s_scale[b][r];
     }
-}
-
-// Any alignment, pitch and number of columns: a warp per row and block, 2-byte loads and 1-byte stores.
-template <int DT>
-__global__ void __launch_bounds__(kThreads)
-g10_fp8_act(const uint16_t* __restrict__ X, int64_t T, int64_t K, int64_t ld, uint8_t* __restrict__ codes, int64_t ldc,
-            float* __restrict__ scale, int64_t lds, int64_t nblk) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");            // as above
-    asm volatile("griddepcontrol.launch_dependents;");
-    const int lane = threadIdx.x & 31;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
-    if (item >= T * nblk) return;                       // whole warps
-    const int64_t row = item / nblk, blk = item % nblk;
-    uint16_t x[4];
-    uint32_t m = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int64_t col = blk * kBlk + lane + 32 * k;
-        x[k] = col < K ? X[row * ld + col] : uint16_t(0);
-        m = max(m, static_cast<uint32_t>(x[k] & 0x7FFFu));
-    }
-    m = __reduce_max_sync(0xFFFFFFFFu, m);
-    const float s = __fdiv_rn(cvt16<DT>(static_cast<uint16_t>(m)), kE4m3Max);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int64_t col = blk * kBlk + lane + 32 * k;
-        if (col < K) codes[row * ldc + col] = static_cast<uint8_t>(pack_e4m3x2(e4m3_quotient_slow(cvt16<DT>(x[k]), s), 0.0f));
-    }
-    if (lane == 0) scale[blk * lds + row] = s;
 }
 
 // ---- weights --------------------------------------------------------------------------------------
@@ -146,10 +154,7 @@ k11_fp8_weight(const uint16_t* __restrict__ W, int64_t N, int64_t K, int64_t ld,
         if constexpr (VEC) {
             if (row < N && col < K) w[i] = ld_stream(reinterpret_cast<const uint4*>(W + row * ld + col));
         } else {
-            uint32_t h[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] = (row < N && col + e < K) ? W[row * ld + col + e] : 0u;
-            w[i] = make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
+            if (row < N && col < K) w[i] = load8_any(W + row * ld + col, K - col);
         }
     }
 #pragma unroll
@@ -167,14 +172,8 @@ k11_fp8_weight(const uint16_t* __restrict__ W, int64_t N, int64_t K, int64_t ld,
         const int64_t row = row0 + 16 * i;
         if (row >= N || col >= K) continue;
         const uint2 c = e4m3_row8<DT>(w[i], s, rs);
-        uint8_t* out = codes + row * ldc + col;
-        if constexpr (VEC) {
-            st_stream(reinterpret_cast<uint2*>(out), c);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (col + e < K) out[e] = static_cast<uint8_t>((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
-        }
+        if constexpr (VEC) st_stream(reinterpret_cast<uint2*>(codes + row * ldc + col), c);
+        else store8_any(codes + row * ldc + col, c, K - col);
     }
 }
 
@@ -194,23 +193,14 @@ int fp8_quantize_act_impl(const void* X, int dtype, int64_t T, int64_t K, int64_
     if (rc != CQ_OK) return rc;
     if (lds < T) return CQ_ERR_SHAPE;
     if (T == 0 || K == 0) return CQ_OK;
-    const bool fast = K % 8 == 0 && ld % 8 == 0 && ldc % 8 == 0 && ptr_aligned(X, 16) && ptr_aligned(codes, 8);
-    uint8_t* c = static_cast<uint8_t*>(codes);
-    if (fast) {
-        const int64_t chunks = (K + kActCols - 1) / kActCols;
-        const int64_t blocks = chunks * ((T + kActRows - 1) / kActRows);
-        if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
-        auto kern = dtype == CQ_F16 ? k10_fp8_act<CQ_F16> : k10_fp8_act<CQ_BF16>;
-        return launch_ex(kern, dim3(static_cast<unsigned>(blocks)), kThreads, 0, st, 1, !tuning_no_pdl(), static_cast<const uint4*>(X), T,
-                         static_cast<int>(K / 8), ld / 8, c, ldc, scale, lds, static_cast<unsigned>(chunks));
-    } else {
-        const int64_t nblk = (K + kBlk - 1) / kBlk;
-        const int64_t blocks = (T * nblk + kThreads / 32 - 1) / (kThreads / 32);
-        if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
-        auto kern = dtype == CQ_F16 ? g10_fp8_act<CQ_F16> : g10_fp8_act<CQ_BF16>;
-        return launch_ex(kern, dim3(static_cast<unsigned>(blocks)), kThreads, 0, st, 1, !tuning_no_pdl(), static_cast<const uint16_t*>(X), T, K,
-                         ld, c, ldc, scale, lds, nblk);
-    }
+    const bool vec = K % 8 == 0 && ld % 8 == 0 && ldc % 8 == 0 && ptr_aligned(X, 16) && ptr_aligned(codes, 8);
+    const int64_t chunks = (K + kActCols - 1) / kActCols;
+    const int64_t blocks = chunks * ((T + kActRows - 1) / kActRows);
+    if (blocks > 0x7FFFFFFF) return CQ_ERR_SHAPE;
+    auto kern = dtype == CQ_F16 ? (vec ? k10_fp8_act<CQ_F16, true> : k10_fp8_act<CQ_F16, false>)
+                                : (vec ? k10_fp8_act<CQ_BF16, true> : k10_fp8_act<CQ_BF16, false>);
+    return launch_ex(kern, dim3(static_cast<unsigned>(blocks)), kThreads, 0, st, 1, !tuning_no_pdl(), static_cast<const uint16_t*>(X), T, K, ld,
+                     static_cast<uint8_t*>(codes), ldc, scale, lds, static_cast<unsigned>(chunks));
 }
 
 }  // namespace cq

@@ -210,7 +210,7 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             const int64_t m0 = static_cast<int64_t>(pos.m) * kTileM + q * 32;
             const int64_t n0 = static_cast<int64_t>(pos.n) * BN + half * kCols;
             uint8_t* out = static_cast<uint8_t*>(p.out);
-            const bool whole = (p.ldo * kElem) % 16 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0;
+            const uint32_t align = static_cast<uint32_t>(p.ldo * kElem) | static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p.out));   // of all rows
 #pragma unroll
             for (int c = 0; c < kCols / kPer; ++c) {
                 __syncwarp();
@@ -228,13 +228,19 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
                 }
                 __syncwarp();
                 const int64_t nc = n0 + c * kPer;
-                if (whole && nc + kPer <= p.N) {
+                if (nc + kPer <= p.N && (align & 15u) == 0u) {
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
                         const int rr = r * 4 + (lane >> 3);
                         const uint4 o = *reinterpret_cast<const uint4*>(patch + rr * 128 + (((lane & 7) + rr) & 7) * 16);
                         if (m0 + rr < p.M)
                             *reinterpret_cast<uint4*>(out + ((m0 + rr) * p.ldo + nc) * kElem + (lane & 7) * 16) = o;
+                    }
+                } else if (nc + kPer <= p.N && (align & 3u) == 0u) {       // a word of each row for each lane
+#pragma unroll 8
+                    for (int rr = 0; rr < 32; ++rr) {
+                        const uint32_t o = *reinterpret_cast<const uint32_t*>(patch + rr * 128 + (((lane >> 2) + rr) & 7) * 16 + (lane & 3) * 4);
+                        if (m0 + rr < p.M) *reinterpret_cast<uint32_t*>(out + ((m0 + rr) * p.ldo + nc) * kElem + lane * 4) = o;
                     }
                 } else {
                     for (int rr = 0; rr < 32 && m0 + rr < p.M; ++rr) {
