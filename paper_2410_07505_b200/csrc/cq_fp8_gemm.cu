@@ -268,13 +268,13 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
 
 // ---- few rows -------------------------------------------------------------------------------------
 // first warps: running sums (four, or eight that halve 64 columns between them); then one for loads, one for products
-template <int BN> __host__ __device__ constexpr int few_sum_warps() { return BN == 64 ? 8 : 4; }
+template <int BN> __host__ __device__ constexpr int few_sum_warps() { return BN >= 64 ? 8 : 4; }
 template <int BN> __host__ __device__ constexpr int few_threads() { return 32 * (few_sum_warps<BN>() + 2); }
-template <int BN> __host__ __device__ constexpr int few_per_sm() { return BN == 64 ? 2 : 3; }
+template <int BN> __host__ __device__ constexpr int few_per_sm() { return BN == 128 ? 1 : BN == 64 ? 2 : 3; }
 constexpr int kFewW = 128;                    // rows of W in a tile
 template <int BN> __host__ __device__ constexpr int few_buffers() { return 4; }    // accumulators: all CTAs of an SM stay within 512 columns
 
-template <int BN> __host__ __device__ constexpr int few_stages() { return BN == 32 ? 3 : 4; }
+template <int BN> __host__ __device__ constexpr int few_stages() { return BN == 32 ? 3 : BN == 128 ? 5 : 4; }
 template <int BN> __host__ __device__ constexpr size_t few_stage_bytes() { return size_t(kFewW) * kBlkK + size_t(BN) * kBlkK; }
 template <int BN> __host__ __device__ constexpr size_t few_smem() {
     return 1024 + few_stages<BN>() * (few_stage_bytes<BN>() + BN * 4);
@@ -523,7 +523,10 @@ static int launch_product(const void* A, int64_t lda, const float* sa, int64_t l
     const int kblocks = static_cast<int>((K + kBlkK - 1) / kBlkK);
     const int sms = sm_count();
     CUtensorMap mapA, mapW;
-    if (M > 64) {
+    // So few tiles of 128 x 128 that a contraction worth splitting can be split in four or more go the other way too
+    // (68 x 3972 x 281, 3 tiles: 16.3 against 9.8 us; split in two it loses: 128 x 8192 x 8192, 64 tiles: 27 against 36 us).
+    const bool split_up = 5 * ((M + 127) / 128) * ((N + 127) / 128) <= sms && kblocks >= 16;
+    if (M > 64 && !split_up) {
         const int64_t mt = (M + kTileM - 1) / kTileM, wide = mt * ((N + 255) / 256), narrow = mt * ((N + 127) / 128);
         // rounds of all SMs times the cost of a block in a tile of either width
         const bool use_wide = ((wide + sms - 1) / sms) * 3 < ((narrow + sms - 1) / sms) * 2;
@@ -535,7 +538,7 @@ static int launch_product(const void* A, int64_t lda, const float* sa, int64_t l
         return use_wide ? launch_main<256, OUT>(mapA, mapW, p, dependent, st)
                         : launch_main<128, OUT>(mapA, mapW, p, dependent, st);
     }
-    const int bn = M <= 16 ? 16 : M <= 32 ? 32 : 64;
+    const int bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
     const int mtiles = static_cast<int>((M + bn - 1) / bn);
     const int64_t ntiles = (N + kFewW - 1) / kFewW;
     if (ntiles * mtiles > (1 << 26)) return CQ_ERR_SHAPE;
@@ -545,7 +548,8 @@ static int launch_product(const void* A, int64_t lda, const float* sa, int64_t l
     switch (bn) {
         case 16: return launch_few<16, OUT>(mapA, mapW, p, ntiles, dependent, st);
         case 32: return launch_few<32, OUT>(mapA, mapW, p, ntiles, dependent, st);
-        default: return launch_few<64, OUT>(mapA, mapW, p, ntiles, dependent, st);
+        case 64: return launch_few<64, OUT>(mapA, mapW, p, ntiles, dependent, st);
+        default: return launch_few<128, OUT>(mapA, mapW, p, ntiles, dependent, st);
     }
 }
 
