@@ -543,10 +543,13 @@ def _addr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _raw(device: int) -> int:
     """The current stream of the tensors' device, which has to be the current one."""
-    if device != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    if device != _current_device():
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{_current_device()}")
     return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
@@ -655,12 +658,17 @@ def fp8_linear(X: torch.Tensor, w: Fp8Weight, out_dtype: torch.dtype | None = No
     N = codes.shape[0]
     ldw = _codes_pitch(codes, N, K, dev, "w")
     _check_weight_scale(scale, N, K, dev, "w")
-    out, odt, ldo = _product_out(out, T, N, out_dtype or X.dtype, X)
-    L = lib()
+    if out is None and out_dtype is None:
+        out, odt, ldo = X.new_empty((T, N)), dt, N or 1
+    else:
+        out, odt, ldo = _product_out(out, T, N, out_dtype or X.dtype, X)
+    L = _lib or lib()
     if workspace is None:
         workspace = X.new_empty(L.cq_fp8_linear_workspace_bytes(T, K), dtype=torch.uint8)
-    _check(L.cq_fp8_linear(X.data_ptr(), dt, T, K, ld, codes.data_ptr(), ldw, scale.data_ptr(), N, out.data_ptr(), odt, ldo,
-                           workspace.data_ptr(), workspace.numel(), _raw(dev)), "cq_fp8_linear")
+    st = L.cq_fp8_linear(X.data_ptr(), dt, T, K, ld, codes.data_ptr(), ldw, scale.data_ptr(), N, out.data_ptr(), odt, ldo,
+                         workspace.data_ptr(), workspace.numel(), _raw(dev))
+    if st:
+        raise CQError(st, "cq_fp8_linear")
     return out
 
 
