@@ -16,6 +16,8 @@ namespace cq {
 constexpr float kE4m3Max = 448.0f;
 constexpr int kBlk = 128;
 
+// (Plain loads, here and in the other kernels that start before the one in front of them has ended, not the read-only
+// path: that is for memory that nobody writes while the kernel exists.)
 // Eight neighbouring elements from any 2-byte aligned place, of which the first n are inside the row (the others read as
 // zeros): whole words as far as the address allows, never a byte outside the row.
 __device__ __forceinline__ uint4 load8_any(const uint16_t* p, int64_t n) {
@@ -24,15 +26,15 @@ __device__ __forceinline__ uint4 load8_any(const uint16_t* p, int64_t n) {
         if ((at & 15u) == 0u) return ld_stream(reinterpret_cast<const uint4*>(p));
         if ((at & 3u) == 0u) {
             const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
-            return make_uint4(__ldg(w), __ldg(w + 1), __ldg(w + 2), __ldg(w + 3));
+            return make_uint4(w[0], w[1], w[2], w[3]);
         }
         const uint32_t* w = reinterpret_cast<const uint32_t*>(p + 1);
-        const uint32_t a = __ldg(p), b = __ldg(w), c = __ldg(w + 1), d = __ldg(w + 2), e = __ldg(p + 7);
+        const uint32_t a = p[0], b = w[0], c = w[1], d = w[2], e = p[7];
         return make_uint4(a | (b << 16), __funnelshift_l(b, c, 16), __funnelshift_l(c, d, 16), (d >> 16) | (e << 16));
     }
     uint32_t h[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = e < n ? __ldg(p + e) : 0u;
+    for (int e = 0; e < 8; ++e) h[e] = e < n ? p[e] : 0u;
     return make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
 }
 // The first n of eight codes to any place.
@@ -91,8 +93,8 @@ constexpr int kActCols = 256 * kActVec;
 // VEC: all rows and codes are aligned and K is a multiple of 8; otherwise each warp goes by its row's address.
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kThreads)
-k10_fp8_act(const uint16_t* __restrict__ X, int64_t T, int64_t K, int64_t ld, uint8_t* __restrict__ codes, int64_t ldc,
-            float* __restrict__ scale, int64_t lds, unsigned col_chunks) {
+k10_fp8_act(const uint16_t* X, int64_t T, int64_t K, int64_t ld, uint8_t* codes, int64_t ldc,
+            float* scale, int64_t lds, unsigned col_chunks) {
     __shared__ float s_scale[2 * kActVec][kActRows];
     // Launched while the kernel before it may still run: everything waits for that one's end.  Only then may the product
     // be launched, which loads weights ahead of its own wait: whatever wrote them is done by then.

@@ -118,7 +118,7 @@ k14_kv_write(const WriteArgs p) {
             w_next[i][0] = w_next[i][1] = make_uint4(0, 0, 0, 0);
             slot_next[i] = -1;
             if (t < T) {
-                slot_next[i] = __ldg(p.slots + t);
+                slot_next[i] = p.slots[t];
                 w_next[i][0] = load_row8<VEC>(src + t * ts);
                 w_next[i][1] = load_row8<VEC>(src + t * ts + D / 2);
             }
@@ -130,7 +130,7 @@ k14_kv_write(const WriteArgs p) {
         const float4* c = reinterpret_cast<const float4*>(pick(p.col, kv) + h * D + v * 8);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const float4 f = __ldg(c + (k >> 1) * (D / 8) + (k & 1));
+            const float4 f = c[(k >> 1) * (D / 8) + (k & 1)];
             r[2 * k] = make_float2(f.x > 0.0f ? __frcp_rn(f.x) : 0.0f, f.y > 0.0f ? __frcp_rn(f.y) : 0.0f);
             r[2 * k + 1] = make_float2(f.z > 0.0f ? __frcp_rn(f.z) : 0.0f, f.w > 0.0f ? __frcp_rn(f.w) : 0.0f);
         }
@@ -245,7 +245,7 @@ k15_kv_read(const ReadArgs p) {
     int64_t slot_next[kReadTokens];
     auto name = [&](int64_t t0) {
 #pragma unroll
-        for (int i = 0; i < kReadTokens; ++i) slot_next[i] = t0 + i < L ? __ldg(p.slots + t0 + i) : -1;
+        for (int i = 0; i < kReadTokens; ++i) slot_next[i] = t0 + i < L ? p.slots[t0 + i] : -1;
     };
     name(static_cast<int64_t>(part) * kReadTokens);
     float2 col[8];
@@ -253,7 +253,7 @@ k15_kv_read(const ReadArgs p) {
         const float4* c = reinterpret_cast<const float4*>(pick(p.c.col, kv) + h * D + v * 8);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const float4 f = __ldg(c + (k >> 1) * (D / 8) + (k & 1));
+            const float4 f = c[(k >> 1) * (D / 8) + (k & 1)];
             col[2 * k] = make_float2(f.x, f.y);
             col[2 * k + 1] = make_float2(f.z, f.w);
         }
@@ -273,7 +273,7 @@ k15_kv_read(const ReadArgs p) {
         a[i] = 0.0f;
         if (slot[i] >= 0 && slot[i] < p.nslots) {
             const uint64_t row = p.pages.row(static_cast<uint32_t>(slot[i]), p.c.H, h);
-            a[i] = __ldg(pick(p.c.scale, kv) + row);
+            a[i] = pick(p.c.scale, kv)[row];
             if constexpr (BITS == 8) {
                 const uint2* src = reinterpret_cast<const uint2*>(pick(p.c.codes, kv) + row * D + v * 8);
                 const uint2 lo = __ldcs(src), hi = __ldcs(src + D / 16);

@@ -12,10 +12,10 @@
 //
 // Work: every (sequence, head, tile of rows) is a group of 64-token units; all units in a row are cut into equal parts,
 // one for each resident CTA, whatever the lengths are.  (A group counts kLead units more than it has, which is what its
-// beginning and end cost, so that a part of many short groups is no longer than one of a few long ones.)  A CTA's four computing warps take 16 tokens of a unit each and
-// keep running maxima, sums and results of their own (no barrier between units); they are joined in a fixed order at the
-// end of a group.  A group that ends in another CTA leaves its sums in the workspace and a second kernel joins those in
-// the order of the tokens: the same bits every time.
+// beginning and end cost, so that a part of many short groups is no longer than one of a few long ones.)  A CTA's four
+// computing warps take 16 tokens of a unit each and keep running references, sums and results of their own (no barrier
+// between units); they are joined in a fixed order at the end of a group.  A group that ends in another CTA leaves its
+// sums in the workspace and a second kernel joins those in a fixed order: the same bits every time.
 // A fifth warp keeps a ring of units filled by asynchronous copies (tensor-map boxes, swizzled so that the fragments'
 // reads meet no bank conflicts, and the tokens' scales), running ahead across groups.  Waits are bounded.
 //
@@ -62,14 +62,14 @@ struct AttendArgs {
 };
 
 // A group that begins in a CTA and ends in a later one: where its sums are to be joined.  parts: 0: there is none.
-struct Split { int b, group, parts, unused; };
+struct __align__(16) Split { int b, group, parts, unused; };
 __device__ __forceinline__ Split* splits_of(const AttendArgs& p, int64_t ctas, int rows, int D) {
     return reinterpret_cast<Split*>(p.part + 2 * ctas * rows * (D + 2));
 }
 
 // ---- the sequence of units ------------------------------------------------------------------------
 __device__ __forceinline__ int seq_len(const AttendArgs& p, int b) {
-    const int n = __ldg(p.lens + b);
+    const int n = __ldcg(p.lens + b);
     return n <= 0 ? 0 : static_cast<int>(min(static_cast<int64_t>(n), p.capacity));
 }
 __device__ __forceinline__ int tiles_of(int len) { return (len + kUnit - 1) / kUnit; }
@@ -278,7 +278,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 const int first = __shfl_sync(0xFFFFFFFFu, idx, 0);
                 if (first + nbox > known_first + 32) {
                     known_first = first;
-                    known_page = static_cast<int64_t>(first + lane) * p.page_size < at.len ? __ldg(table + first + lane) : -1;
+                    known_page = static_cast<int64_t>(first + lane) * p.page_size < at.len ? __ldcg(table + first + lane) : -1;
                 }
                 const int page = __shfl_sync(0xFFFFFFFFu, known_page, idx - known_first);
                 const bool there = mine && tok < at.len && page >= 0 && page < p.pages;
@@ -344,7 +344,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 uint2 w = make_uint2(0, 0);
                 if (there) {
                     if (p.q_vec) {
-                        w = __ldg(reinterpret_cast<const uint2*>(src + e));
+                        w = *reinterpret_cast<const uint2*>(src + e);
                     } else {
                         w.x = src[e] | (static_cast<uint32_t>(src[e + 1]) << 16);
                         w.y = src[e + 2] | (static_cast<uint32_t>(src[e + 3]) << 16);
@@ -353,7 +353,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 const float2 lo = unpack16x2<FINE ? CQ_F16 : CQ_BF16>(w.x), hi = unpack16x2<FINE ? CQ_F16 : CQ_BF16>(w.y);
                 v[e] = lo.x; v[e + 1] = lo.y; v[e + 2] = hi.x; v[e + 3] = hi.y;
                 if (kcol != nullptr) {
-                    const float4 c = __ldg(reinterpret_cast<const float4*>(kcol + e));
+                    const float4 c = *reinterpret_cast<const float4*>(kcol + e);
                     v[e] *= c.x; v[e + 1] *= c.y; v[e + 2] *= c.z; v[e + 3] *= c.w;
                 }
 #pragma unroll
@@ -688,7 +688,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 const int rr = rt * ROWS + row, i = rr / p.G, g = rr - i * p.G;
                 const int64_t dst = (static_cast<int64_t>(b) * p.Lq + i) * p.Hq + head * p.G + g;
                 float res = sum == 0.0f ? 0.0f : __fdiv_rn(v, sum);
-                if (p.col[1] != nullptr) res *= __ldg(p.col[1] + static_cast<int64_t>(head) * D + d);
+                if (p.col[1] != nullptr) res *= __ldcg(p.col[1] + static_cast<int64_t>(head) * D + d);
                 static_cast<uint16_t*>(p.out)[dst * D + d] = pack16<FINE ? CQ_F16 : CQ_BF16>(res);
                 if (p.lse != nullptr && d == 0) p.lse[dst] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
             } else {
@@ -713,7 +713,8 @@ k17_kv_join(const AttendArgs p, int ctas, int rows_per_tile) {
     __shared__ float s_w[kJoinParts], s_red[kJoinThreads / 32], s_v[kTeams][D];
     asm volatile("griddepcontrol.launch_dependents;");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const Split sp = splits_of(p, ctas, rows_per_tile, D)[blockIdx.x];
+    const int4 at = __ldcg(reinterpret_cast<const int4*>(splits_of(p, ctas, rows_per_tile, D) + blockIdx.x));
+    const Split sp{at.x, at.y, at.z, at.w};
     const int head = sp.group / p.row_tiles, rt = sp.group - head * p.row_tiles;
     const int row = blockIdx.y, r = rt * rows_per_tile + row;
     if (sp.parts == 0 || r >= p.G * p.Lq) return;
@@ -736,7 +737,7 @@ k17_kv_join(const AttendArgs p, int ctas, int rows_per_tile) {
     };
     float top = -INFINITY;
     for (int k = threadIdx.x; k < n; k += kJoinThreads) {
-        const float m = stats[slot(k) * 2];
+        const float m = __ldcg(stats + slot(k) * 2);
         s_w[k] = m;
         top = fmaxf(top, m);
     }
@@ -746,13 +747,13 @@ k17_kv_join(const AttendArgs p, int ctas, int rows_per_tile) {
     for (int k = threadIdx.x; k < n; k += kJoinThreads) {
         const float f = ex2(s_w[k] - ref);
         s_w[k] = f;
-        sum = __fmaf_rn(stats[slot(k) * 2 + 1], f, sum);
+        sum = __fmaf_rn(__ldcg(stats + slot(k) * 2 + 1), f, sum);
     }
     sum = over_block(sum, true);                                // (its barriers also publish the weights)
     const int d = threadIdx.x % D, team = threadIdx.x / D;
     float v = 0.0f;
 #pragma unroll 8
-    for (int k = team; k < n; k += kTeams) v = __fmaf_rn(p.part[slot(k) * D + d], s_w[k], v);
+    for (int k = team; k < n; k += kTeams) v = __fmaf_rn(__ldcg(p.part + slot(k) * D + d), s_w[k], v);
     s_v[team][d] = v;
     __syncthreads();
     if (team != 0) return;
@@ -761,7 +762,7 @@ k17_kv_join(const AttendArgs p, int ctas, int rows_per_tile) {
     const int i = r / p.G, g = r - i * p.G;
     const int64_t row_id = (static_cast<int64_t>(sp.b) * p.Lq + i) * p.Hq + head * p.G + g;
     float res = sum == 0.0f ? 0.0f : __fdiv_rn(v, sum);
-    if (p.col[1] != nullptr) res *= __ldg(p.col[1] + static_cast<int64_t>(head) * D + d);
+    if (p.col[1] != nullptr) res *= __ldcg(p.col[1] + static_cast<int64_t>(head) * D + d);
     static_cast<uint16_t*>(p.out)[row_id * D + d] = pack16<DT>(res);
     if (p.lse != nullptr && d == 0) p.lse[row_id] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
