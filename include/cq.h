@@ -14,7 +14,7 @@
  *   - Every data pointer is a DEVICE pointer owned by the caller.  The library allocates
  *     nothing, frees nothing and keeps no per-call state.  The only state it has is process-wide
  *     and for measurement: the knobs of cq_set_tuning and the event pair of cq_set_timing_events
- *     (both thread-safe, neither changes a result), the sticky health flag read by cq_stage_fault,
+ *     (both thread-safe, neither changes a result), the sticky health flags read by cq_stage_fault and cq_serve_fault,
  *     and the fixed scratch array of cq_quantize_act_noalloc.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the default stream).  All work is
  *     enqueued on it; no call synchronises; scalar results are written to device memory.

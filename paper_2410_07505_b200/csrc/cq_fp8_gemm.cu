@@ -4,15 +4,22 @@
 //
 // The scales change from block to block along the contraction, so a block's 128-long inner sum is formed by itself
 // (four tcgen05.mma of 32, fp32 in tensor memory) and added to the running result in fp32 registers with the block's
-// factor, one fused multiply-add for an element and block.  Two accumulator buffers in tensor memory let the tensor
-// cores form the next block while the epilogue warps read the last one.  Tiles arrive by TMA (128-byte swizzle, zero
-// fill past the edges, so odd sizes need no other path); every wait is bounded.
+// factor, one fused multiply-add for an element and block.  Two to four accumulator buffers in tensor memory let the
+// tensor cores form the next block while the epilogue warps read the last one.  Tiles arrive by TMA (128-byte swizzle,
+// zero fill past the edges, so odd sizes need no other path); every wait is bounded.
 //
-// Two kernels, chosen by the number of rows of A:
+// Two kernels, chosen by the number of tiles that the product has (launch_product):
 //   k12_product      tiles of 128 rows of A x 256 (or 128) rows of W, one persistent CTA an SM
-//   k13_product_few  the operands swapped (128 rows of W x 16..64 rows of A) and the contraction split over a
+//   k13_product_few  the operands swapped (128 rows of W x 16..128 rows of A) and the contraction split over a
 //                    thread-block cluster, joined through distributed shared memory in rank order (no atomics: the
 //                    same bits every time); few rows of A leave the read of W as the bound
+//
+// Measured (quantizer included, operands not in L2): 4096 x 8192 x 28672 (rows x K x N) 0.85 ms from a cool chip and 0.99 ms
+// in a long run, which the power limit sets (2.26 and 1.94 PFLOP/s); 1 x 8192 x 8192 15.2 us (4.4 TB/s of weights),
+// 48 x 5120 x 13824 22.3 us, 777 x 2060 x 1003 16.3 us.  The first is bound by shared memory: a block's operands (48 KB for
+// 256 columns) are written once and read once, 768 cycles at 128 bytes each, beside 512 of products and 256 of
+// multiply-adds.  Pairs of CTAs, which would halve the reads of W, lose more by the exchange of each block's sums between
+// their SMs.  The next two are the read of W and about 5 us of launches, first loads and joins; the last is those alone.
 #include "cq_serve.cuh"
 
 #include <atomic>
