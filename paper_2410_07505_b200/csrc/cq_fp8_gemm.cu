@@ -9,14 +9,15 @@
 // zero fill past the edges, so odd sizes need no other path); every wait is bounded.
 //
 // Two kernels, chosen by the number of tiles that the product has (launch_product):
-//   k12_product      tiles of 128 rows of A x 256 (or 128) rows of W, one persistent CTA an SM
+//   k12_product      tiles of 128 rows of A x 256 (or 128) rows of W, one persistent CTA an SM; or, for few tiles, a pair
+//                    of CTAs for a tile that take half of the contraction each
 //   k13_product_few  the operands swapped (128 rows of W x 16..128 rows of A) and the contraction split over a
 //                    thread-block cluster, joined through distributed shared memory in rank order (no atomics: the
 //                    same bits every time); few rows of A leave the read of W as the bound
 //
 // Measured (quantizer included, operands not in L2): 4096 x 8192 x 28672 (rows x K x N) 0.85 ms from a cool chip and 0.99 ms
 // in a long run, which the power limit sets (2.26 and 1.94 PFLOP/s); 1 x 8192 x 8192 15.2 us (4.4 TB/s of weights),
-// 48 x 5120 x 13824 22.3 us, 777 x 2060 x 1003 16.3 us.  The first is bound by shared memory: a block's operands (48 KB for
+// 48 x 5120 x 13824 22.3 us, 777 x 2060 x 1003 15.6 us.  The first is bound by shared memory: a block's operands (48 KB for
 // 256 columns) are written once and read once, 768 cycles at 128 bytes each, beside 512 of products and 256 of
 // multiply-adds.  Pairs of CTAs, which would halve the reads of W, lose more by the exchange of each block's sums between
 // their SMs.  The next two are the read of W and about 5 us of launches, first loads and joins; the last is those alone.
@@ -40,6 +41,19 @@ __device__ __forceinline__ uint16_t to16(float v) {
 __device__ __forceinline__ void mma_block(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) tc_mma_fp8(d, a + 2 * k, b + 2 * k, idesc, k != 0);      // 32 bytes further along the swizzled row
+}
+
+// ---- thread-block clusters ----------------------------------------------------------------------------
+__device__ __forceinline__ float ld_cluster(uint32_t local, uint32_t rank) {
+    uint32_t remote;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // ---- many rows ------------------------------------------------------------------------------------
@@ -71,7 +85,8 @@ __device__ __forceinline__ TilePos tile_at(int64_t t, int mtiles, int ntiles) {
     return {g * kGroupM + static_cast<int>(r % rows), static_cast<int>(r / rows)};
 }
 
-template <int BN, int OUT>
+// SPLIT: two CTAs of a cluster take half of the contraction each, one tile a cluster; each finishes half of the columns.
+template <int BN, int OUT, bool SPLIT>
 __global__ void __launch_bounds__(kMainThreads, 1)
 k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapW, const MainArgs p) {
     constexpr int ST = main_stages<BN>();
@@ -109,6 +124,8 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     const int64_t ntotal = static_cast<int64_t>(p.mtiles) * p.ntiles;
+    const int rank = SPLIT ? blockIdx.x & 1 : 0;
+    const int kb_first = SPLIT && rank == 1 ? p.kblocks / 2 : 0, kb_end = SPLIT && rank == 0 ? p.kblocks / 2 : p.kblocks;
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -117,11 +134,11 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             uint32_t round = 0, issued = 0;
             bool ok = true;
             asm volatile("griddepcontrol.wait;" ::: "memory");
-            for (int64_t t = blockIdx.x; ok && t < ntotal; t += gridDim.x) {
+            for (int64_t t = SPLIT ? blockIdx.x >> 1 : blockIdx.x; ok && t < ntotal; t += SPLIT ? ntotal : gridDim.x) {
                 const TilePos pos = tile_at(t, p.mtiles, p.ntiles);
                 const int64_t m0 = static_cast<int64_t>(pos.m) * kTileM;
                 const uint32_t sbytes = static_cast<uint32_t>(min(int64_t(128), (p.M - m0 + 3) & ~int64_t(3))) * 4;
-                for (int kb = 0; kb < p.kblocks; ++kb) {
+                for (int kb = kb_first; kb < kb_end; ++kb) {
                     if (!(ok = role_wait(&empty[s], round ^ 1u, &s_dead))) break;
                     if (elect_one()) {
                         mbar_expect_tx(&full[s], static_cast<uint32_t>(kA + kB) + sbytes);
@@ -144,8 +161,8 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
             int s = 0, b = 0, pending = 0;
             uint32_t round = 0, turn = 0;
             bool ok = true;
-            for (int64_t t = blockIdx.x; ok && t < ntotal; t += gridDim.x) {
-                for (int kb = 0; kb < p.kblocks; ++kb) {
+            for (int64_t t = SPLIT ? blockIdx.x >> 1 : blockIdx.x; ok && t < ntotal; t += SPLIT ? ntotal : gridDim.x) {
+                for (int kb = kb_first; kb < kb_end; ++kb) {
                     if (!(ok = role_wait(&full[s], round, &s_dead) && role_wait(&tempty[b], turn ^ 1u, &s_dead))) break;
                     tc_fence_after();
                     if (elect_one()) {
@@ -164,6 +181,11 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
                     for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&tfull[b], turn); ++polls) {}
                 }
         }
+        if constexpr (SPLIT) {
+            __syncwarp();
+            cluster_sync_all();
+            cluster_sync_all();
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int ew = warp - 4, half = ew >> 2, q = ew & 3;      // half of the columns and 32 rows of the CTA's tile for each warp
@@ -174,15 +196,15 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
         int s = 0, b = 0;
         uint32_t round = 0, turn = 0;
         bool ok = true;
-        for (int64_t t = blockIdx.x; ok && t < ntotal; t += gridDim.x) {
+        for (int64_t t = SPLIT ? blockIdx.x >> 1 : blockIdx.x; ok && t < ntotal; t += SPLIT ? ntotal : gridDim.x) {
             const TilePos pos = tile_at(t, p.mtiles, p.ntiles);
             const int64_t nb = min((static_cast<int64_t>(pos.n) * BN + half * kCols) / 128, nblocks - 1);
             const float* sw = p.sw + nb * p.kblocks;
             float acc[kCols];
 #pragma unroll
             for (int i = 0; i < kCols; ++i) acc[i] = 0.0f;
-            float w = __ldg(sw);
-            for (int kb = 0; kb < p.kblocks; ++kb) {
+            float w = __ldg(sw + kb_first);
+            for (int kb = kb_first; kb < kb_end; ++kb) {
                 const float w_next = __ldg(sw + min(kb + 1, p.kblocks - 1));
                 if (!(ok = role_wait(&tfull[b], turn, &s_dead) && role_wait(&full[s], round, &s_dead))) break;
                 tc_fence_after();
@@ -208,6 +230,23 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
                 w = w_next;
                 if (++s == ST) { s = 0; round ^= 1u; }
                 if (++b == TB) { b = 0; turn ^= 1u; }
+            }
+            if constexpr (SPLIT) {
+                // every product of this CTA has completed, so the stages may be written over
+                float* part = reinterpret_cast<float*>(smem) + q * kCols * 32 + lane;
+                if (half != rank) {
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i) part[i * 32] = acc[i];
+                }
+                __syncwarp();
+                cluster_sync_all();
+                if (half == rank) {
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i) acc[i] = __fadd_rn(acc[i], ld_cluster(smem_u32(part + i * 32), rank ^ 1));
+                }
+                __syncwarp();
+                cluster_sync_all();               // nobody leaves while its sums are being read
+                if (half != rank) break;
             }
             if (!ok) break;
             // through a 4 KB patch of shared memory (a row of 128 bytes for each lane, 16-byte pieces rotated by the row)
@@ -295,18 +334,6 @@ struct FewArgs {
     int64_t M, N;
     int kblocks, mtiles, split;
 };
-
-__device__ __forceinline__ float ld_cluster(uint32_t local, uint32_t rank) {
-    uint32_t remote;
-    float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
-    return v;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 
 template <int BN, int OUT>
 __global__ void __launch_bounds__(few_threads<BN>(), few_per_sm<BN>())
@@ -514,14 +541,14 @@ static int launch_few(const CUtensorMap& a, const CUtensorMap& w, FewArgs p, int
                      dependent, a, w, p);
 }
 
-template <int BN, int OUT>
+template <int BN, int OUT, bool SPLIT>
 static int launch_main(const CUtensorMap& a, const CUtensorMap& w, const MainArgs& p, bool dependent, cudaStream_t st) {
     static thread_local LaunchMemo memo;
-    if (resident_ctas(k12_product<BN, OUT>, kMainThreads, main_smem<BN>(), main_smem<BN>(), memo) < 1) return CQ_ERR_CUDA;
+    if (resident_ctas(k12_product<BN, OUT, SPLIT>, kMainThreads, main_smem<BN>(), main_smem<BN>(), memo) < 1) return CQ_ERR_CUDA;
     const int64_t tiles = static_cast<int64_t>(p.mtiles) * p.ntiles;
     const int sms = sm_count();
-    const unsigned grid = static_cast<unsigned>(tiles < sms ? tiles : sms);
-    return launch_ex(k12_product<BN, OUT>, dim3(grid), kMainThreads, main_smem<BN>(), st, 1, dependent, a, w, p);
+    const unsigned grid = static_cast<unsigned>(SPLIT ? 2 * tiles : tiles < sms ? tiles : sms);
+    return launch_ex(k12_product<BN, OUT, SPLIT>, dim3(grid), kMainThreads, main_smem<BN>(), st, SPLIT ? 2 : 1, dependent, a, w, p);
 }
 
 template <int OUT>
@@ -531,7 +558,7 @@ static int launch_product(const void* A, int64_t lda, const float* sa, int64_t l
     const int sms = sm_count();
     CUtensorMap mapA, mapW;
     // So few tiles of 128 x 128 that a contraction worth splitting can be split in four or more go the other way too
-    // (68 x 3972 x 281, 3 tiles: 16.3 against 9.8 us; split in two it loses: 128 x 8192 x 8192, 64 tiles: 27 against 36 us).
+    // (68 x 3972 x 281, 3 tiles: 16.3 against 9.8 us; split in two that way it loses: 128 x 8192 x 8192, 64 tiles: 27 against 36 us).
     const bool split_up = 5 * ((M + 127) / 128) * ((N + 127) / 128) <= sms && kblocks >= 16;
     if (M > 64 && !split_up) {
         const int64_t mt = (M + kTileM - 1) / kTileM, wide = mt * ((N + 255) / 256), narrow = mt * ((N + 127) / 128);
@@ -542,8 +569,12 @@ static int launch_product(const void* A, int64_t lda, const float* sa, int64_t l
         if (!make_byte_map(&mapA, A, K, M, lda, kBlkK, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
             !make_byte_map(&mapW, W, K, N, ldw, kBlkK, bn, CU_TENSOR_MAP_SWIZZLE_128B)) return CQ_ERR_CUDA;
         const MainArgs p{sa, lds, sw, out, ldo, M, N, kblocks, static_cast<int>(mt), static_cast<int>((N + bn - 1) / bn)};
-        return use_wide ? launch_main<256, OUT>(mapA, mapW, p, dependent, st)
-                        : launch_main<128, OUT>(mapA, mapW, p, dependent, st);
+        // Narrow tiles for less than half of the SMs (an eighth left for what clusters cannot fill) split the contraction in two:
+        // 128 x 8192 x 8192 (64 tiles) 26.4 -> 19.5 us, 777 x 2060 x 1003 (56 tiles, 17 blocks) 12.5 -> 11.3; below 16 blocks the join
+        // takes what it gives (128 x 1600 x 8192, 13 blocks: 8.9 and 9.0).
+        if (16 * narrow <= 7 * sms && kblocks >= 16) return launch_main<128, OUT, true>(mapA, mapW, p, dependent, st);
+        return use_wide ? launch_main<256, OUT, false>(mapA, mapW, p, dependent, st)
+                        : launch_main<128, OUT, false>(mapA, mapW, p, dependent, st);
     }
     const int bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
     const int mtiles = static_cast<int>((M + bn - 1) / bn);

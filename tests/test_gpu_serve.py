@@ -179,6 +179,28 @@ def test_fp8_matmul_half_outputs_and_repeats(cq):
             assert torch.equal(got, cq.fp8_matmul(A, W, torch.float16))   # the same bits every time
 
 
+# Few tiles and a long contraction of 16 blocks or more (an odd number, a partial last block, edges in both directions):
+# two CTAs share a tile.  The tolerance is the one of every product.
+@pytest.mark.parametrize("M,N,K", ((65, 4000, 2048), (130, 2000, 2100), (257, 1290, 2431), (500, 1999, 4000)))
+def test_fp8_matmul_with_the_contraction_split(cq, M, N, K):
+    a, sa, w, sw = operands(M, N, K, M + K)
+    sa, sw = sa * 0 + 0.01, sw * 0 + 0.02
+    A, W = on_device(cq, a, sa, w, sw)
+    y, mag = ref.fp8_product(a, sa, w, sw)
+    for dtype in (torch.bfloat16, torch.float16, torch.float32):
+        ar = Arena()
+        ar.add("out", (M, N + 3), dtype)
+        ar.build()
+        ar["out"].fill_(7)
+        out = ar["out"][:, :N]
+        cq.fp8_matmul(A, W, dtype, out=out)
+        ar.check("fp8_matmul")
+        check_product(out, y, mag, dtype)
+        assert bool((ar["out"][:, N:] == 7).all())
+        assert torch.equal(out, cq.fp8_matmul(A, W, dtype))
+    assert cq.serve_fault() == 0
+
+
 def test_fp8_matmul_empty(cq):
     A, W = on_device(cq, *operands(5, 7, 64, 0))
     out = cq.fp8_matmul(cq.Fp8Act(A.codes[:0], A.scale[:, :0]), W)
