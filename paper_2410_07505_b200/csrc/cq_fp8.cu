@@ -9,8 +9,8 @@
 // largest), so that everything computed from the block is NaN rather than a wrong number.
 //
 // Both are bound by HBM: 2 bytes read and 1 byte written for an element, the block's maximum found in registers.
-// Measured, tensors larger than L2: weights 28672 x 8192 126 us (5.6 TB/s, 85 % of a copy's rate); 1003 x 2060, 9 us, is
-// latency.
+// Measured, tensors larger than L2: weights 28672 x 8192 109 us (6.5 TB/s, 99 % of a copy's rate; up to 127 us behind work that
+// has lowered the clocks); 1003 x 2060, 7 to 9 us, is latency.
 #include "cq_serve.cuh"
 
 namespace cq {
@@ -141,6 +141,8 @@ k10_fp8_act(const uint16_t* X, int64_t T, int64_t K, int64_t ld, uint8_t* codes,
 
 // ---- weights --------------------------------------------------------------------------------------
 // One CTA per 128 x 128 block, held in registers between the maximum and the codes (eight 16-byte loads a thread).
+// (64 registers, four CTAs an SM: enough loads in flight.  Five spill, 144 us; CTAs that walk over blocks with the next one's
+// loads ahead of this one's codes: 129 us with two an SM, 125 with three.)
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kThreads)
 k11_fp8_weight(const uint16_t* __restrict__ W, int64_t N, int64_t K, int64_t ld, uint8_t* __restrict__ codes, int64_t ldc,
