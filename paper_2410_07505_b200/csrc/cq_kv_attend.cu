@@ -25,12 +25,17 @@
 // nominal exponent, which costs a sum about 2^-13 of one code: nothing beside a logit's other terms, but too much for a
 // result whose likely tokens hold code 0, so a value's code goes in exactly, as fp16 1024 + code + bias minus 1024 + bias.
 // A query row (times kf) is scaled by a power of two into [2^14, 2^15) before it is rounded, so its rounding is 2^-12 of
-// each element; probabilities times va are scaled by 2^10 over a power of two above the largest va seen, so small ones
-// keep 11 bits down to 2^-24 of the reference.  Logits, maxima, sums and results are fp32.
+// each element.  A row's probabilities times va go in as fp16 in units of a power of two that put its largest between 2^4 and 2^16:
+// what lies 2^-18 below that has 11 bits, what lies below has fewer.  Logits, maxima, sums and results are fp32.
 // A bf16 result hides these roundings (2^-12 and 2^-12 beside 2^-9); an fp16 result does not, so for fp16 (FINE) queries
 // and probabilities go in as two halves each, the second what the first leaves, at twice the products.
-// The running reference of a row is a logit that was the largest when it was taken; it is only renewed, with all sums and
-// results rescaled, when some logit exceeds it by more than 5 in base 2, which probabilities up to 2^5 times 2^10 allow.
+// The running reference of a row is a logit that was the largest when it was taken, rounded up to a whole number (base 2).  It is
+// renewed, with the row's sum and results rescaled, when some logit exceeds it by more than 10; the row's unit likewise, when some
+// probability times va nears the end of fp16.  Both are the row's own and follow from what it sees alone: a token behind a
+// query's position, whatever its scales are, leaves no trace in that query's bits (its probability times va is set to 0, not formed:
+// 0 times an infinite va is none).  One unit for all rows of a warp, above the largest va, took 2 to 7 % less time (4 x 100003 INT4,
+// 16 rows a head: 114 against 118 us), but lost rows beside a large value that they do not see or give no weight: with 1e30 behind
+// it, a value of 100 read as 0.  Less room above the reference (2^5) makes rows ask more often: 124 us.
 #include "cq_kv.cuh"
 
 namespace cq {
@@ -42,6 +47,10 @@ constexpr int kAttWarps = 4;
 constexpr int kAttThreads = 32 * (kAttWarps + 1);
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNoRef = -3.402823466e38f;      // the reference of a row that has seen nothing
+constexpr float kMostProb = 1024.0f;            // a probability may be so many times the reference's,
+constexpr float kMostUnits = 61440.0f;          // and a probability times va be so many of its row's units (fp16 ends at 65504);
+constexpr int kPlace = 5;                       // new units put the row's largest between 2^4 and 2^5 of them
 
 struct AttendArgs {
     const void* q; int64_t qb, ql, qh;          // strides of sequences, tokens and heads, in elements
@@ -144,6 +153,21 @@ struct Cursor {
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {          // NaN if either is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float over_tokens(float v) {          // maximum over the lanes that hold the same rows (lane & 3)
+    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 4));
+    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 8));
+    return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 16));
+}
+__device__ __forceinline__ float lg2(float x) {
+    float r;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 __device__ __forceinline__ float pow2i(int e) { return e < -126 ? 0.0f : __int_as_float((e + 127) << 23); }
@@ -406,14 +430,13 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             fac[nt][1] = s_fac[nt * 8 + 2 * r4 + 1];
         }
         // results of channels g8 * D/8 + 2 t, + 1 (elements 0 1 | 2 3) and rows 2 r4, 2 r4 + 1
-        float o[NT][MT][4], ref[NT][2], l[NT][2];               // ref: references, in base 2
-        bool fresh = true;                                     // no token yet (a row that does not see the first will see none)
-        int va_exp = -100;                                     // results are held in units of 2^(va_exp - 10)
-        float va_unit = pow2i(10 - va_exp), va_top = pow2i(va_exp);
+        float o[NT][MT][4], ref[NT][2], l[NT][2];               // ref: references, in base 2; below every logit where nothing was seen
+        float unit[NT][2], finest = 1.0f;                      // powers of two: results are held in units of 1 / unit; the largest of this lane's
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            ref[nt][0] = ref[nt][1] = 0.0f;
+            ref[nt][0] = ref[nt][1] = kNoRef;
             l[nt][0] = l[nt][1] = 0.0f;
+            unit[nt][0] = unit[nt][1] = 1.0f;
 #pragma unroll
             for (int t = 0; t < MT; ++t) o[nt][t][0] = o[nt][t][1] = o[nt][t][2] = o[nt][t][3] = 0.0f;
         }
@@ -489,8 +512,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 if (g8 >= valid) va[0] = 0.0f;                 // what lies past the end may be anything
                 if (g8 + 8 >= valid) va[1] = 0.0f;
                 const bool edge = tok0 + 15 > len - p.Lq;      // some row does not see some token
-                float x[NT][2][2], pr[NT][2][2];               // [row][token]: logits in units of fac, probabilities
-                float most = 0.0f;
+                float x[NT][2][2];                             // [row][token]: logits in units of fac
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -509,6 +531,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                         }
                 }
                 // a product with fac is rounded once, as the reference, and used for all that refers to it: its rounding cancels
+                float pr[NT][2][2], most = 0.0f;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -517,42 +540,67 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                         pr[nt][e][1] = ex2(__fmaf_rn(x[nt][e][1], fac[nt][e], -ref[nt][e]));
                         most = fmaxf(most, fmaxf(pr[nt][e][0], pr[nt][e][1]));
                     }
-                if (__any_sync(0xFFFFFFFFu, most > 32.0f || fmaxf(va[0], va[1]) >= va_top) || fresh) {    // new references and units
-                    const uint32_t vtop = __reduce_max_sync(0xFFFFFFFFu, max(__float_as_uint(va[0]) & 0x7FFFFFFFu, __float_as_uint(va[1]) & 0x7FFFFFFFu));
-                    const int new_exp = max(va_exp, min(126, static_cast<int>(vtop >> 23) - 126));        // 2^new_exp > every va
-                    const float vshift = pow2i(max(va_exp - new_exp, -127));
-                    va_exp = new_exp;
-                    va_unit = pow2i(10 - va_exp);
-                    va_top = pow2i(va_exp);
+                float pv[NT][2][2];                            // probability times va, in the row's units
+                if (__any_sync(0xFFFFFFFFu, most > kMostProb || !(max_nan(fabsf(va[0]), fabsf(va[1])) * finest * most <= kMostUnits))) {
+                    // Perhaps new references and units, for the rows that need them; a va that is not finite comes here too.
+                    // All rows at once, so that their shuffles overlap; a row that needs nothing is multiplied by 1.
+                    const unsigned row = 0x11111111u << r4;    // the lanes of this lane's rows
+                    const float lv[2] = {lg2(fabsf(va[0])), lg2(fabsf(va[1]))};
+                    float top[NT][2], heavy[NT][2];            // in base 2: the largest logit, the largest probability times va
+                    unsigned asks = 0;
+                    finest = 0.0f;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        float shrink[2];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float top = fmaxf(x[nt][e][0], x[nt][e][1]);
-                            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
-                            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
-                            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-                            top = __fmul_rn(top, fac[nt][e]);
-                            float next = fresh ? top : fmaxf(ref[nt][e], top);
-                            if (next == -INFINITY) next = 0.0f;
-                            const float keep = fresh ? 0.0f : ex2(ref[nt][e] - next);
-                            ref[nt][e] = next;
-                            l[nt][e] *= keep;
-                            shrink[e] = keep * vshift;
-                            pr[nt][e][0] = ex2(__fmaf_rn(x[nt][e][0], fac[nt][e], -next));
-                            pr[nt][e][1] = ex2(__fmaf_rn(x[nt][e][1], fac[nt][e], -next));
+                            float most_units = 0.0f;
+                            heavy[nt][e] = -INFINITY;
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+                                if (x[nt][e][k] != -INFINITY) {
+                                    most_units = fmaxf(most_units, fabsf(pr[nt][e][k] * va[k] * unit[nt][e]));
+                                    heavy[nt][e] = fmaxf(heavy[nt][e], __fmaf_rn(x[nt][e][k], fac[nt][e], lv[k]));
+                                }
+                            const bool high = fmaxf(pr[nt][e][0], pr[nt][e][1]) > kMostProb;
+                            if ((__ballot_sync(0xFFFFFFFFu, high) & row) != 0u) asks |= 3u << (4 * nt + 2 * e);
+                            if ((__ballot_sync(0xFFFFFFFFu, most_units > kMostUnits) & row) != 0u) asks |= 1u << (4 * nt + 2 * e);
+                            top[nt][e] = __fmul_rn(over_tokens(fmaxf(x[nt][e][0], x[nt][e][1])), fac[nt][e]);
+                            heavy[nt][e] = over_tokens(heavy[nt][e]);
                         }
 #pragma unroll
-                        for (int t = 0; t < MT; ++t) {
-                            o[nt][t][0] *= shrink[0]; o[nt][t][1] *= shrink[1];
-                            o[nt][t][2] *= shrink[0]; o[nt][t][3] *= shrink[1];
+                        for (int e = 0; e < 2; ++e) {
+                            const unsigned ask = (asks >> (4 * nt + 2 * e)) & 3u;
+                            // whole numbers, so that no bits are lost; `held`: what the row's results are held under, with the new reference
+                            const float next = (ask & 2u) != 0u ? ceilf(top[nt][e]) : ref[nt][e], fall = ref[nt][e] - next;
+                            const int had = static_cast<int>(__float_as_uint(unit[nt][e]) >> 23) - 127;
+                            const float held = static_cast<float>(kPlace - had) + fall, need = floorf(heavy[nt][e] - next) + 1.0f;
+                            const int now = ask != 0u ? static_cast<int>(fminf(fmaxf(kPlace - fmaxf(held, need), -116.0f), 110.0f)) : had;
+                            const float keep = ex2(fall + static_cast<float>(now - had));
+                            unit[nt][e] = pow2i(now);
+                            finest = fmaxf(finest, unit[nt][e]);
+                            ref[nt][e] = next;
+                            l[nt][e] *= ex2(fall);
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                pr[nt][e][k] = ex2(__fmaf_rn(x[nt][e][k], fac[nt][e], -next));
+                                pv[nt][e][k] = x[nt][e][k] == -INFINITY ? 0.0f : pr[nt][e][k] * va[k] * unit[nt][e];
+                            }
+#pragma unroll
+                            for (int t = 0; t < MT; ++t) {
+                                o[nt][t][e] *= keep;
+                                o[nt][t][2 + e] *= keep;
+                            }
                         }
                     }
-                    fresh = false;
+                } else {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            pv[nt][e][0] = pr[nt][e][0] * va[0] * unit[nt][e];
+                            pv[nt][e][1] = pr[nt][e][1] * va[1] * unit[nt][e];
+                        }
                 }
-                va[0] *= va_unit;
-                va[1] *= va_unit;
                 uint32_t pf[(FINE ? 2 : 1) * NT][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
@@ -560,12 +608,11 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                     l[nt][1] += pr[nt][1][0] + pr[nt][1][1];
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        float lo = pr[nt][0][k] * va[k], hi = pr[nt][1][k] * va[k];
                         if constexpr (FINE) {
-                            pf[nt][k] = transpose8x8(split_half2(lo, hi));
-                            pf[NT + nt][k] = transpose8x8(pack_half2(lo, hi));
+                            pf[nt][k] = transpose8x8(split_half2(pv[nt][0][k], pv[nt][1][k]));
+                            pf[NT + nt][k] = transpose8x8(pack_half2(pv[nt][0][k], pv[nt][1][k]));
                         } else {
-                            pf[nt][k] = transpose8x8(pack_half2(lo, hi));
+                            pf[nt][k] = transpose8x8(pack_half2(pv[nt][0][k], pv[nt][1][k]));
                         }
                     }
                 }
@@ -658,7 +705,7 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                         const int row = nt * 8 + 2 * r4 + e;
                         if (row < rows) {
                             const float top = fmaxf(fmaxf(s_m[0][row], s_m[1][row]), fmaxf(s_m[2][row], s_m[3][row]));
-                            const float f = ex2(ref[nt][e] - (top == -INFINITY ? 0.0f : top)) * pow2i(va_exp) * (1.0f / 1024.0f);
+                            const float f = ex2(ref[nt][e] - (top == -INFINITY ? 0.0f : top)) * __uint_as_float((254u << 23) - __float_as_uint(unit[nt][e]));
                             float* dst = s_o + (warp & 1) * ROWS * PITCH + row * PITCH + g8 * (D / 8);
 #pragma unroll
                             for (int t = 0; t < MT; ++t) {
