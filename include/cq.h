@@ -344,8 +344,8 @@ int cq_kv_read(const void* k_codes, const void* v_codes, const float* k_scale, c
  *   out[b, i, h'] = softmax_j(softmax_scale * q . k_j) v_j
  *   Q     16-bit, element (b, i, h', d) at b * q_batch_stride + i * q_token_stride + h' * q_head_stride + d
  *   out   dense [B][Lq][Hq][D] of Q's dtype;  lse  float [B][Lq][Hq], the logarithm of the softmax's sum; nullable
- * What a query does not see has no effect on its result, bit for bit, infinite and NaN scales included; a value head with an
- * infinity or NaN that it sees makes its result NaN.  Probabilities times value scales are rounded to fp16 (CQ_F16: to two of them, the
+ * What a query does not see has no effect on its result, bit for bit, infinite and NaN scales included; a key or value
+ * head with an infinity or NaN that it sees makes its result NaN.  Probabilities times value scales are rounded to fp16 (CQ_F16: to two of them, the
  * second for what the first leaves): a token keeps 11 bits (22) where its probability times its value scale is at least 2^-18 of its
  * row's largest, fewer below, and counts as 0 below 2^-29 of it.
  * A query that sees no token gets zeros (lse: -infinity).  Tokens of a page number outside the cache are not

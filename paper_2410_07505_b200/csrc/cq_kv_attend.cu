@@ -507,7 +507,9 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                     }
                 }
                 // -- probabilities
-                const float ka[2] = {sc[g8], sc[g8 + 8]};
+                // an infinite key scale goes in as NaN: a head that held an infinity has codes 0, whose sum is 0 up to a rounding of
+                // either sign, and times the infinity that would be NaN or a token without probability as it falls
+                const float ka[2] = {__fmaf_rn(sc[g8], 0.0f, sc[g8]), __fmaf_rn(sc[g8 + 8], 0.0f, sc[g8 + 8])};
                 float va[2] = {sc[kUnit + g8], sc[kUnit + g8 + 8]};
                 if (g8 >= valid) va[0] = 0.0f;                 // what lies past the end may be anything
                 if (g8 + 8 >= valid) va[1] = 0.0f;

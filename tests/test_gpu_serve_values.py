@@ -161,3 +161,30 @@ def test_values_near_the_ends_of_the_type(cq):  # noqa: F811
     for b in range(n):
         want = torch.from_numpy(codes[1][table[b, 0], 0, 0] * float(scales[1][table[b, 0], 0, 0])).float().to(torch.bfloat16)
         assert torch.equal(out[b, 0, 0].cpu(), want) and torch.equal(out[b, 0, 1].cpu(), want)
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f16"))
+@pytest.mark.parametrize("col", (False, True))
+@pytest.mark.parametrize("Lq,Hq,H,D,page,bits", SHAPES + ((1, 8, 1, 128, 16, 8), (1, 8, 1, 64, 16, 4)))
+@pytest.mark.parametrize("bad", (math.inf, -math.inf, math.nan))
+def test_a_key_that_is_not_finite_makes_the_queries_that_see_it_nan(cq, dtype, col, Lq, Hq, H, D, page, bits, bad):  # noqa: F811
+    """Written through kv_write: such a head has codes 0 and a scale that is not finite, and reads back as NaN."""
+    lens = [Lq, 70, 333]
+    cache, _, _, _, table = sequences(cq, lens, H, D, page, bits, col, 21)
+    q = normal((len(lens), Lq, Hq, D), 22, DT[dtype], outliers=False).cuda()
+    want, want_lse = attend(cq, cache, q, table, lens)
+    for b, n in ((1, 70), (2, 333)):
+        at = n - 1 if b == 1 else n - Lq                              # seen by the last query alone; by all of them
+        x = normal((1, H, D), 23, DT[dtype], outliers=False)
+        slot = torch.tensor([int(table[b, at // page]) * page + at % page], device="cuda")
+        kept = cq.kv_read(cache, slot, torch.float32)[1].to(DT[dtype])
+        x[:, 0, 5] = bad                                              # one head of the token
+        cq.kv_write(cache, x.cuda(), kept, slot)
+        assert bool(torch.isnan(cq.kv_read(cache, slot)[0][0, 0]).all())
+    got, got_lse = attend(cq, cache, q, table, lens)
+    G = Hq // H
+    assert torch.equal(got[0], want[0]) and torch.equal(got_lse[0], want_lse[0])
+    assert torch.equal(got[1, :-1], want[1, :-1]) and torch.equal(got_lse[1, :-1], want_lse[1, :-1])
+    for rows, lse in ((got[1, -1:, :G], got_lse[1, -1:, :G]), (got[2, :, :G], got_lse[2, :, :G])):
+        assert bool(torch.isnan(rows).all()) and bool(torch.isnan(lse).all())
+    assert bool(torch.isfinite(got[1:, :, G:]).all())
