@@ -674,7 +674,8 @@ def fp8_linear(X: torch.Tensor, w: Fp8Weight, out_dtype: torch.dtype | None = No
 
 # ----------------------------------------------------------------------------- key/value cache
 class KVCache:
-    """A paged cache of quantized keys and values (layout in include/cq.h); checks its tensors once, when it is made.
+    """A paged cache of quantized keys and values (layout in include/cq.h); checks its tensors once, when it is made, and keeps
+    their addresses: its fields cannot be replaced (make another cache), their contents are the caller's to change.
 
     k_codes, v_codes   int8 [pages, H, page_size, D] (bits = 8) or uint8 [pages, H, page_size, D / 2] (bits = 4)
     k_scale, v_scale   float32 [pages, H, page_size]
@@ -707,11 +708,16 @@ class KVCache:
                     raise ValueError(f"channel factors must be contiguous float32 [{H}, {D}] on cuda:{dev}")
         if dev < 0:
             raise TypeError("expected CUDA tensors")
-        self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.bits = k_codes, v_codes, k_scale, v_scale, bits
-        self.k_col, self.v_col, self.device, self._index = k_col, v_col, k_codes.device, dev
-        self.pages, self.heads, self.page_size, self.head_dim = pages, H, page, D
-        self._args = (k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _addr(k_col), _addr(v_col),
-                      bits, pages, page, H, D)
+        args = (k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _addr(k_col), _addr(v_col),
+                bits, pages, page, H, D)
+        for name, value in zip(self.__slots__, (k_codes, v_codes, k_scale, v_scale, bits, k_col, v_col, pages, page, H, D,
+                                                k_codes.device, dev, args)):
+            object.__setattr__(self, name, value)
+
+    def _fixed(self, *_):
+        raise AttributeError("a KVCache's fields are fixed when it is made")
+
+    __setattr__ = __delattr__ = __copy__ = __deepcopy__ = __reduce__ = _fixed
 
     @classmethod
     def empty(cls, pages: int, page_size: int, heads: int, head_dim: int, bits: int = 8, *, k_col=None, v_col=None, device="cuda"):
