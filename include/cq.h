@@ -298,7 +298,8 @@ int cq_fp8_quantize_weight(const void* W, int dtype, int64_t N, int64_t K, int64
  * out[m, n] = sum over blocks b of  a_scale[b, m] * w_scale[n / 128, b] * sum_{k in b} A[m, k] W[n, k]
  * of operands as written above (W is stored [output channels x input channels]); fp32 sums, rounded once.
  *   A [M x lda], W [N x ldw]  device codes, 16-byte aligned, lda and ldw multiples of 16 (bytes beyond K are not used)
- *   a_scale                   16-byte aligned, lds a multiple of 4, >= M
+ *   a_scale                   16-byte aligned, lds a multiple of 4, >= M; every row, the last included, is read up to M rounded up to
+ *                             a multiple of 4 (what lies behind M is not used)
  *   out                       device [M x ldo] of out_dtype (CQ_F16, CQ_BF16, CQ_F32); ldo >= N
  * K == 0 writes zeros.  CQ_ERR_ALIGN for operands that are not laid out so.
  */

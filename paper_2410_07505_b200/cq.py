@@ -523,7 +523,7 @@ BLOCK = 128                   # elements under one scale: along a row of activat
 
 class Fp8Act(NamedTuple):
     """Block-quantized activations: e4m3 codes [T, K] (row pitch a multiple of 16) and their scales [ceil(K / 128), T]
-    (row pitch a multiple of 4)."""
+    (row pitch a multiple of 4; every row is read up to a multiple of 4)."""
     codes: torch.Tensor
     scale: torch.Tensor
 
@@ -593,6 +593,18 @@ def _act_scale_pitch(scale: torch.Tensor, nb: int, T: int, dev: int, what: str) 
     return pitch if nb > 1 else max(pitch, _up(T, 4))
 
 
+def _act_scale(nb: int, T: int, device) -> torch.Tensor:
+    return torch.empty((nb, _up(T, 4)), dtype=_F32, device=device)[:, :T]
+
+
+def _whole_rows(scale: torch.Tensor) -> torch.Tensor:
+    """The scales themselves, or a copy where their storage ends before the last row does (up to a multiple of 4)."""
+    nb, T = scale.shape
+    if nb == 0 or scale.storage_offset() + (nb - 1) * scale.stride(0) + _up(T, 4) <= scale.untyped_storage().nbytes() // 4:
+        return scale
+    return _act_scale(nb, T, scale.device).copy_(scale)
+
+
 def _check_weight_scale(scale: torch.Tensor, N: int, K: int, dev: int, what: str) -> None:
     shape = ((N + 127) // 128, (K + 127) // 128)
     if scale.dtype != _F32 or scale.shape != shape or scale.get_device() != dev or not scale.is_contiguous():
@@ -604,7 +616,7 @@ def fp8_quantize_act(X: torch.Tensor, *, out: Fp8Act | None = None) -> Fp8Act:
     T, K, ld, dt, dev = _matrix16(X)
     nb = -(-K // BLOCK)
     if out is None:
-        out = Fp8Act(_fp8_codes(T, K, X.device), torch.empty_strided((nb, T), (_up(T, 4), 1), dtype=_F32, device=X.device))
+        out = Fp8Act(_fp8_codes(T, K, X.device), _act_scale(nb, T, X.device))
     codes, scale = out
     _check(lib().cq_fp8_quantize_act(X.data_ptr(), dt, T, K, ld, codes.data_ptr(), _codes_pitch(codes, T, K, dev, "out"), scale.data_ptr(),
                                      _act_scale_pitch(scale, nb, T, dev, "out"), _raw(dev)), "cq_fp8_quantize_act")
@@ -643,9 +655,12 @@ def fp8_matmul(a: Fp8Act, w: Fp8Weight, out_dtype: torch.dtype = torch.bfloat16,
         raise TypeError("expected CUDA tensors")
     lda, ldw = _codes_pitch(a.codes, T, K, dev, "a"), _codes_pitch(w.codes, N, K, dev, "w")
     lds = _act_scale_pitch(a.scale, -(-K // BLOCK), T, dev, "a")
+    scale = _whole_rows(a.scale)
+    if scale is not a.scale:
+        lds = scale.stride(0)
     _check_weight_scale(w.scale, N, K, dev, "w")
     out, dt, ldo = _product_out(out, T, N, out_dtype, a.codes)
-    _check(lib().cq_fp8_matmul(a.codes.data_ptr(), lda, a.scale.data_ptr(), lds, w.codes.data_ptr(), ldw, w.scale.data_ptr(), T, N, K,
+    _check(lib().cq_fp8_matmul(a.codes.data_ptr(), lda, scale.data_ptr(), lds, w.codes.data_ptr(), ldw, w.scale.data_ptr(), T, N, K,
                                out.data_ptr(), dt, ldo, _raw(dev)), "cq_fp8_matmul")
     return out
 

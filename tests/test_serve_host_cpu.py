@@ -31,3 +31,24 @@ def test_a_cache_cannot_be_copied():
     for how in (copy.copy, copy.deepcopy):
         with pytest.raises((AttributeError, TypeError)):
             how(cache)
+
+
+# ----------------------------------------------------------------------------- scales of activations
+def storage_end(t: torch.Tensor) -> int:
+    return t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+
+
+@pytest.mark.parametrize("nb,T", ((1, 1), (1, 4), (2, 5), (3, 7), (64, 130)))
+def test_rows_of_activation_scales_are_whole(nb, T):
+    """The product copies scales in groups of four: the last row too has to be there up to a multiple of 4."""
+    up = -(-T // 4) * 4
+    made = cq._act_scale(nb, T, "cpu")
+    assert made.shape == (nb, T) and made.stride() == (up, 1) and storage_end(made) >= nb * up
+    assert cq._whole_rows(made) is made
+    short = torch.empty_strided((nb, T), (up, 1))
+    short.copy_(torch.arange(nb * T).view(nb, T))
+    whole = cq._whole_rows(short)
+    assert torch.equal(whole, short) and whole.stride(0) % 4 == 0 and storage_end(whole) >= (nb - 1) * whole.stride(0) + up
+    assert (whole is short) == (T == up)
+    wide = torch.zeros(nb, up + 4)[:, :T]
+    assert cq._whole_rows(wide) is wide
