@@ -21,14 +21,19 @@ from . import cq
 class AttentionLayer:
     def __init__(self, w_qkv: torch.Tensor, w_out: torch.Tensor, heads: int, kv_heads: int, *, sequences: int, longest: int,
                  bits: int = 8, page_size: int = 64, alpha: float = 0.15):
-        """w_qkv [(heads + 2 kv_heads) * D, hidden], w_out [hidden, heads * D], both 16-bit on the GPU."""
+        """w_qkv [(heads + 2 kv_heads) * D, hidden], w_out [hidden, heads * D], both 16-bit on the GPU.
+        A sequence has room for `longest` tokens, rounded up to whole pages."""
         self.heads, self.kv_heads, self.alpha, self.bits, self.page_size = heads, kv_heads, alpha, bits, page_size
         self.head_dim = w_out.shape[1] // heads
         self.w_qkv, self.w_out = cq.fp8_quantize_weight(w_qkv), cq.fp8_quantize_weight(w_out)
         per_seq = -(-longest // page_size)
         dev = w_qkv.device
-        self.page_table = torch.arange(sequences * per_seq, dtype=torch.int32, device=dev).view(sequences, per_seq)
+        # behind the last page stands one that is none, for positions beyond it
+        self._pages = torch.full((sequences, per_seq + 1), -1, dtype=torch.int32, device=dev)
+        self.page_table = self._pages[:, :per_seq]
+        self.page_table.copy_(torch.arange(sequences * per_seq, dtype=torch.int32, device=dev).view(sequences, per_seq))
         self.lens = torch.zeros(sequences, dtype=torch.int32, device=dev)
+        self._room, self._filled = per_seq * page_size, [0] * sequences      # tokens of each sequence, as the host knows them
         self.cache = None
 
     def _split(self, x: torch.Tensor):
@@ -37,7 +42,8 @@ class AttentionLayer:
         return qkv.split((self.heads, self.kv_heads, self.kv_heads), dim=1)
 
     def _slots(self, seq: torch.Tensor, pos: torch.Tensor) -> torch.Tensor:
-        page = self.page_table[seq, pos // self.page_size].long()
+        """Slots of positions; below 0, which the cache skips, for those beyond a sequence's last page."""
+        page = self._pages[seq, (pos // self.page_size).clamp_(max=self._pages.shape[1] - 1)].long()
         return page * self.page_size + pos % self.page_size
 
     def _calibrate(self, k: torch.Tensor, v: torch.Tensor) -> None:
@@ -47,8 +53,10 @@ class AttentionLayer:
                                       device=k.device)
 
     def prompt(self, x: torch.Tensor, seq: int) -> torch.Tensor:
-        """The prompt x [T, hidden] of sequence `seq`; the layer's outputs [T, hidden]."""
-        T = x.shape[0]
+        """The prompt x [T, hidden] of sequence `seq`; the layer's outputs [T, hidden].  What the sequence held is replaced."""
+        T, seq = x.shape[0], range(len(self._filled))[seq]
+        if not 1 <= T <= self._room:
+            raise ValueError(f"a prompt of {T} tokens: a sequence holds 1 to {self._room}")
         q, k, v = self._split(x)
         if self.cache is None:
             self._calibrate(k, v)
@@ -56,6 +64,7 @@ class AttentionLayer:
         slots = self._slots(torch.full_like(pos, seq), pos)
         cq.kv_write(self.cache, k, v, slots)
         self.lens[seq] = T
+        self._filled[seq] = T
         k, v = cq.kv_read(self.cache, slots, x.dtype)               # what later tokens will see of the prompt
         G = self.heads // self.kv_heads
         logits = torch.einsum("ihgd,jhd->hgij", q.view(T, self.kv_heads, G, -1).float(), k.float()) / math.sqrt(self.head_dim)
@@ -66,10 +75,17 @@ class AttentionLayer:
     def step(self, x: torch.Tensor) -> torch.Tensor:
         """One token for every sequence, x [sequences, hidden]; the layer's outputs [sequences, hidden]."""
         B = x.shape[0]
+        if B != len(self._filled):
+            raise ValueError(f"{B} tokens for {len(self._filled)} sequences")
+        if self.cache is None:
+            raise ValueError("a step before any prompt: the prompt calibrates the cache")
+        if max(self._filled) >= self._room:
+            raise ValueError(f"a sequence has its {self._room} tokens already")
         q, k, v = self._split(x)
         pos = self.lens.long()
         cq.kv_write(self.cache, k, v, self._slots(torch.arange(B, device=x.device), pos))
         self.lens += 1
+        self._filled = [n + 1 for n in self._filled]
         out = cq.kv_attention(q.unsqueeze(1), self.cache, self.page_table, self.lens)
         return cq.fp8_linear(out.view(B, -1), self.w_out)
 
