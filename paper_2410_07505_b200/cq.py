@@ -543,6 +543,13 @@ def _addr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
+def _workspace_of(workspace: torch.Tensor, dev: int):
+    """(address, bytes) of a caller's workspace."""
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous memory on cuda:{dev}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
@@ -681,7 +688,7 @@ def fp8_linear(X: torch.Tensor, w: Fp8Weight, out_dtype: torch.dtype | None = No
     if workspace is None:
         workspace = X.new_empty(L.cq_fp8_linear_workspace_bytes(T, K), dtype=torch.uint8)
     st = L.cq_fp8_linear(X.data_ptr(), dt, T, K, ld, codes.data_ptr(), ldw, scale.data_ptr(), N, out.data_ptr(), odt, ldo,
-                         workspace.data_ptr(), workspace.numel(), _raw(dev))
+                         *_workspace_of(workspace, dev), _raw(dev))
     if st:
         raise CQError(st, "cq_fp8_linear")
     return out
@@ -818,7 +825,7 @@ def kv_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, lens
         workspace = q.new_empty(L.cq_kv_attention_workspace_bytes(D), dtype=torch.uint8)
     _check(L.cq_kv_attention(q.data_ptr(), dt, qs[0], qs[1], qs[2], B, Lq, Hq, *cache._args, page_table.data_ptr(), width,
                              row if B > 1 else width, lens.data_ptr(), D ** -0.5 if scale is None else float(scale), out.data_ptr(), _addr(lse),
-                             workspace.data_ptr(), workspace.numel(), _raw(dev)), "cq_kv_attention")
+                             *_workspace_of(workspace, dev), _raw(dev)), "cq_kv_attention")
     return out
 
 

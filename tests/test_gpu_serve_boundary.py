@@ -50,3 +50,22 @@ def test_a_full_layer_refuses_steps_and_goes_on(cq, bits):  # noqa: F811
     layer.prompt(x[:62], 0)                                             # the sequence begins anew
     layer.prompt(x[:5], 1)
     assert torch.equal(layer.step(x[62:64]), first)
+
+
+def test_workspaces_of_another_device_or_layout_are_refused(cq):  # noqa: F811
+    x = normal((4, 256), 1, torch.bfloat16).cuda()
+    w = cq.fp8_quantize_weight(x)
+    need = int(cq.lib().cq_fp8_linear_workspace_bytes(4, 256))
+    cache = cq.KVCache.empty(2, 16, 2, 64)
+    q = torch.zeros(1, 1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    table, lens = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    more = cq.kv_attention_workspace_bytes(64)
+    for n, call in ((need, lambda ws: cq.fp8_linear(x, w, workspace=ws)), (more, lambda ws: cq.kv_attention(q, cache, table, lens, workspace=ws))):
+        for bad in (torch.empty(n, dtype=torch.uint8), torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2],
+                    torch.empty(1, dtype=torch.uint8, device="cuda").expand(n)):
+            with pytest.raises(ValueError):
+                call(bad)
+        with pytest.raises(cq.CQError):
+            call(torch.empty(n - 1, dtype=torch.uint8, device="cuda"))
+        want = call(None)
+        assert torch.equal(call(torch.empty(-(-n // 4), dtype=torch.float32, device="cuda")), want)      # sized in bytes, not elements

@@ -52,3 +52,12 @@ def test_rows_of_activation_scales_are_whole(nb, T):
     assert (whole is short) == (T == up)
     wide = torch.zeros(nb, up + 4)[:, :T]
     assert cq._whole_rows(wide) is wide
+
+
+# ----------------------------------------------------------------------------- workspaces
+def test_a_workspace_has_to_be_contiguous_memory_of_the_calls_device():
+    here = torch.zeros(64, dtype=torch.float32)
+    assert cq._workspace_of(here, -1) == (here.data_ptr(), 256)          # bytes, whatever the type
+    for bad, dev in ((here, 0), (here[::2], -1), (torch.zeros(1).expand(1 << 20), -1)):
+        with pytest.raises(ValueError):
+            cq._workspace_of(bad, dev)
