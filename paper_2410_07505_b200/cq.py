@@ -695,6 +695,13 @@ def fp8_linear(X: torch.Tensor, w: Fp8Weight, out_dtype: torch.dtype | None = No
 
 
 # ----------------------------------------------------------------------------- key/value cache
+def _check_cache_shape(pages: int, page_size: int, heads: int, head_dim: int) -> None:
+    """The library's own rule (it has the last word), so that a cache that no call takes is refused when it is made."""
+    if (head_dim != 64 and head_dim != 128) or page_size % 16 or not 16 <= page_size <= 4096 or not 1 <= heads <= 4096 \
+            or pages < 0 or pages * heads * page_size > (1 << 31) - 4096:
+        raise CQError(2, "KVCache")
+
+
 class KVCache:
     """A paged cache of quantized keys and values (layout in include/cq.h); checks its tensors once, when it is made, and keeps
     their addresses: its fields cannot be replaced (make another cache), their contents are the caller's to change.
@@ -714,6 +721,7 @@ class KVCache:
             raise ValueError("codes must be [pages, heads, page_size, head_dim]")
         pages, H, page, width = shape
         D, want = (width, torch.int8) if bits == 8 else (2 * width, torch.uint8)
+        _check_cache_shape(pages, page, H, D)
         dev = k_codes.get_device()
         for t in (k_codes, v_codes):
             if t.dtype != want or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
@@ -746,6 +754,7 @@ class KVCache:
         """A cache of zeros."""
         if bits not in (4, 8):
             raise CQError(4, "KVCache.empty")
+        _check_cache_shape(pages, page_size, heads, head_dim)
         width, dt = (head_dim, torch.int8) if bits == 8 else (head_dim // 2, torch.uint8)
         codes = [torch.zeros((pages, heads, page_size, width), dtype=dt, device=device) for _ in range(2)]
         scale = [torch.zeros((pages, heads, page_size), dtype=torch.float32, device=device) for _ in range(2)]

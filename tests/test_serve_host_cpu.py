@@ -61,3 +61,23 @@ def test_a_workspace_has_to_be_contiguous_memory_of_the_calls_device():
     for bad, dev in ((here, 0), (here[::2], -1), (torch.zeros(1).expand(1 << 20), -1)):
         with pytest.raises(ValueError):
             cq._workspace_of(bad, dev)
+
+
+# ----------------------------------------------------------------------------- shapes of a cache
+@pytest.mark.parametrize("page_size,heads,head_dim,bits", ((16, 2, 80, 8), (16, 2, 256, 8), (16, 2, 65, 4), (16, 2, 129, 4), (16, 2, 0, 8),
+                                                           (8, 2, 64, 8), (24, 2, 64, 8), (8192, 2, 64, 8), (0, 2, 64, 8), (16, 0, 64, 8),
+                                                           (16, 5000, 64, 8)))
+def test_a_cache_of_a_shape_that_no_call_takes_is_refused_when_it_is_made(page_size, heads, head_dim, bits):
+    with pytest.raises(cq.CQError) as e:
+        cq.KVCache.empty(2, page_size, heads, head_dim, bits, device="cpu")
+    assert e.value.status == 2
+    if head_dim % 2 == 0:
+        codes = torch.zeros(2, heads, page_size, head_dim if bits == 8 else head_dim // 2, dtype=torch.int8 if bits == 8 else torch.uint8)
+        scale = torch.zeros(2, heads, page_size)
+        with pytest.raises(cq.CQError):
+            cq.KVCache(codes, codes, scale, scale, bits)
+
+
+def test_a_cache_of_more_rows_than_a_call_can_count_is_refused_when_it_is_made():
+    with pytest.raises(cq.CQError):
+        cq.KVCache.empty(1 << 26, 16, 2, 64, device="meta")
