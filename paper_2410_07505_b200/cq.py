@@ -588,7 +588,7 @@ def _codes_pitch(codes: torch.Tensor, rows: int, K: int, dev: int, what: str) ->
     pitch, inner = codes.stride()
     if inner != 1 and K > 1 and rows > 0:
         raise ValueError(f"{what}.codes: columns must be contiguous")
-    return pitch if rows > 1 else max(pitch, _up(K, 16))
+    return pitch if rows > 1 else _up(K, 16)
 
 
 def _act_scale_pitch(scale: torch.Tensor, nb: int, T: int, dev: int, what: str) -> int:
@@ -597,7 +597,7 @@ def _act_scale_pitch(scale: torch.Tensor, nb: int, T: int, dev: int, what: str) 
     pitch, inner = scale.stride()
     if inner != 1 and T > 1 and nb > 0:
         raise ValueError(f"{what}.scale: a block's scales must be contiguous")
-    return pitch if nb > 1 else max(pitch, _up(T, 4))
+    return pitch if nb > 1 else _up(T, 4)
 
 
 def _act_scale(nb: int, T: int, device) -> torch.Tensor:

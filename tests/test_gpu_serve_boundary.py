@@ -69,3 +69,19 @@ def test_workspaces_of_another_device_or_layout_are_refused(cq):  # noqa: F811
             call(torch.empty(n - 1, dtype=torch.uint8, device="cuda"))
         want = call(None)
         assert torch.equal(call(torch.empty(-(-n // 4), dtype=torch.float32, device="cuda")), want)      # sized in bytes, not elements
+
+
+def test_one_row_of_an_odd_pitch_goes_through_the_product(cq):  # noqa: F811
+    a, sa, w, sw = operands(1, 70, 100, 5)
+    A, W = on_device(cq, a, sa, w, sw)
+    wide = torch.zeros(3, 264, dtype=torch.uint8, device="cuda")
+    wide[0, :100] = A.codes.view(torch.uint8)
+    scale = torch.zeros(2, 9, device="cuda")
+    scale[:1, :1] = A.scale
+    odd = cq.Fp8Act(wide.view(torch.float8_e4m3fn)[:1, :100], scale[:1, :1])
+    got = cq.fp8_matmul(odd, W, torch.float32)
+    y, mag = ref.fp8_product(a, sa, w, sw)
+    check_product(got, y, mag, torch.float32)
+    row = cq.Fp8Weight(wide.view(torch.float8_e4m3fn)[:1, :100], torch.ones(1, 1, device="cuda"))       # one output channel
+    y, mag = ref.fp8_product(a, sa, a, sw[:1] * 0 + 1)
+    check_product(cq.fp8_matmul(odd, row, torch.float32), y, mag, torch.float32)

@@ -81,3 +81,13 @@ def test_a_cache_of_a_shape_that_no_call_takes_is_refused_when_it_is_made(page_s
 def test_a_cache_of_more_rows_than_a_call_can_count_is_refused_when_it_is_made():
     with pytest.raises(cq.CQError):
         cq.KVCache.empty(1 << 26, 16, 2, 64, device="meta")
+
+
+# ----------------------------------------------------------------------------- pitches
+def test_the_pitch_of_a_single_row_does_not_matter():
+    codes = torch.zeros(4, 264, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    assert cq._codes_pitch(codes[:1, :100], 1, 100, -1, "a") == 112
+    assert cq._codes_pitch(codes[:, :100], 4, 100, -1, "a") == 264         # the library refuses this one
+    scale = torch.zeros(3, 9)
+    assert cq._act_scale_pitch(scale[:1, :5], 1, 5, -1, "a") == 8
+    assert cq._act_scale_pitch(scale[:, :5], 3, 5, -1, "a") == 9
