@@ -47,6 +47,7 @@ constexpr int kAttWarps = 4;
 constexpr int kAttThreads = 32 * (kAttWarps + 1);
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLeastFac = 1.17549435e-38f;    // 2^-126
 constexpr float kNoRef = -3.402823466e38f;      // the reference of a row that has seen nothing
 constexpr float kMostProb = 1024.0f;            // a probability may be so many times the reference's,
 constexpr float kMostUnits = 61440.0f;          // and a probability times va be so many of its row's units (fp16 ends at 65504);
@@ -417,7 +418,8 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
             sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
             if (r4 == 0) {
-                s_fac[warp * 8 + g8] = pow2i(-up_exp) * p.softmax_scale * (kLog2e * 16777216.0f);       // codes come in as 2^-24
+                // codes come in as 2^-24; not 0, which times the -infinity of an unseen token would be NaN
+                s_fac[warp * 8 + g8] = fmaxf(pow2i(-up_exp) * p.softmax_scale * (kLog2e * 16777216.0f), kLeastFac);
                 s_start[warp * 8 + g8] = -sum * (kBias / 16777216.0f);
                 s_last[warp * 8 + g8] = there ? len - p.Lq + i : -1;
             }

@@ -188,3 +188,14 @@ def test_a_key_that_is_not_finite_makes_the_queries_that_see_it_nan(cq, dtype, c
     for rows, lse in ((got[1, -1:, :G], got_lse[1, -1:, :G]), (got[2, :, :G], got_lse[2, :, :G])):
         assert bool(torch.isnan(rows).all()) and bool(torch.isnan(lse).all())
     assert bool(torch.isfinite(got[1:, :, G:]).all())
+
+
+@pytest.mark.parametrize("dtype,size,scale", (("bf16", 1e-28, 1e-30), ("bf16", 1.0, 1e-46), ("f16", 1.0, 1e-60), ("bf16", 1e-38, 0.1)))
+def test_logits_that_vanish_give_the_mean_of_what_is_seen(cq, dtype, size, scale):  # noqa: F811
+    """Queries and softmax scales so small that their product is no float: all that a query sees weighs the same."""
+    lens, Lq, D, page = [100, 3], 3, 64, 16
+    cache, codes, scales, cols, table = sequences(cq, lens, 2, D, page, 8, True, 31)
+    q = normal((2, Lq, 4, D), 32, torch.float32, outliers=False).mul(size).to(DT[dtype])
+    out, lse = attend(cq, cache, q.cuda(), table, lens, scale=scale)
+    for b, n in enumerate(lens):
+        check_sequence(out[b], lse[b], q[b], table[b], n, codes, scales, cols, page, scale, dtype)
