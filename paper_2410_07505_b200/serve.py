@@ -48,7 +48,9 @@ class AttentionLayer:
 
     def _calibrate(self, k: torch.Tensor, v: torch.Tensor) -> None:
         shape = (self.kv_heads, self.head_dim)
-        col = [cq.absmax_cols(x.reshape(x.shape[0], -1)).pow(1.0 - self.alpha).view(shape) for x in (k, v)]
+        # (c_j^(1 - alpha); 1 for a channel of which the prompt says nothing: a factor of 0 would drop what later tokens hold there)
+        top = [cq.absmax_cols(x.reshape(x.shape[0], -1)).view(shape) for x in (k, v)]
+        col = [torch.where((c > 0) & torch.isfinite(c), c.pow(1.0 - self.alpha), 1.0) for c in top]
         self.cache = cq.KVCache.empty(self.page_table.numel(), self.page_size, *shape, self.bits, k_col=col[0], v_col=col[1],
                                       device=k.device)
 

@@ -115,3 +115,21 @@ def test_positions_beyond_the_last_slot_name_no_slot(plain):
     pos = torch.tensor([11, 12, 13, 16, 1000])
     got = a._slots(torch.ones(5, dtype=torch.long), pos).tolist()
     assert got[0] == 23 and all(s < 0 for s in got[1:])
+
+
+@pytest.mark.parametrize("alpha", (0.15, 0.5, 1.0))
+def test_channels_that_the_prompt_does_not_calibrate_have_factor_1(plain, alpha):
+    """A factor of 0 would store 0 for whatever later tokens hold in the channel, an infinite one NaN."""
+    a = layer(alpha=alpha)
+    a.w_qkv = a.w_qkv.clone()
+    key = HEADS * D
+    a.w_qkv[key + 3] = 0                                        # channel 3 of key head 0: 0 in the prompt
+    a.w_qkv[key + KV * D + D + 5] = float("inf")                # channel 5 of value head 1
+    x = tokens(4).abs()
+    a.prompt(x, 0)
+    (_, _, k_col, v_col), = plain.caches
+    assert k_col[0, 3] == 1 and v_col[1, 5] == 1
+    want = (x @ a.w_qkv.t())[:, key:key + KV * D].abs().amax(0).pow(1 - alpha).view(KV, D)
+    want[0, 3] = 1
+    torch.testing.assert_close(k_col, want, rtol=1e-6, atol=0)
+    assert bool(torch.isfinite(v_col).all()) and bool((v_col > 0).all())
