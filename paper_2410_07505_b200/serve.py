@@ -122,6 +122,8 @@ def demo(hidden: int, heads: int, kv_heads: int, prompt: int, steps: int, bits: 
             got[b].append(out[b:b + 1])
     torch.cuda.synchronize()
     took = time.perf_counter() - began
+    if cq.serve_fault():
+        raise RuntimeError("a bounded wait gave up in one of the kernels: the results are not to be used")
     err = {}
     for part, at in (("prompt", slice(0, prompt)), ("steps", slice(prompt, None))):
         off = ref = 0.0

@@ -85,3 +85,12 @@ def test_one_row_of_an_odd_pitch_goes_through_the_product(cq):  # noqa: F811
     row = cq.Fp8Weight(wide.view(torch.float8_e4m3fn)[:1, :100], torch.ones(1, 1, device="cuda"))       # one output channel
     y, mag = ref.fp8_product(a, sa, a, sw[:1] * 0 + 1)
     check_product(cq.fp8_matmul(odd, row, torch.float32), y, mag, torch.float32)
+
+
+def test_the_demo_does_not_report_results_of_a_wait_that_gave_up(cq, monkeypatch):  # noqa: F811
+    from paper_2410_07505_b200 import serve
+    args = dict(hidden=256, heads=4, kv_heads=2, prompt=20, steps=2, bits=8)
+    assert serve.demo(**args)["relative_error_steps"] < 0.2
+    monkeypatch.setattr(cq, "serve_fault", lambda: 1)
+    with pytest.raises(RuntimeError):
+        serve.demo(**args)
