@@ -277,7 +277,8 @@ int cq_set_timing_events(void* before_quantize_pass, void* after_quantize_pass);
 
 /* ------------------------------------------------------------------------------------------------
  * Serving a quantized model: a linear layer on 8-bit floats, and a quantized key/value cache with the
- * attention that reads it.  (The paper stops at quantized operands; these consume them.)
+ * attention that reads it.  (The paper stops at quantized operands.  These quantize 16-bit operands into formats of their
+ * own; none reads the codes of the functions above.)
  * ------------------------------------------------------------------------------------------------
  *
  * Block quantization to e4m3 (the 8-bit float with 4 exponent and 3 fraction bits, largest value 448):
@@ -346,9 +347,9 @@ int cq_kv_read(const void* k_codes, const void* v_codes, const float* k_scale, c
  *   Q     16-bit, element (b, i, h', d) at b * q_batch_stride + i * q_token_stride + h' * q_head_stride + d
  *   out   dense [B][Lq][Hq][D] of Q's dtype;  lse  float [B][Lq][Hq], the logarithm of the softmax's sum; nullable
  * What a query does not see has no effect on its result, bit for bit, infinite and NaN scales included; a key or value
- * head with an infinity or NaN that it sees makes its result NaN.  Probabilities times value scales are rounded to fp16 (CQ_F16: to two of them, the
- * second for what the first leaves): a token keeps 11 bits (22) where its probability times its value scale is at least 2^-18 of its
- * row's largest, fewer below, and counts as 0 below 2^-29 of it.
+ * head with an infinity or NaN that it sees makes its result NaN.  Queries times channel factors and probabilities times value
+ * scales enter the products as fp16, for CQ_F16 as two such numbers each: an element of the one is off by at most 2^-11 (2^-22) of
+ * itself plus 2^-35 of its row's largest, one of the other by 2^-11 (2^-22) of itself plus 2^-29 of its row's largest.
  * A query that sees no token gets zeros (lse: -infinity).  Tokens of a page number outside the cache are not
  * seen; lens beyond table_width * page_size are cut to it, below 0 they count as 0.  Whatever lies in slots behind a
  * sequence's end has no effect.  softmax_scale lies above 0 (CQ_ERR_ALPHA otherwise).  The result does not depend on what other

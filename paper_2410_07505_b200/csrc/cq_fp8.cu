@@ -10,7 +10,7 @@
 //
 // Both are bound by HBM: 2 bytes read and 1 byte written for an element, the block's maximum found in registers.
 // Measured, tensors larger than L2: weights 28672 x 8192 109 us (6.5 TB/s, 99 % of a copy's rate; up to 127 us behind work that
-// has lowered the clocks); 1003 x 2060, 7 to 9 us, is latency.
+// has lowered the clocks); 1003 x 2060, 7 to 9 us, is latency.  Activations 4096 x 8192 19.9 us (5.1 TB/s), 1 x 8192 2.3 us.
 #include "cq_serve.cuh"
 
 namespace cq {

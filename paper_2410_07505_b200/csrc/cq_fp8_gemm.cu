@@ -19,8 +19,9 @@
 // in a long run, which the power limit sets (2.26 and 1.94 PFLOP/s); 1 x 8192 x 8192 15.2 us (4.4 TB/s of weights),
 // 48 x 5120 x 13824 22.3 us, 777 x 2060 x 1003 15.6 us.  The first is bound by shared memory: a block's operands (48 KB for
 // 256 columns) are written once and read once, 768 cycles at 128 bytes each, beside 512 of products and 256 of
-// multiply-adds.  Pairs of CTAs, which would halve the reads of W, lose more by the exchange of each block's sums between
-// their SMs.  The next two are the read of W and about 5 us of launches, first loads and joins; the last is those alone.
+// multiply-adds.  Pairs of CTAs, which would halve the reads of W, took 1580 us where this took 952; the cause was not
+// isolated.  The next two are the read of W and about 5 us of launches, first loads and joins (the second also 2 parts of 108
+// tiles on 148 SMs, 1.37 times the average on the busiest); the last is those alone.
 #include "cq_serve.cuh"
 
 #include <atomic>
