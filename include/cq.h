@@ -363,7 +363,31 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
                     const int* page_table, int64_t table_width, int64_t table_stride, const int* lens, double softmax_scale,
                     void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Health check of the product and the attention, as cq_stage_fault is of the quantizers: 1 if a bounded wait in one of their
+/*
+ * Causal attention over packed prompts: rows q_starts[b] .. q_starts[b + 1] of Q are the queries of sequence b, rows k_starts[b] ..
+ * k_starts[b + 1] of K and V its keys and values; of Lq queries and Lk keys query i sees the keys j <= Lk - Lq + i (the queries are the
+ * sequence's last tokens); query heads h * Hq / H .. share key/value head h:
+ *   out[i, h'] = softmax_j(softmax_scale * q . k_j) v_j
+ *   Q, K, V  16-bit of one dtype [Tq][Hq][D], [Tk][H][D], [Tk][H][D], element (t, h, d) at t * token_stride + h * head_stride + d;
+ *            16-byte aligned, strides above 0 and multiples of 8 (those of an axis of one element do not matter); D is 64 or 128
+ *   q_starts, k_starts  device int32 [B + 1], not falling; what they say beyond Tq and Tk is cut off
+ *   out      dense [Tq][Hq][D] of that dtype, 16-byte aligned;  lse  float [Tq][Hq], the logarithm of the softmax's sum; nullable
+ * A query that sees no key gets zeros (lse: -infinity).  Rows of out and lse before q_starts[0] and from q_starts[B] on are not written.
+ * Keys and values that a query does not see have no effect on its result, infinities and NaN included; an infinity or NaN in a value
+ * that it sees makes that channel of its result one (or the other), one in a key its whole row NaN, but for logits of -infinity,
+ * which count as not seen.  Logits and sums are fp32 (a logit beyond its range is infinite); each weight, relative to a reference of its row at
+ * most 2^8 below the largest so far, is rounded once to the dtype before it meets the values (fp16: after a factor of 2^7).
+ * softmax_scale lies in [2^-100, 1e30] (CQ_ERR_ALPHA otherwise).  Equal calls give equal bits.
+ * workspace: device, 256-byte aligned, >= cq_prompt_attention_workspace_bytes(...) (0 where there are tiles enough: then it may
+ * be NULL); contents undefined after.
+ */
+size_t cq_prompt_attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D);
+int cq_prompt_attention(const void* Q, int64_t q_token_stride, int64_t q_head_stride, const void* K, int64_t k_token_stride,
+                        int64_t k_head_stride, const void* V, int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t B,
+                        int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D, const int* q_starts, const int* k_starts,
+                        double softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Health check of the product and the attentions, as cq_stage_fault is of the quantizers: 1 if a bounded wait in one of their
  * kernels ever gave up on the current device.  Synchronises the device. */
 int cq_serve_fault(unsigned int* fault_host);
 

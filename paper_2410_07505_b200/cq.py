@@ -28,8 +28,10 @@ EXPORTS = (
     "cq_vector_max", "cq_quantize_act_given",
     "cq_fp8_quantize_act", "cq_fp8_quantize_weight", "cq_fp8_matmul", "cq_fp8_linear_workspace_bytes", "cq_fp8_linear",
     "cq_kv_write", "cq_kv_read", "cq_kv_attention_workspace_bytes", "cq_kv_attention", "cq_serve_fault",
+    "cq_prompt_attention_workspace_bytes", "cq_prompt_attention",
 )
-_SIZES = ("cq_workspace_bytes", "cq_host_scratch_bytes", "cq_fp8_linear_workspace_bytes", "cq_kv_attention_workspace_bytes")
+_SIZES = ("cq_workspace_bytes", "cq_host_scratch_bytes", "cq_fp8_linear_workspace_bytes", "cq_kv_attention_workspace_bytes",
+          "cq_prompt_attention_workspace_bytes")
 
 
 class CQError(RuntimeError):
@@ -90,6 +92,10 @@ def lib() -> C.CDLL:
         L.cq_kv_attention.argtypes = [vp, ci, i64, i64, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, ci, i64, i64, i64, i64,
                                       vp, i64, i64, vp, dbl, vp, vp, vp, sz, vp]
         L.cq_serve_fault.argtypes = [vp]
+        L.cq_prompt_attention_workspace_bytes.restype = sz
+        L.cq_prompt_attention_workspace_bytes.argtypes = [i64] * 6
+        L.cq_prompt_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, ci, i64, i64, i64, i64, i64, i64, vp, vp, dbl, vp, vp,
+                                          vp, sz, vp]
         L.cq_set_tuning.argtypes = [C.c_char_p, ci]
         L.cq_set_timing_events.argtypes = [vp, vp]
         for name in EXPORTS:
@@ -838,8 +844,71 @@ def kv_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, lens
     return out
 
 
+# ----------------------------------------------------------------------------- prompts
+def _heads16(x: torch.Tensor, tokens, heads, head_dim, dtype, dev: int, what: str):
+    """Strides of tokens and heads of a 16-bit CUDA tensor [tokens, heads, head_dim] (None: any)."""
+    shape = x.shape
+    if x.dtype != dtype or len(shape) != 3 or x.get_device() != dev or any(n is not None and n != m for n, m in zip((tokens, heads, head_dim), shape)):
+        raise ValueError(f"{what} must be {dtype} [{tokens or 'tokens'}, {heads or 'heads'}, {head_dim}] on cuda:{dev}")
+    token, head, inner = x.stride()
+    if inner != 1 and x.numel() > 0:
+        raise ValueError(f"{what}: head elements must be contiguous")
+    return token, head
+
+
+def _starts(starts: torch.Tensor, B, dev: int, what: str) -> int:
+    if starts.dtype != _I32 or starts.dim() != 1 or starts.shape[0] < 1 or not starts.is_contiguous() or starts.get_device() != dev \
+            or (B is not None and starts.shape[0] != B + 1):
+        raise ValueError(f"{what} must be a contiguous int32 vector of {'sequences' if B is None else B} + 1 on cuda:{dev}")
+    return starts.shape[0] - 1
+
+
+def prompt_attention_workspace_bytes(sequences: int, queries: int, keys: int, query_heads: int, heads: int, head_dim: int) -> int:
+    return int(lib().cq_prompt_attention_workspace_bytes(sequences, queries, keys, query_heads, heads, head_dim))
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: torch.Tensor, k_starts: torch.Tensor | None = None, *,
+                     scale: float | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Causal attention over packed prompts, q [Tq, Hq, D], k and v [Tk, H, D] (float16 / bfloat16; strides of tokens and heads
+    multiples of 8).
+
+    Sequence b's queries are the rows q_starts[b] .. q_starts[b + 1] (int32 [B + 1]), its keys those of k_starts (default: the same); the
+    queries are its last tokens.  `scale` multiplies the logits (default 1 / sqrt(D)); `lse` float32 [Tq, Hq] receives the
+    logarithm of the softmax's sum.  Rows outside the sequences are not written."""
+    dt, dev = _DT16.get(q.dtype), q.get_device()
+    if dt is None or q.dim() != 3 or dev < 0:
+        raise TypeError("q must be a float16 / bfloat16 CUDA tensor [tokens, heads, head_dim]")
+    Tq, Hq, D = shape = q.shape
+    qs = _heads16(q, Tq, Hq, D, q.dtype, dev, "q")
+    ks = _heads16(k, None, None, D, q.dtype, dev, "k")
+    Tk, H, _ = k.shape
+    vs = _heads16(v, Tk, H, D, q.dtype, dev, "v")
+    B = _starts(q_starts, None, dev, "q_starts")
+    if k_starts is None:
+        k_starts = q_starts
+    else:
+        _starts(k_starts, B, dev, "k_starts")
+    if out is None:
+        out = q.new_empty(shape)
+    elif out.shape != shape or out.dtype != q.dtype or out.get_device() != dev or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape and dtype")
+    if lse is not None and (lse.shape != shape[:2] or lse.dtype != _F32 or lse.get_device() != dev or not lse.is_contiguous()):
+        raise ValueError("lse must be a contiguous float32 [Tq, Hq] tensor")
+    L = _lib or lib()
+    if workspace is None:
+        need = L.cq_prompt_attention_workspace_bytes(B, Tq, Tk, Hq, H, D)
+        workspace = q.new_empty(need, dtype=torch.uint8) if need else None
+    ws = (0, 0) if workspace is None else _workspace_of(workspace, dev)
+    st = L.cq_prompt_attention(q.data_ptr(), *qs, k.data_ptr(), *ks, v.data_ptr(), *vs, dt, B, Tq, Tk, Hq, H, D, q_starts.data_ptr(),
+                               k_starts.data_ptr(), D ** -0.5 if scale is None else float(scale), out.data_ptr(), _addr(lse), *ws, _raw(dev))
+    if st:
+        raise CQError(st, "cq_prompt_attention")
+    return out
+
+
 def serve_fault() -> int:
-    """1 if a bounded wait of fp8_matmul, fp8_linear or kv_attention ever gave up on the current device, else 0."""
+    """1 if a bounded wait of fp8_matmul, fp8_linear, kv_attention or prompt_attention ever gave up on the current device, else 0."""
     flag = C.c_uint(0)
     _check(lib().cq_serve_fault(C.byref(flag)), "cq_serve_fault")
     return int(flag.value)

@@ -933,10 +933,11 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
 
 int cq_serve_fault(unsigned int* fault_host) {
     if (fault_host == nullptr) return CQ_ERR_NULL;
-    unsigned int product = 0, attention = 0;
+    unsigned int product = 0, attention = 0, prompt = 0;
     int rc = cq::fp8_stage_fault(&product);
     if (rc == CQ_OK) rc = cq::attn_stage_fault(&attention);
-    if (rc == CQ_OK) *fault_host = product | attention;
+    if (rc == CQ_OK) rc = cq::prompt_stage_fault(&prompt);
+    if (rc == CQ_OK) *fault_host = product | attention | prompt;
     return rc;
 }
 

@@ -1,0 +1,737 @@
+// Causal attention over packed prompts on the 5th-generation tensor cores.
+//
+// For sequence b with Lq queries and Lk keys (rows q_starts[b].. of Q and k_starts[b].. of K and V), query i sees the keys
+// j <= Lk - Lq + i; G = Hq / H query heads share a key/value head:
+//   out[i] = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(c q_i . k_j - ref_i),   c = softmax_scale log2(e)
+// in one pass over the keys.  ref_i is the largest c q_i . k_j so far, renewed only when a block exceeds it by 2^kSlack, so
+// that the running result is hardly ever rescaled.  Sums and references are fp32; p is rounded once to the inputs' 16 bits,
+// as an operand of the second product (kind::f16 takes both operands in one type), in fp16 with 2^kBias in front so that small
+// weights keep their bits.
+#include "cq_serve.cuh"
+
+#include <algorithm>
+#include <atomic>
+
+namespace cq {
+
+__device__ unsigned int g_prompt_fault = 0;   // set if a bounded wait ever gave up
+
+constexpr int kPromptThreads = 384;           // warps 0..3, 4..7: softmax of the two tiles; warp 8: loads; warp 9: products; two idle
+constexpr int kTileRows = 128;                // rows of a tile: tokens x the query heads that go together
+constexpr int kKeys = 128;                    // keys of a block
+constexpr float kSlack = 8.0f;
+constexpr int kMaxSplits = 16;
+template <int DT> __host__ __device__ constexpr float prompt_bias() { return DT == CQ_F16 ? 7.0f : 0.0f; }   // 2^(7 + 8) < 65504
+
+template <int D> __host__ __device__ constexpr int prompt_stages() { return D == 128 ? 5 : 8; }
+template <int D> __host__ __device__ constexpr size_t prompt_tile() { return size_t(128) * D * 2; }         // bytes of a tile of Q and of a block of K or V
+template <int D> __host__ __device__ constexpr size_t prompt_smem() { return (2 + prompt_stages<D>()) * prompt_tile<D>() + 512; }
+
+struct PromptArgs {
+    const int* q_starts; const int* k_starts;
+    const uint16_t* v; int64_t vt, vh;        // strides of tokens and heads
+    uint16_t* out; float* lse; float* part;
+    float c;
+    int Tq, Tk, B, Hq, G;
+    int g, tokens;                            // a tile: `tokens` tokens x g query heads
+    int groups;                               // (key heads) x (groups of g query heads of each)
+    int splits;                               // parts of the keys of each item
+};
+
+// Two tiles of one sequence and head group, over the key blocks [jb, je).
+struct PromptItem {
+    int q0, tokens;                           // first row of Q, tokens of the item; tokens < 0: no more items
+    int k0, sees, keys;                       // first row of K; keys that the item's first token sees (may be below 1); keys of the sequence
+    int kv, head0, part;
+    int jb, end[2];                           // key blocks of the tiles: [jb, end[t]), none where end[t] <= jb
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ void tile_load3(void* dst_smem, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 :: "r"(smem_u32(dst_smem)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
+}
+// D[tmem] (+)= A B, 16-bit operands, fp32 accumulation; A in shared memory or (_ts) in tensor memory
+__device__ __forceinline__ void tc_mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u) : "memory");
+}
+__device__ __forceinline__ void tc_mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u) : "memory");
+}
+// fp32 accumulator, 16-bit operands of one type; `rows_b`: B lies row by row along N (rows of the contraction)
+template <int DT> __host__ __device__ constexpr uint32_t idesc_f16(uint32_t m, uint32_t n, bool rows_b) {
+    constexpr uint32_t type = DT == CQ_BF16 ? 1u : 0u;
+    return (1u << 4) | (type << 7) | (type << 10) | (rows_b ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+// [128 rows along the contraction][64 elements along N] per 16 KB, 128-byte swizzle: 64 elements further along N lie 16 KB
+// further, eight rows of the contraction 1024 bytes further.
+__device__ __forceinline__ uint64_t smem_desc_n128(const void* tile) {
+    const uint64_t addr = smem_u32(tile);
+    return ((addr & 0x3FFFFu) >> 4) | (uint64_t(16384 >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+                 :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                    "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                    "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const float (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 :: "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]),
+                    "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// All lanes wait and agree on what came of it, so that a warp's roles never part.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* dead) {
+    return __all_sync(0xFFFFFFFFu, role_wait(bar, parity, dead)) != 0;
+}
+
+// nonzero bit 15 or 31 where a 16-bit element is an infinity or NaN
+template <int DT>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    constexpr uint32_t exponent = DT == CQ_BF16 ? 0x7F807F80u : 0x7C007C00u, one = DT == CQ_BF16 ? 0x00800080u : 0x04000400u;
+    return ((w & exponent) + one) & 0x80008000u;
+}
+
+// ---- which item is the i-th ---------------------------------------------------------------------------------
+struct Sequence { int q0, k0, lq, lk; };
+__device__ __forceinline__ Sequence sequence_at(const PromptArgs& p, int b) {
+    const int q0 = min(max(__ldg(p.q_starts + b), 0), p.Tq), q1 = min(max(__ldg(p.q_starts + b + 1), q0), p.Tq);
+    const int k0 = min(max(__ldg(p.k_starts + b), 0), p.Tk), k1 = min(max(__ldg(p.k_starts + b + 1), k0), p.Tk);
+    return {q0, k0, q1 - q0, k1 - k0};
+}
+// Pairs of tiles of the sequence that need at least x blocks of keys.  Later pairs need more, the i-th
+// ceil((lk - lq + min((i + 1) 2 tokens, lq)) / 128) of them.
+__device__ __forceinline__ int pairs_from(const Sequence& s, int tokens2, int x) {
+    const int n = (s.lq + tokens2 - 1) / tokens2;
+    if (x <= 0 || n == 0) return n;
+    const int room = (x - 1) * kKeys;                           // pairs whose last token sees no more need less
+    if (s.lk <= room) return 0;
+    const int below = room - (s.lk - s.lq);
+    return n - min(below > 0 ? below / tokens2 : 0, n - 1);
+}
+
+// The items in the order of their work, the longest first: all head groups of a pair of tiles side by side, the pairs of all
+// sequences by the number of their key blocks (found by bisection over that number).  Computed by a whole warp.
+__device__ __forceinline__ bool find_item(const PromptArgs& p, int64_t index, int total_pairs, int most_blocks, PromptItem& it) {
+    const int lane = threadIdx.x & 31;
+    const int per_pair = p.groups * p.splits;
+    const int64_t rank64 = index / per_pair;
+    if (rank64 >= total_pairs) return false;
+    const int rank = static_cast<int>(rank64);
+    const int within = static_cast<int>(index - rank64 * per_pair);
+    const int tokens2 = 2 * p.tokens;
+    auto count = [&](int x) {
+        int n = 0;
+        for (int b = lane; b < p.B; b += 32) n += pairs_from(sequence_at(p, b), tokens2, x);
+        return __reduce_add_sync(0xFFFFFFFFu, n);
+    };
+    int lo = 0, hi = most_blocks + 1;                           // count(lo) > rank, count(hi) <= rank
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (count(mid) > rank) lo = mid; else hi = mid;
+    }
+    int skip = rank - count(hi);                                // of the pairs with exactly lo blocks
+    Sequence seq{};
+    int pair = -1;
+    for (int b0 = 0; b0 < p.B && pair < 0; b0 += 32) {
+        const bool have = b0 + lane < p.B;
+        const Sequence s = have ? sequence_at(p, b0 + lane) : Sequence{0, 0, 0, 0};
+        const int from = pairs_from(s, tokens2, lo);
+        int mine = from - pairs_from(s, tokens2, hi), before = mine;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xFFFFFFFFu, before, off);
+            if (lane >= off) before += o;
+        }
+        const int all = __shfl_sync(0xFFFFFFFFu, before, 31);
+        before -= mine;
+        const bool here = skip >= before && skip < before + mine;
+        const unsigned who = __ballot_sync(0xFFFFFFFFu, here);
+        if (who != 0u) {
+            const int src = __ffs(who) - 1;
+            const int at = (s.lq + tokens2 - 1) / tokens2 - from + (skip - before);
+            seq.q0 = __shfl_sync(0xFFFFFFFFu, s.q0, src);
+            seq.k0 = __shfl_sync(0xFFFFFFFFu, s.k0, src);
+            seq.lq = __shfl_sync(0xFFFFFFFFu, s.lq, src);
+            seq.lk = __shfl_sync(0xFFFFFFFFu, s.lk, src);
+            pair = __shfl_sync(0xFFFFFFFFu, at, src);
+        }
+        skip -= all;
+    }
+    if (pair < 0) return false;
+    const int group = within / p.splits, per_kv = p.G / p.g;
+    it.part = within - group * p.splits;
+    it.kv = group / per_kv;
+    it.head0 = it.kv * p.G + (group - it.kv * per_kv) * p.g;
+    const int i0 = pair * tokens2;
+    it.q0 = seq.q0 + i0;
+    it.tokens = min(tokens2, seq.lq - i0);
+    it.k0 = seq.k0;
+    it.keys = seq.lk;
+    it.sees = seq.lk - seq.lq + i0 + 1;
+    int n[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int last = min((t + 1) * p.tokens, it.tokens) - 1;
+        n[t] = last < t * p.tokens ? 0 : (max(it.sees + last, 0) + kKeys - 1) / kKeys;
+    }
+    const int blocks = max(n[0], n[1]);
+    it.jb = static_cast<int>(static_cast<int64_t>(blocks) * it.part / p.splits);
+    const int stop = static_cast<int>(static_cast<int64_t>(blocks) * (it.part + 1) / p.splits);
+    it.end[0] = min(stop, n[0]);
+    it.end[1] = min(stop, n[1]);
+    return true;
+}
+
+// ---- the kernel ------------------------------------------------------------------------------------------------
+template <int D, int DT>
+__global__ void __launch_bounds__(kPromptThreads, 1)
+k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
+           const PromptArgs p) {
+    constexpr int ST = prompt_stages<D>();
+    constexpr uint32_t kTile = static_cast<uint32_t>(prompt_tile<D>());
+    constexpr float kBias = prompt_bias<DT>();
+    // No static shared memory, so that the dynamic part starts on the 1024-byte boundary that the swizzle wants.
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t* s_q = smem;                                        // [tile][half of D][128 rows][128 bytes]
+    uint8_t* s_kv = s_q + 2 * kTile;                            // [stage][half of D][128 keys][128 bytes]
+    uint64_t* full = reinterpret_cast<uint64_t*>(s_kv + ST * kTile);
+    uint64_t* empty = full + ST;
+    uint64_t* q_full = empty + ST;
+    uint64_t* q_empty = q_full + 2;
+    uint64_t* s_full = q_empty + 2;
+    uint64_t* p_full = s_full + 2;
+    uint64_t* o_full = p_full + 2;
+    uint64_t* i_full = o_full + 2;
+    uint64_t* i_empty = i_full + 2;
+    uint64_t* drain = i_empty + 2;
+    PromptItem* s_item = reinterpret_cast<PromptItem*>(drain + 1);
+    uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(s_item + 2);
+    volatile uint32_t& s_dead = *(reinterpret_cast<volatile uint32_t*>(s_item + 2) + 1);
+    volatile uint32_t& s_poison = *(reinterpret_cast<volatile uint32_t*>(s_item + 2) + 2);
+    static_assert((2 * ST + 15) * 8 + 2 * sizeof(PromptItem) + 12 <= 512, "barriers");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    asm volatile("griddepcontrol.launch_dependents;");
+    if (threadIdx.x == 0) {
+        if ((smem_u32(smem) & 1023u) != 0u) atomicExch(&g_prompt_fault, 1u);      // cannot be: see above
+        for (int i = 0; i < ST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1);
+            mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); mbar_init(&o_full[i], 1);
+            mbar_init(&i_full[i], 1); mbar_init(&i_empty[i], 9);
+        }
+        mbar_init(drain, 1);
+        mbar_init_fence();
+        s_dead = 0;
+        s_poison = 0;
+        prefetch_map(&mapQ);
+        prefetch_map(&mapK);
+        prefetch_map(&mapV);
+    }
+    if (warp == 9) tmem_alloc(&s_tmem, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");    // 128 x 72 + 256 x 216 = 384 x 168
+        if (warp == 8) {
+            // ---- items and loads
+            int total = 0, most = 0;
+            for (int b = lane; b < p.B; b += 32) {
+                const Sequence s = sequence_at(p, b);
+                total += pairs_from(s, 2 * p.tokens, 0);
+                if (s.lq > 0) most = max(most, (s.lk + kKeys - 1) / kKeys);
+            }
+            total = __reduce_add_sync(0xFFFFFFFFu, total);
+            most = __reduce_max_sync(0xFFFFFFFFu, most);
+            bool ok = true;
+            int s = 0;
+            uint32_t round = 0, issued = 0, q_round[2] = {0, 0};
+            bool q_open[2] = {false, false};
+            for (uint32_t n = 0; ok; ++n) {
+                PromptItem it;
+                // in rounds of one item for each CTA, every other one in reverse, so that none gets the longest of each
+                const int64_t index = static_cast<int64_t>(n) * gridDim.x + ((n & 1u) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+                const bool have = find_item(p, index, total, most, it);
+                if (!have) it.tokens = -1;
+                if (!(ok = warp_wait(&i_empty[n & 1], ((n >> 1) & 1) ^ 1u, &s_dead))) break;
+                if (lane == 0) {
+                    s_item[n & 1] = it;
+                    mbar_arrive(&i_full[n & 1]);
+                }
+                __syncwarp();
+                if (!have) break;
+    #pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    if (it.end[t] > it.jb) {
+                        if (!(ok = warp_wait(&q_empty[t], q_round[t] ^ 1u, &s_dead))) break;
+                        if (elect_one()) {
+                            mbar_expect_tx(&q_full[t], p.g * p.tokens * D * 2);
+    #pragma unroll
+                            for (int h = 0; h < D / 64; ++h)
+                                tile_load3(s_q + t * kTile + h * 16384, &mapQ, h * 64, it.head0, it.q0 + t * p.tokens, &q_full[t]);
+                        }
+                        q_open[t] = true;
+                        q_round[t] ^= 1u;
+                    }
+                const int je = max(it.end[0], it.end[1]);
+                for (int j = it.jb; ok && j < je; ++j)
+    #pragma unroll
+                    for (int kv = 0; kv < 2; ++kv) {
+                        if (!(ok = warp_wait(&empty[s], round ^ 1u, &s_dead))) break;
+                        if (elect_one()) {
+                            mbar_expect_tx(&full[s], kTile);
+    #pragma unroll
+                            for (int h = 0; h < D / 64; ++h)
+                                tile_load3(s_kv + s * kTile + h * 16384, kv == 0 ? &mapK : &mapV, h * 64, it.kv, it.k0 + j * kKeys, &full[s]);
+                        }
+                        issued = min(issued + 1, uint32_t(ST));
+                        if (++s == ST) { s = 0; round ^= 1u; }
+                    }
+            }
+            if (!ok) {                            // copies still in flight land before the CTA leaves
+                for (; issued > 0; --issued) {
+                    if (--s < 0) { s = ST - 1; round ^= 1u; }
+                    for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&full[s], round); ++polls) {}
+                }
+                for (int t = 0; t < 2; ++t)
+                    if (q_open[t])
+                        for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&q_full[t], q_round[t] ^ 1u); ++polls) {}
+            }
+        } else if (warp == 9) {
+            // ---- products
+            constexpr uint32_t idesc_s = idesc_f16<DT>(128, kKeys, false), idesc_o = idesc_f16<DT>(128, D, true);
+            const uint64_t desc_q = smem_desc_k128(s_q), desc_k = smem_desc_k128(s_kv), desc_v = smem_desc_n128(s_kv);
+            bool ok = true;
+            int s = 0;
+            uint32_t round = 0, p_round[2] = {0, 0}, q_round[2] = {0, 0};
+            auto step = [&](int& stage, uint32_t& r) { if (++stage == ST) { stage = 0; r ^= 1u; } };
+            auto logits = [&](int t, int stage) {                   // S_t = Q_t K^T
+    #pragma unroll
+                for (int k = 0; k < D / 16; ++k)                    // 32 bytes further along the swizzled row, 16 KB to the other half
+                    tc_mma_f16(tmem + t * 128, desc_q + ((t * kTile + (k >> 2) * 16384 + (k & 3) * 32) >> 4),
+                               desc_k + ((stage * kTile + (k >> 2) * 16384 + (k & 3) * 32) >> 4), idesc_s, k != 0);
+            };
+            for (uint32_t n = 0; ok; ++n) {
+                if (!(ok = warp_wait(&i_full[n & 1], (n >> 1) & 1, &s_dead))) break;
+                const int jb = s_item[n & 1].jb, end[2] = {s_item[n & 1].end[0], s_item[n & 1].end[1]};
+                const bool last = s_item[n & 1].tokens < 0;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&i_empty[n & 1]);
+                if (last) break;
+                const int je = max(end[0], end[1]);
+                if (je <= jb) continue;
+                for (int j = jb - 1; ok && j < je; ++j) {           // results of block j, logits of block j + 1
+                    const int sv = s;
+                    if (j >= jb) {
+                        if (!(ok = warp_wait(&full[s], round, &s_dead))) break;
+                        step(s, round);
+                    }
+                    const int sk = s;
+                    if (j + 1 < je) {
+                        if (!(ok = warp_wait(&full[s], round, &s_dead))) break;
+                        step(s, round);
+                    }
+    #pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        if (j >= jb && j < end[t]) {
+                            if (!(ok = warp_wait(&p_full[t], p_round[t], &s_dead))) break;
+                            p_round[t] ^= 1u;
+                            tc_fence_after();
+                            if (elect_one()) {
+    #pragma unroll
+                                for (int k = 0; k < kKeys / 16; ++k)
+                                    tc_mma_f16_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, desc_v + ((sv * kTile + k * 2048) >> 4), idesc_o,
+                                                  j > jb || k != 0);
+                                if (j + 1 == end[t]) tc_commit(&o_full[t]);
+                            }
+                        }
+                        if (j + 1 < end[t]) {
+                            if (j < jb) {
+                                if (!(ok = warp_wait(&q_full[t], q_round[t], &s_dead))) break;
+                                q_round[t] ^= 1u;
+                            }
+                            tc_fence_after();
+                            if (elect_one()) {                      // (behind the product that reads the weights in the same columns)
+                                logits(t, sk);
+                                tc_commit(&s_full[t]);
+                                if (j + 2 == end[t]) tc_commit(&q_empty[t]);
+                            }
+                        }
+                    }
+                    if (!ok) break;
+                    if (elect_one()) {
+                        if (j >= jb) tc_commit(&empty[sv]);
+                        if (j + 1 < je) tc_commit(&empty[sk]);
+                    }
+                }
+            }
+            if (!ok) {                            // products in flight end before the CTA leaves
+                __syncwarp();
+                if (elect_one()) tc_commit(drain);
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(drain, 0); ++polls) {}
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        // ---- softmax: one row of a tile for each thread
+        const int t = warp >> 2, row = threadIdx.x & 127;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t at_s = tmem + t * 128 + lanes, at_o = tmem + 256 + t * 128 + lanes;
+        const int token = t * p.tokens + row / p.g, head = row % p.g;
+        const bool in_tile = row < p.g * p.tokens;
+        uint32_t s_round = 0, o_round = 0, slot = 0;            // `slot`: places of the ring that items before this one took
+        bool ok = true;
+        for (uint32_t n = 0; ok; ++n) {
+            if (!(ok = warp_wait(&i_full[n & 1], (n >> 1) & 1, &s_dead))) break;
+            const PromptItem it = s_item[n & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&i_empty[n & 1]);
+            if (it.tokens < 0) break;
+            const int jb = it.jb, end = t == 0 ? it.end[0] : it.end[1];
+            const uint32_t first_slot = slot;
+            slot += 2 * max(max(it.end[0], it.end[1]) - jb, 0);
+            if (t * p.tokens >= it.tokens) continue;            // no such tile
+            const int sees = it.sees + token;                   // this row's keys are the first `sees`
+            const int all_see = it.sees + t * p.tokens;         // those that every row of the tile sees
+            float ref = -INFINITY, sum = 0.0f;
+            for (int j = jb; j < end; ++j) {
+                if (!(ok = warp_wait(&s_full[t], s_round, &s_dead))) break;
+                s_round ^= 1u;
+                tc_fence_after();
+                float x[4][32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_ld32(at_s + q * 32, x[q]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_ld_wait(x[q]);
+                const bool edge = (j + 1) * kKeys > all_see;
+                if (edge) {
+                    const int lim = sees - j * kKeys;
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) x[i >> 5][i & 31] = i < lim ? x[i >> 5][i & 31] : -INFINITY;
+                    // A weight of 0 does not hide an infinity or NaN in V from the product: such elements become 0 in shared memory
+                    // and are added to the rows that see them at the end.
+                    const uint32_t place = first_slot + 2 * (j - jb) + 1;
+                    if (!(ok = warp_wait(&full[place % ST], (place / ST) & 1, &s_dead))) break;
+                    uint4* v4 = reinterpret_cast<uint4*>(s_kv + (place % ST) * kTile) + row;
+                    uint32_t bad = 0;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        const uint4 w = v4[i * 128];
+                        bad |= not_finite<DT>(w.x) | not_finite<DT>(w.y) | not_finite<DT>(w.z) | not_finite<DT>(w.w);
+                    }
+                    if (bad != 0u) {
+                        s_poison = 1u;
+                        __threadfence_block();
+                        for (int i = 0; i < D / 8; ++i) {
+                            uint16_t* e = reinterpret_cast<uint16_t*>(v4 + i * 128);
+                            for (int k = 0; k < 8; ++k)
+                                if (not_finite<DT>(e[k]) != 0u) e[k] = 0;
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    __syncwarp();
+                }
+                float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < 128; ++i) m[i & 3] = fmaxf(m[i & 3], x[i >> 5][i & 31]);
+                const float top = __fmul_rn(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), p.c);
+                const bool renew = top > ref + (kBias + kSlack);
+                float keep = 1.0f;
+                if (renew) {
+                    keep = ex2(ref - (top - kBias));
+                    ref = top - kBias;
+                    sum *= keep;
+                }
+                if (j > jb && __any_sync(0xFFFFFFFFu, renew)) {
+#pragma unroll
+                    for (int q = 0; q < D / 16; ++q) {
+                        float o[16];
+                        tmem_ld16(at_o + q * 16, o);
+                        tmem_ld_wait(o);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] *= keep;
+                        tmem_st16(at_o + q * 16, o);
+                    }
+                }
+                const float neg = ref == -INFINITY ? 0.0f : -ref;
+                float l[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t r[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int e = h * 64 + 2 * i;
+                        const float a = ex2(__fmaf_rn(x[e >> 5][e & 31], p.c, neg)), b = ex2(__fmaf_rn(x[e >> 5][(e & 31) + 1], p.c, neg));
+                        l[i & 1] += a;
+                        l[2 + (i & 1)] += b;
+                        r[i] = pack16x2<DT>(a, b);
+                    }
+                    tmem_st32(at_s + h * 32, r);
+                }
+                sum += (l[0] + l[1]) + (l[2] + l[3]);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[t]);
+            }
+            if (!ok) break;
+            const bool any = end > jb;
+            if (any) {
+                if (!(ok = warp_wait(&o_full[t], o_round, &s_dead))) break;
+                o_round ^= 1u;
+                tc_fence_after();
+            }
+            // ---- results of this row
+            const bool mine = in_tile && token < it.tokens;
+            const bool poison = s_poison != 0u;
+            const int64_t place = (static_cast<int64_t>(it.q0) + token) * p.Hq + it.head0 + head;
+            const float inv = sum == 0.0f ? 0.0f : __frcp_rn(sum);
+            const int from = max(jb, max(it.sees, 0) / kKeys) * kKeys, to = min(sees, end * kKeys);     // keys whose V may have been emptied
+            const int64_t rows = static_cast<int64_t>(p.Tq) * p.Hq;
+            float* part = p.part + (it.part * rows + place) * D;
+#pragma unroll
+            for (int q = 0; q < D / 32; ++q) {
+                float o[32];
+                __syncwarp();
+                if (any) {
+                    tmem_ld32(at_o + q * 32, o);
+                    tmem_ld_wait(o);
+                }
+                if (sum == 0.0f || !any) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = 0.0f;
+                }
+                if (poison && mine)
+                    for (int j = from; j < to; ++j) {
+                        const uint16_t* v = p.v + (static_cast<int64_t>(it.k0) + j) * p.vt + it.kv * p.vh + q * 32;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (not_finite<DT>(v[i]) != 0u) o[i] += cvt16<DT>(v[i]);
+                    }
+                if (!mine) continue;
+                if (p.splits > 1) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        reinterpret_cast<float4*>(part + q * 32)[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float* e = o + 8 * i;
+                        reinterpret_cast<uint4*>(p.out + place * D + q * 32)[i] =
+                            make_uint4(pack16x2<DT>(e[0] * inv, e[1] * inv), pack16x2<DT>(e[2] * inv, e[3] * inv),
+                                       pack16x2<DT>(e[4] * inv, e[5] * inv), pack16x2<DT>(e[6] * inv, e[7] * inv));
+                    }
+                }
+            }
+            if (mine) {
+                if (p.splits > 1)
+                    *reinterpret_cast<float2*>(p.part + p.splits * rows * D + (it.part * rows + place) * 2) = make_float2(ref, sum);
+                else if (p.lse != nullptr)
+                    p.lse[place] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.69314718f;
+            }
+            tc_fence_before();
+            __syncwarp();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    __syncwarp();
+    if (warp == 9) tmem_free(tmem, 512);
+    if (threadIdx.x == 0 && s_dead != 0u) atomicExch(&g_prompt_fault, 1u);
+}
+
+// ---- join of the parts of split items: a warp for each row --------------------------------------------------
+template <int D, int DT>
+__global__ void __launch_bounds__(256)
+k23_prompt_join(const PromptArgs p) {
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int64_t rows = static_cast<int64_t>(p.Tq) * p.Hq;
+    const int64_t first = static_cast<int64_t>(min(max(__ldg(p.q_starts), 0), p.Tq)) * p.Hq;
+    const int64_t stop = static_cast<int64_t>(min(max(__ldg(p.q_starts + p.B), 0), p.Tq)) * p.Hq;
+    const float2* stats = reinterpret_cast<const float2*>(p.part + p.splits * rows * D);
+    for (int64_t row = first + static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5); row < stop; row += static_cast<int64_t>(gridDim.x) * 8) {
+        float2 st = make_float2(-INFINITY, 0.0f);
+        if (lane < p.splits) st = __ldcg(stats + lane * rows + row);
+        float top = st.x;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, off));
+        const float f = st.y == 0.0f ? 0.0f : ex2(st.x - top);
+        float sum = st.y * f;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+        float o[D / 32] = {};
+        for (int s = 0; s < p.splits; ++s) {
+            const float fs = __shfl_sync(0xFFFFFFFFu, f, s);
+            if (__shfl_sync(0xFFFFFFFFu, st.y, s) == 0.0f) continue;
+            const float* part = p.part + (s * rows + row) * D + lane * (D / 32);
+            if constexpr (D == 128) {
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(part));
+                o[0] = __fmaf_rn(v.x, fs, o[0]); o[1] = __fmaf_rn(v.y, fs, o[1]);
+                o[2] = __fmaf_rn(v.z, fs, o[2]); o[3] = __fmaf_rn(v.w, fs, o[3]);
+            } else {
+                const float2 v = __ldcg(reinterpret_cast<const float2*>(part));
+                o[0] = __fmaf_rn(v.x, fs, o[0]); o[1] = __fmaf_rn(v.y, fs, o[1]);
+            }
+        }
+        const float inv = sum == 0.0f ? 0.0f : __frcp_rn(sum);
+        uint32_t* out = reinterpret_cast<uint32_t*>(p.out + row * D) + lane * (D / 64);
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) out[i] = pack16x2<DT>(o[2 * i] * inv, o[2 * i + 1] * inv);
+        if (p.lse != nullptr && lane == 0) p.lse[row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------
+int prompt_stage_fault(unsigned int* fault_host) {
+    return cudaMemcpyFromSymbol(fault_host, g_prompt_fault, sizeof(unsigned int)) == cudaSuccess ? CQ_OK : CQ_ERR_CUDA;
+}
+
+// Query heads of a key head that share a tile: the largest divisor of G up to 16 whose tiles have at least 120 of 128 rows.
+// (All rows of a tile read the same keys, so heads side by side make the tile's tokens few: less of the diagonal is computed in vain,
+// and short sequences leave fewer rows empty.)
+static int heads_of_tile(int G) {
+    for (int g = G < 16 ? G : 16; g > 1; --g)
+        if (G % g == 0 && g * (kTileRows / g) >= 120) return g;
+    return 1;
+}
+
+struct PromptPlan { int g, tokens, groups, splits; int64_t items; };
+static PromptPlan prompt_plan(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t H) {
+    PromptPlan r;
+    const int G = static_cast<int>(Hq / H);
+    r.g = heads_of_tile(G);
+    r.tokens = kTileRows / r.g;
+    r.groups = static_cast<int>(Hq / r.g);
+    r.items = (Tq / (2 * r.tokens) + std::min(B, Tq)) * r.groups;        // at most
+    // Items for less than half of the SMs: the keys of each are split, four blocks or more to a part.
+    int64_t splits = r.items > 0 ? sm_count() / r.items : 1;
+    splits = std::min(splits, Tk / std::max<int64_t>(B, 1) / (4 * kKeys));
+    r.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(splits, kMaxSplits)));
+    r.items *= r.splits;
+    return r;
+}
+
+static bool make_head_map(CUtensorMap* map, const void* base, int64_t D, int64_t heads, int64_t tokens, int64_t head_stride, int64_t token_stride,
+                          int box_heads, int box_tokens) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<Encode> known{nullptr};
+    Encode encode = known.load(std::memory_order_acquire);
+    if (encode == nullptr) {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess || fn == nullptr) {
+            cudaGetLastError();
+            return false;
+        }
+        encode = reinterpret_cast<Encode>(fn);
+        known.store(encode, std::memory_order_release);
+    }
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(head_stride) * 2, static_cast<cuuint64_t>(token_stride) * 2};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_heads), static_cast<cuuint32_t>(box_tokens)}, steps[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base), dims, strides, box, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int DT>
+static int launch_prompt(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PromptArgs& p, int64_t items, cudaStream_t st) {
+    static thread_local LaunchMemo memo;
+    if (resident_ctas(k22_prompt<D, DT>, kPromptThreads, prompt_smem<D>(), prompt_smem<D>(), memo) < 1) return CQ_ERR_CUDA;
+    const int64_t grid = std::min<int64_t>(items, sm_count());
+    const int rc = launch_ex(k22_prompt<D, DT>, dim3(static_cast<unsigned>(grid)), kPromptThreads, prompt_smem<D>(), st, 1, !tuning_no_pdl(), q, k, v, p);
+    if (rc != CQ_OK || p.splits == 1) return rc;
+    const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(p.Tq) * p.Hq + 7) / 8, 8 * sm_count());
+    return launch_ex(k23_prompt_join<D, DT>, dim3(static_cast<unsigned>(blocks)), 256, 0, st, 1, !tuning_no_pdl(), p);
+}
+
+static bool prompt_shape_ok(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D) {
+    return (D == 64 || D == 128) && H >= 1 && Hq >= H && Hq % H == 0 && Hq <= (1 << 16) && B >= 0 && B <= (1 << 20) && Tq >= 0 && Tk >= 0 &&
+           Tq < (int64_t(1) << 30) && Tk < (int64_t(1) << 30);
+}
+
+// Strides that a tensor map can hold: multiples of 16 bytes below 2^40.  The stride of an axis of one element is never used.
+static int64_t used_stride(int64_t n, int64_t stride, int64_t dense) { return n > 1 ? stride : dense; }
+static int check_strides(const void* X, int64_t tokens, int64_t heads, int64_t token_stride, int64_t head_stride) {
+    if (!ptr_aligned(X, 16)) return CQ_ERR_ALIGN;
+    for (const int64_t s : {used_stride(tokens, token_stride, 8), used_stride(heads, head_stride, 8)}) {
+        if (s <= 0 || s >= (int64_t(1) << 38)) return CQ_ERR_SHAPE;
+        if (s % 8 != 0) return CQ_ERR_ALIGN;
+    }
+    return CQ_OK;
+}
+
+}  // namespace cq
+
+extern "C" {
+
+size_t cq_prompt_attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D) {
+    using namespace cq;
+    if (!prompt_shape_ok(B, Tq, Tk, Hq, H, D)) return 0;
+    const PromptPlan plan = prompt_plan(B, Tq, Tk, Hq, H);
+    return plan.splits == 1 ? 0 : sizeof(float) * plan.splits * static_cast<size_t>(Tq) * Hq * (D + 2);
+}
+
+int cq_prompt_attention(const void* Q, int64_t q_token_stride, int64_t q_head_stride, const void* K, int64_t k_token_stride,
+                        int64_t k_head_stride, const void* V, int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t B,
+                        int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D, const int* q_starts, const int* k_starts,
+                        double softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace cq;
+    if (!prompt_shape_ok(B, Tq, Tk, Hq, H, D)) return CQ_ERR_SHAPE;
+    if (dtype != CQ_F16 && dtype != CQ_BF16) return CQ_ERR_DTYPE;
+    if (!(softmax_scale >= 0x1p-100 && softmax_scale <= 1e30)) return CQ_ERR_ALPHA;
+    if (B == 0 || Tq == 0) return CQ_OK;
+    if (Q == nullptr || out == nullptr || q_starts == nullptr || k_starts == nullptr || (Tk > 0 && (K == nullptr || V == nullptr))) return CQ_ERR_NULL;
+    if (!ptr_aligned(out, 16) || !ptr_aligned(lse, 4) || !ptr_aligned(q_starts, 4) || !ptr_aligned(k_starts, 4)) return CQ_ERR_ALIGN;
+    int rc = check_strides(Q, Tq, Hq, q_token_stride, q_head_stride);
+    if (rc == CQ_OK && Tk > 0) rc = check_strides(K, Tk, H, k_token_stride, k_head_stride);
+    if (rc == CQ_OK && Tk > 0) rc = check_strides(V, Tk, H, v_token_stride, v_head_stride);
+    if (rc != CQ_OK) return rc;
+    const PromptPlan plan = prompt_plan(B, Tq, Tk, Hq, H);
+    const size_t need = cq_prompt_attention_workspace_bytes(B, Tq, Tk, Hq, H, D);
+    if (need > 0 && (workspace == nullptr || !ptr_aligned(workspace, 256) || workspace_bytes < need)) return CQ_ERR_WORKSPACE;
+    PromptArgs p;
+    p.q_starts = q_starts; p.k_starts = k_starts;
+    p.v = static_cast<const uint16_t*>(V); p.vt = v_token_stride; p.vh = v_head_stride;
+    p.out = static_cast<uint16_t*>(out); p.lse = lse; p.part = static_cast<float*>(workspace);
+    p.c = static_cast<float>(softmax_scale * 1.4426950408889634);
+    p.Tq = static_cast<int>(Tq); p.Tk = static_cast<int>(Tk); p.B = static_cast<int>(B); p.Hq = static_cast<int>(Hq); p.G = static_cast<int>(Hq / H);
+    p.g = plan.g; p.tokens = plan.tokens; p.groups = plan.groups; p.splits = plan.splits;
+    CUtensorMap mapQ, mapK, mapV;
+    // without keys no block is ever loaded: any valid map stands for theirs
+    const void* k = Tk > 0 ? K : Q;
+    const void* v = Tk > 0 ? V : Q;
+    const int64_t keys = Tk > 0 ? Tk : 1;
+    if (!make_head_map(&mapQ, Q, D, Hq, Tq, used_stride(Hq, q_head_stride, D), used_stride(Tq, q_token_stride, Hq * D), plan.g, plan.tokens) ||
+        !make_head_map(&mapK, k, D, Tk > 0 ? H : 1, keys, used_stride(Tk > 0 ? H : 1, k_head_stride, D), used_stride(keys, k_token_stride, H * D), 1, kKeys) ||
+        !make_head_map(&mapV, v, D, Tk > 0 ? H : 1, keys, used_stride(Tk > 0 ? H : 1, v_head_stride, D), used_stride(keys, v_token_stride, H * D), 1, kKeys))
+        return CQ_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (D == 128) return dtype == CQ_F16 ? launch_prompt<128, CQ_F16>(mapQ, mapK, mapV, p, plan.items, st) : launch_prompt<128, CQ_BF16>(mapQ, mapK, mapV, p, plan.items, st);
+    return dtype == CQ_F16 ? launch_prompt<64, CQ_F16>(mapQ, mapK, mapV, p, plan.items, st) : launch_prompt<64, CQ_BF16>(mapQ, mapK, mapV, p, plan.items, st);
+}
+
+}  // extern "C"

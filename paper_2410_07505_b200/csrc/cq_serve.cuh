@@ -51,6 +51,7 @@ inline int launch_ex(void (*kern)(KArgs...), dim3 grid, unsigned block, size_t s
 
 int fp8_stage_fault(unsigned int* fault_host);   // flag of the 8-bit float product
 int attn_stage_fault(unsigned int* fault_host);  // flag of the attention over the cache
+int prompt_stage_fault(unsigned int* fault_host);  // flag of the attention over prompts
 
 // ---- device: waits ----------------------------------------------------------------------------
 __device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
