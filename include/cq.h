@@ -387,6 +387,42 @@ int cq_prompt_attention(const void* Q, int64_t q_token_stride, int64_t q_head_st
                         int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D, const int* q_starts, const int* k_starts,
                         double softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Norms of queries and keys for each head and their rotation by position.  For each token t and head, over its D channels:
+ *   y_d = w_d x_d / sqrt(mean_d x_d^2 + eps)                      (eps >= 0; y = x where eps < 0)
+ *   pair i < R / 2 of the first R channels, f = positions[t] * freq[i]:  (a, b) -> (a cos f - b sin f, a sin f + b cos f)
+ * the pair being channels (i, i + R / 2), or (2 i, 2 i + 1) with `neighbours`; channels from R on stay as they are.
+ *   Q, K          16-bit of one dtype [T][Hq][D], [T][H][D]: element (t, h, d) at t * token_stride + h * head_stride + d; q_out, k_out of that
+ *                 dtype likewise.  An output may be its input (the same address and strides); other overlaps are not allowed
+ *   positions     device int64 [T], 8-byte aligned; freq  device double [R / 2] (radians a position).  f is formed in 64 bits: an angle is off
+ *                 by 2^-52 of itself and 2^-24
+ *   q_weight, k_weight  device [D] of that dtype; null: ones.  Null where eps < 0 (CQ_ERR_ALPHA)
+ * 1 <= D <= 512, R even, 0 <= R <= D, up to 65536 heads.  16-byte aligned rows (strides multiples of 8), D a multiple of 8 up to 256 and
+ * R of 16: fast; anything else (2-byte aligned) is served by a slower kernel.  Sums and products are fp32 (64 bits where squares
+ * leave its range), the result is rounded once.  A row with an infinity or NaN is NaN in the channels that the formula makes so.
+ */
+int cq_norm_rotate(const void* Q, int64_t q_token_stride, int64_t q_head_stride, int64_t Hq, const void* K, int64_t k_token_stride,
+                   int64_t k_head_stride, int64_t H, int dtype, int64_t T, int64_t D, int64_t R, int neighbours,
+                   const int64_t* positions, const double* freq, const void* q_weight, const void* k_weight, double eps,
+                   void* q_out, int64_t qo_token_stride, int64_t qo_head_stride, void* k_out, int64_t ko_token_stride,
+                   int64_t ko_head_stride, void* stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection (cq_fp8_linear or any other that left y):
+ *   out[t] = y[t] + scale[a] B_a (A_a X[t]),  a = index[t];  out[t] = y[t] where a lies outside 0 .. n - 1
+ *   X      16-bit [T][ldx], ldx >= K;  A  dense [n][R][K], B  dense [n][N][R] of X's dtype, B 16-byte aligned;  scale  float [n], null: ones
+ *   index  device int32 [T]
+ *   y      [T][ldy] of y_dtype (CQ_F16, CQ_BF16, CQ_F32), out [T][ldo] of the same; ldy, ldo >= N.  out may be y (with the same pitch)
+ * R is a multiple of 8 up to 128 (pad with zeros), T up to 4194240.  16-byte aligned rows of X and A (of y and out) with K (N) a multiple of 8: fast.
+ * A_a X[t] is summed in fp32 and enters the second product as two 16-bit halves relative to the token's largest: off by 2^-16 of itself
+ * and 2^-24 of that (fp16; bf16 2^-17 of itself).  The result is fp32 and rounded once.  A token's result depends on no other token.  Equal calls give equal bits.
+ * workspace: device, 256-byte aligned, >= cq_adapter_add_workspace_bytes(T, R); contents undefined after.
+ */
+size_t cq_adapter_add_workspace_bytes(int64_t T, int64_t R);
+int cq_adapter_add(const void* X, int dtype, int64_t T, int64_t K, int64_t ldx, const void* A, const void* B, const float* scale, int64_t n,
+                   int64_t R, int64_t N, const int* index, const void* y, int y_dtype, int64_t ldy, void* out, int64_t ldo,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
 /* Health check of the product and the attentions, as cq_stage_fault is of the quantizers: 1 if a bounded wait in one of their
  * kernels ever gave up on the current device.  Synchronises the device. */
 int cq_serve_fault(unsigned int* fault_host);

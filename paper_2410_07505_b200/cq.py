@@ -28,10 +28,10 @@ EXPORTS = (
     "cq_vector_max", "cq_quantize_act_given",
     "cq_fp8_quantize_act", "cq_fp8_quantize_weight", "cq_fp8_matmul", "cq_fp8_linear_workspace_bytes", "cq_fp8_linear",
     "cq_kv_write", "cq_kv_read", "cq_kv_attention_workspace_bytes", "cq_kv_attention", "cq_serve_fault",
-    "cq_prompt_attention_workspace_bytes", "cq_prompt_attention",
+    "cq_prompt_attention_workspace_bytes", "cq_prompt_attention", "cq_norm_rotate", "cq_adapter_add_workspace_bytes", "cq_adapter_add",
 )
 _SIZES = ("cq_workspace_bytes", "cq_host_scratch_bytes", "cq_fp8_linear_workspace_bytes", "cq_kv_attention_workspace_bytes",
-          "cq_prompt_attention_workspace_bytes")
+          "cq_prompt_attention_workspace_bytes", "cq_adapter_add_workspace_bytes")
 
 
 class CQError(RuntimeError):
@@ -96,6 +96,11 @@ def lib() -> C.CDLL:
         L.cq_prompt_attention_workspace_bytes.argtypes = [i64] * 6
         L.cq_prompt_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, ci, i64, i64, i64, i64, i64, i64, vp, vp, dbl, vp, vp,
                                           vp, sz, vp]
+        L.cq_norm_rotate.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, ci, i64, i64, i64, ci, vp, vp, vp, vp, dbl, vp, i64, i64, vp, i64,
+                                     i64, vp]
+        L.cq_adapter_add_workspace_bytes.restype = sz
+        L.cq_adapter_add_workspace_bytes.argtypes = [i64, i64]
+        L.cq_adapter_add.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, i64, i64, i64, vp, vp, ci, i64, vp, i64, vp, sz, vp]
         L.cq_set_tuning.argtypes = [C.c_char_p, ci]
         L.cq_set_timing_events.argtypes = [vp, vp]
         for name in EXPORTS:
@@ -904,6 +909,97 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts
                                k_starts.data_ptr(), D ** -0.5 if scale is None else float(scale), out.data_ptr(), _addr(lse), *ws, _raw(dev))
     if st:
         raise CQError(st, "cq_prompt_attention")
+    return out
+
+
+def rotation_freq(rotated: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """float64 [rotated / 2]: base^(-2 i / rotated) radians a position, the frequencies of `norm_rotate`."""
+    return float(base) ** (-torch.arange(0, rotated, 2, dtype=torch.float64, device=device) / rotated)
+
+
+def norm_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, q_weight: torch.Tensor | None = None,
+                k_weight: torch.Tensor | None = None, *, eps: float | None = 1e-6, neighbours: bool = False, out=None):
+    """(queries, keys) normalised for each head and rotated by their positions; q [T, Hq, D], k [T, H, D] (float16 / bfloat16, any
+    strides of tokens and heads).
+
+    positions int64 [T], freq float64 [R / 2] (radians a position): the first R channels of a head are rotated, channel i with i + R / 2
+    or, with `neighbours`, 2 i with 2 i + 1.  Weights [D] of q's dtype (default: ones); `eps` = None leaves the norms out.
+    `out` = a pair of tensors to fill, which may be (q, k) themselves."""
+    dt, dev = _DT16.get(q.dtype), q.get_device()
+    if dt is None or q.dim() != 3 or dev < 0:
+        raise TypeError("q must be a float16 / bfloat16 CUDA tensor [tokens, heads, head_dim]")
+    T, Hq, D = q.shape
+    qs, ks = _heads16(q, T, Hq, D, q.dtype, dev, "q"), _heads16(k, T, None, D, q.dtype, dev, "k")
+    H = k.shape[1]
+    if positions.dtype != _I64 or positions.shape != (T,) or not positions.is_contiguous() or positions.get_device() != dev:
+        raise ValueError(f"positions must be a contiguous int64 vector of {T} on cuda:{dev}")
+    if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or freq.get_device() != dev:
+        raise ValueError(f"freq must be a contiguous float64 vector on cuda:{dev}")
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype != q.dtype or w.shape != (D,) or not w.is_contiguous() or w.get_device() != dev):
+            raise ValueError(f"weights must be contiguous {q.dtype} vectors of {D} on cuda:{dev}")
+    if eps is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("weights belong to the norms: eps is None")
+    if eps is not None and not eps >= 0.0:
+        raise ValueError("eps must not be below 0")
+    if out is None:
+        out = q.new_empty((T, Hq, D)), q.new_empty((T, H, D))
+    q_out, k_out = out
+    qo, ko = _heads16(q_out, T, Hq, D, q.dtype, dev, "out[0]"), _heads16(k_out, T, H, D, q.dtype, dev, "out[1]")
+    st = (_lib or lib()).cq_norm_rotate(q.data_ptr(), *qs, Hq, k.data_ptr(), *ks, H, dt, T, D, 2 * freq.shape[0], int(neighbours),
+                                        positions.data_ptr(), freq.data_ptr(), _addr(q_weight), _addr(k_weight),
+                                        -1.0 if eps is None else float(eps), q_out.data_ptr(), *qo, k_out.data_ptr(), *ko, _raw(dev))
+    if st:
+        raise CQError(st, "cq_norm_rotate")
+    return out
+
+
+# ----------------------------------------------------------------------------- adapters
+class Adapters(NamedTuple):
+    """Low-rank adapters of one projection: A [n, R, in channels], B [n, out channels, R] (16-bit, dense) and a factor for each
+    (float32 [n]; None: ones).  R is a multiple of 8 up to 128."""
+    A: torch.Tensor
+    B: torch.Tensor
+    scale: torch.Tensor | None = None
+
+
+def adapter_add_workspace_bytes(tokens: int, rank: int) -> int:
+    return int(lib().cq_adapter_add_workspace_bytes(tokens, rank))
+
+
+def adapter_add(y: torch.Tensor, x: torch.Tensor, adapters: Adapters, index: torch.Tensor, *, out: torch.Tensor | None = None,
+                workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """y [T, N] + scale_a B_a (A_a x) for tokens x [T, K] whose adapters are a = index[t] (int32 [T]; outside 0 .. n - 1: none).
+
+    y is what the shared projection gave (float16, bfloat16 or float32), x has the adapters' dtype; `out` may be y itself."""
+    T, K, ldx, dt, dev = _matrix16(x)
+    A, B, scale = adapters
+    if A.dim() != 3 or B.dim() != 3 or A.shape[2] != K or A.shape[:2] != (B.shape[0], B.shape[2]):
+        raise ValueError(f"adapters must be A [n, R, {K}] and B [n, out channels, R]")
+    n, R, _ = A.shape
+    N = B.shape[1]
+    for w in (A, B):
+        if w.dtype != x.dtype or w.get_device() != dev or not w.is_contiguous():
+            raise ValueError(f"adapters must be contiguous {x.dtype} tensors on cuda:{dev}")
+    if scale is not None and (scale.dtype != _F32 or scale.shape != (n,) or scale.get_device() != dev or not scale.is_contiguous()):
+        raise ValueError(f"scale must be a contiguous float32 vector of {n} on cuda:{dev}")
+    if index.dtype != _I32 or index.shape != (T,) or index.get_device() != dev or not index.is_contiguous():
+        raise ValueError(f"index must be a contiguous int32 vector of {T} on cuda:{dev}")
+    ydt = _DT.get(y.dtype)
+    if ydt is None:
+        raise TypeError("expected float16, bfloat16 or float32 results of the projection")
+    if y.shape != (T, N) or y.get_device() != dev or (y.stride(1) != 1 and N > 1 and T > 0):
+        raise ValueError(f"y must be [{T}, {N}] on cuda:{dev} with contiguous columns")
+    out, _, ldo = _product_out(out, T, N, y.dtype, x)
+    if out.data_ptr() == y.data_ptr() and out.stride() != y.stride() and T > 1:
+        raise ValueError("out begins where y does and has other strides")
+    L = _lib or lib()
+    if workspace is None:
+        workspace = x.new_empty(L.cq_adapter_add_workspace_bytes(T, R), dtype=torch.uint8)
+    st = L.cq_adapter_add(x.data_ptr(), dt, T, K, ldx, A.data_ptr(), B.data_ptr(), _addr(scale), n, R, N, index.data_ptr(), y.data_ptr(), ydt,
+                          y.stride(0) if T > 1 else max(N, 1), out.data_ptr(), ldo, *_workspace_of(workspace, dev), _raw(dev))
+    if st:
+        raise CQError(st, "cq_adapter_add")
     return out
 
 
