@@ -395,7 +395,7 @@ int cq_prompt_attention(const void* Q, int64_t q_token_stride, int64_t q_head_st
  *   Q, K          16-bit of one dtype [T][Hq][D], [T][H][D]: element (t, h, d) at t * token_stride + h * head_stride + d; q_out, k_out of that
  *                 dtype likewise.  An output may be its input (the same address and strides); other overlaps are not allowed
  *   positions     device int64 [T], 8-byte aligned; freq  device double [R / 2] (radians a position).  f is formed in 64 bits: an angle is off
- *                 by 2^-52 of itself and 2^-24
+ *                 by 2^-51 of itself and 2^-21
  *   q_weight, k_weight  device [D] of that dtype; null: ones.  Null where eps < 0 (CQ_ERR_ALPHA)
  * 1 <= D <= 512, R even, 0 <= R <= D, up to 65536 heads.  16-byte aligned rows (strides multiples of 8), D a multiple of 8 up to 256 and
  * R of 16: fast; anything else (2-byte aligned) is served by a slower kernel.  Sums and products are fp32 (64 bits where squares
