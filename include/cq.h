@@ -415,7 +415,8 @@ int cq_norm_rotate(const void* Q, int64_t q_token_stride, int64_t q_head_stride,
  *   y      [T][ldy] of y_dtype (CQ_F16, CQ_BF16, CQ_F32), out [T][ldo] of the same; ldy, ldo >= N.  out may be y (with the same pitch)
  * R is a multiple of 8 up to 128 (pad with zeros), T up to 4194240.  16-byte aligned rows of X and A (of y and out) with K (N) a multiple of 8: fast.
  * A_a X[t] is summed in fp32 and enters the second product as two 16-bit halves relative to the token's largest: off by 2^-16 of itself
- * and 2^-24 of that (fp16; bf16 2^-17 of itself).  The result is fp32 and rounded once.  A token's result depends on no other token.  Equal calls give equal bits.
+ * and 2^-24 of that (fp16; bf16 2^-17 of itself).  The result is fp32 and rounded once.  A token's result depends on no other token's values; its last
+ * bits may depend on how many of the 64 neighbouring tokens share its adapter.  Equal calls give equal bits.
  * workspace: device, 256-byte aligned, >= cq_adapter_add_workspace_bytes(T, R); contents undefined after.
  */
 size_t cq_adapter_add_workspace_bytes(int64_t T, int64_t R);

@@ -31,7 +31,7 @@ struct AdapterArgs {
     uint16_t* high; uint16_t* low; float* factor;               // [T][R], [T][R], [T]
     int64_t T, K, N;
     int R, n;
-    bool vec_k, vec_n;                                          // rows of x and A (y and out) in 16-byte accesses
+    int vec_k, vec_n;                                           // elements of one access to rows of x and A (of y and out)
 };
 
 // The window's tokens by adapter.  s_rank[i]: how many adapters appear before the one that token i is the first of; -1 if it is not.
@@ -92,20 +92,45 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t a0, const ui
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// eight elements of a row from column k on, zeros from column `end` on
-template <bool VEC>
-__device__ __forceinline__ uint4 piece8(const uint16_t* row, int64_t k, int64_t end) {
-    if constexpr (VEC) {
-        return k < end ? __ldcg(reinterpret_cast<const uint4*>(row + k)) : make_uint4(0, 0, 0, 0);
+// eight elements of a row from column k on (a multiple of 8), zeros from column `end` on; `vec` elements at a time, all of which
+// lie before `end` or none
+__device__ __forceinline__ uint4 piece8(const uint16_t* row, int64_t k, int64_t end, int vec) {
+    if (vec == 8) return k < end ? __ldcg(reinterpret_cast<const uint4*>(row + k)) : make_uint4(0, 0, 0, 0);
+    uint32_t v[4];
+    if (vec >= 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = k + 2 * i < end ? __ldcg(reinterpret_cast<const uint32_t*>(row + k) + i) : 0;
     } else {
-        uint32_t v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t lo = k + 2 * i < end ? __ldcg(row + k + 2 * i) : 0, hi = k + 2 * i + 1 < end ? __ldcg(row + k + 2 * i + 1) : 0;
             v[i] = lo | hi << 16;
         }
-        return make_uint4(v[0], v[1], v[2], v[3]);
     }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+// the same into shared memory, asynchronously where the alignment allows
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool have) {
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(have ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" :: "r"(dst), "l"(src), "n"(BYTES), "r"(have ? BYTES : 0) : "memory");
+}
+__device__ __forceinline__ void stage8(uint8_t* dst, const uint16_t* row, int64_t k, int64_t end, int vec) {
+    const uint32_t at = smem_u32(dst);
+    if (vec == 8) {
+        copy_async<16>(at, k < end ? row + k : row, k < end);
+    } else if (vec == 4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) copy_async<8>(at + 8 * i, k + 4 * i < end ? row + k + 4 * i : row, k + 4 * i < end);
+    } else if (vec == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) copy_async<4>(at + 4 * i, k + 2 * i < end ? row + k + 2 * i : row, k + 2 * i < end);
+    } else {
+        *reinterpret_cast<uint4*>(dst) = piece8(row, k, end, 1);
+    }
+}
+__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], const uint8_t* p) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_u32(p)) : "memory");
 }
 
 __device__ __forceinline__ float ld_rank(const float* p, uint32_t rank) {
@@ -121,99 +146,156 @@ __device__ __forceinline__ void cluster_barrier() {
 }
 
 // ---- h = A x ----------------------------------------------------------------------------------------------------
-// grid (parts of the contraction = cluster, windows, adapters of a window in turn).  Up to 32 tokens: all eight warps split the part;
-// more: four warps for either half of them.  Sums of warps meet in shared memory in a fixed tree, those of the cluster's blocks through
-// distributed shared memory in rank order: equal calls give equal bits.
-template <int MT>                             // MT x 16 rows of A
-constexpr size_t shrink_smem() { return size_t(4) * MT * 16 * 33 * 4 + size_t(kWindow) * (MT * 16 + 1) * 4; }
+// grid (parts of the contraction = cluster, windows, adapters of a window in turn).  Up to eight tokens of an adapter: fragments straight
+// from memory, the eight warps split the part.  More: tiles of x and A of 64 along the contraction through shared memory, a ring of asynchronous
+// copies ahead.  Sums of warps meet in shared memory, those of the cluster's blocks through distributed shared memory in rank order: equal
+// calls give equal bits.
+constexpr int kUnit = 64;                     // contraction of one stage
+template <int MT> __host__ __device__ constexpr int shrink_stages() { return MT <= 2 ? 6 : MT == 4 ? 5 : 3; }
+template <int MT> __host__ __device__ constexpr size_t shrink_stage() { return size_t(kWindow + MT * 16) * kUnit * 2; }
+template <int MT> __host__ __device__ constexpr size_t shrink_smem() { return shrink_stages<MT>() * shrink_stage<MT>() + size_t(kWindow) * (MT * 16 + 1) * 4; }
 
-template <int MT, int DT, bool VEC>
-__global__ void __launch_bounds__(kAdThreads, MT <= 4 ? 2 : 1)
+template <int MT, int DT>                     // MT x 16 rows of A
+__global__ void __launch_bounds__(kAdThreads, 2)
 k25_adapter_in(const AdapterArgs p) {
-    constexpr int kRows = MT * 16;
-    extern __shared__ float s_mem[];
-    float* s_red = s_mem;                                       // [4][kRows][33]
-    float* s_h = s_mem + 4 * kRows * 33;                        // [token][kRows + 1]
+    constexpr int kRows = MT * 16, ST = shrink_stages<MT>();
+    constexpr size_t kStage = shrink_stage<MT>();
+    extern __shared__ __align__(128) uint8_t s_mem[];
+    float* s_red = reinterpret_cast<float*>(s_mem);             // [4][kRows][9], over the stages
+    float* s_h = reinterpret_cast<float*>(s_mem + ST * kStage); // [token][kRows + 1]
+    static_assert(size_t(4) * kRows * 9 * 4 <= ST * kStage, "sums of warps");
     __shared__ Window w;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");         // (only now: the next kernel reads B and y before this one ends)
     const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kWindow;
     const int valid = static_cast<int>(min(static_cast<int64_t>(kWindow), p.T - t0));
     read_window(p, t0, w);
     const int rank = blockIdx.x, ranks = gridDim.x;
-    const int64_t units = (p.K + kUnitK - 1) / kUnitK, u0 = units * rank / ranks, u1 = units * (rank + 1) / ranks;
+    const int64_t units = (p.K + kUnit - 1) / kUnit, u0 = units * rank / ranks, u1 = units * (rank + 1) / ranks;
     for (int which = blockIdx.z; which < w.n; which += gridDim.z) {
         const int a = w.idx[w.first[which]];
         pick_tokens(w, a, valid);
         const int count = w.count;
-        const bool halves = count > 32;
-        const int first = halves ? (warp >> 2) * 32 : 0, split = halves ? 4 : 8, part = halves ? warp & 3 : warp;
-        const int groups = min(4, (count - first + 7) / 8);
         const uint16_t* A = p.A + static_cast<int64_t>(a) * p.R * p.K;
-        const uint16_t* rows[4];
+        if (count <= 8) {
+            constexpr int kAhead = MT == 1 ? 4 : MT == 2 ? 2 : 1;       // steps whose loads are issued together
+            const uint16_t* x = g < count ? p.x + (t0 + w.list[g]) * p.ldx : nullptr;
+            float acc[MT][4] = {};
+            for (int64_t u = 2 * u0 + warp; u < 2 * u1; u += 8 * kAhead) {
+                uint4 xb[kAhead], wa[kAhead][MT][2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int m = first + j * 8 + g;
-            rows[j] = m < count ? p.x + (t0 + w.list[m]) * p.ldx : nullptr;
-        }
-        float acc[MT][4][4] = {};
-        for (int64_t u = u0 + part; u < u1; u += split) {
-            const int64_t k = u * kUnitK + t4 * 8;
-            uint4 xb[4], wa[MT][2];
+                for (int s = 0; s < kAhead; ++s) {
+                    const int64_t k = u + 8 * s < 2 * u1 ? (u + 8 * s) * kUnitK + t4 * 8 : p.K + 8;      // (nothing: zeros)
+                    xb[s] = x != nullptr ? piece8(x, k, p.K, p.vec_k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                xb[j] = make_uint4(0, 0, 0, 0);
-                if (rows[j] != nullptr) xb[j] = piece8<VEC>(rows[j], k, p.K);
-            }
+                    for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const int r = i * 16 + hh * 8 + g;
-                    wa[i][hh] = make_uint4(0, 0, 0, 0);
-                    if (r < p.R) wa[i][hh] = piece8<VEC>(A + r * p.K, k, p.K);
+                        for (int hh = 0; hh < 2; ++hh) {
+                            const int r = i * 16 + hh * 8 + g;
+                            wa[s][i][hh] = r < p.R ? piece8(A + r * p.K, k, p.K, p.vec_k) : make_uint4(0, 0, 0, 0);
+                        }
                 }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (j >= groups) break;
+                for (int s = 0; s < kAhead; ++s)
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    mma16<DT>(acc[i][j], wa[i][0].x, wa[i][1].x, wa[i][0].y, wa[i][1].y, xb[j].x, xb[j].y);
-                    mma16<DT>(acc[i][j], wa[i][0].z, wa[i][1].z, wa[i][0].w, wa[i][1].w, xb[j].z, xb[j].w);
+                    for (int i = 0; i < MT; ++i) {
+                        mma16<DT>(acc[i], wa[s][i][0].x, wa[s][i][1].x, wa[s][i][0].y, wa[s][i][1].y, xb[s].x, xb[s].y);
+                        mma16<DT>(acc[i], wa[s][i][0].z, wa[s][i][1].z, wa[s][i][0].w, wa[s][i][1].w, xb[s].z, xb[s].w);
+                    }
+            }
+            // acc[i]: rows i * 16 + g (+ 8), tokens 2 t4 (+ 1)
+            for (int step = 4; step > 0; step >>= 1) {
+                float* buf = s_red + (warp % step) * kRows * 9;
+                if (warp >= step && warp < 2 * step) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) buf[(i * 16 + g + (e >> 1) * 8) * 9 + 2 * t4 + (e & 1)] = acc[i][e];
+                }
+                __syncthreads();
+                if (warp < step) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][e] += buf[(i * 16 + g + (e >> 1) * 8) * 9 + 2 * t4 + (e & 1)];
+                }
+                __syncthreads();
+            }
+            if (warp == 0) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s_h[(2 * t4 + (e & 1)) * (kRows + 1) + i * 16 + g + (e >> 1) * 8] = acc[i][e];
+            }
+        } else {
+            // Rows of 128 bytes, 16-byte pieces swapped by the row so that eight rows of one piece lie in different banks.
+            auto stage = [&](int64_t u) {
+                uint8_t* sx = s_mem + (u - u0) % ST * kStage;
+                uint8_t* sa = sx + size_t(kWindow) * kUnit * 2;
+#pragma unroll
+                for (int i = tid; i < kWindow * 8; i += kAdThreads) {
+                    const int r = i >> 3, c = i & 7;
+                    if (r < count) stage8(sx + r * 128 + ((c ^ (r & 7)) << 4), p.x + (t0 + w.list[r]) * p.ldx, u * kUnit + c * 8, p.K, p.vec_k);
+                }
+#pragma unroll
+                for (int i = tid; i < kRows * 8; i += kAdThreads) {
+                    const int r = i >> 3, c = i & 7;
+                    if (r < p.R) stage8(sa + r * 128 + ((c ^ (r & 7)) << 4), A + r * p.K, u * kUnit + c * 8, p.K, p.vec_k);
+                }
+            };
+            // warps: two halves of the tokens x four; those share out the rows of A (16 each, 32 of 128), or, with fewer, a stage's steps of 16
+            constexpr int MI = MT == 8 ? 2 : 1, KS = MT >= 4 ? 1 : 4 / MT;
+            const int half = warp >> 2, m = (warp & 3) % (MT < 4 ? MT : 4), ks = (warp & 3) / (MT < 4 ? MT : 4);
+            float acc[MI][4][4] = {};
+            for (int s = 0; s < ST - 1; ++s) {
+                if (u0 + s < u1) stage(u0 + s);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+            for (int64_t u = u0; u < u1; ++u) {
+                asm volatile("cp.async.wait_group %0;" :: "n"(ST - 2) : "memory");
+                __syncthreads();
+                if (u + ST - 1 < u1) stage(u + ST - 1);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                if (half * 32 < count) {
+                    const uint8_t* sx = s_mem + (u - u0) % ST * kStage + half * 32 * 128;
+                    const uint8_t* sa = s_mem + (u - u0) % ST * kStage + size_t(kWindow) * kUnit * 2;
+#pragma unroll
+                    for (int kk = ks; kk < 4; kk += KS) {
+                        uint32_t fa[MI][4], fb[2][4];
+#pragma unroll
+                        for (int i = 0; i < MI; ++i) {
+                            const int r = (m + 4 * i) * 16 + (lane & 15);
+                            load_matrices(fa[i], sa + r * 128 + (((kk * 2 + (lane >> 4)) ^ (r & 7)) << 4));
+                        }
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int r = j * 16 + (lane & 7) + ((lane >> 4) << 3);
+                            load_matrices(fb[j], sx + r * 128 + (((kk * 2 + ((lane >> 3) & 1)) ^ (r & 7)) << 4));
+                        }
+#pragma unroll
+                        for (int i = 0; i < MI; ++i)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) mma16<DT>(acc[i][j], fa[i][0], fa[i][1], fa[i][2], fa[i][3], fb[j >> 1][(j & 1) * 2], fb[j >> 1][(j & 1) * 2 + 1]);
+                    }
                 }
             }
-        }
-        // acc[i][j]: rows i * 16 + g (+ 8), tokens j * 8 + 2 t4 (+ 1) of this warp's 32
-        for (int step = split / 2; step > 0; step >>= 1) {
-            const int slot = halves ? (warp >> 2) * 2 + (part % step) : part % step;      // (at most two for either half, four without)
-            float* buf = s_red + slot * kRows * 33;
-            if (part >= step && part < 2 * step) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+            for (int s = 0; s < KS; ++s) {
+                if (ks == s) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int i = 0; i < MI; ++i)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) buf[(i * 16 + g + (e >> 1) * 8) * 33 + j * 8 + 2 * t4 + (e & 1)] = acc[i][j][e];
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float* at = s_h + (half * 32 + j * 8 + 2 * t4 + (e & 1)) * (kRows + 1) + (m + 4 * i) * 16 + g + (e >> 1) * 8;
+                                *at = s == 0 ? acc[i][j][e] : *at + acc[i][j][e];
+                            }
+                }
+                if (s + 1 < KS) __syncthreads();
             }
-            __syncthreads();
-            if (part < step) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][e] += buf[(i * 16 + g + (e >> 1) * 8) * 33 + j * 8 + 2 * t4 + (e & 1)];
-            }
-            __syncthreads();
-        }
-        if (part == 0) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s_h[(first + j * 8 + 2 * t4 + (e & 1)) * (kRows + 1) + i * 16 + g + (e >> 1) * 8] = acc[i][j][e];
         }
         __syncthreads();
         if (ranks > 1) cluster_barrier();
@@ -225,14 +307,20 @@ k25_adapter_in(const AdapterArgs p) {
             for (int i = 0; i < kPer; ++i) {
                 const int r = lane + 32 * i;
                 h[i] = 0.0f;
-                if (r < p.R)
-                    for (int k = 0; k < ranks; ++k) h[i] += ranks > 1 ? ld_rank(s_h + m * (kRows + 1) + r, k) : s_h[m * (kRows + 1) + r];
+                if (r < p.R) {
+                    if (ranks > 1) {
+#pragma unroll 8
+                        for (int k = 0; k < ranks; ++k) h[i] += ld_rank(s_h + m * (kRows + 1) + r, k);
+                    } else {
+                        h[i] = s_h[m * (kRows + 1) + r];
+                    }
+                }
                 const float v = fabsf(h[i]);
                 top = fmaxf(top, v < INFINITY ? v : 0.0f);
             }
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, off));
-            // 2^e, the power of two at or below the largest (e of 0 has the range of fp32's normal numbers): h 2^-e lies below 2
+            // 2^e, the power of two at or below the largest, within fp32's normal numbers: h 2^-e lies below 2
             const uint32_t e = min(max(__float_as_uint(top) >> 23, 2u), 252u);
             const float down = __uint_as_float((254u - e) << 23);
             const int64_t t = t0 + w.list[m];
@@ -254,57 +342,98 @@ k25_adapter_in(const AdapterArgs p) {
 
 // ---- out = y + B h ---------------------------------------------------------------------------------------------------
 // grid (blocks of 256 columns, windows, adapters of a window in turn).  A warp keeps its 32 columns of B_a in registers and takes the adapter's
-// tokens 16 at a time.  The four products of 8 columns share them out so that each lane ends up with 8 neighbouring columns.
+// tokens 16 at a time, y of the next 16 on the way.  The four products of 8 columns share them out so that each lane ends up with 8
+// neighbouring columns.
+template <int YT> struct Piece { uint32_t r[YT == CQ_F32 ? 8 : 4]; };           // 8 columns of a row of y
+
 template <int YT>
-__device__ __forceinline__ void add_store8(const AdapterArgs& p, int64_t t, int64_t col, const float (&d)[8], float f) {
-    if (col >= p.N) return;
-    constexpr int kElem = YT == CQ_F32 ? 4 : 2;
-    const uint8_t* y = static_cast<const uint8_t*>(p.y) + (t * p.ldy + col) * kElem;
-    uint8_t* out = static_cast<uint8_t*>(p.out) + (t * p.ldo + col) * kElem;
-    if (p.vec_n) {
-        if constexpr (YT == CQ_F32) {
-            float4 a = __ldcg(reinterpret_cast<const float4*>(y)), b = __ldcg(reinterpret_cast<const float4*>(y) + 1);
-            a.x = __fmaf_rn(d[0], f, a.x); a.y = __fmaf_rn(d[1], f, a.y); a.z = __fmaf_rn(d[2], f, a.z); a.w = __fmaf_rn(d[3], f, a.w);
-            b.x = __fmaf_rn(d[4], f, b.x); b.y = __fmaf_rn(d[5], f, b.y); b.z = __fmaf_rn(d[6], f, b.z); b.w = __fmaf_rn(d[7], f, b.w);
-            reinterpret_cast<float4*>(out)[0] = a;
-            reinterpret_cast<float4*>(out)[1] = b;
-        } else {
-            const uint4 w = __ldcg(reinterpret_cast<const uint4*>(y));
-            const uint32_t r[4] = {w.x, w.y, w.z, w.w};
-            uint32_t o[4];
+__device__ __forceinline__ Piece<YT> load_piece(const AdapterArgs& p, int64_t t, int64_t col) {
+    Piece<YT> v = {};
+    if (t < 0 || col >= p.N) return v;
+    if constexpr (YT == CQ_F32) {
+        const uint32_t* y = static_cast<const uint32_t*>(p.y) + t * p.ldy + col;
+        if (p.vec_n == 4) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 v = unpack16x2<YT>(r[i]);
-                o[i] = pack16x2<YT>(__fmaf_rn(d[2 * i], f, v.x), __fmaf_rn(d[2 * i + 1], f, v.y));
-            }
-            *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
+            for (int i = 0; i < 2; ++i)
+                if (col + 4 * i < p.N) {
+                    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(y) + i);
+                    v.r[4 * i] = w.x; v.r[4 * i + 1] = w.y; v.r[4 * i + 2] = w.z; v.r[4 * i + 3] = w.w;
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (col + i < p.N) v.r[i] = __ldcg(y + i);
         }
     } else {
-        const int64_t n = min(int64_t(8), p.N - col);
+        const uint4 w = piece8(static_cast<const uint16_t*>(p.y) + t * p.ldy, col, p.N, p.vec_n);
+        v.r[0] = w.x; v.r[1] = w.y; v.r[2] = w.z; v.r[3] = w.w;
+    }
+    return v;
+}
+// y + f d, rounded once
+template <int YT>
+__device__ __forceinline__ void add_store(const AdapterArgs& p, int64_t t, int64_t col, const Piece<YT>& y, const float (&d)[8], float f) {
+    if (t < 0 || col >= p.N) return;
+    if constexpr (YT == CQ_F32) {
+        float* out = static_cast<float*>(p.out) + t * p.ldo + col;
+        float o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) {
-                if constexpr (YT == CQ_F32) reinterpret_cast<float*>(out)[i] = __fmaf_rn(d[i], f, __ldcg(reinterpret_cast<const float*>(y) + i));
-                else reinterpret_cast<uint16_t*>(out)[i] = pack16<YT>(__fmaf_rn(d[i], f, cvt16<YT>(__ldcg(reinterpret_cast<const uint16_t*>(y) + i))));
-            }
+        for (int i = 0; i < 8; ++i) o[i] = __fmaf_rn(d[i], f, __uint_as_float(y.r[i]));
+        if (p.vec_n == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (col + 4 * i < p.N) reinterpret_cast<float4*>(out)[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (col + i < p.N) out[i] = o[i];
+        }
+    } else {
+        uint16_t* out = static_cast<uint16_t*>(p.out) + t * p.ldo + col;
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 v = unpack16x2<YT>(y.r[i]);
+            o[i] = pack16x2<YT>(__fmaf_rn(d[2 * i], f, v.x), __fmaf_rn(d[2 * i + 1], f, v.y));
+        }
+        if (p.vec_n == 8) {
+            *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
+        } else if (p.vec_n >= 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + 2 * i < p.N) reinterpret_cast<uint32_t*>(out)[i] = o[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (col + i < p.N) out[i] = static_cast<uint16_t>(o[i >> 1] >> (16 * (i & 1)));
+        }
     }
 }
 
+// words between rows of h in shared memory: 8 more than a multiple of 32, so that the rows of a fragment lie in different banks
+template <int MT> __host__ __device__ constexpr int h_pitch() { return MT * 8 + (MT == 1 ? 0 : MT == 2 ? 24 : 8); }
+
 template <int MT, int DT, int YT>
-__global__ void __launch_bounds__(kAdThreads)
+__global__ void __launch_bounds__(kAdThreads, MT <= 2 ? 3 : 2)
 k26_adapter_out(const AdapterArgs p) {
+    constexpr int kPitch = h_pitch<MT>();
+    constexpr int kHeld = MT == 8 ? 32 : kWindow;               // tokens whose h is in shared memory at a time
     __shared__ Window w;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    __shared__ __align__(16) uint32_t s_h[2][kHeld][kPitch];
+    __shared__ float s_f[kWindow];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     asm volatile("griddepcontrol.launch_dependents;");
     const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kWindow;
     const int valid = static_cast<int>(min(static_cast<int64_t>(kWindow), p.T - t0));
     read_window(p, t0, w);
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kExpandCols + warp * 32;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kExpandCols + warp * 32, col = n0 + 8 * t4;
     bool waited = false;
     for (int which = blockIdx.z; which < w.n; which += gridDim.z) {
         const int a = w.idx[w.first[which]];
         pick_tokens(w, a, valid);
         const int count = w.count;
+        auto token = [&](int m) { return m < count ? t0 + w.list[m] : int64_t(-1); };
+        Piece<YT> ya = load_piece<YT>(p, token(g), col), yb = load_piece<YT>(p, token(8 + g), col);
         // product j takes columns n0 + 8 (q / 2) + 2 j + q % 2, q = 0 .. 7
         uint2 b[4][MT];
 #pragma unroll
@@ -322,31 +451,43 @@ k26_adapter_out(const AdapterArgs p) {
             asm volatile("griddepcontrol.wait;" ::: "memory");
             waited = true;
         }
-        for (int m0 = 0; m0 < count; m0 += 16) {
-            const int64_t ta = m0 + g < count ? t0 + w.list[m0 + g] : -1, tb = m0 + 8 + g < count ? t0 + w.list[m0 + 8 + g] : -1;
-            float acc[4][4] = {};
+        for (int base = 0; base < count; base += kHeld) {
+            if (base > 0) __syncthreads();
+            const int held = min(kHeld, count - base), pieces = p.R / 8;         // 16 bytes each
+            for (int i = tid; i < 2 * held * pieces; i += kAdThreads) {
+                const int part = i >= held * pieces ? 1 : 0, at = i - part * held * pieces, m = at / pieces, c = at - m * pieces;
+                const uint16_t* h = (part == 0 ? p.high : p.low) + (t0 + w.list[base + m]) * p.R + c * 8;
+                *reinterpret_cast<uint4*>(&s_h[part][m][c * 4]) = __ldcg(reinterpret_cast<const uint4*>(h));
+            }
+            for (int i = tid; i < held; i += kAdThreads) s_f[i] = __ldcg(p.factor + t0 + w.list[base + i]);
+            __syncthreads();
+            for (int m0 = 0; m0 < held; m0 += 16) {
+                const bool have_a = m0 + g < held, have_b = m0 + 8 + g < held;
+                const Piece<YT> na = load_piece<YT>(p, token(base + m0 + 16 + g), col), nb = load_piece<YT>(p, token(base + m0 + 24 + g), col);
+                float acc[4][4] = {};
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int k = i * 16 + t4 * 4;
-                if (i * 16 >= p.R) break;
+                for (int i = 0; i < MT; ++i) {
+                    if (i * 16 >= p.R) break;
+                    const bool have_k = i * 16 + t4 * 4 < p.R;
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const uint16_t* h = part == 0 ? p.high : p.low;
-                    uint2 ha = make_uint2(0, 0), hb = ha;
-                    if (ta >= 0 && k < p.R) ha = __ldcg(reinterpret_cast<const uint2*>(h + ta * p.R + k));
-                    if (tb >= 0 && k < p.R) hb = __ldcg(reinterpret_cast<const uint2*>(h + tb * p.R + k));
+                    for (int part = 0; part < 2; ++part) {
+                        uint2 ha = make_uint2(0, 0), hb = ha;
+                        if (have_a && have_k) ha = *reinterpret_cast<const uint2*>(&s_h[part][m0 + g][i * 8 + t4 * 2]);
+                        if (have_b && have_k) hb = *reinterpret_cast<const uint2*>(&s_h[part][m0 + 8 + g][i * 8 + t4 * 2]);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) mma16<DT>(acc[j], ha.x, hb.x, ha.y, hb.y, b[j][i].x, b[j][i].y);
+                        for (int j = 0; j < 4; ++j) mma16<DT>(acc[j], ha.x, hb.x, ha.y, hb.y, b[j][i].x, b[j][i].y);
+                    }
                 }
-            }
-            const int64_t col = n0 + 8 * t4;
-            if (ta >= 0) {
-                const float d[8] = {acc[0][0], acc[0][1], acc[1][0], acc[1][1], acc[2][0], acc[2][1], acc[3][0], acc[3][1]};
-                add_store8<YT>(p, ta, col, d, __ldcg(p.factor + ta));
-            }
-            if (tb >= 0) {
-                const float d[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
-                add_store8<YT>(p, tb, col, d, __ldcg(p.factor + tb));
+                if (have_a) {
+                    const float d[8] = {acc[0][0], acc[0][1], acc[1][0], acc[1][1], acc[2][0], acc[2][1], acc[3][0], acc[3][1]};
+                    add_store<YT>(p, token(base + m0 + g), col, ya, d, s_f[m0 + g]);
+                }
+                if (have_b) {
+                    const float d[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
+                    add_store<YT>(p, token(base + m0 + 8 + g), col, yb, d, s_f[m0 + 8 + g]);
+                }
+                ya = na;
+                yb = nb;
             }
         }
     }
@@ -354,8 +495,10 @@ k26_adapter_out(const AdapterArgs p) {
     if (blockIdx.z == 0 && p.out != p.y) {    // tokens without an adapter
         pick_tokens(w, -1, valid);
         const float zero[8] = {-0.0f, -0.0f, -0.0f, -0.0f, -0.0f, -0.0f, -0.0f, -0.0f};       // (y + -0 is y)
-        for (int i = threadIdx.x; i < w.count * (kExpandCols / 8); i += kAdThreads)
-            add_store8<YT>(p, t0 + w.list[i / (kExpandCols / 8)], static_cast<int64_t>(blockIdx.x) * kExpandCols + (i % (kExpandCols / 8)) * 8, zero, 0.0f);
+        for (int i = tid; i < w.count * (kExpandCols / 8); i += kAdThreads) {
+            const int64_t t = t0 + w.list[i / (kExpandCols / 8)], c = static_cast<int64_t>(blockIdx.x) * kExpandCols + (i % (kExpandCols / 8)) * 8;
+            add_store<YT>(p, t, c, load_piece<YT>(p, t, c), zero, 0.0f);
+        }
     }
 }
 
@@ -363,26 +506,23 @@ k26_adapter_out(const AdapterArgs p) {
 static size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 static size_t adapter_workspace(int64_t T, int64_t R) { return 2 * up256(sizeof(uint16_t) * T * R) + up256(sizeof(float) * T); }
 
-template <int MT, int DT, bool VEC>
-static int launch_in(const AdapterArgs& p, dim3 grid, cudaStream_t st) {
-    static thread_local LaunchMemo memo;
-    // (the static shared memory counts towards the 48 KB that need no leave)
-    constexpr size_t smem = shrink_smem<MT>(), limit = smem > 47 * 1024 ? smem : 0;
-    if (resident_ctas(k25_adapter_in<MT, DT, VEC>, kAdThreads, smem, limit, memo) < 1) return CQ_ERR_CUDA;
-    return launch_ex(k25_adapter_in<MT, DT, VEC>, grid, kAdThreads, smem, st, grid.x, !tuning_no_pdl(), p);
-}
-
 template <int MT, int DT>
 static int launch_adapter(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     const int sms = sm_count();
     const int64_t windows = (p.T + kWindow - 1) / kWindow;
     const int64_t adapters = std::min<int64_t>(kWindow, std::min<int64_t>(p.n, p.T));
     if (windows > 65535) return CQ_ERR_SHAPE;
-    // parts of the contraction of 512 or more, up to a portable cluster; a block for each adapter of a window while they all fit
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(8, p.K / 512));
+    // parts of the contraction of 512 or more, up to a portable cluster and while the windows' blocks fit twice an SM; a block for each
+    // adapter of a window while they all fit
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, p.K / 512), 2 * sms / windows));
     const int64_t slots = std::max<int64_t>(1, std::min<int64_t>(adapters, 4 * sms / (windows * parts)));
+    static thread_local LaunchMemo memo;
+    // (the static shared memory counts towards the 48 KB that need no leave)
+    constexpr size_t smem = shrink_smem<MT>();
+    static_assert(smem > 48 * 1024, "leave is asked for");
+    if (resident_ctas(k25_adapter_in<MT, DT>, kAdThreads, smem, smem, memo) < 1) return CQ_ERR_CUDA;
     const dim3 grid(static_cast<unsigned>(parts), static_cast<unsigned>(windows), static_cast<unsigned>(slots));
-    const int rc = p.vec_k ? launch_in<MT, DT, true>(p, grid, st) : launch_in<MT, DT, false>(p, grid, st);
+    const int rc = launch_ex(k25_adapter_in<MT, DT>, grid, kAdThreads, smem, st, grid.x, !tuning_no_pdl(), p);
     if (rc != CQ_OK) return rc;
     const int64_t cols = (p.N + kExpandCols - 1) / kExpandCols;
     const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(adapters, 16 * sms / (windows * cols)));
@@ -426,8 +566,11 @@ int cq_adapter_add(const void* X, int dtype, int64_t T, int64_t K, int64_t ldx, 
     p.low = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(workspace) + up256(sizeof(uint16_t) * T * R));
     p.factor = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 2 * up256(sizeof(uint16_t) * T * R));
     p.T = T; p.K = K; p.N = N; p.R = static_cast<int>(R); p.n = static_cast<int>(n);
-    p.vec_k = K % 8 == 0 && (T == 1 || ldx % 8 == 0) && ptr_aligned(X, 16) && ptr_aligned(A, 16);
-    p.vec_n = N % 8 == 0 && (T == 1 || (ldy % 8 == 0 && ldo % 8 == 0)) && ptr_aligned(y, 16) && ptr_aligned(out, 16);
+    // the widest access that every row's beginning and length allow
+    for (p.vec_k = 8; p.vec_k > 1; p.vec_k /= 2)
+        if (K % p.vec_k == 0 && (T == 1 || ldx % p.vec_k == 0) && ptr_aligned(X, 2 * p.vec_k) && ptr_aligned(A, 2 * p.vec_k)) break;
+    for (p.vec_n = static_cast<int>(16 / elem); p.vec_n > 1; p.vec_n /= 2)
+        if (N % p.vec_n == 0 && (T == 1 || (ldy % p.vec_n == 0 && ldo % p.vec_n == 0)) && ptr_aligned(y, elem * p.vec_n) && ptr_aligned(out, elem * p.vec_n)) break;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return dtype == CQ_F16 ? launch_adapter_rank<CQ_F16>(p, y_dtype, st) : launch_adapter_rank<CQ_BF16>(p, y_dtype, st);
 }

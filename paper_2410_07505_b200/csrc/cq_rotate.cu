@@ -4,8 +4,9 @@
 //   (a, b) -> (a cos f - b sin f, a sin f + b cos f),   f = position * freq[pair]
 //
 // Bound by HBM (2 bytes in, 2 out).  A row's channels lie eight to a lane, so that its mean is a few shuffles and a pair is either in
-// one lane (neighbours) or one shuffle away (halves).  The angles of a token are the same for all of its heads: a block forms them
-// once a token, as a fraction of a turn in 64 bits (position * freq passes 2^24 radians, where 32 bits hold no angle).
+// one lane (neighbours) or one shuffle away (halves).  The angles of a token are the same for all of its heads: a block forms those of
+// a few tokens at a time, as a fraction of a turn in 64 bits (position * freq passes 2^24 radians, where 32 bits hold no angle), and
+// each lane keeps its token's, times the weights: an element then costs a product, a multiply-add and the row's factor.
 #include "cq_serve.cuh"
 
 #include <algorithm>
@@ -29,14 +30,17 @@ struct RotateArgs {
     bool norm, neighbours;
     double eps;
     int slices;                               // blocks that share a token's heads
+    int group;                                // tokens that a block takes at a time
 };
 
-// cos and sin of position * freq[i], i < n
-__device__ __forceinline__ void angles(const RotateArgs& p, int64_t t, float* s_cos, float* s_sin) {
-    const double pos = static_cast<double>(p.positions[t]);
-    for (int i = threadIdx.x; i < p.R / 2; i += kRotateThreads) {
-        const double turns = pos * (p.freq[i] * 0.15915494309189535);
-        sincospif(2.0f * static_cast<float>(turns - rint(turns)), s_sin + i, s_cos + i);
+// cos and sin of position * freq[i] for `group` tokens from t0 on: [token][R / 2]
+__device__ __forceinline__ void angles(const RotateArgs& p, int64_t t0, float* s_cos, float* s_sin) {
+    const int half = p.R / 2;
+    for (int at = threadIdx.x; at < p.group * half; at += kRotateThreads) {
+        const int token = at / half, i = at - token * half;
+        if (t0 + token >= p.T) break;
+        const double turns = static_cast<double>(p.positions[t0 + token]) * (p.freq[i] * 0.15915494309189535);
+        sincospif(2.0f * static_cast<float>(turns - rint(turns)), s_sin + at, s_cos + at);
     }
 }
 
@@ -54,16 +58,21 @@ __device__ __forceinline__ void unpack8(const uint4& w, float (&v)[8]) {
     }
 }
 
-// W lanes for a row, eight channels each; rows in 16-byte accesses, R a multiple of 16.
-template <int W, int DT>
-__global__ void __launch_bounds__(kRotateThreads)
+// W lanes for a row, eight channels each; rows in 16-byte accesses, R a multiple of 16.  The block's rows are `group` tokens x
+// kRows / group heads at a time.
+constexpr int kMaxGroup = 8;
+constexpr int kFastDim = 256;
+
+template <int W, int DT, bool NORM>
+__global__ void __launch_bounds__(kRotateThreads, 3)
 k24_norm_rotate(const RotateArgs p) {
-    constexpr int kRows = kRotateThreads / W;                   // rows of one pass
-    constexpr int kAhead = 4;                                   // passes whose loads are issued together
-    __shared__ float s_cos[2][kMaxRotated / 2], s_sin[2][kMaxRotated / 2];
+    constexpr int kRows = kRotateThreads / W;
+    constexpr int kAhead = 4;                                   // rows whose loads are issued together
+    __shared__ float s_cos[2][kMaxGroup * kFastDim / 2], s_sin[2][kMaxGroup * kFastDim / 2];
     asm volatile("griddepcontrol.launch_dependents;");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x % W, row = threadIdx.x / W;
+    const int token = row % p.group, first = row / p.group, step = kRows / p.group;
     const int d0 = lane * 8;
     const bool have = d0 < p.D;
     const int half = p.R / 2;
@@ -72,109 +81,101 @@ k24_norm_rotate(const RotateArgs p) {
     const int partner = p.neighbours || !rotated ? lane : second ? lane - half / 8 : lane + half / 8;
     const int angle0 = p.neighbours ? d0 / 2 : second ? d0 - half : d0;
     const int slice = blockIdx.x % p.slices;
+    const int64_t stride = static_cast<int64_t>(gridDim.x / p.slices) * p.group;
     int buffer = 0;
-    for (int64_t t = blockIdx.x / p.slices; t < p.T; t += gridDim.x / p.slices, buffer ^= 1) {
+    for (int64_t t0 = static_cast<int64_t>(blockIdx.x / p.slices) * p.group; t0 < p.T; t0 += stride, buffer ^= 1) {
+        const int64_t t = t0 + token;
         bool ready = false;
-        float c[8], s[8];
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
             const RotateSide& a = p.side[kv];
             const int h0 = static_cast<int>(static_cast<int64_t>(a.heads) * slice / p.slices), h1 = static_cast<int>(static_cast<int64_t>(a.heads) * (slice + 1) / p.slices);
-            uint4 w = make_uint4(0, 0, 0, 0), wp = w;
-            if (a.w != nullptr && have) {
-                w = *reinterpret_cast<const uint4*>(a.w + d0);
-                wp = *reinterpret_cast<const uint4*>(a.w + partner * 8);
-            }
-            for (int hb = h0; hb < h1 || !ready; hb += kRows * kAhead) {
+            const uint16_t* x_row = a.x + t * a.xt + d0;
+            uint16_t* y_row = a.y + t * a.yt + d0;
+            const bool live = have && t < p.T;
+            float c[8], s[8];                                   // y = (x c + partner s) factor
+            for (int hb = h0; hb < h1 || (kv == 0 && !ready); hb += step * kAhead) {
                 uint4 x[kAhead];
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
-                    const int h = hb + u * kRows + row;
+                    const int h = hb + u * step + first;
                     x[u] = make_uint4(0, 0, 0, 0);
-                    if (have && h < h1) x[u] = *reinterpret_cast<const uint4*>(a.x + t * a.xt + h * a.xh + d0);
+                    if (live && h < h1) x[u] = __ldcs(reinterpret_cast<const uint4*>(x_row + h * a.xh));
                 }
-                if (!ready) {                                   // (behind the first loads)
-                    angles(p, t, s_cos[buffer], s_sin[buffer]);
-                    __syncthreads();
-                    ready = true;
+                if (hb == h0) {                                 // (behind the first loads)
+                    if (!ready) {
+                        angles(p, t0, s_cos[buffer], s_sin[buffer]);
+                        __syncthreads();
+                        ready = true;
+                    }
+                    float w[8], wp[8];
+                    if (NORM && a.w != nullptr && have) {
+                        unpack8<DT>(*reinterpret_cast<const uint4*>(a.w + d0), w);
+                        unpack8<DT>(*reinterpret_cast<const uint4*>(a.w + partner * 8), wp);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = wp[i] = 1.0f;
+                    }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int at = rotated ? angle0 + (p.neighbours ? i / 2 : i) : 0;
-                        c[i] = rotated ? s_cos[buffer][at] : 1.0f;
-                        s[i] = rotated ? s_sin[buffer][at] : 0.0f;
-                    }
-                    if (!p.neighbours && !second) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) s[i] = -s[i];
+                        const int at = token * half + angle0 + (p.neighbours ? i / 2 : i);
+                        const bool later = p.neighbours ? (i & 1) != 0 : second;
+                        const float other = p.neighbours ? w[i ^ 1] : wp[i];
+                        c[i] = rotated ? s_cos[buffer][at] * w[i] : w[i];
+                        s[i] = rotated ? (later ? s_sin[buffer][at] : -s_sin[buffer][at]) * other : 0.0f;
                     }
                 }
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
-                    if (hb + u * kRows >= h1) break;            // the same for the whole block
+                    if (hb + u * step >= h1) break;             // the same for the whole block
                     float v[8], o[8];
                     unpack8<DT>(x[u], v);
-                    uint4 xp = x[u];
-                    if (!p.neighbours) {
-                        xp.x = __shfl_sync(0xFFFFFFFFu, xp.x, partner, W);
-                        xp.y = __shfl_sync(0xFFFFFFFFu, xp.y, partner, W);
-                        xp.z = __shfl_sync(0xFFFFFFFFu, xp.z, partner, W);
-                        xp.w = __shfl_sync(0xFFFFFFFFu, xp.w, partner, W);
+                    if (p.neighbours) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) o[i] = v[i ^ 1];
+                    } else {
+                        uint4 xp;
+                        xp.x = __shfl_sync(0xFFFFFFFFu, x[u].x, partner, W);
+                        xp.y = __shfl_sync(0xFFFFFFFFu, x[u].y, partner, W);
+                        xp.z = __shfl_sync(0xFFFFFFFFu, x[u].z, partner, W);
+                        xp.w = __shfl_sync(0xFFFFFFFFu, x[u].w, partner, W);
+                        unpack8<DT>(xp, o);
                     }
-                    unpack8<DT>(xp, o);
-                    if (p.norm) {
+                    if (!rotated) {                             // (an infinity times a sine of 0)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) o[i] = 0.0f;
+                    }
+                    float y[8];
+                    const int h = hb + u * step + first;
+                    if constexpr (NORM) {
                         float sum = 0.0f;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) sum = __fmaf_rn(v[i], v[i], sum);
 #pragma unroll
                         for (int off = W / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off, W);
                         const float f = rsqrtf(__fmaf_rn(sum, 1.0f / static_cast<float>(p.D), static_cast<float>(p.eps)));
-                        // squares that fp32 cannot hold, or that are all zero: the factor in 64 bits
-                        const bool wide_row = hb + u * kRows + row < h1 && !(sum > 1e-25f && sum < 1e35f);
-                        double wide = 0.0;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] = __fmaf_rn(v[i], c[i], o[i] * s[i]) * f;
+                        // squares that fp32 cannot hold, or that are all zero: in 64 bits
+                        const bool wide_row = live && h < h1 && !(sum > 1e-25f && sum < 1e35f);
                         if (__any_sync(0xFFFFFFFFu, wide_row)) {
+                            double wide = 0.0;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) wide += static_cast<double>(v[i]) * v[i];
 #pragma unroll
                             for (int off = W / 2; off > 0; off >>= 1) wide += __shfl_xor_sync(0xFFFFFFFFu, wide, off, W);
                             wide = wide_factor(wide, p.D, p.eps);
-                        }
-                        if (wide_row) {
+                            if (wide_row) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                v[i] = static_cast<float>(v[i] * wide);
-                                o[i] = static_cast<float>(o[i] * wide);
+                                for (int i = 0; i < 8; ++i) y[i] = static_cast<float>((static_cast<double>(v[i]) * c[i] + static_cast<double>(o[i]) * s[i]) * wide);
                             }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) { v[i] *= f; o[i] *= f; }
-                        }
-                        if (a.w != nullptr) {
-                            float g[8];
-                            unpack8<DT>(w, g);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) v[i] *= g[i];
-                            unpack8<DT>(wp, g);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) o[i] *= g[i];
-                        }
-                    }
-                    float y[8];
-                    if (!rotated) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] = v[i];
-                    } else if (p.neighbours) {
-#pragma unroll
-                        for (int i = 0; i < 8; i += 2) {
-                            y[i] = __fmaf_rn(v[i], c[i], -(v[i + 1] * s[i]));
-                            y[i + 1] = __fmaf_rn(v[i], s[i], v[i + 1] * c[i]);
                         }
                     } else {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) y[i] = __fmaf_rn(v[i], c[i], o[i] * s[i]);
                     }
-                    const int h = hb + u * kRows + row;
-                    if (have && h < h1)
-                        *reinterpret_cast<uint4*>(a.y + t * a.yt + h * a.yh + d0) =
+                    if (live && h < h1)
+                        *reinterpret_cast<uint4*>(y_row + h * a.yh) =
                             make_uint4(pack16x2<DT>(y[0], y[1]), pack16x2<DT>(y[2], y[3]), pack16x2<DT>(y[4], y[5]), pack16x2<DT>(y[6], y[7]));
                 }
             }
@@ -233,20 +234,29 @@ k24_norm_rotate_any(const RotateArgs p) {
     }
 }
 
+template <int W, int DT>
+static int launch_rotate_rows(const RotateArgs& p, dim3 grid, cudaStream_t st) {
+    if (p.norm) return launch_ex(k24_norm_rotate<W, DT, true>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
+    return launch_ex(k24_norm_rotate<W, DT, false>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
+}
+
 template <int DT>
 static int launch_rotate(RotateArgs& p, bool fast, cudaStream_t st) {
-    const int W = !fast ? 32 : p.D <= 64 ? 8 : p.D <= 128 ? 16 : 32;
-    const int rows = kRotateThreads / W;
-    // few tokens: a block takes one pass over a slice of their heads, so that all SMs have some
+    const int W = p.D <= 64 ? 8 : p.D <= 128 ? 16 : 32;
+    const int rows = fast ? kRotateThreads / W : kRotateThreads / 32;
     const int heads = std::max(p.side[0].heads, p.side[1].heads);
+    // As many tokens at a time as leave all SMs some blocks; few tokens: a token's heads are shared out, a pass to a block.
+    p.group = 1;
+    while (fast && p.group < kMaxGroup && p.T / (2 * p.group) >= 6 * sm_count()) p.group *= 2;
+    const int64_t groups = (p.T + p.group - 1) / p.group;
     const int64_t most = std::max(1, (heads + rows - 1) / rows);
-    p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 4 * sm_count() / p.T)));
-    const int64_t tokens = std::min<int64_t>(p.T, std::max(1, 16 * sm_count() / p.slices));
-    const dim3 grid(static_cast<unsigned>(tokens * p.slices));
+    p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 6 * sm_count() / groups)));
+    const int64_t blocks = std::min<int64_t>(groups, std::max(1, 48 * sm_count() / p.slices));
+    const dim3 grid(static_cast<unsigned>(blocks * p.slices));
     if (!fast) return launch_ex(k24_norm_rotate_any<DT>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
-    if (W == 8) return launch_ex(k24_norm_rotate<8, DT>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
-    if (W == 16) return launch_ex(k24_norm_rotate<16, DT>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
-    return launch_ex(k24_norm_rotate<32, DT>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
+    if (W == 8) return launch_rotate_rows<8, DT>(p, grid, st);
+    if (W == 16) return launch_rotate_rows<16, DT>(p, grid, st);
+    return launch_rotate_rows<32, DT>(p, grid, st);
 }
 
 }  // namespace cq
@@ -272,8 +282,8 @@ extern "C" int cq_norm_rotate(const void* Q, int64_t q_token_stride, int64_t q_h
     p.side[1] = RotateSide{static_cast<const uint16_t*>(K), k_token_stride, k_head_stride, static_cast<uint16_t*>(k_out), ko_token_stride, ko_head_stride,
                            static_cast<const uint16_t*>(k_weight), static_cast<int>(H)};
     p.positions = positions; p.freq = freq; p.T = T; p.D = static_cast<int>(D); p.R = static_cast<int>(R);
-    p.norm = eps >= 0.0; p.neighbours = neighbours != 0; p.eps = eps; p.slices = 1;
-    bool fast = D % 8 == 0 && D <= 256 && R % 16 == 0;
+    p.norm = eps >= 0.0; p.neighbours = neighbours != 0; p.eps = eps; p.slices = p.group = 1;
+    bool fast = D % 8 == 0 && D <= kFastDim && R % 16 == 0;
     for (const RotateSide& a : p.side) {
         if (a.heads == 0) continue;
         int64_t strides = 0;
