@@ -34,52 +34,55 @@ struct AdapterArgs {
     int vec_k, vec_n;                                           // elements of one access to rows of x and A (of y and out)
 };
 
-// The window's tokens by adapter.  s_rank[i]: how many adapters appear before the one that token i is the first of; -1 if it is not.
+// A window's adapters, two tokens to a lane of every warp (-1: none), and the tokens of one of them in order, in shared memory.
 struct Window {
-    int idx[kWindow];
-    int first[kWindow];                       // adapters in order of appearance: their first token
-    int list[kWindow];                        // tokens of the adapter at hand
-    int n, count, none;
+    int lo, hi;
+    __device__ __forceinline__ void read(const AdapterArgs& p, int64_t t0) {
+        const int lane = threadIdx.x & 31;
+        lo = t0 + lane < p.T ? __ldcg(p.index + t0 + lane) : -1;
+        hi = t0 + 32 + lane < p.T ? __ldcg(p.index + t0 + 32 + lane) : -1;
+        if (lo >= p.n) lo = -1;
+        if (hi >= p.n) hi = -1;
+    }
+    __device__ __forceinline__ uint64_t any() const {                   // tokens with an adapter
+        return __ballot_sync(0xFFFFFFFFu, lo >= 0) | static_cast<uint64_t>(__ballot_sync(0xFFFFFFFFu, hi >= 0)) << 32;
+    }
+    __device__ __forceinline__ int at(int token) const { return __shfl_sync(0xFFFFFFFFu, token < 32 ? lo : hi, token & 31); }
+    __device__ __forceinline__ uint64_t with(int a) const {             // tokens of adapter a
+        return __ballot_sync(0xFFFFFFFFu, lo == a) | static_cast<uint64_t>(__ballot_sync(0xFFFFFFFFu, hi == a)) << 32;
+    }
 };
-__device__ __forceinline__ void read_window(const AdapterArgs& p, int64_t t0, Window& w) {
-    const int tid = threadIdx.x;
-    if (tid < kWindow) {
-        const int64_t t = t0 + tid;
-        const int a = t < p.T ? __ldcg(p.index + t) : -1;
-        w.idx[tid] = a >= 0 && a < p.n ? a : -1;
+// The adapters of a window that the slot-th of `slots` blocks takes, in order of their first tokens.
+struct Turn {
+    uint64_t left;
+    int rank;
+    bool alone;                               // a block for each token: this one's, if no earlier token has the same adapter
+    __device__ __forceinline__ Turn(const Window& w, int slots) : left(w.any()), rank(0), alone(slots >= kWindow) {}
+    // the next adapter and its tokens; false when there is none
+    __device__ __forceinline__ bool next(const Window& w, int slot, int slots, int& a, uint64_t& tokens) {
+        if (alone) {
+            if (!(left >> slot & 1u)) return false;
+            a = w.at(slot);
+            tokens = w.with(a);
+            left = 0;
+            return __ffsll(tokens) - 1 == slot;
+        }
+        while (left != 0) {
+            a = w.at(__ffsll(left) - 1);
+            tokens = w.with(a);
+            left &= ~tokens;
+            if (rank++ % slots == slot) return true;
+        }
+        return false;
     }
-    __syncthreads();
-    if (tid < kWindow) {
-        const int a = w.idx[tid];
-        bool earlier = false;
-#pragma unroll 8
-        for (int j = 0; j < kWindow; ++j) earlier = earlier || (j < tid && w.idx[j] == a);
-        const unsigned lead = __ballot_sync(0xFFFFFFFFu, a >= 0 && !earlier);
-        if ((tid & 31) == 0) w.list[tid >> 5] = static_cast<int>(lead);
-    }
-    __syncthreads();
-    if (tid < kWindow) {
-        const unsigned lo = static_cast<unsigned>(w.list[0]), hi = static_cast<unsigned>(w.list[1]);
-        const unsigned mine = tid < 32 ? lo : hi;
-        const int before = __popc(mine & ((1u << (tid & 31)) - 1u)) + (tid < 32 ? 0 : __popc(lo));
-        if (mine >> (tid & 31) & 1u) w.first[before] = tid;
-        if (tid == 0) w.n = __popc(lo) + __popc(hi);
-    }
-    __syncthreads();
-}
-// The tokens of adapter `a` in order (a = -1: those without one).
-__device__ __forceinline__ void pick_tokens(Window& w, int a, int valid) {
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        const int lane = threadIdx.x;
-        const unsigned lo = __ballot_sync(0xFFFFFFFFu, lane < valid && w.idx[lane] == a);
-        const unsigned hi = __ballot_sync(0xFFFFFFFFu, 32 + lane < valid && w.idx[32 + lane] == a);
-        const unsigned below = (1u << lane) - 1u;
-        if (lo >> lane & 1u) w.list[__popc(lo & below)] = lane;
-        if (hi >> lane & 1u) w.list[__popc(lo) + __popc(hi & below)] = 32 + lane;
-        if (lane == 0) w.count = __popc(lo) + __popc(hi);
-    }
-    __syncthreads();
+};
+// The tokens of a set in order, written by one warp.
+__device__ __forceinline__ void write_list(uint64_t tokens, uint8_t* list) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t lo = static_cast<uint32_t>(tokens), hi = static_cast<uint32_t>(tokens >> 32), below = (1u << lane) - 1u;
+    if (lo >> lane & 1u) list[__popc(lo & below)] = static_cast<uint8_t>(lane);
+    if (hi >> lane & 1u) list[__popc(lo) + __popc(hi & below)] = static_cast<uint8_t>(32 + lane);
+    __syncwarp();
 }
 
 template <int DT>
@@ -164,23 +167,26 @@ k25_adapter_in(const AdapterArgs p) {
     float* s_red = reinterpret_cast<float*>(s_mem);             // [4][kRows][9], over the stages
     float* s_h = reinterpret_cast<float*>(s_mem + ST * kStage); // [token][kRows + 1]
     static_assert(size_t(4) * kRows * 9 * 4 <= ST * kStage, "sums of warps");
-    __shared__ Window w;
+    __shared__ uint8_t s_list[kAdThreads / 32][kWindow];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+    uint8_t* list = s_list[warp];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");         // (only now: the next kernel reads B and y before this one ends)
     const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kWindow;
-    const int valid = static_cast<int>(min(static_cast<int64_t>(kWindow), p.T - t0));
-    read_window(p, t0, w);
+    Window w;
+    w.read(p, t0);
     const int rank = blockIdx.x, ranks = gridDim.x;
     const int64_t units = (p.K + kUnit - 1) / kUnit, u0 = units * rank / ranks, u1 = units * (rank + 1) / ranks;
-    for (int which = blockIdx.z; which < w.n; which += gridDim.z) {
-        const int a = w.idx[w.first[which]];
-        pick_tokens(w, a, valid);
-        const int count = w.count;
+    Turn turn(w, gridDim.z);
+    int a;
+    uint64_t tokens;
+    while (turn.next(w, blockIdx.z, gridDim.z, a, tokens)) {
+        write_list(tokens, list);
+        const int count = __popcll(tokens);
         const uint16_t* A = p.A + static_cast<int64_t>(a) * p.R * p.K;
         if (count <= 8) {
             constexpr int kAhead = MT == 1 ? 4 : MT == 2 ? 2 : 1;       // steps whose loads are issued together
-            const uint16_t* x = g < count ? p.x + (t0 + w.list[g]) * p.ldx : nullptr;
+            const uint16_t* x = g < count ? p.x + (t0 + list[g]) * p.ldx : nullptr;
             float acc[MT][4] = {};
             for (int64_t u = 2 * u0 + warp; u < 2 * u1; u += 8 * kAhead) {
                 uint4 xb[kAhead], wa[kAhead][MT][2];
@@ -236,7 +242,7 @@ k25_adapter_in(const AdapterArgs p) {
 #pragma unroll
                 for (int i = tid; i < kWindow * 8; i += kAdThreads) {
                     const int r = i >> 3, c = i & 7;
-                    if (r < count) stage8(sx + r * 128 + ((c ^ (r & 7)) << 4), p.x + (t0 + w.list[r]) * p.ldx, u * kUnit + c * 8, p.K, p.vec_k);
+                    if (r < count) stage8(sx + r * 128 + ((c ^ (r & 7)) << 4), p.x + (t0 + list[r]) * p.ldx, u * kUnit + c * 8, p.K, p.vec_k);
                 }
 #pragma unroll
                 for (int i = tid; i < kRows * 8; i += kAdThreads) {
@@ -323,7 +329,7 @@ k25_adapter_in(const AdapterArgs p) {
             // 2^e, the power of two at or below the largest, within fp32's normal numbers: h 2^-e lies below 2
             const uint32_t e = min(max(__float_as_uint(top) >> 23, 2u), 252u);
             const float down = __uint_as_float((254u - e) << 23);
-            const int64_t t = t0 + w.list[m];
+            const int64_t t = t0 + list[m];
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const int r = lane + 32 * i;
@@ -336,7 +342,9 @@ k25_adapter_in(const AdapterArgs p) {
             }
             if (lane == 0) p.factor[t] = __uint_as_float(e << 23) * (p.scale != nullptr ? p.scale[a] : 1.0f);
         }
-        if (ranks > 1) cluster_barrier();     // nobody writes its sums over while they are being read
+        // nobody writes its sums over while they are being read
+        if (ranks > 1) cluster_barrier();
+        else __syncthreads();
     }
 }
 
@@ -418,21 +426,24 @@ __global__ void __launch_bounds__(kAdThreads, MT <= 2 ? 3 : 2)
 k26_adapter_out(const AdapterArgs p) {
     constexpr int kPitch = h_pitch<MT>();
     constexpr int kHeld = MT == 8 ? 32 : kWindow;               // tokens whose h is in shared memory at a time
-    __shared__ Window w;
+    __shared__ uint8_t s_list[kAdThreads / 32][kWindow];
     __shared__ __align__(16) uint32_t s_h[2][kHeld][kPitch];
-    __shared__ float s_f[kWindow];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+    uint8_t* list = s_list[warp];
     asm volatile("griddepcontrol.launch_dependents;");
     const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kWindow;
-    const int valid = static_cast<int>(min(static_cast<int64_t>(kWindow), p.T - t0));
-    read_window(p, t0, w);
+    Window w;
+    w.read(p, t0);
     const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kExpandCols + warp * 32, col = n0 + 8 * t4;
     bool waited = false;
-    for (int which = blockIdx.z; which < w.n; which += gridDim.z) {
-        const int a = w.idx[w.first[which]];
-        pick_tokens(w, a, valid);
-        const int count = w.count;
-        auto token = [&](int m) { return m < count ? t0 + w.list[m] : int64_t(-1); };
+    Turn turn(w, gridDim.z);
+    int a;
+    uint64_t tokens;
+    while (turn.next(w, blockIdx.z, gridDim.z, a, tokens)) {
+        __syncwarp();
+        write_list(tokens, list);
+        const int count = __popcll(tokens);
+        auto token = [&](int m) { return m < count ? t0 + list[m] : int64_t(-1); };
         Piece<YT> ya = load_piece<YT>(p, token(g), col), yb = load_piece<YT>(p, token(8 + g), col);
         // product j takes columns n0 + 8 (q / 2) + 2 j + q % 2, q = 0 .. 7
         uint2 b[4][MT];
@@ -451,18 +462,21 @@ k26_adapter_out(const AdapterArgs p) {
             asm volatile("griddepcontrol.wait;" ::: "memory");
             waited = true;
         }
+        const bool few = count <= 16;                           // then h comes from memory, else from shared memory
         for (int base = 0; base < count; base += kHeld) {
-            if (base > 0) __syncthreads();
             const int held = min(kHeld, count - base), pieces = p.R / 8;         // 16 bytes each
-            for (int i = tid; i < 2 * held * pieces; i += kAdThreads) {
-                const int part = i >= held * pieces ? 1 : 0, at = i - part * held * pieces, m = at / pieces, c = at - m * pieces;
-                const uint16_t* h = (part == 0 ? p.high : p.low) + (t0 + w.list[base + m]) * p.R + c * 8;
-                *reinterpret_cast<uint4*>(&s_h[part][m][c * 4]) = __ldcg(reinterpret_cast<const uint4*>(h));
+            if (!few) {
+                __syncthreads();
+                for (int i = tid; i < 2 * held * pieces; i += kAdThreads) {
+                    const int part = i >= held * pieces ? 1 : 0, at = i - part * held * pieces, m = at / pieces, c = at - m * pieces;
+                    const uint16_t* h = (part == 0 ? p.high : p.low) + (t0 + list[base + m]) * p.R + c * 8;
+                    *reinterpret_cast<uint4*>(&s_h[part][m][c * 4]) = __ldcg(reinterpret_cast<const uint4*>(h));
+                }
+                __syncthreads();
             }
-            for (int i = tid; i < held; i += kAdThreads) s_f[i] = __ldcg(p.factor + t0 + w.list[base + i]);
-            __syncthreads();
             for (int m0 = 0; m0 < held; m0 += 16) {
-                const bool have_a = m0 + g < held, have_b = m0 + 8 + g < held;
+                const int64_t ta = token(base + m0 + g), tb = token(base + m0 + 8 + g);
+                const float fa = ta >= 0 ? __ldcg(p.factor + ta) : 0.0f, fb = tb >= 0 ? __ldcg(p.factor + tb) : 0.0f;
                 const Piece<YT> na = load_piece<YT>(p, token(base + m0 + 16 + g), col), nb = load_piece<YT>(p, token(base + m0 + 24 + g), col);
                 float acc[4][4] = {};
 #pragma unroll
@@ -472,20 +486,22 @@ k26_adapter_out(const AdapterArgs p) {
 #pragma unroll
                     for (int part = 0; part < 2; ++part) {
                         uint2 ha = make_uint2(0, 0), hb = ha;
-                        if (have_a && have_k) ha = *reinterpret_cast<const uint2*>(&s_h[part][m0 + g][i * 8 + t4 * 2]);
-                        if (have_b && have_k) hb = *reinterpret_cast<const uint2*>(&s_h[part][m0 + 8 + g][i * 8 + t4 * 2]);
+                        if (few) {
+                            const uint16_t* h = (part == 0 ? p.high : p.low) + i * 16 + t4 * 4;
+                            if (ta >= 0 && have_k) ha = __ldcg(reinterpret_cast<const uint2*>(h + ta * p.R));
+                            if (tb >= 0 && have_k) hb = __ldcg(reinterpret_cast<const uint2*>(h + tb * p.R));
+                        } else {
+                            if (ta >= 0 && have_k) ha = *reinterpret_cast<const uint2*>(&s_h[part][m0 + g][i * 8 + t4 * 2]);
+                            if (tb >= 0 && have_k) hb = *reinterpret_cast<const uint2*>(&s_h[part][m0 + 8 + g][i * 8 + t4 * 2]);
+                        }
 #pragma unroll
                         for (int j = 0; j < 4; ++j) mma16<DT>(acc[j], ha.x, hb.x, ha.y, hb.y, b[j][i].x, b[j][i].y);
                     }
                 }
-                if (have_a) {
-                    const float d[8] = {acc[0][0], acc[0][1], acc[1][0], acc[1][1], acc[2][0], acc[2][1], acc[3][0], acc[3][1]};
-                    add_store<YT>(p, token(base + m0 + g), col, ya, d, s_f[m0 + g]);
-                }
-                if (have_b) {
-                    const float d[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
-                    add_store<YT>(p, token(base + m0 + 8 + g), col, yb, d, s_f[m0 + 8 + g]);
-                }
+                const float da[8] = {acc[0][0], acc[0][1], acc[1][0], acc[1][1], acc[2][0], acc[2][1], acc[3][0], acc[3][1]};
+                const float db[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
+                add_store<YT>(p, ta, col, ya, da, fa);
+                add_store<YT>(p, tb, col, yb, db, fb);
                 ya = na;
                 yb = nb;
             }
@@ -493,10 +509,13 @@ k26_adapter_out(const AdapterArgs p) {
     }
     if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
     if (blockIdx.z == 0 && p.out != p.y) {    // tokens without an adapter
-        pick_tokens(w, -1, valid);
+        const int valid = static_cast<int>(min(static_cast<int64_t>(kWindow), p.T - t0));
+        const uint64_t bare = ~w.any() & (valid < 64 ? (uint64_t(1) << valid) - 1u : ~uint64_t(0));
+        __syncwarp();
+        write_list(bare, list);
         const float zero[8] = {-0.0f, -0.0f, -0.0f, -0.0f, -0.0f, -0.0f, -0.0f, -0.0f};       // (y + -0 is y)
-        for (int i = tid; i < w.count * (kExpandCols / 8); i += kAdThreads) {
-            const int64_t t = t0 + w.list[i / (kExpandCols / 8)], c = static_cast<int64_t>(blockIdx.x) * kExpandCols + (i % (kExpandCols / 8)) * 8;
+        for (int i = lane; i < __popcll(bare) * 4; i += 32) {   // this warp's 32 columns
+            const int64_t t = t0 + list[i >> 2], c = n0 + (i & 3) * 8;
             add_store<YT>(p, t, c, load_piece<YT>(p, t, c), zero, 0.0f);
         }
     }

@@ -44,6 +44,20 @@ __device__ __forceinline__ void angles(const RotateArgs& p, int64_t t0, float* s
     }
 }
 
+// the sum of a row's squares in 64 bits, on all W lanes
+template <int W, int DT>
+__device__ __noinline__ double row_squares(uint4 x) {
+    double sum = 0.0;
+    const uint32_t r[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 e = unpack16x2<DT>(r[i]);
+        sum += static_cast<double>(e.x) * e.x + static_cast<double>(e.y) * e.y;
+    }
+#pragma unroll
+    for (int off = W / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off, W);
+    return sum;
+}
 // 1 / sqrt(mean + eps)
 __device__ __noinline__ double wide_factor(double sum, int D, double eps) { return 1.0 / sqrt(sum / D + eps); }
 
@@ -63,7 +77,7 @@ __device__ __forceinline__ void unpack8(const uint4& w, float (&v)[8]) {
 constexpr int kMaxGroup = 8;
 constexpr int kFastDim = 256;
 
-template <int W, int DT, bool NORM>
+template <int W, int DT, bool NORM, bool NEAR>                 // NEAR: neighbours are pairs
 __global__ void __launch_bounds__(kRotateThreads, 3)
 k24_norm_rotate(const RotateArgs p) {
     constexpr int kRows = kRotateThreads / W;
@@ -78,8 +92,8 @@ k24_norm_rotate(const RotateArgs p) {
     const int half = p.R / 2;
     const bool rotated = d0 < p.R, second = d0 >= half;
     // the lane with the other channels of this one's pairs (halves), and the first of its angles
-    const int partner = p.neighbours || !rotated ? lane : second ? lane - half / 8 : lane + half / 8;
-    const int angle0 = p.neighbours ? d0 / 2 : second ? d0 - half : d0;
+    const int partner = NEAR || !rotated ? lane : second ? lane - half / 8 : lane + half / 8;
+    const int angle0 = NEAR ? d0 / 2 : second ? d0 - half : d0;
     const int slice = blockIdx.x % p.slices;
     const int64_t stride = static_cast<int64_t>(gridDim.x / p.slices) * p.group;
     int buffer = 0;
@@ -90,19 +104,22 @@ k24_norm_rotate(const RotateArgs p) {
         for (int kv = 0; kv < 2; ++kv) {
             const RotateSide& a = p.side[kv];
             const int h0 = static_cast<int>(static_cast<int64_t>(a.heads) * slice / p.slices), h1 = static_cast<int>(static_cast<int64_t>(a.heads) * (slice + 1) / p.slices);
-            const uint16_t* x_row = a.x + t * a.xt + d0;
-            uint16_t* y_row = a.y + t * a.yt + d0;
+            // this lane's heads: h0 + first, every `step`-th, `rows` of them; `most` of any lane of the block
             const bool live = have && t < p.T;
+            const int rows = live && h1 - h0 > first ? (h1 - h0 - first + step - 1) / step : 0, most = (h1 - h0 + step - 1) / step;
+            const uint16_t* x_at = a.x + t * a.xt + (h0 + first) * a.xh + d0;
+            uint16_t* y_at = a.y + t * a.yt + (h0 + first) * a.yh + d0;
+            const int64_t x_step = step * a.xh, y_step = step * a.yh;
             float c[8], s[8];                                   // y = (x c + partner s) factor
-            for (int hb = h0; hb < h1 || (kv == 0 && !ready); hb += step * kAhead) {
+            for (int done = 0; done < most || (kv == 0 && !ready); done += kAhead) {
                 uint4 x[kAhead];
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
-                    const int h = hb + u * step + first;
                     x[u] = make_uint4(0, 0, 0, 0);
-                    if (live && h < h1) x[u] = __ldcs(reinterpret_cast<const uint4*>(x_row + h * a.xh));
+                    if (done + u < rows) x[u] = __ldcs(reinterpret_cast<const uint4*>(x_at));
+                    x_at += x_step;
                 }
-                if (hb == h0) {                                 // (behind the first loads)
+                if (done == 0) {                                // (behind the first loads)
                     if (!ready) {
                         angles(p, t0, s_cos[buffer], s_sin[buffer]);
                         __syncthreads();
@@ -118,65 +135,76 @@ k24_norm_rotate(const RotateArgs p) {
                     }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int at = token * half + angle0 + (p.neighbours ? i / 2 : i);
-                        const bool later = p.neighbours ? (i & 1) != 0 : second;
-                        const float other = p.neighbours ? w[i ^ 1] : wp[i];
+                        const int at = token * half + angle0 + (NEAR ? i / 2 : i);
+                        const bool later = NEAR ? (i & 1) != 0 : second;
+                        const float other = NEAR ? w[i ^ 1] : wp[i];
                         c[i] = rotated ? s_cos[buffer][at] * w[i] : w[i];
                         s[i] = rotated ? (later ? s_sin[buffer][at] : -s_sin[buffer][at]) * other : 0.0f;
                     }
                 }
+                float f[kAhead];
+                uint32_t moved = 0;                             // bits u, u + 4: row u is moved by 2^64, by 2^-64
+                if constexpr (NORM) {
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        float v[8];
+                        unpack8<DT>(x[u], v);
+                        f[u] = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[u] = __fmaf_rn(v[i], v[i], f[u]);
+                    }
+#pragma unroll
+                    for (int off = W / 2; off > 0; off >>= 1)
+#pragma unroll
+                        for (int u = 0; u < kAhead; ++u) f[u] += __shfl_xor_sync(0xFFFFFFFFu, f[u], off, W);
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u)
+                        if (done + u < rows && !(f[u] > 1e-25f && f[u] < 1e35f)) moved |= f[u] > 1.0f ? 16u << u : 1u << u;
+                    const bool any = __any_sync(0xFFFFFFFFu, moved != 0u);
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const float mean = __fmaf_rn(f[u], 1.0f / static_cast<float>(p.D), static_cast<float>(p.eps));
+                        if (any) {                              // squares that fp32 cannot hold, or that are all zero: the sum in 64 bits
+                            const double wide = row_squares<W, DT>(x[u]);
+                            if (moved >> u & 0x11u) f[u] = static_cast<float>(wide_factor(wide, p.D, p.eps) * (moved >> u & 1u ? 0x1p-64 : 0x1p64));
+                            else f[u] = rsqrtf(mean);
+                        } else {
+                            f[u] = rsqrtf(mean);
+                        }
+                    }
+                }
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
-                    if (hb + u * step >= h1) break;             // the same for the whole block
+                    if (done + u >= most) break;                // the same for the whole block
                     float v[8], o[8];
                     unpack8<DT>(x[u], v);
-                    if (p.neighbours) {
+                    if constexpr (NEAR) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) o[i] = v[i ^ 1];
+                        for (int i = 0; i < 8; ++i) o[i] = rotated ? v[i ^ 1] : 0.0f;      // (an infinity times a sine of 0)
                     } else {
                         uint4 xp;
                         xp.x = __shfl_sync(0xFFFFFFFFu, x[u].x, partner, W);
                         xp.y = __shfl_sync(0xFFFFFFFFu, x[u].y, partner, W);
                         xp.z = __shfl_sync(0xFFFFFFFFu, x[u].z, partner, W);
                         xp.w = __shfl_sync(0xFFFFFFFFu, x[u].w, partner, W);
+                        if (!rotated) xp = make_uint4(0, 0, 0, 0);
                         unpack8<DT>(xp, o);
                     }
-                    if (!rotated) {                             // (an infinity times a sine of 0)
+                    if (NORM && (moved >> u & 0x11u)) {
+                        const float move = moved >> u & 1u ? 0x1p64f : 0x1p-64f;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) o[i] = 0.0f;
+                        for (int i = 0; i < 8; ++i) { v[i] *= move; o[i] *= move; }
                     }
                     float y[8];
-                    const int h = hb + u * step + first;
-                    if constexpr (NORM) {
-                        float sum = 0.0f;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) sum = __fmaf_rn(v[i], v[i], sum);
-#pragma unroll
-                        for (int off = W / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off, W);
-                        const float f = rsqrtf(__fmaf_rn(sum, 1.0f / static_cast<float>(p.D), static_cast<float>(p.eps)));
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] = __fmaf_rn(v[i], c[i], o[i] * s[i]) * f;
-                        // squares that fp32 cannot hold, or that are all zero: in 64 bits
-                        const bool wide_row = live && h < h1 && !(sum > 1e-25f && sum < 1e35f);
-                        if (__any_sync(0xFFFFFFFFu, wide_row)) {
-                            double wide = 0.0;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) wide += static_cast<double>(v[i]) * v[i];
-#pragma unroll
-                            for (int off = W / 2; off > 0; off >>= 1) wide += __shfl_xor_sync(0xFFFFFFFFu, wide, off, W);
-                            wide = wide_factor(wide, p.D, p.eps);
-                            if (wide_row) {
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) y[i] = static_cast<float>((static_cast<double>(v[i]) * c[i] + static_cast<double>(o[i]) * s[i]) * wide);
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] = __fmaf_rn(v[i], c[i], o[i] * s[i]);
+                    for (int i = 0; i < 8; ++i) {
+                        y[i] = __fmaf_rn(v[i], c[i], o[i] * s[i]);
+                        if constexpr (NORM) y[i] *= f[u];
                     }
-                    if (live && h < h1)
-                        *reinterpret_cast<uint4*>(y_row + h * a.yh) =
+                    if (done + u < rows)
+                        *reinterpret_cast<uint4*>(y_at) =
                             make_uint4(pack16x2<DT>(y[0], y[1]), pack16x2<DT>(y[2], y[3]), pack16x2<DT>(y[4], y[5]), pack16x2<DT>(y[6], y[7]));
+                    y_at += y_step;
                 }
             }
         }
@@ -234,10 +262,14 @@ k24_norm_rotate_any(const RotateArgs p) {
     }
 }
 
+template <int W, int DT, bool NORM>
+static int launch_rotate_pairs(const RotateArgs& p, dim3 grid, cudaStream_t st) {
+    if (p.neighbours) return launch_ex(k24_norm_rotate<W, DT, NORM, true>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
+    return launch_ex(k24_norm_rotate<W, DT, NORM, false>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
+}
 template <int W, int DT>
 static int launch_rotate_rows(const RotateArgs& p, dim3 grid, cudaStream_t st) {
-    if (p.norm) return launch_ex(k24_norm_rotate<W, DT, true>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
-    return launch_ex(k24_norm_rotate<W, DT, false>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
+    return p.norm ? launch_rotate_pairs<W, DT, true>(p, grid, st) : launch_rotate_pairs<W, DT, false>(p, grid, st);
 }
 
 template <int DT>
@@ -247,7 +279,7 @@ static int launch_rotate(RotateArgs& p, bool fast, cudaStream_t st) {
     const int heads = std::max(p.side[0].heads, p.side[1].heads);
     // As many tokens at a time as leave all SMs some blocks; few tokens: a token's heads are shared out, a pass to a block.
     p.group = 1;
-    while (fast && p.group < kMaxGroup && p.T / (2 * p.group) >= 6 * sm_count()) p.group *= 2;
+    while (fast && p.group < kMaxGroup && p.T / (2 * p.group) >= 2 * sm_count()) p.group *= 2;
     const int64_t groups = (p.T + p.group - 1) / p.group;
     const int64_t most = std::max(1, (heads + rows - 1) / rows);
     p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 6 * sm_count() / groups)));
