@@ -10,7 +10,7 @@
 //
 // h is fp32 until it is written: as two 16-bit halves (h 2^-e = high + low, e from the token's largest |h|), so that the second
 // product, on 16-bit operands, sees 16 bits of it or more, and fp16 neither overflows nor loses small tokens.
-#include "cq_serve.cuh"
+#include "cq_adapter.cuh"
 
 #include <algorithm>
 
@@ -19,20 +19,6 @@ namespace cq {
 constexpr int kWindow = 64;                   // tokens that are sorted by adapter together
 constexpr int kAdThreads = 256;
 constexpr int kUnitK = 32;                    // contraction of one step: a 16-byte piece for each of the four lanes of a row
-constexpr int kExpandCols = 256;              // columns of a block of the second kernel, 32 for each warp
-constexpr int kMaxRank = 128;
-
-struct AdapterArgs {
-    const uint16_t* x; int64_t ldx;
-    const void* y; int64_t ldy;
-    void* out; int64_t ldo;
-    const uint16_t* A; const uint16_t* B; const float* scale;
-    const int* index;
-    uint16_t* high; uint16_t* low; float* factor;               // [T][R], [T][R], [T]
-    int64_t T, K, N;
-    int R, n;
-    int vec_k, vec_n;                                           // elements of one access to rows of x and A (of y and out)
-};
 
 // A window's adapters, two tokens to a lane of every warp (-1: none), and the tokens of one of them in order, in shared memory.
 struct Window {
@@ -134,18 +120,6 @@ __device__ __forceinline__ void stage8(uint8_t* dst, const uint16_t* row, int64_
 }
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], const uint8_t* p) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_u32(p)) : "memory");
-}
-
-__device__ __forceinline__ float ld_rank(const float* p, uint32_t rank) {
-    uint32_t remote;
-    float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
-    return v;
-}
-__device__ __forceinline__ void cluster_barrier() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // ---- h = A x ----------------------------------------------------------------------------------------------------
@@ -307,40 +281,7 @@ k25_adapter_in(const AdapterArgs p) {
         if (ranks > 1) cluster_barrier();
         // a warp for each token of this block's share
         for (int m = rank + warp * ranks; m < count; m += ranks * (kAdThreads / 32)) {
-            constexpr int kPer = (kRows + 31) / 32;
-            float h[kPer], top = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const int r = lane + 32 * i;
-                h[i] = 0.0f;
-                if (r < p.R) {
-                    if (ranks > 1) {
-#pragma unroll 8
-                        for (int k = 0; k < ranks; ++k) h[i] += ld_rank(s_h + m * (kRows + 1) + r, k);
-                    } else {
-                        h[i] = s_h[m * (kRows + 1) + r];
-                    }
-                }
-                const float v = fabsf(h[i]);
-                top = fmaxf(top, v < INFINITY ? v : 0.0f);
-            }
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, off));
-            // 2^e, the power of two at or below the largest, within fp32's normal numbers: h 2^-e lies below 2
-            const uint32_t e = min(max(__float_as_uint(top) >> 23, 2u), 252u);
-            const float down = __uint_as_float((254u - e) << 23);
-            const int64_t t = t0 + list[m];
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const int r = lane + 32 * i;
-                if (r < p.R) {
-                    const float v = h[i] * down;
-                    const uint16_t hi = pack16<DT>(v);
-                    p.high[t * p.R + r] = hi;
-                    p.low[t * p.R + r] = fabsf(v) < INFINITY ? pack16<DT>(v - cvt16<DT>(hi)) : 0;
-                }
-            }
-            if (lane == 0) p.factor[t] = __uint_as_float(e << 23) * (p.scale != nullptr ? p.scale[a] : 1.0f);
+            finish_token<DT>(p, s_h + m * (kRows + 1), ranks, t0 + list[m], a);
         }
         // nobody writes its sums over while they are being read
         if (ranks > 1) cluster_barrier();
@@ -349,7 +290,7 @@ k25_adapter_in(const AdapterArgs p) {
 }
 
 // ---- out = y + B h ---------------------------------------------------------------------------------------------------
-// grid (blocks of 256 columns, windows, adapters of a window in turn).  A warp keeps its 32 columns of B_a in registers and takes the adapter's
+// grid (blocks of 32 columns for each warp, windows, adapters of a window in turn).  A warp keeps its 32 columns of B_a in registers and takes the adapter's
 // tokens 16 at a time, y of the next 16 on the way.  The four products of 8 columns share them out so that each lane ends up with 8
 // neighbouring columns.
 template <int YT> struct Piece { uint32_t r[YT == CQ_F32 ? 8 : 4]; };           // 8 columns of a row of y
@@ -434,7 +375,7 @@ k26_adapter_out(const AdapterArgs p) {
     const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kWindow;
     Window w;
     w.read(p, t0);
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kExpandCols + warp * 32, col = n0 + 8 * t4;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * blockDim.x + warp * 32, col = n0 + 8 * t4;
     bool waited = false;
     Turn turn(w, gridDim.z);
     int a;
@@ -467,7 +408,7 @@ k26_adapter_out(const AdapterArgs p) {
             const int held = min(kHeld, count - base), pieces = p.R / 8;         // 16 bytes each
             if (!few) {
                 __syncthreads();
-                for (int i = tid; i < 2 * held * pieces; i += kAdThreads) {
+                for (int i = tid; i < 2 * held * pieces; i += blockDim.x) {
                     const int part = i >= held * pieces ? 1 : 0, at = i - part * held * pieces, m = at / pieces, c = at - m * pieces;
                     const uint16_t* h = (part == 0 ? p.high : p.low) + (t0 + list[base + m]) * p.R + c * 8;
                     *reinterpret_cast<uint4*>(&s_h[part][m][c * 4]) = __ldcg(reinterpret_cast<const uint4*>(h));
@@ -523,7 +464,9 @@ k26_adapter_out(const AdapterArgs p) {
 
 // ---- host ----------------------------------------------------------------------------------------------------------
 static size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-static size_t adapter_workspace(int64_t T, int64_t R) { return 2 * up256(sizeof(uint16_t) * T * R) + up256(sizeof(float) * T); }
+static size_t adapter_workspace(int64_t T, int64_t R) {
+    return 2 * up256(sizeof(uint16_t) * T * R) + 2 * up256(sizeof(float) * T) + sizeof(int) * kTileInfo * ((T + kTileTokens - 1) / kTileTokens);
+}
 
 template <int MT, int DT>
 static int launch_adapter(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
@@ -543,12 +486,16 @@ static int launch_adapter(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     const dim3 grid(static_cast<unsigned>(parts), static_cast<unsigned>(windows), static_cast<unsigned>(slots));
     const int rc = launch_ex(k25_adapter_in<MT, DT>, grid, kAdThreads, smem, st, grid.x, !tuning_no_pdl(), p);
     if (rc != CQ_OK) return rc;
-    const int64_t cols = (p.N + kExpandCols - 1) / kExpandCols;
+    // two, four or eight warps to a block: the most with which there are two blocks an SM
+    int warps = 8;
+    while (warps > 2 && windows * ((p.N + 32 * warps - 1) / (32 * warps)) < 2 * sms) warps /= 2;
+    const int64_t cols = (p.N + 32 * warps - 1) / (32 * warps);
     const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(adapters, 16 * sms / (windows * cols)));
     const dim3 grid2(static_cast<unsigned>(cols), static_cast<unsigned>(windows), static_cast<unsigned>(turns));
-    if (y_dtype == CQ_F32) return launch_ex(k26_adapter_out<MT, DT, CQ_F32>, grid2, kAdThreads, 0, st, 1, !tuning_no_pdl(), p);
-    if (y_dtype == CQ_F16) return launch_ex(k26_adapter_out<MT, DT, CQ_F16>, grid2, kAdThreads, 0, st, 1, !tuning_no_pdl(), p);
-    return launch_ex(k26_adapter_out<MT, DT, CQ_BF16>, grid2, kAdThreads, 0, st, 1, !tuning_no_pdl(), p);
+    const unsigned threads = 32u * warps;
+    if (y_dtype == CQ_F32) return launch_ex(k26_adapter_out<MT, DT, CQ_F32>, grid2, threads, 0, st, 1, !tuning_no_pdl(), p);
+    if (y_dtype == CQ_F16) return launch_ex(k26_adapter_out<MT, DT, CQ_F16>, grid2, threads, 0, st, 1, !tuning_no_pdl(), p);
+    return launch_ex(k26_adapter_out<MT, DT, CQ_BF16>, grid2, threads, 0, st, 1, !tuning_no_pdl(), p);
 }
 
 template <int DT>
@@ -582,8 +529,13 @@ int cq_adapter_add(const void* X, int dtype, int64_t T, int64_t K, int64_t ldx, 
     p.x = static_cast<const uint16_t*>(X); p.ldx = ldx; p.y = y; p.ldy = ldy; p.out = out; p.ldo = ldo;
     p.A = static_cast<const uint16_t*>(A); p.B = static_cast<const uint16_t*>(B); p.scale = scale; p.index = index;
     p.high = static_cast<uint16_t*>(workspace);
-    p.low = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(workspace) + up256(sizeof(uint16_t) * T * R));
-    p.factor = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 2 * up256(sizeof(uint16_t) * T * R));
+    uint8_t* at = static_cast<uint8_t*>(workspace) + up256(sizeof(uint16_t) * T * R);
+    p.low = reinterpret_cast<uint16_t*>(at);
+    at += up256(sizeof(uint16_t) * T * R);
+    p.factor = reinterpret_cast<float*>(at);
+    at += up256(sizeof(float) * T);
+    p.slot = reinterpret_cast<int*>(at);
+    p.info = reinterpret_cast<int*>(at + up256(sizeof(int) * T));
     p.T = T; p.K = K; p.N = N; p.R = static_cast<int>(R); p.n = static_cast<int>(n);
     // the widest access that every row's beginning and length allow
     for (p.vec_k = 8; p.vec_k > 1; p.vec_k /= 2)
@@ -591,6 +543,7 @@ int cq_adapter_add(const void* X, int dtype, int64_t T, int64_t K, int64_t ldx, 
     for (p.vec_n = static_cast<int>(16 / elem); p.vec_n > 1; p.vec_n /= 2)
         if (N % p.vec_n == 0 && (T == 1 || (ldy % p.vec_n == 0 && ldo % p.vec_n == 0)) && ptr_aligned(y, elem * p.vec_n) && ptr_aligned(out, elem * p.vec_n)) break;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (adapter_tiles_fit(p, y_dtype)) return launch_adapter_tiles(p, dtype, y_dtype, st);
     return dtype == CQ_F16 ? launch_adapter_rank<CQ_F16>(p, y_dtype, st) : launch_adapter_rank<CQ_BF16>(p, y_dtype, st);
 }
 

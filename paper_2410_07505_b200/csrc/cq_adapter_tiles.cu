@@ -1,0 +1,522 @@
+// Low-rank adapters for many tokens (cq_adapter.cu has the formula and the kernels for few): both products on tcgen05, everything
+// that is large through TMA.
+//
+// The tokens are taken in tiles of 128 neighbours.  A prompt's tokens share an adapter, so a tile has one or two; one that has more
+// (tokens of many requests) costs a product for each, in which the rows of the others are computed in vain, and nothing else.
+//   k27  h = A x: a tile's x against the rows of up to 128 / R adapters side by side, so that x is read once for them; the contraction
+//        is split over a cluster and joined through distributed shared memory in rank order
+//   k28  out = y + B h: persistent over 128 x 256-byte tiles of y; those stream through a ring in shared memory in which the
+//        epilogue adds the product to the rows that have the adapter at hand.  Bound by HBM (y in, out out)
+#include "cq_adapter.cuh"
+
+#include <algorithm>
+
+namespace cq {
+
+__device__ unsigned int g_adapter_fault = 0;  // set if a bounded wait ever gave up
+
+__device__ __forceinline__ bool agreed_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* dead) {
+    return __all_sync(0xFFFFFFFFu, role_wait(bar, parity, dead)) != 0;
+}
+__device__ __forceinline__ void tile_store(const CUtensorMap* map, const void* src_smem, int32_t x, int32_t y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                 :: "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(src_smem)) : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, float (&v)[8]) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]) :: "memory");
+}
+
+// ---- h = A x --------------------------------------------------------------------------------------------------------
+constexpr int kInThreads = 256;               // warp 0: loads, warp 1: products, warps 4..7: rows of the sums
+constexpr int kInCols = 128;                  // rows of A (of several adapters) side by side
+constexpr int kInMaxStages = 5;
+constexpr size_t kXTile = size_t(kTileTokens) * 128, kATile = size_t(kInCols) * 128;
+
+static int in_stages(int R) { return R <= 64 ? kInMaxStages : 4; }
+static size_t in_smem(int R) { return 1024 + in_stages(R) * (kXTile + kATile) + size_t(kTileTokens) * (R + 1) * 4; }
+
+template <int DT>
+__global__ void __launch_bounds__(kInThreads, 1)
+k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapA, const AdapterArgs p, int stages) {
+    extern __shared__ __align__(1024) uint8_t smem[];           // (behind the static part: moved to a 1024-byte boundary below)
+    __shared__ uint64_t full[kInMaxStages], empty[kInMaxStages], d_full[2], d_empty[2], drain;
+    __shared__ __align__(16) int s_idx[kTileTokens];
+    __shared__ int s_first[kTileTokens], s_rank[kTileTokens], s_adapter[kTileTokens], s_leads[4];
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile uint32_t s_dead;
+    uint8_t* s_x = smem + ((1024u - (smem_u32(smem) & 1023u)) & 1023u);
+    uint8_t* s_a = s_x + stages * kXTile;
+    float* s_h = reinterpret_cast<float*>(s_a + stages * kATile);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        for (int i = 0; i < kInMaxStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&d_full[i], 1); mbar_init(&d_empty[i], 4); }
+        mbar_init(&drain, 1);
+        mbar_init_fence();
+        s_dead = 0;
+        prefetch_map(&mapX);
+        prefetch_map(&mapA);
+    }
+    if (warp == 1) tmem_alloc(&s_tmem, 2 * kInCols);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kTileTokens;
+    // the tile's adapters in order of their first tokens
+    if (tid < kTileTokens) {
+        const int a = t0 + tid < p.T ? __ldcg(p.index + t0 + tid) : -1;
+        s_idx[tid] = a < p.n ? a : -1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (tid < kTileTokens) {
+        const int a = s_idx[tid];
+        int first = (warp << 5) + __ffs(__match_any_sync(0xFFFFFFFFu, a)) - 1;
+        for (int j = warp * 8 - 1; j >= 0; --j) {               // four tokens of the warps before
+            const int4 v = reinterpret_cast<const int4*>(s_idx)[j];
+            first = v.w == a ? 4 * j + 3 : first;
+            first = v.z == a ? 4 * j + 2 : first;
+            first = v.y == a ? 4 * j + 1 : first;
+            first = v.x == a ? 4 * j : first;
+        }
+        s_first[tid] = first;
+        const unsigned lead = __ballot_sync(0xFFFFFFFFu, a >= 0 && first == tid);
+        s_rank[tid] = __popc(lead & ((1u << lane) - 1u));
+        if (lane == 0) s_leads[warp] = __popc(lead);
+    }
+    __syncthreads();
+    const int count = s_leads[0] + s_leads[1] + s_leads[2] + s_leads[3];
+    if (tid < kTileTokens && s_idx[tid] >= 0 && s_first[tid] == tid) {
+        int rank = s_rank[tid];
+        for (int w = 0; w < warp; ++w) rank += s_leads[w];
+        s_rank[tid] = rank;
+        s_adapter[rank] = s_idx[tid];
+    }
+    __syncthreads();
+    const uint32_t tmem = s_tmem;
+    const int rank = blockIdx.x, ranks = gridDim.x;
+    const int kblocks = static_cast<int>((p.K + 63) / 64), kb0 = static_cast<int>(static_cast<int64_t>(kblocks) * rank / ranks),
+              kb1 = static_cast<int>(static_cast<int64_t>(kblocks) * (rank + 1) / ranks);
+    const int per = kInCols / p.R, groups = (count + per - 1) / per;
+    if (rank == 0 && tid < kTileTokens) {
+        if (tid == 0) p.info[blockIdx.y * static_cast<int64_t>(kTileInfo)] = count;
+        if (tid < count) p.info[blockIdx.y * static_cast<int64_t>(kTileInfo) + 1 + tid] = s_adapter[tid];
+        if (t0 + tid < p.T) p.slot[t0 + tid] = s_idx[tid] >= 0 ? s_rank[s_first[tid]] : -1;
+    }
+
+    if (warp == 0) {
+        int s = 0;
+        uint32_t round = 0;
+        int issued = 0;
+        bool ok = true;
+        for (int gr = 0; ok && gr < groups; ++gr) {
+            const int n = min(per, count - gr * per);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!(ok = agreed_wait(&empty[s], round ^ 1u, &s_dead))) break;
+                if (elect_one()) {
+                    mbar_expect_tx(&full[s], static_cast<uint32_t>(kXTile) + n * p.R * 128);
+                    tile_load(s_x + s * kXTile, &mapX, kb * 128, static_cast<int32_t>(t0), &full[s]);
+                    for (int i = 0; i < n; ++i)
+                        tile_load(s_a + s * kATile + i * p.R * 128, &mapA, kb * 128, s_adapter[gr * per + i] * p.R, &full[s]);
+                }
+                issued = min(issued + 1, stages);
+                if (++s == stages) { s = 0; round ^= 1u; }
+            }
+        }
+        if (!ok)                              // copies still in flight land before the CTA leaves
+            for (; issued > 0; --issued) {
+                if (--s < 0) { s = stages - 1; round ^= 1u; }
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&full[s], round); ++polls) {}
+            }
+    } else if (warp == 1) {
+        const uint64_t desc_x = smem_desc_k128(s_x), desc_a = smem_desc_k128(s_a);
+        int s = 0;
+        uint32_t round = 0;
+        bool ok = true;
+        for (int gr = 0; ok && gr < groups; ++gr) {
+            const int b = gr & 1, cols = (min(per, count - gr * per) * p.R + 15) & ~15;
+            const uint32_t idesc = idesc_f16<DT>(128, cols, false);
+            if (!(ok = agreed_wait(&d_empty[b], ((gr >> 1) & 1) ^ 1u, &s_dead))) break;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!(ok = agreed_wait(&full[s], round, &s_dead))) break;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        tc_mma_f16(tmem + b * kInCols, desc_x + ((s * kXTile) >> 4) + 2 * k, desc_a + ((s * kATile) >> 4) + 2 * k, idesc, kb > kb0 || k > 0);
+                    tc_commit(&empty[s]);
+                    if (kb + 1 == kb1) tc_commit(&d_full[b]);
+                }
+                if (++s == stages) { s = 0; round ^= 1u; }
+            }
+        }
+        if (!ok) {                            // products in flight end before the CTA leaves
+            __syncwarp();
+            if (elect_one()) tc_commit(&drain);
+            for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&drain, 0); ++polls) {}
+        }
+    } else if (warp >= 4) {
+        const int token = (warp & 3) * 32 + lane;
+        const int mine = s_idx[token] >= 0 ? s_rank[s_first[token]] : -1;
+        const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        float* h = s_h + token * (p.R + 1);
+        bool ok = true;
+        for (int gr = 0; ok && gr < groups; ++gr) {
+            const int b = gr & 1, n = min(per, count - gr * per);
+            if (!(ok = agreed_wait(&d_full[b], (gr >> 1) & 1, &s_dead))) break;
+            tc_fence_after();
+            for (int i = 0; i < n; ++i) {
+                const bool here = mine == gr * per + i;
+                if (!__any_sync(0xFFFFFFFFu, here)) continue;
+                for (int c = 0; c < p.R; c += 8) {
+                    float v[8];
+                    __syncwarp();
+                    tmem_ld8(at + b * kInCols + i * p.R + c, v);
+                    if (here) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) h[c + k] = v[k];
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&d_empty[b]);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    __syncwarp();
+    if (warp == 1) tmem_free(tmem, 2 * kInCols);
+    __syncwarp();
+    if (ranks > 1) cluster_barrier();
+    for (int m = rank + warp * ranks; m < kTileTokens; m += ranks * (kInThreads / 32))
+        if (s_idx[m] >= 0) finish_token<DT>(p, s_h + m * (p.R + 1), ranks, t0 + m, s_idx[m]);
+    __syncwarp();
+    if (ranks > 1) cluster_barrier();         // nobody leaves while its sums are being read
+    if (tid == 0 && s_dead != 0u) atomicExch(&g_adapter_fault, 1u);
+}
+
+// ---- out = y + B h ---------------------------------------------------------------------------------------------------
+constexpr int kOutThreads = 384;              // warp 0: loads, warp 1: products, warp 2: stores, warps 4..11: y + the product
+constexpr size_t kYTile = size_t(kTileTokens) * 256;
+constexpr int kOutBuffers = 4;                // accumulators
+
+template <int HB> __host__ __device__ constexpr int y_stages() { return HB == 1 ? 4 : 3; }       // HB: halves of 64 of the rank
+template <int HB> __host__ __device__ constexpr int b_stages() { return HB == 1 ? 3 : 2; }
+template <int YT> __host__ __device__ constexpr int out_cols() { return YT == CQ_F32 ? 64 : 128; }
+template <int HB, int YT> __host__ __device__ constexpr size_t b_tile() { return size_t(HB) * out_cols<YT>() * 128; }
+template <int HB, int YT> __host__ __device__ constexpr size_t out_smem() {
+    return 2 * HB * kXTile + y_stages<HB>() * kYTile + b_stages<HB>() * b_tile<HB, YT>() + 512;
+}
+
+struct OutItem { int64_t first, end; int cols; };               // items of this CTA; columns of tiles, the fastest of an item's two places
+__device__ __forceinline__ OutItem out_items(const AdapterArgs& p, int width) {
+    const int cols = static_cast<int>((p.N + width - 1) / width);
+    const int64_t items = (p.T + kTileTokens - 1) / kTileTokens * cols;
+    return {items * blockIdx.x / gridDim.x, items * (blockIdx.x + 1) / gridDim.x, cols};
+}
+
+template <int HB, int DT, int YT>
+__global__ void __launch_bounds__(kOutThreads, 1)
+k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_constant__ CUtensorMap mapLow, const __grid_constant__ CUtensorMap mapB,
+                      const __grid_constant__ CUtensorMap mapY, const __grid_constant__ CUtensorMap mapOut, const AdapterArgs p) {
+    constexpr int SY = y_stages<HB>(), SB = b_stages<HB>(), CT = out_cols<YT>();
+    constexpr size_t kB = b_tile<HB, YT>();
+    // No static shared memory, so that the dynamic part starts on the 1024-byte boundary that the swizzle wants.
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t* s_h = smem;                                        // [high, low][half of the rank][128 tokens][128 bytes]
+    uint8_t* s_y = s_h + 2 * HB * kXTile;                       // [stage][half of the columns][128 tokens][128 bytes]
+    uint8_t* s_b = s_y + SY * kYTile;                           // [stage][half of the rank][CT columns][128 bytes]
+    uint64_t* y_full = reinterpret_cast<uint64_t*>(s_b + SB * kB);
+    uint64_t* y_empty = y_full + SY;
+    uint64_t* o_full = y_empty + SY;
+    uint64_t* b_full = o_full + SY;
+    uint64_t* b_empty = b_full + SB;
+    uint64_t* d_full = b_empty + SB;
+    uint64_t* d_empty = d_full + kOutBuffers;
+    uint64_t* h_full = d_empty + kOutBuffers;
+    uint64_t* h_empty = h_full + 1;
+    uint64_t* drain = h_empty + 1;
+    uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(drain + 1);
+    volatile uint32_t& s_dead = *(reinterpret_cast<volatile uint32_t*>(drain + 1) + 1);
+    static_assert((3 * SY + 2 * SB + 2 * kOutBuffers + 3) * 8 + 8 <= 512, "barriers");
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    asm volatile("griddepcontrol.launch_dependents;");
+    if (tid == 0) {
+        if ((smem_u32(smem) & 1023u) != 0u) atomicExch(&g_adapter_fault, 1u);      // cannot be: see above
+        for (int i = 0; i < SY; ++i) { mbar_init(&y_full[i], 1); mbar_init(&y_empty[i], 1); mbar_init(&o_full[i], 8); }
+        for (int i = 0; i < SB; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_empty[i], 1); }
+        for (int i = 0; i < kOutBuffers; ++i) { mbar_init(&d_full[i], 1); mbar_init(&d_empty[i], 8); }
+        mbar_init(h_full, 1);
+        mbar_init(h_empty, 1);
+        mbar_init(drain, 1);
+        mbar_init_fence();
+        s_dead = 0;
+        prefetch_map(&mapHigh);
+        prefetch_map(&mapLow);
+        prefetch_map(&mapB);
+        prefetch_map(&mapY);
+        prefetch_map(&mapOut);
+    }
+    if (warp == 1) tmem_alloc(&s_tmem, kOutBuffers * CT);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const OutItem work = out_items(p, CT);
+
+    if (warp == 0) {
+        int ys = 0, bs = 0, y_issued = 0, b_issued = 0, count = 0;
+        uint32_t y_round = 0, b_round = 0, h_round = 0;
+        int64_t tile = -1;
+        bool ok = true, h_open = false;
+        const int* info = p.info;
+        for (int64_t it = work.first; ok && it < work.end; ++it) {
+            const int64_t tl = it / work.cols;
+            const int col = static_cast<int>(it - tl * work.cols) * CT;
+            const int32_t t0 = static_cast<int32_t>(tl) * kTileTokens;
+            if (!(ok = agreed_wait(&y_empty[ys], y_round ^ 1u, &s_dead))) break;
+            if (elect_one()) {
+                mbar_expect_tx(&y_full[ys], static_cast<uint32_t>(kYTile));
+                tile_load(s_y + ys * kYTile, &mapY, col * (YT == CQ_F32 ? 4 : 2), t0, &y_full[ys]);
+                tile_load(s_y + ys * kYTile + kXTile, &mapY, col * (YT == CQ_F32 ? 4 : 2) + 128, t0, &y_full[ys]);
+            }
+            y_issued = min(y_issued + 1, SY);
+            if (++ys == SY) { ys = 0; y_round ^= 1u; }
+            if (tl != tile) {
+                tile = tl;
+                info = p.info + tl * kTileInfo;
+                count = __ldcg(info);
+                if (count > 0) {
+                    if (!(ok = agreed_wait(h_empty, h_round ^ 1u, &s_dead))) break;
+                    if (elect_one()) {
+                        mbar_expect_tx(h_full, static_cast<uint32_t>(2 * HB * kXTile));
+#pragma unroll
+                        for (int h = 0; h < HB; ++h) {
+                            tile_load(s_h + h * kXTile, &mapHigh, h * 128, t0, h_full);
+                            tile_load(s_h + (HB + h) * kXTile, &mapLow, h * 128, t0, h_full);
+                        }
+                    }
+                    h_open = true;
+                    h_round ^= 1u;
+                }
+            }
+            for (int d = 0; ok && d < count; ++d) {
+                const int row = __ldcg(info + 1 + d) * static_cast<int>(p.N) + col;
+                if (!(ok = agreed_wait(&b_empty[bs], b_round ^ 1u, &s_dead))) break;
+                if (elect_one()) {
+                    mbar_expect_tx(&b_full[bs], static_cast<uint32_t>(kB));
+#pragma unroll
+                    for (int h = 0; h < HB; ++h) tile_load(s_b + bs * kB + h * (CT * 128), &mapB, h * 128, row, &b_full[bs]);
+                }
+                b_issued = min(b_issued + 1, SB);
+                if (++bs == SB) { bs = 0; b_round ^= 1u; }
+            }
+        }
+        if (!ok) {                            // copies still in flight land before the CTA leaves
+            for (; y_issued > 0; --y_issued) {
+                if (--ys < 0) { ys = SY - 1; y_round ^= 1u; }
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&y_full[ys], y_round); ++polls) {}
+            }
+            for (; b_issued > 0; --b_issued) {
+                if (--bs < 0) { bs = SB - 1; b_round ^= 1u; }
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&b_full[bs], b_round); ++polls) {}
+            }
+            if (h_open)
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(h_full, h_round ^ 1u); ++polls) {}
+        }
+    } else if (warp == 1) {
+        const uint32_t idesc = idesc_f16<DT>(128, CT, false);
+        const uint64_t desc_h = smem_desc_k128(s_h), desc_b = smem_desc_k128(s_b);
+        const int steps = (p.R + 15) / 16;
+        int bs = 0, db = 0, count = 0;
+        uint32_t b_round = 0, d_round = 0, h_round = 0;
+        int64_t tile = -1;
+        bool ok = true;
+        for (int64_t it = work.first; ok && it < work.end; ++it) {
+            const int64_t tl = it / work.cols;
+            if (tl != tile) {
+                tile = tl;
+                count = __ldcg(p.info + tl * kTileInfo);
+                if (count > 0) {
+                    if (!(ok = agreed_wait(h_full, h_round, &s_dead))) break;
+                    h_round ^= 1u;
+                }
+            }
+            const bool last = it + 1 == work.end || (it + 1) / work.cols != tl;
+            for (int d = 0; ok && d < count; ++d) {
+                if (!(ok = agreed_wait(&b_full[bs], b_round, &s_dead) && agreed_wait(&d_empty[db], d_round ^ 1u, &s_dead))) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    for (int part = 0; part < 2; ++part)
+                        for (int k = 0; k < steps; ++k)
+                            tc_mma_f16(tmem + db * CT, desc_h + (((part * HB + (k >> 2)) * kXTile + (k & 3) * 32) >> 4),
+                                       desc_b + ((bs * kB + (k >> 2) * (CT * 128) + (k & 3) * 32) >> 4), idesc, part > 0 || k > 0);
+                    tc_commit(&b_empty[bs]);
+                    tc_commit(&d_full[db]);
+                    if (last && d + 1 == count) tc_commit(h_empty);
+                }
+                if (++bs == SB) { bs = 0; b_round ^= 1u; }
+                if (++db == kOutBuffers) { db = 0; d_round ^= 1u; }
+            }
+        }
+        if (!ok) {                            // products in flight end before the CTA leaves
+            __syncwarp();
+            if (elect_one()) tc_commit(drain);
+            for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(drain, 0); ++polls) {}
+        }
+    } else if (warp == 2) {
+        int ys = 0;
+        uint32_t y_round = 0;
+        bool ok = true;
+        for (int64_t it = work.first; it < work.end; ++it) {
+            const int64_t tl = it / work.cols;
+            const int col = static_cast<int>(it - tl * work.cols) * CT;
+            if (!(ok = agreed_wait(&o_full[ys], y_round, &s_dead))) break;
+            if (elect_one()) {
+                const int32_t x = col * (YT == CQ_F32 ? 4 : 2), t0 = static_cast<int32_t>(tl) * kTileTokens;
+                tile_store(&mapOut, s_y + ys * kYTile, x, t0);
+                if (col + CT / 2 < p.N) tile_store(&mapOut, s_y + ys * kYTile + kXTile, x + 128, t0);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                if (it > work.first) mbar_arrive(&y_empty[ys > 0 ? ys - 1 : SY - 1]);   // the buffer of the item before has been read
+            }
+            if (++ys == SY) { ys = 0; y_round ^= 1u; }
+        }
+        __syncwarp();
+        if (elect_one()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    } else if (warp >= 4) {
+        constexpr int kCols = CT / 2;                           // of each warp
+        const int half = (warp - 4) >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * kCols;
+        int ys = 0, db = 0, count = 0, mine = -1;
+        uint32_t y_round = 0, d_round = 0;
+        float f = 0.0f;
+        int64_t tile = -1;
+        bool ok = true;
+        for (int64_t it = work.first; ok && it < work.end; ++it) {
+            const int64_t tl = it / work.cols;
+            if (tl != tile) {
+                tile = tl;
+                count = __ldcg(p.info + tl * kTileInfo);
+                const int64_t t = tl * kTileTokens + row;
+                mine = t < p.T ? __ldcg(p.slot + t) : -1;
+                f = mine >= 0 ? __ldcg(p.factor + t) : 0.0f;
+            }
+            if (!(ok = agreed_wait(&y_full[ys], y_round, &s_dead))) break;
+            uint8_t* y = s_y + ys * kYTile + half * kXTile + row * 128;
+            for (int d = 0; d < count; ++d) {
+                if (!(ok = agreed_wait(&d_full[db], d_round, &s_dead))) break;
+                tc_fence_after();
+                if (__any_sync(0xFFFFFFFFu, mine == d)) {
+                    float v[kCols / 32][32];
+#pragma unroll
+                    for (int q = 0; q < kCols / 32; ++q) tmem_ld32(at + db * CT + q * 32, v[q]);
+#pragma unroll
+                    for (int q = 0; q < kCols / 32; ++q) tmem_ld_wait(v[q]);
+                    if (mine == d) {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            uint4* piece = reinterpret_cast<uint4*>(y + ((c ^ (row & 7)) << 4));
+                            const uint4 w = *piece;
+                            const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+                            uint32_t o[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if constexpr (YT == CQ_F32) {
+                                    o[i] = __float_as_uint(__fmaf_rn(v[0][4 * c + i], f, __uint_as_float(r[i])));
+                                } else {
+                                    const float2 b = unpack16x2<YT>(r[i]);
+                                    const int e = 8 * c + 2 * i;
+                                    o[i] = pack16x2<YT>(__fmaf_rn(v[e >> 5][e & 31], f, b.x), __fmaf_rn(v[e >> 5][(e & 31) + 1], f, b.y));
+                                }
+                            }
+                            *piece = make_uint4(o[0], o[1], o[2], o[3]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&d_empty[db]);
+                if (++db == kOutBuffers) { db = 0; d_round ^= 1u; }
+            }
+            if (!ok) break;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&o_full[ys]);
+            if (++ys == SY) { ys = 0; y_round ^= 1u; }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    __syncwarp();
+    if (warp == 1) tmem_free(tmem, kOutBuffers * CT);
+    if (tid == 0 && s_dead != 0u) atomicExch(&g_adapter_fault, 1u);
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------
+int adapter_stage_fault(unsigned int* fault_host) {
+    return cudaMemcpyFromSymbol(fault_host, g_adapter_fault, sizeof(unsigned int)) == cudaSuccess ? CQ_OK : CQ_ERR_CUDA;
+}
+
+bool adapter_tiles_fit(const AdapterArgs& p, int y_dtype) {
+    const int64_t elem = y_dtype == CQ_F32 ? 4 : 2, most = (int64_t(1) << 31) - 1024;
+    return p.T >= kTileTokens && p.K >= 64 && p.n >= 1 && p.vec_k == 8 && p.vec_n == 16 / elem && 2 * p.K < most && elem * p.N < most &&
+           static_cast<int64_t>(p.n) * p.R < most && p.n * p.N < most && p.ldx < (int64_t(1) << 38) && p.ldy < (int64_t(1) << 37) && p.ldo < (int64_t(1) << 37);
+}
+
+template <int HB, int DT, int YT>
+static int launch_out_tiles(const AdapterArgs& p, cudaStream_t st) {
+    constexpr int64_t elem = YT == CQ_F32 ? 4 : 2;
+    CUtensorMap high, low, b, y, out;
+    const auto sw = CU_TENSOR_MAP_SWIZZLE_128B;
+    if (!make_byte_map(&high, p.high, 2 * p.R, p.T, 2 * p.R, 128, kTileTokens, sw) || !make_byte_map(&low, p.low, 2 * p.R, p.T, 2 * p.R, 128, kTileTokens, sw) ||
+        !make_byte_map(&b, p.B, 2 * p.R, p.n * p.N, 2 * p.R, 128, out_cols<YT>(), sw) ||
+        !make_byte_map(&y, p.y, elem * p.N, p.T, elem * p.ldy, 128, kTileTokens, sw) ||
+        !make_byte_map(&out, p.out, elem * p.N, p.T, elem * p.ldo, 128, kTileTokens, sw)) return CQ_ERR_CUDA;
+    static thread_local LaunchMemo memo;
+    constexpr size_t smem = out_smem<HB, YT>();
+    if (resident_ctas(k28_adapter_out_tiles<HB, DT, YT>, kOutThreads, smem, smem, memo) < 1) return CQ_ERR_CUDA;
+    const int64_t items = (p.T + kTileTokens - 1) / kTileTokens * ((p.N + out_cols<YT>() - 1) / out_cols<YT>());
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(items, sm_count()));
+    return launch_ex(k28_adapter_out_tiles<HB, DT, YT>, dim3(grid), kOutThreads, smem, st, 1, !tuning_no_pdl(), high, low, b, y, out, p);
+}
+
+template <int DT>
+static int launch_tiles(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
+    CUtensorMap x, a;
+    if (!make_byte_map(&x, p.x, 2 * p.K, p.T, 2 * p.ldx, 128, kTileTokens, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_byte_map(&a, p.A, 2 * p.K, static_cast<uint64_t>(p.n) * p.R, 2 * p.K, 128, p.R, CU_TENSOR_MAP_SWIZZLE_128B)) return CQ_ERR_CUDA;
+    static thread_local LaunchMemo memo;
+    const size_t smem = in_smem(p.R);
+    if (resident_ctas(k27_adapter_in_tiles<DT>, kInThreads, smem, std::max(in_smem(64), in_smem(kMaxRank)), memo) < 1) return CQ_ERR_CUDA;
+    // as many parts of the contraction, four blocks of 64 each or more, as leave one block an SM
+    const int64_t tiles = (p.T + kTileTokens - 1) / kTileTokens;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, (p.K + 63) / 64 / 4), sm_count() / tiles));
+    int rc = launch_ex(k27_adapter_in_tiles<DT>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(tiles)), kInThreads, smem, st,
+                       static_cast<unsigned>(parts), !tuning_no_pdl(), x, a, p, in_stages(p.R));
+    if (rc != CQ_OK) return rc;
+    if (p.R <= 64) {
+        if (y_dtype == CQ_F32) return launch_out_tiles<1, DT, CQ_F32>(p, st);
+        return y_dtype == CQ_F16 ? launch_out_tiles<1, DT, CQ_F16>(p, st) : launch_out_tiles<1, DT, CQ_BF16>(p, st);
+    }
+    if (y_dtype == CQ_F32) return launch_out_tiles<2, DT, CQ_F32>(p, st);
+    return y_dtype == CQ_F16 ? launch_out_tiles<2, DT, CQ_F16>(p, st) : launch_out_tiles<2, DT, CQ_BF16>(p, st);
+}
+
+int launch_adapter_tiles(const AdapterArgs& p, int dtype, int y_dtype, cudaStream_t st) {
+    return dtype == CQ_F16 ? launch_tiles<CQ_F16>(p, y_dtype, st) : launch_tiles<CQ_BF16>(p, y_dtype, st);
+}
+
+}  // namespace cq

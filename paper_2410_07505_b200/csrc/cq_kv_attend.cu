@@ -36,6 +36,7 @@
 // 0 times an infinite va is none).  One unit for all rows of a warp, above the largest va, took 2 to 7 % less time (4 x 100003 INT4,
 // 16 rows a head: 114 against 118 us), but lost rows beside a large value that they do not see or give no weight: with 1e30 behind
 // it, a value of 100 read as 0.  Less room above the reference (2^5) makes rows ask more often: 124 us.
+#include "cq_adapter.cuh"
 #include "cq_kv.cuh"
 
 namespace cq {
@@ -933,11 +934,12 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
 
 int cq_serve_fault(unsigned int* fault_host) {
     if (fault_host == nullptr) return CQ_ERR_NULL;
-    unsigned int product = 0, attention = 0, prompt = 0;
+    unsigned int product = 0, attention = 0, prompt = 0, adapter = 0;
     int rc = cq::fp8_stage_fault(&product);
     if (rc == CQ_OK) rc = cq::attn_stage_fault(&attention);
     if (rc == CQ_OK) rc = cq::prompt_stage_fault(&prompt);
-    if (rc == CQ_OK) *fault_host = product | attention | prompt;
+    if (rc == CQ_OK) rc = cq::adapter_stage_fault(&adapter);
+    if (rc == CQ_OK) *fault_host = product | attention | prompt | adapter;
     return rc;
 }
 

@@ -55,22 +55,6 @@ __device__ __forceinline__ void tile_load3(void* dst_smem, const CUtensorMap* ma
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  :: "r"(smem_u32(dst_smem)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
 }
-// D[tmem] (+)= A B, 16-bit operands, fp32 accumulation; A in shared memory or (_ts) in tensor memory
-__device__ __forceinline__ void tc_mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u) : "memory");
-}
-__device__ __forceinline__ void tc_mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u) : "memory");
-}
-// fp32 accumulator, 16-bit operands of one type; `rows_b`: B lies row by row along N (rows of the contraction)
-template <int DT> __host__ __device__ constexpr uint32_t idesc_f16(uint32_t m, uint32_t n, bool rows_b) {
-    constexpr uint32_t type = DT == CQ_BF16 ? 1u : 0u;
-    return (1u << 4) | (type << 7) | (type << 10) | (rows_b ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
-}
 // [128 rows along the contraction][64 elements along N] per 16 KB, 128-byte swizzle: 64 elements further along N lie 16 KB
 // further, eight rows of the contraction 1024 bytes further.
 __device__ __forceinline__ uint64_t smem_desc_n128(const void* tile) {

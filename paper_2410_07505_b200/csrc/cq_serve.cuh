@@ -113,6 +113,17 @@ __device__ __forceinline__ void tc_mma_fp8(uint32_t d, uint64_t a, uint64_t b, u
                  :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u) : "memory");
 }
 
+// D[tmem] (+)= A B, 16-bit operands, fp32 accumulation; A in shared memory or (_ts) in tensor memory
+__device__ __forceinline__ void tc_mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u) : "memory");
+}
+__device__ __forceinline__ void tc_mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u) : "memory");
+}
 // Operand tile of rows of 128 bytes along the contraction, 128-byte swizzle, eight rows (1024 bytes) per group.
 __device__ __forceinline__ uint64_t smem_desc_k128(const void* tile) {
     const uint64_t addr = smem_u32(tile);
@@ -120,6 +131,12 @@ __device__ __forceinline__ uint64_t smem_desc_k128(const void* tile) {
 }
 // Instruction descriptor: fp32 accumulator, e4m3 x e4m3, both operands contiguous along the contraction.
 __host__ __device__ constexpr uint32_t idesc_fp8(uint32_t m, uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((m >> 4) << 24); }
+
+// fp32 accumulator, 16-bit operands of one type; `rows_b`: B lies row by row along N (rows of the contraction)
+template <int DT> __host__ __device__ constexpr uint32_t idesc_f16(uint32_t m, uint32_t n, bool rows_b) {
+    constexpr uint32_t type = DT == CQ_BF16 ? 1u : 0u;
+    return (1u << 4) | (type << 7) | (type << 10) | (rows_b ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
 
 // 32 columns of this warp's 32 lanes
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {

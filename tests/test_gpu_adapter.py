@@ -70,7 +70,7 @@ def some_index(T, n, seed, kind):
 @pytest.mark.parametrize("dtype", ("bf16", "f16"))
 @pytest.mark.parametrize("R", (8, 16, 24, 32, 40, 64, 96, 128))
 def test_ranks(cq, dtype, R):  # noqa: F811
-    for T, K, N in ((1, 512, 264), (70, 1032, 300)):
+    for T, K, N in ((1, 512, 264), (70, 1032, 300), (200, 1032, 296)):
         y, x = tokens(T, K, N, dtype, R)
         check(cq, y, x, adapters(cq, 5, K, N, R, dtype, R + 1), some_index(T, 5, R, "mixed"))
 
@@ -90,24 +90,36 @@ def test_odd_widths(cq, K, N):  # noqa: F811
         check(cq, y, x, adapters(cq, 3, K, N, 16, dtype, K), some_index(T, 3, T, "mixed"))
 
 
+@pytest.mark.parametrize("T,K,N,n", ((128, 64, 8, 3), (129, 72, 1000, 200), (257, 136, 128, 1), (640, 520, 2056, 130), (511, 2048, 520, 4), (1500, 72, 264, 60)))
+@pytest.mark.parametrize("R", (8, 24, 64, 128))
+def test_many_tokens(cq, T, K, N, n, R):  # noqa: F811
+    """Tiles of 128 tokens with one adapter, a few, or one for each token."""
+    y, x = tokens(T, K, N, "bf16", T + R)
+    ad = adapters(cq, n, K, N, R, "bf16", n)
+    check(cq, y, x, ad, some_index(T, n, R, "mixed"))
+    check(cq, y.float(), x, ad, some_index(T, n, R, "runs"))
+
+
 def test_long_contractions_and_wide_results(cq):  # noqa: F811
-    for T, K, N, R in ((3, 8192, 6000, 16), (90, 8200, 2048, 64)):
+    for T, K, N, R in ((3, 8192, 6000, 16), (90, 8200, 2048, 64), (150, 8192, 2048, 128)):
         y, x = tokens(T, K, N, "bf16", T)
         check(cq, y, x, adapters(cq, 4, K, N, R, "bf16", T), some_index(T, 4, T, "runs"))
 
 
-def test_results_of_other_types_strides_and_in_place(cq):  # noqa: F811
-    T, K, N = 40, 520, 264
+@pytest.mark.parametrize("T", (40, 300))
+def test_results_of_other_types_strides_and_in_place(cq, T):  # noqa: F811
+    K, N = 520, 264
     ad, index = adapters(cq, 3, K, N, 16, "f16", 1), some_index(T, 3, 2, "mixed")
     for y_dtype in (torch.float32, torch.bfloat16, torch.float16):
-        for ld, skew in ((N, 0), (N + 3, 0), (N, 2 if y_dtype != torch.float32 else 4)):
+        for ld, skew in ((N, 0), (N + 8, 0), (N + 3, 0), (N, 2 if y_dtype != torch.float32 else 4)):
             y, x = tokens(T, K, N, "f16", 3, y_dtype)
             ar = Arena()
             ar.add("y", T * ld, y_dtype, skew=skew)
-            ar.add("x", T * (K + 5), torch.float16, skew=skew & 2)
+            pitch = K + (8 if ld % 8 == 0 else 5)
+            ar.add("x", T * pitch, torch.float16, skew=skew & 2)
             ar.build()
             ar["y"].fill_(9)
-            y2, x2 = ar["y"].view(T, ld)[:, :N], ar["x"].view(T, K + 5)[:, :K]
+            y2, x2 = ar["y"].view(T, ld)[:, :N], ar["x"].view(T, pitch)[:, :K]
             y2.copy_(y)
             x2.copy_(x)
             want = check(cq, y2, x2, ad, index)
@@ -151,9 +163,10 @@ def test_a_token_depends_on_no_other(cq):  # noqa: F811
         assert torch.equal(got, want)
 
 
-def test_inner_values_beyond_the_types_range(cq):  # noqa: F811
+@pytest.mark.parametrize("T", (9, 140))
+def test_inner_values_beyond_the_types_range(cq, T):  # noqa: F811
     """fp16: |A x| above 65504 and below 2^-24 for whole tokens."""
-    T, K, N, R = 9, 512, 64, 16
+    K, N, R = 512, 64, 16
     y, x = tokens(T, K, N, "f16", 9)
     ad, index = adapters(cq, 2, K, N, R, "f16", 10), some_index(T, 2, 1, "turns")
     x = x * 0 + torch.randn(T, K, device="cuda").half()
@@ -166,8 +179,9 @@ def test_inner_values_beyond_the_types_range(cq):  # noqa: F811
     check(cq, y, (x.float() * 1e-4).half(), small, index)
 
 
-def test_equal_calls_give_equal_bits_on_streams_and_from_graphs(cq):  # noqa: F811
-    T, K, N = 100, 1024, 520
+@pytest.mark.parametrize("T", (100, 500))
+def test_equal_calls_give_equal_bits_on_streams_and_from_graphs(cq, T):  # noqa: F811
+    K, N = 1024, 520
     y, x = tokens(T, K, N, "bf16", 11)
     ad, index = adapters(cq, 6, K, N, 32, "bf16", 12), some_index(T, 6, 13, "mixed")
     want = cq.adapter_add(y, x, ad, index)
