@@ -90,15 +90,23 @@ __device__ __forceinline__ uint4 piece8(const uint16_t* row, int64_t k, int64_t 
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = k + 2 * i < end ? __ldcg(reinterpret_cast<const uint32_t*>(row + k) + i) : 0;
     } else {
+        // aligned words that hold an element of the piece, moved by half a word where the row begins in the middle of one
+        const uint16_t* at = row + k;
+        const bool odd = (reinterpret_cast<uintptr_t>(at) & 2u) != 0u;
+        const uint32_t* words = reinterpret_cast<const uint32_t*>(at - (odd ? 1 : 0));
+        const int n = static_cast<int>(min(max(end - k, int64_t(0)), int64_t(8)));                    // elements there are
+        uint32_t r[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) r[i] = n > 0 && 2 * i < n + (odd ? 1 : 0) ? __ldcg(words + i) : 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = k + 2 * i < end ? __ldcg(row + k + 2 * i) : 0, hi = k + 2 * i + 1 < end ? __ldcg(row + k + 2 * i + 1) : 0;
-            v[i] = lo | hi << 16;
+            v[i] = odd ? __funnelshift_r(r[i], r[i + 1], 16) : r[i];
+            if (2 * i + 1 >= n) v[i] = 2 * i >= n ? 0 : v[i] & 0xFFFFu;
         }
     }
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
-// the same into shared memory, asynchronously where the alignment allows
+// the same into shared memory, asynchronously; vec of 2 or more
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool have) {
     if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(have ? 16 : 0) : "memory");
@@ -111,11 +119,9 @@ __device__ __forceinline__ void stage8(uint8_t* dst, const uint16_t* row, int64_
     } else if (vec == 4) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) copy_async<8>(at + 8 * i, k + 4 * i < end ? row + k + 4 * i : row, k + 4 * i < end);
-    } else if (vec == 2) {
+    } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) copy_async<4>(at + 4 * i, k + 2 * i < end ? row + k + 2 * i : row, k + 2 * i < end);
-    } else {
-        *reinterpret_cast<uint4*>(dst) = piece8(row, k, end, 1);
     }
 }
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], const uint8_t* p) {
@@ -129,7 +135,8 @@ __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], const uint8_t* p
 // calls give equal bits.
 constexpr int kUnit = 64;                     // contraction of one stage
 template <int MT> __host__ __device__ constexpr int shrink_stages() { return MT <= 2 ? 6 : MT == 4 ? 5 : 3; }
-template <int MT> __host__ __device__ constexpr size_t shrink_stage() { return size_t(kWindow + MT * 16) * kUnit * 2; }
+constexpr int kRowBytes = 144;                // of a stage where rows of x and A begin anywhere; 128 where they do not
+template <int MT> __host__ __device__ constexpr size_t shrink_stage() { return size_t(kWindow + MT * 16) * kRowBytes; }
 template <int MT> __host__ __device__ constexpr size_t shrink_smem() { return shrink_stages<MT>() * shrink_stage<MT>() + size_t(kWindow) * (MT * 16 + 1) * 4; }
 
 template <int MT, int DT>                     // MT x 16 rows of A
@@ -142,11 +149,13 @@ k25_adapter_in(const AdapterArgs p) {
     float* s_h = reinterpret_cast<float*>(s_mem + ST * kStage); // [token][kRows + 1]
     static_assert(size_t(4) * kRows * 9 * 4 <= ST * kStage, "sums of warps");
     __shared__ uint8_t s_list[kAdThreads / 32][kWindow];
+    __shared__ TileSort s_sort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     uint8_t* list = s_list[warp];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");         // (only now: the next kernel reads B and y before this one ends)
     const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kWindow;
+    if (p.tiles && blockIdx.x == 0 && blockIdx.z == 0 && t0 % kTileTokens == 0) sort_tile(p, t0, s_sort, true);
     Window w;
     w.read(p, t0);
     const int rank = blockIdx.x, ranks = gridDim.x;
@@ -209,24 +218,50 @@ k25_adapter_in(const AdapterArgs p) {
                     for (int e = 0; e < 4; ++e) s_h[(2 * t4 + (e & 1)) * (kRows + 1) + i * 16 + g + (e >> 1) * 8] = acc[i][e];
             }
         } else {
-            // Rows of 128 bytes, 16-byte pieces swapped by the row so that eight rows of one piece lie in different banks.
+            // Rows of 128 bytes, 16-byte pieces swapped by the row so that eight rows of one piece lie in different banks; or, where rows
+            // begin in the middle of words, the 33 words that hold the row's 64 elements, at 144 bytes a row.
+            const bool loose = p.vec_k == 1;
+            auto stage_row = [&](uint8_t* base, int r, int c, const uint16_t* row, int64_t u) {
+                if (!loose) {
+                    stage8(base + r * 128 + ((c ^ (r & 7)) << 4), row, u * kUnit + c * 8, p.K, p.vec_k);
+                } else {
+                    const uint16_t* at = row + u * kUnit;
+                    const int odd = (reinterpret_cast<uintptr_t>(at) & 2u) != 0u ? 1 : 0;
+                    const int64_t left = p.K - u * kUnit + odd;         // elements from the first word on
+                    for (int i = c; i < 33; i += 8) {
+                        const int64_t bytes = min(max((left - 2 * i) * 2, int64_t(0)), int64_t(4));
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;"
+                                     :: "r"(smem_u32(base + r * kRowBytes + 4 * i)), "l"(bytes > 0 ? at - odd + 2 * i : at - odd), "r"(static_cast<int>(bytes)) : "memory");
+                    }
+                }
+            };
+            const size_t a_at = size_t(kWindow) * (loose ? kRowBytes : 128);
             auto stage = [&](int64_t u) {
                 uint8_t* sx = s_mem + (u - u0) % ST * kStage;
-                uint8_t* sa = sx + size_t(kWindow) * kUnit * 2;
+                uint8_t* sa = sx + a_at;
 #pragma unroll
                 for (int i = tid; i < kWindow * 8; i += kAdThreads) {
-                    const int r = i >> 3, c = i & 7;
-                    if (r < count) stage8(sx + r * 128 + ((c ^ (r & 7)) << 4), p.x + (t0 + list[r]) * p.ldx, u * kUnit + c * 8, p.K, p.vec_k);
+                    const int r = i >> 3;
+                    if (r < count) stage_row(sx, r, i & 7, p.x + (t0 + list[r]) * p.ldx, u);
                 }
 #pragma unroll
                 for (int i = tid; i < kRows * 8; i += kAdThreads) {
-                    const int r = i >> 3, c = i & 7;
-                    if (r < p.R) stage8(sa + r * 128 + ((c ^ (r & 7)) << 4), A + r * p.K, u * kUnit + c * 8, p.K, p.vec_k);
+                    const int r = i >> 3;
+                    if (r < p.R) stage_row(sa, r, i & 7, A + r * p.K, u);
                 }
             };
+            // which rows that this lane reads begin in the middle of a word (stages are of whole words)
+            auto shift_of = [&](const uint16_t* row) { return (reinterpret_cast<uintptr_t>(row) & 2u) != 0u ? 16u : 0u; };
             // warps: two halves of the tokens x four; those share out the rows of A (16 each, 32 of 128), or, with fewer, a stage's steps of 16
             constexpr int MI = MT == 8 ? 2 : 1, KS = MT >= 4 ? 1 : 4 / MT;
             const int half = warp >> 2, m = (warp & 3) % (MT < 4 ? MT : 4), ks = (warp & 3) / (MT < 4 ? MT : 4);
+            uint32_t shift_a[MI][2], shift_x[4];
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) shift_a[i][e] = shift_of(A + ((m + 4 * i) * 16 + g + e * 8) * p.K);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) shift_x[j] = half * 32 + j * 8 + g < count ? shift_of(p.x + (t0 + list[half * 32 + j * 8 + g]) * p.ldx) : 0u;
             float acc[MI][4][4] = {};
             for (int s = 0; s < ST - 1; ++s) {
                 if (u0 + s < u1) stage(u0 + s);
@@ -238,20 +273,38 @@ k25_adapter_in(const AdapterArgs p) {
                 if (u + ST - 1 < u1) stage(u + ST - 1);
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 if (half * 32 < count) {
-                    const uint8_t* sx = s_mem + (u - u0) % ST * kStage + half * 32 * 128;
-                    const uint8_t* sa = s_mem + (u - u0) % ST * kStage + size_t(kWindow) * kUnit * 2;
+                    const uint8_t* sx = s_mem + (u - u0) % ST * kStage + half * 32 * (loose ? kRowBytes : 128);
+                    const uint8_t* sa = s_mem + (u - u0) % ST * kStage + a_at;
 #pragma unroll
                     for (int kk = ks; kk < 4; kk += KS) {
                         uint32_t fa[MI][4], fb[2][4];
+                        if (!loose) {
 #pragma unroll
-                        for (int i = 0; i < MI; ++i) {
-                            const int r = (m + 4 * i) * 16 + (lane & 15);
-                            load_matrices(fa[i], sa + r * 128 + (((kk * 2 + (lane >> 4)) ^ (r & 7)) << 4));
-                        }
+                            for (int i = 0; i < MI; ++i) {
+                                const int r = (m + 4 * i) * 16 + (lane & 15);
+                                load_matrices(fa[i], sa + r * 128 + (((kk * 2 + (lane >> 4)) ^ (r & 7)) << 4));
+                            }
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const int r = j * 16 + (lane & 7) + ((lane >> 4) << 3);
-                            load_matrices(fb[j], sx + r * 128 + (((kk * 2 + ((lane >> 3) & 1)) ^ (r & 7)) << 4));
+                            for (int j = 0; j < 2; ++j) {
+                                const int r = j * 16 + (lane & 7) + ((lane >> 4) << 3);
+                                load_matrices(fb[j], sx + r * 128 + (((kk * 2 + ((lane >> 3) & 1)) ^ (r & 7)) << 4));
+                            }
+                        } else {
+                            auto pair = [&](const uint8_t* base, int r, int word, uint32_t shift) {
+                                const uint32_t* at = reinterpret_cast<const uint32_t*>(base + r * kRowBytes) + word;
+                                return __funnelshift_r(at[0], at[1], shift);
+                            };
+#pragma unroll
+                            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {           // rows g, g + 8; the first and second eight of the contraction
+                                    const int r = (m + 4 * i) * 16 + g + (e & 1) * 8;
+                                    fa[i][e] = pair(sa, r, kk * 8 + t4 + (e >> 1) * 4, shift_a[i][e & 1]);
+                                }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) fb[j >> 1][(j & 1) * 2 + e] = pair(sx, j * 8 + g, kk * 8 + t4 + e * 4, shift_x[j]);
                         }
 #pragma unroll
                         for (int i = 0; i < MI; ++i)
@@ -359,6 +412,41 @@ __device__ __forceinline__ void add_store(const AdapterArgs& p, int64_t t, int64
     }
 }
 
+// 32 columns from n0 on of up to 16 rows of y, plus d [16][36]: a word or an element of a row for each lane
+template <int YT>
+__device__ __forceinline__ void add_rows(const AdapterArgs& p, const float* d, const uint8_t* list, int count, int64_t t0, int64_t n0) {
+    const int lane = threadIdx.x & 31;
+    const uint16_t* y = static_cast<const uint16_t*>(p.y);
+    uint16_t* out = static_cast<uint16_t*>(p.out);
+    if (p.vec_n >= 2) {
+        const int64_t n = n0 + 2 * (lane & 15);
+        if (n >= p.N) return;
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int m = 2 * i + (lane >> 4);
+            if (m < count) w[i] = __ldcg(reinterpret_cast<const uint32_t*>(y + (t0 + list[m]) * p.ldy + n));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int m = 2 * i + (lane >> 4);
+            if (m >= count) continue;
+            const float2 v = unpack16x2<YT>(w[i]);
+            *reinterpret_cast<uint32_t*>(out + (t0 + list[m]) * p.ldo + n) = pack16x2<YT>(v.x + d[m * 36 + 2 * (lane & 15)], v.y + d[m * 36 + 2 * (lane & 15) + 1]);
+        }
+    } else {
+        const int64_t n = n0 + lane;
+        if (n >= p.N) return;
+        uint16_t w[16];
+#pragma unroll
+        for (int m = 0; m < 16; ++m)
+            if (m < count) w[m] = __ldcg(y + (t0 + list[m]) * p.ldy + n);
+#pragma unroll
+        for (int m = 0; m < 16; ++m)
+            if (m < count) out[(t0 + list[m]) * p.ldo + n] = pack16<YT>(cvt16<YT>(w[m]) + d[m * 36 + lane]);
+    }
+}
+
 // words between rows of h in shared memory: 8 more than a multiple of 32, so that the rows of a fragment lie in different banks
 template <int MT> __host__ __device__ constexpr int h_pitch() { return MT * 8 + (MT == 1 ? 0 : MT == 2 ? 24 : 8); }
 
@@ -369,6 +457,7 @@ k26_adapter_out(const AdapterArgs p) {
     constexpr int kHeld = MT == 8 ? 32 : kWindow;               // tokens whose h is in shared memory at a time
     __shared__ uint8_t s_list[kAdThreads / 32][kWindow];
     __shared__ __align__(16) uint32_t s_h[2][kHeld][kPitch];
+    __shared__ float s_d[YT == CQ_F32 ? 1 : kAdThreads / 32][16 * 36];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     uint8_t* list = s_list[warp];
     asm volatile("griddepcontrol.launch_dependents;");
@@ -385,7 +474,12 @@ k26_adapter_out(const AdapterArgs p) {
         write_list(tokens, list);
         const int count = __popcll(tokens);
         auto token = [&](int m) { return m < count ? t0 + list[m] : int64_t(-1); };
-        Piece<YT> ya = load_piece<YT>(p, token(g), col), yb = load_piece<YT>(p, token(8 + g), col);
+        const bool direct = YT == CQ_F32 || p.vec_n == 8;
+        Piece<YT> ya = {}, yb = {};
+        if (direct) {
+            ya = load_piece<YT>(p, token(g), col);
+            yb = load_piece<YT>(p, token(8 + g), col);
+        }
         // product j takes columns n0 + 8 (q / 2) + 2 j + q % 2, q = 0 .. 7
         uint2 b[4][MT];
 #pragma unroll
@@ -418,7 +512,11 @@ k26_adapter_out(const AdapterArgs p) {
             for (int m0 = 0; m0 < held; m0 += 16) {
                 const int64_t ta = token(base + m0 + g), tb = token(base + m0 + 8 + g);
                 const float fa = ta >= 0 ? __ldcg(p.factor + ta) : 0.0f, fb = tb >= 0 ? __ldcg(p.factor + tb) : 0.0f;
-                const Piece<YT> na = load_piece<YT>(p, token(base + m0 + 16 + g), col), nb = load_piece<YT>(p, token(base + m0 + 24 + g), col);
+                Piece<YT> na = {}, nb = {};
+                if (direct) {
+                    na = load_piece<YT>(p, token(base + m0 + 16 + g), col);
+                    nb = load_piece<YT>(p, token(base + m0 + 24 + g), col);
+                }
                 float acc[4][4] = {};
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
@@ -439,10 +537,25 @@ k26_adapter_out(const AdapterArgs p) {
                         for (int j = 0; j < 4; ++j) mma16<DT>(acc[j], ha.x, hb.x, ha.y, hb.y, b[j][i].x, b[j][i].y);
                     }
                 }
-                const float da[8] = {acc[0][0], acc[0][1], acc[1][0], acc[1][1], acc[2][0], acc[2][1], acc[3][0], acc[3][1]};
-                const float db[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
-                add_store<YT>(p, ta, col, ya, da, fa);
-                add_store<YT>(p, tb, col, yb, db, fb);
+                if (direct) {
+                    const float da[8] = {acc[0][0], acc[0][1], acc[1][0], acc[1][1], acc[2][0], acc[2][1], acc[3][0], acc[3][1]};
+                    const float db[8] = {acc[0][2], acc[0][3], acc[1][2], acc[1][3], acc[2][2], acc[2][3], acc[3][2], acc[3][3]};
+                    add_store<YT>(p, ta, col, ya, da, fa);
+                    add_store<YT>(p, tb, col, yb, db, fb);
+                } else {
+                    // rows that begin anywhere: the products go through shared memory, so that a warp's accesses to a row lie side by side
+                    float* d = s_d[warp];
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            d[g * 36 + 8 * t4 + 2 * j + e] = acc[j][e] * fa;
+                            d[(8 + g) * 36 + 8 * t4 + 2 * j + e] = acc[j][2 + e] * fb;
+                        }
+                    __syncwarp();
+                    if constexpr (YT != CQ_F32) add_rows<YT>(p, d, list + base + m0, min(16, held - m0), t0, n0);
+                }
                 ya = na;
                 yb = nb;
             }
@@ -471,6 +584,7 @@ static size_t adapter_workspace(int64_t T, int64_t R) {
 template <int MT, int DT>
 static int launch_adapter(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     const int sms = sm_count();
+    const bool in_tiles = adapter_in_tiles(p);
     const int64_t windows = (p.T + kWindow - 1) / kWindow;
     const int64_t adapters = std::min<int64_t>(kWindow, std::min<int64_t>(p.n, p.T));
     if (windows > 65535) return CQ_ERR_SHAPE;
@@ -484,11 +598,14 @@ static int launch_adapter(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     static_assert(smem > 48 * 1024, "leave is asked for");
     if (resident_ctas(k25_adapter_in<MT, DT>, kAdThreads, smem, smem, memo) < 1) return CQ_ERR_CUDA;
     const dim3 grid(static_cast<unsigned>(parts), static_cast<unsigned>(windows), static_cast<unsigned>(slots));
-    const int rc = launch_ex(k25_adapter_in<MT, DT>, grid, kAdThreads, smem, st, grid.x, !tuning_no_pdl(), p);
+    int rc = CQ_OK;
+    if (in_tiles) rc = launch_adapter_in_tiles(p, DT, st);
+    else rc = launch_ex(k25_adapter_in<MT, DT>, grid, kAdThreads, smem, st, grid.x, !tuning_no_pdl(), p);
     if (rc != CQ_OK) return rc;
+    if (p.tiles) return launch_adapter_out_tiles(p, DT, y_dtype, st);
     // two, four or eight warps to a block: the most with which there are two blocks an SM
     int warps = 8;
-    while (warps > 2 && windows * ((p.N + 32 * warps - 1) / (32 * warps)) < 2 * sms) warps /= 2;
+    while (warps > 2 && windows * adapters * ((p.N + 32 * warps - 1) / (32 * warps)) < 2 * sms) warps /= 2;
     const int64_t cols = (p.N + 32 * warps - 1) / (32 * warps);
     const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(adapters, 16 * sms / (windows * cols)));
     const dim3 grid2(static_cast<unsigned>(cols), static_cast<unsigned>(windows), static_cast<unsigned>(turns));
@@ -543,7 +660,7 @@ int cq_adapter_add(const void* X, int dtype, int64_t T, int64_t K, int64_t ldx, 
     for (p.vec_n = static_cast<int>(16 / elem); p.vec_n > 1; p.vec_n /= 2)
         if (N % p.vec_n == 0 && (T == 1 || (ldy % p.vec_n == 0 && ldo % p.vec_n == 0)) && ptr_aligned(y, elem * p.vec_n) && ptr_aligned(out, elem * p.vec_n)) break;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (adapter_tiles_fit(p, y_dtype)) return launch_adapter_tiles(p, dtype, y_dtype, st);
+    p.tiles = adapter_out_tiles(p, y_dtype);
     return dtype == CQ_F16 ? launch_adapter_rank<CQ_F16>(p, y_dtype, st) : launch_adapter_rank<CQ_BF16>(p, y_dtype, st);
 }
 

@@ -20,11 +20,14 @@ struct AdapterArgs {
     int64_t T, K, N;
     int R, n;
     int vec_k, vec_n;                                           // elements of one access to rows of x and A (of y and out)
+    bool tiles;                                                 // the second kernel wants `slot` and `info`
 };
 
-// Many tokens on the 5th-generation tensor cores (cq_adapter_tiles.cu).
-bool adapter_tiles_fit(const AdapterArgs& p, int y_dtype);
-int launch_adapter_tiles(const AdapterArgs& p, int dtype, int y_dtype, cudaStream_t st);
+// Many tokens on the 5th-generation tensor cores (cq_adapter_tiles.cu): whether either kernel takes them, and its launch.
+bool adapter_in_tiles(const AdapterArgs& p);
+bool adapter_out_tiles(const AdapterArgs& p, int y_dtype);
+int launch_adapter_in_tiles(const AdapterArgs& p, int dtype, cudaStream_t st);
+int launch_adapter_out_tiles(const AdapterArgs& p, int dtype, int y_dtype, cudaStream_t st);
 int adapter_stage_fault(unsigned int* fault_host);
 
 __device__ __forceinline__ float ld_rank(const float* p, uint32_t rank) {
@@ -37,6 +40,56 @@ __device__ __forceinline__ float ld_rank(const float* p, uint32_t rank) {
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// The adapters of a tile in order of their first tokens, by a block of 128 threads or more; returns how many.
+struct __align__(16) TileSort {
+    int idx[kTileTokens];                     // of each token (-1: none)
+    int first[kTileTokens], rank[kTileTokens], slot[kTileTokens], adapter[kTileTokens], leads[4];
+};
+__device__ __forceinline__ int sort_tile(const AdapterArgs& p, int64_t t0, TileSort& s, bool write) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid < kTileTokens) {
+        const int a = t0 + tid < p.T ? __ldcg(p.index + t0 + tid) : -1;
+        s.idx[tid] = a >= 0 && a < p.n ? a : -1;
+    }
+    __syncthreads();
+    if (tid < kTileTokens) {
+        const int a = s.idx[tid];
+        int first = (warp << 5) + __ffs(__match_any_sync(0xFFFFFFFFu, a)) - 1;
+        for (int j = warp * 8 - 1; j >= 0; --j) {               // four tokens of the warps before
+            const int4 v = reinterpret_cast<const int4*>(s.idx)[j];
+            first = v.w == a ? 4 * j + 3 : first;
+            first = v.z == a ? 4 * j + 2 : first;
+            first = v.y == a ? 4 * j + 1 : first;
+            first = v.x == a ? 4 * j : first;
+        }
+        s.first[tid] = first;
+        const unsigned lead = __ballot_sync(0xFFFFFFFFu, a >= 0 && first == tid);
+        s.rank[tid] = __popc(lead & ((1u << lane) - 1u));
+        if (lane == 0) s.leads[warp] = __popc(lead);
+    }
+    __syncthreads();
+    const int count = s.leads[0] + s.leads[1] + s.leads[2] + s.leads[3];
+    if (tid < kTileTokens && s.idx[tid] >= 0 && s.first[tid] == tid) {
+        int rank = s.rank[tid];
+        for (int w = 0; w < warp; ++w) rank += s.leads[w];
+        s.rank[tid] = rank;
+        s.adapter[rank] = s.idx[tid];
+    }
+    __syncthreads();
+    if (tid < kTileTokens) {
+        const int slot = s.idx[tid] >= 0 ? s.rank[s.first[tid]] : -1;
+        s.slot[tid] = slot;
+        if (write) {
+            int* info = p.info + t0 / kTileTokens * kTileInfo;
+            if (tid == 0) info[0] = count;
+            if (tid < count) info[1 + tid] = s.adapter[tid];
+            if (t0 + tid < p.T) p.slot[t0 + tid] = slot;
+        }
+    }
+    __syncthreads();
+    return count;
 }
 
 // h[r] = the sum of `ranks` blocks' s_h[r], in rank order, as two 16-bit halves and a factor; a warp for each token.

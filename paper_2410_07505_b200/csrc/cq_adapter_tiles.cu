@@ -45,8 +45,7 @@ __global__ void __launch_bounds__(kInThreads, 1)
 k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapA, const AdapterArgs p, int stages) {
     extern __shared__ __align__(1024) uint8_t smem[];           // (behind the static part: moved to a 1024-byte boundary below)
     __shared__ uint64_t full[kInMaxStages], empty[kInMaxStages], d_full[2], d_empty[2], drain;
-    __shared__ __align__(16) int s_idx[kTileTokens];
-    __shared__ int s_first[kTileTokens], s_rank[kTileTokens], s_adapter[kTileTokens], s_leads[4];
+    __shared__ TileSort s_sort;
     __shared__ uint32_t s_tmem;
     __shared__ volatile uint32_t s_dead;
     uint8_t* s_x = smem + ((1024u - (smem_u32(smem) & 1023u)) & 1023u);
@@ -67,49 +66,15 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kTileTokens;
-    // the tile's adapters in order of their first tokens
-    if (tid < kTileTokens) {
-        const int a = t0 + tid < p.T ? __ldcg(p.index + t0 + tid) : -1;
-        s_idx[tid] = a < p.n ? a : -1;
-    }
+    const int count = sort_tile(p, t0, s_sort, blockIdx.x == 0);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (tid < kTileTokens) {
-        const int a = s_idx[tid];
-        int first = (warp << 5) + __ffs(__match_any_sync(0xFFFFFFFFu, a)) - 1;
-        for (int j = warp * 8 - 1; j >= 0; --j) {               // four tokens of the warps before
-            const int4 v = reinterpret_cast<const int4*>(s_idx)[j];
-            first = v.w == a ? 4 * j + 3 : first;
-            first = v.z == a ? 4 * j + 2 : first;
-            first = v.y == a ? 4 * j + 1 : first;
-            first = v.x == a ? 4 * j : first;
-        }
-        s_first[tid] = first;
-        const unsigned lead = __ballot_sync(0xFFFFFFFFu, a >= 0 && first == tid);
-        s_rank[tid] = __popc(lead & ((1u << lane) - 1u));
-        if (lane == 0) s_leads[warp] = __popc(lead);
-    }
-    __syncthreads();
-    const int count = s_leads[0] + s_leads[1] + s_leads[2] + s_leads[3];
-    if (tid < kTileTokens && s_idx[tid] >= 0 && s_first[tid] == tid) {
-        int rank = s_rank[tid];
-        for (int w = 0; w < warp; ++w) rank += s_leads[w];
-        s_rank[tid] = rank;
-        s_adapter[rank] = s_idx[tid];
-    }
-    __syncthreads();
     const uint32_t tmem = s_tmem;
     const int rank = blockIdx.x, ranks = gridDim.x;
     const int kblocks = static_cast<int>((p.K + 63) / 64), kb0 = static_cast<int>(static_cast<int64_t>(kblocks) * rank / ranks),
               kb1 = static_cast<int>(static_cast<int64_t>(kblocks) * (rank + 1) / ranks);
     const int per = kInCols / p.R, groups = (count + per - 1) / per;
-    if (rank == 0 && tid < kTileTokens) {
-        if (tid == 0) p.info[blockIdx.y * static_cast<int64_t>(kTileInfo)] = count;
-        if (tid < count) p.info[blockIdx.y * static_cast<int64_t>(kTileInfo) + 1 + tid] = s_adapter[tid];
-        if (t0 + tid < p.T) p.slot[t0 + tid] = s_idx[tid] >= 0 ? s_rank[s_first[tid]] : -1;
-    }
-
     if (warp == 0) {
         int s = 0;
         uint32_t round = 0;
@@ -123,7 +88,7 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
                     mbar_expect_tx(&full[s], static_cast<uint32_t>(kXTile) + n * p.R * 128);
                     tile_load(s_x + s * kXTile, &mapX, kb * 128, static_cast<int32_t>(t0), &full[s]);
                     for (int i = 0; i < n; ++i)
-                        tile_load(s_a + s * kATile + i * p.R * 128, &mapA, kb * 128, s_adapter[gr * per + i] * p.R, &full[s]);
+                        tile_load(s_a + s * kATile + i * p.R * 128, &mapA, kb * 128, s_sort.adapter[gr * per + i] * p.R, &full[s]);
                 }
                 issued = min(issued + 1, stages);
                 if (++s == stages) { s = 0; round ^= 1u; }
@@ -163,7 +128,7 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
         }
     } else if (warp >= 4) {
         const int token = (warp & 3) * 32 + lane;
-        const int mine = s_idx[token] >= 0 ? s_rank[s_first[token]] : -1;
+        const int mine = s_sort.slot[token];
         const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         float* h = s_h + token * (p.R + 1);
         bool ok = true;
@@ -197,7 +162,7 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
     __syncwarp();
     if (ranks > 1) cluster_barrier();
     for (int m = rank + warp * ranks; m < kTileTokens; m += ranks * (kInThreads / 32))
-        if (s_idx[m] >= 0) finish_token<DT>(p, s_h + m * (p.R + 1), ranks, t0 + m, s_idx[m]);
+        if (s_sort.idx[m] >= 0) finish_token<DT>(p, s_h + m * (p.R + 1), ranks, t0 + m, s_sort.idx[m]);
     __syncwarp();
     if (ranks > 1) cluster_barrier();         // nobody leaves while its sums are being read
     if (tid == 0 && s_dead != 0u) atomicExch(&g_adapter_fault, 1u);
@@ -216,17 +181,19 @@ template <int HB, int YT> __host__ __device__ constexpr size_t out_smem() {
     return 2 * HB * kXTile + y_stages<HB>() * kYTile + b_stages<HB>() * b_tile<HB, YT>() + 512;
 }
 
-struct OutItem { int64_t first, end; int cols; };               // items of this CTA; columns of tiles, the fastest of an item's two places
-__device__ __forceinline__ OutItem out_items(const AdapterArgs& p, int width) {
+// Items of this CTA: first, first + step .. below end.  The columns of tiles are the faster of an item's two places.
+struct OutItem { int64_t first, end; int step, cols; };
+__device__ __forceinline__ OutItem out_items(const AdapterArgs& p, int width, int group) {
     const int cols = static_cast<int>((p.N + width - 1) / width);
     const int64_t items = (p.T + kTileTokens - 1) / kTileTokens * cols;
-    return {items * blockIdx.x / gridDim.x, items * (blockIdx.x + 1) / gridDim.x, cols};
+    const int at = blockIdx.x / group, groups = gridDim.x / group;
+    return {items * at / groups + blockIdx.x % group, items * (at + 1) / groups, group, cols};
 }
 
 template <int HB, int DT, int YT>
 __global__ void __launch_bounds__(kOutThreads, 1)
 k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_constant__ CUtensorMap mapLow, const __grid_constant__ CUtensorMap mapB,
-                      const __grid_constant__ CUtensorMap mapY, const __grid_constant__ CUtensorMap mapOut, const AdapterArgs p) {
+                      const __grid_constant__ CUtensorMap mapY, const __grid_constant__ CUtensorMap mapOut, const AdapterArgs p, int group) {
     constexpr int SY = y_stages<HB>(), SB = b_stages<HB>(), CT = out_cols<YT>();
     constexpr size_t kB = b_tile<HB, YT>();
     // No static shared memory, so that the dynamic part starts on the 1024-byte boundary that the swizzle wants.
@@ -272,7 +239,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const OutItem work = out_items(p, CT);
+    const OutItem work = out_items(p, CT, group);
 
     if (warp == 0) {
         int ys = 0, bs = 0, y_issued = 0, b_issued = 0, count = 0;
@@ -280,7 +247,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
         int64_t tile = -1;
         bool ok = true, h_open = false;
         const int* info = p.info;
-        for (int64_t it = work.first; ok && it < work.end; ++it) {
+        for (int64_t it = work.first; ok && it < work.end; it += work.step) {
             const int64_t tl = it / work.cols;
             const int col = static_cast<int>(it - tl * work.cols) * CT;
             const int32_t t0 = static_cast<int32_t>(tl) * kTileTokens;
@@ -342,7 +309,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
         uint32_t b_round = 0, d_round = 0, h_round = 0;
         int64_t tile = -1;
         bool ok = true;
-        for (int64_t it = work.first; ok && it < work.end; ++it) {
+        for (int64_t it = work.first; ok && it < work.end; it += work.step) {
             const int64_t tl = it / work.cols;
             if (tl != tile) {
                 tile = tl;
@@ -352,7 +319,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
                     h_round ^= 1u;
                 }
             }
-            const bool last = it + 1 == work.end || (it + 1) / work.cols != tl;
+            const bool last = it + work.step >= work.end || (it + work.step) / work.cols != tl;
             for (int d = 0; ok && d < count; ++d) {
                 if (!(ok = agreed_wait(&b_full[bs], b_round, &s_dead) && agreed_wait(&d_empty[db], d_round ^ 1u, &s_dead))) break;
                 tc_fence_after();
@@ -378,7 +345,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
         int ys = 0;
         uint32_t y_round = 0;
         bool ok = true;
-        for (int64_t it = work.first; it < work.end; ++it) {
+        for (int64_t it = work.first; it < work.end; it += work.step) {
             const int64_t tl = it / work.cols;
             const int col = static_cast<int>(it - tl * work.cols) * CT;
             if (!(ok = agreed_wait(&o_full[ys], y_round, &s_dead))) break;
@@ -387,8 +354,8 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
                 tile_store(&mapOut, s_y + ys * kYTile, x, t0);
                 if (col + CT / 2 < p.N) tile_store(&mapOut, s_y + ys * kYTile + kXTile, x + 128, t0);
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                if (it > work.first) mbar_arrive(&y_empty[ys > 0 ? ys - 1 : SY - 1]);   // the buffer of the item before has been read
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                mbar_arrive(&y_empty[ys]);
             }
             if (++ys == SY) { ys = 0; y_round ^= 1u; }
         }
@@ -403,7 +370,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
         float f = 0.0f;
         int64_t tile = -1;
         bool ok = true;
-        for (int64_t it = work.first; ok && it < work.end; ++it) {
+        for (int64_t it = work.first; ok && it < work.end; it += work.step) {
             const int64_t tl = it / work.cols;
             if (tl != tile) {
                 tile = tl;
@@ -470,10 +437,16 @@ int adapter_stage_fault(unsigned int* fault_host) {
     return cudaMemcpyFromSymbol(fault_host, g_adapter_fault, sizeof(unsigned int)) == cudaSuccess ? CQ_OK : CQ_ERR_CUDA;
 }
 
-bool adapter_tiles_fit(const AdapterArgs& p, int y_dtype) {
-    const int64_t elem = y_dtype == CQ_F32 ? 4 : 2, most = (int64_t(1) << 31) - 1024;
-    return p.T >= kTileTokens && p.K >= 64 && p.n >= 1 && p.vec_k == 8 && p.vec_n == 16 / elem && 2 * p.K < most && elem * p.N < most &&
-           static_cast<int64_t>(p.n) * p.R < most && p.n * p.N < most && p.ldx < (int64_t(1) << 38) && p.ldy < (int64_t(1) << 37) && p.ldo < (int64_t(1) << 37);
+// A tile of fewer than 128 tokens is mostly empty, and what a tensor map cannot hold goes the other way too.
+constexpr int64_t kMapMost = (int64_t(1) << 31) - 1024;
+bool adapter_in_tiles(const AdapterArgs& p) {
+    return p.T >= kTileTokens && p.K >= 64 && p.n >= 1 && p.vec_k == 8 && 2 * p.K < kMapMost && static_cast<int64_t>(p.n) * p.R < kMapMost &&
+           p.ldx < (int64_t(1) << 38);
+}
+bool adapter_out_tiles(const AdapterArgs& p, int y_dtype) {
+    const int64_t elem = y_dtype == CQ_F32 ? 4 : 2;
+    return p.T >= kTileTokens && p.n >= 1 && p.vec_n == 16 / elem && elem * p.N < kMapMost && p.n * p.N < kMapMost && p.ldy < (int64_t(1) << 37) &&
+           p.ldo < (int64_t(1) << 37);
 }
 
 template <int HB, int DT, int YT>
@@ -490,11 +463,14 @@ static int launch_out_tiles(const AdapterArgs& p, cudaStream_t st) {
     if (resident_ctas(k28_adapter_out_tiles<HB, DT, YT>, kOutThreads, smem, smem, memo) < 1) return CQ_ERR_CUDA;
     const int64_t items = (p.T + kTileTokens - 1) / kTileTokens * ((p.N + out_cols<YT>() - 1) / out_cols<YT>());
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>(items, sm_count()));
-    return launch_ex(k28_adapter_out_tiles<HB, DT, YT>, dim3(grid), kOutThreads, smem, st, 1, !tuning_no_pdl(), high, low, b, y, out, p);
+    // blocks in groups that take neighbouring columns at one time, so that rows of y pass through memory in long pieces: 4096 x 28672
+    // 131 us with every block on a run of its own, 127 in groups of 4, 105 of 37 (a quarter of the SMs), 109 of 74, 114 of 148
+    const int group = grid >= 16 && grid % 4 == 0 ? grid / 4 : 1;
+    return launch_ex(k28_adapter_out_tiles<HB, DT, YT>, dim3(grid), kOutThreads, smem, st, 1, !tuning_no_pdl(), high, low, b, y, out, p, group);
 }
 
 template <int DT>
-static int launch_tiles(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
+static int launch_in_tiles(const AdapterArgs& p, cudaStream_t st) {
     CUtensorMap x, a;
     if (!make_byte_map(&x, p.x, 2 * p.K, p.T, 2 * p.ldx, 128, kTileTokens, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_byte_map(&a, p.A, 2 * p.K, static_cast<uint64_t>(p.n) * p.R, 2 * p.K, 128, p.R, CU_TENSOR_MAP_SWIZZLE_128B)) return CQ_ERR_CUDA;
@@ -504,9 +480,15 @@ static int launch_tiles(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     // as many parts of the contraction, four blocks of 64 each or more, as leave one block an SM
     const int64_t tiles = (p.T + kTileTokens - 1) / kTileTokens;
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, (p.K + 63) / 64 / 4), sm_count() / tiles));
-    int rc = launch_ex(k27_adapter_in_tiles<DT>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(tiles)), kInThreads, smem, st,
-                       static_cast<unsigned>(parts), !tuning_no_pdl(), x, a, p, in_stages(p.R));
-    if (rc != CQ_OK) return rc;
+    return launch_ex(k27_adapter_in_tiles<DT>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(tiles)), kInThreads, smem, st,
+                     static_cast<unsigned>(parts), !tuning_no_pdl(), x, a, p, in_stages(p.R));
+}
+int launch_adapter_in_tiles(const AdapterArgs& p, int dtype, cudaStream_t st) {
+    return dtype == CQ_F16 ? launch_in_tiles<CQ_F16>(p, st) : launch_in_tiles<CQ_BF16>(p, st);
+}
+
+template <int DT>
+static int launch_out_rank(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     if (p.R <= 64) {
         if (y_dtype == CQ_F32) return launch_out_tiles<1, DT, CQ_F32>(p, st);
         return y_dtype == CQ_F16 ? launch_out_tiles<1, DT, CQ_F16>(p, st) : launch_out_tiles<1, DT, CQ_BF16>(p, st);
@@ -514,9 +496,8 @@ static int launch_tiles(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     if (y_dtype == CQ_F32) return launch_out_tiles<2, DT, CQ_F32>(p, st);
     return y_dtype == CQ_F16 ? launch_out_tiles<2, DT, CQ_F16>(p, st) : launch_out_tiles<2, DT, CQ_BF16>(p, st);
 }
-
-int launch_adapter_tiles(const AdapterArgs& p, int dtype, int y_dtype, cudaStream_t st) {
-    return dtype == CQ_F16 ? launch_tiles<CQ_F16>(p, y_dtype, st) : launch_tiles<CQ_BF16>(p, y_dtype, st);
+int launch_adapter_out_tiles(const AdapterArgs& p, int dtype, int y_dtype, cudaStream_t st) {
+    return dtype == CQ_F16 ? launch_out_rank<CQ_F16>(p, y_dtype, st) : launch_out_rank<CQ_BF16>(p, y_dtype, st);
 }
 
 }  // namespace cq
