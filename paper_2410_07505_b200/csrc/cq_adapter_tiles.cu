@@ -51,7 +51,7 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
     uint8_t* s_x = smem + ((1024u - (smem_u32(smem) & 1023u)) & 1023u);
     uint8_t* s_a = s_x + stages * kXTile;
     float* s_h = reinterpret_cast<float*>(s_a + stages * kATile);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
 
     if (tid == 0) {
         for (int i = 0; i < kInMaxStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
@@ -214,7 +214,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
     uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(drain + 1);
     volatile uint32_t& s_dead = *(reinterpret_cast<volatile uint32_t*>(drain + 1) + 1);
     static_assert((3 * SY + 2 * SB + 2 * kOutBuffers + 3) * 8 + 8 <= 512, "barriers");
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
 
     asm volatile("griddepcontrol.launch_dependents;");
     if (tid == 0) {

@@ -7,6 +7,19 @@
 // that the running result is hardly ever rescaled.  Sums and references are fp32; p is rounded once to the inputs' 16 bits,
 // as an operand of the second product (kind::f16 takes both operands in one type), in fp16 with 2^kBias in front so that small
 // weights keep their bits.
+//
+// A persistent CTA takes pairs of tiles of 128 rows (tokens x query heads of one key head) over blocks of 128 keys, longest first.  Q, K
+// and V come by TMA; the logits S = Q K^T of either tile stand in tensor memory (128 columns), the weights take their place (64), the
+// results O are the other half of it.  While a tile's four warps form its weights, one row to a thread, the other tile's products run:
+// S of the next block can begin only when O has taken in this one's weights, so that a tile alone would leave the tensor cores idle.
+// What bounds it is that chain: products 768 cycles from the last weights to the next logits, signals about 200, loads and maxima 400 to 600, 128
+// exponentials a row 1250 (the unit's 1024 and their tail), for either tile in turn; the tensor cores are busy 61 % of the time, the unit for
+// exponentials 62 %.  Everything the softmax issues delays the products as well: a product costs its warp some 30 issue slots, which it shares
+// with two softmax warps.  Tried and dropped: logits in two buffers of 64 keys (products of 64 columns are bound by shared memory, 970 us),
+// two threads to a row (1220 us), a share of the exponentials by polynomial (895 us).
+// Measured (GPU alone, operands not in L2): 1 x 8192 tokens, 64 / 8 heads of 128, bf16 889 us (1240 TFLOP/s; 1090 in a long run, which the power limit
+// sets); 12 packed prompts up to 2060 tokens, 64 / 8 heads, fp16 350 us; 1000 tokens behind 19011, 32 heads of 64 260 us (bound by exponentials:
+// 139 us at one a lane and clock); 1000 tokens, 32 / 8 heads 28.6 us.
 #include "cq_serve.cuh"
 
 #include <algorithm>
@@ -16,7 +29,7 @@ namespace cq {
 
 __device__ unsigned int g_prompt_fault = 0;   // set if a bounded wait ever gave up
 
-constexpr int kPromptThreads = 384;           // warps 0..3, 4..7: softmax of the two tiles; warp 8: loads; warp 9: products; two idle
+constexpr int kPromptThreads = 384;           // warps 0..3, 4..7: softmax of the two tiles; warp 8: loads; warps 9, 10: products of either tile; one idle
 constexpr int kTileRows = 128;                // rows of a tile: tokens x the query heads that go together
 constexpr int kKeys = 128;                    // keys of a block
 constexpr float kSlack = 8.0f;
@@ -51,6 +64,32 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// Two numbers at a time: half of the instructions, which the warps that issue the products compete with.
+__device__ __forceinline__ uint64_t both(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 apart(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ void tile_load3(void* dst_smem, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, uint64_t* bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  :: "r"(smem_u32(dst_smem)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
@@ -61,13 +100,10 @@ __device__ __forceinline__ uint64_t smem_desc_n128(const void* tile) {
     const uint64_t addr = smem_u32(tile);
     return ((addr & 0x3FFFFu) >> 4) | (uint64_t(16384 >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
 }
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
                  :: "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-                    "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-                    "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr) : "memory");
+                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr) : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const float (&r)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
@@ -79,6 +115,14 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // All lanes wait and agree on what came of it, so that a warp's roles never part.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* dead) {
     return __all_sync(0xFFFFFFFFu, role_wait(bar, parity, dead)) != 0;
+}
+
+// Two weights 2^(c x - ref), added to a pair of sums and rounded to a pair.
+template <int DT>
+__device__ __forceinline__ uint32_t weights(float x0, float x1, uint64_t c, uint64_t neg, uint64_t& sums) {
+    const float2 u = apart(fma2(both(x0, x1), c, neg)), p = make_float2(ex2(u.x), ex2(u.y));
+    sums = add2(sums, both(p.x, p.y));
+    return pack16x2<DT>(p.x, p.y);
 }
 
 // nonzero bit 15 or 31 where a 16-bit element is an infinity or NaN
@@ -197,27 +241,27 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
     uint64_t* q_empty = q_full + 2;
     uint64_t* s_full = q_empty + 2;
     uint64_t* p_full = s_full + 2;
-    uint64_t* o_full = p_full + 2;
+    uint64_t* o_full = p_full + 4;                              // (p_full: two halves of the keys for each tile)
     uint64_t* i_full = o_full + 2;
     uint64_t* i_empty = i_full + 2;
     uint64_t* drain = i_empty + 2;
-    PromptItem* s_item = reinterpret_cast<PromptItem*>(drain + 1);
+    uint64_t* turn = drain + 2;
+    PromptItem* s_item = reinterpret_cast<PromptItem*>(turn + 2);
     uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(s_item + 2);
     volatile uint32_t& s_dead = *(reinterpret_cast<volatile uint32_t*>(s_item + 2) + 1);
     volatile uint32_t& s_poison = *(reinterpret_cast<volatile uint32_t*>(s_item + 2) + 2);
-    static_assert((2 * ST + 15) * 8 + 2 * sizeof(PromptItem) + 12 <= 512, "barriers");
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    static_assert((2 * ST + 20) * 8 + 2 * sizeof(PromptItem) + 12 <= 512, "barriers");
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x == 0) {
         if ((smem_u32(smem) & 1023u) != 0u) atomicExch(&g_prompt_fault, 1u);      // cannot be: see above
-        for (int i = 0; i < ST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+        for (int i = 0; i < ST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 2); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1);
-            mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); mbar_init(&o_full[i], 1);
-            mbar_init(&i_full[i], 1); mbar_init(&i_empty[i], 9);
+            mbar_init(&s_full[i], 1); mbar_init(&p_full[2 * i], 4); mbar_init(&p_full[2 * i + 1], 4); mbar_init(&o_full[i], 1);
+            mbar_init(&i_full[i], 1); mbar_init(&i_empty[i], 10); mbar_init(&drain[i], 1); mbar_init(&turn[i], 4);
         }
-        mbar_init(drain, 1);
         mbar_init_fence();
         s_dead = 0;
         s_poison = 0;
@@ -261,13 +305,13 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                 }
                 __syncwarp();
                 if (!have) break;
-    #pragma unroll
+#pragma unroll
                 for (int t = 0; t < 2; ++t)
                     if (it.end[t] > it.jb) {
                         if (!(ok = warp_wait(&q_empty[t], q_round[t] ^ 1u, &s_dead))) break;
                         if (elect_one()) {
                             mbar_expect_tx(&q_full[t], p.g * p.tokens * D * 2);
-    #pragma unroll
+#pragma unroll
                             for (int h = 0; h < D / 64; ++h)
                                 tile_load3(s_q + t * kTile + h * 16384, &mapQ, h * 64, it.head0, it.q0 + t * p.tokens, &q_full[t]);
                         }
@@ -276,12 +320,12 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                     }
                 const int je = max(it.end[0], it.end[1]);
                 for (int j = it.jb; ok && j < je; ++j)
-    #pragma unroll
+#pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
                         if (!(ok = warp_wait(&empty[s], round ^ 1u, &s_dead))) break;
                         if (elect_one()) {
                             mbar_expect_tx(&full[s], kTile);
-    #pragma unroll
+#pragma unroll
                             for (int h = 0; h < D / 64; ++h)
                                 tile_load3(s_kv + s * kTile + h * 16384, kv == 0 ? &mapK : &mapV, h * 64, it.kv, it.k0 + j * kKeys, &full[s]);
                         }
@@ -298,78 +342,77 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                     if (q_open[t])
                         for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&q_full[t], q_round[t] ^ 1u); ++polls) {}
             }
-        } else if (warp == 9) {
-            // ---- products
+        } else if (warp <= 10) {
+            // ---- products, a warp for each tile: a wait costs the tensor cores' queue, which holds two or three products, about 90
+            // cycles, unless the other warp feeds it meanwhile
             constexpr uint32_t idesc_s = idesc_f16<DT>(128, kKeys, false), idesc_o = idesc_f16<DT>(128, D, true);
-            const uint64_t desc_q = smem_desc_k128(s_q), desc_k = smem_desc_k128(s_kv), desc_v = smem_desc_n128(s_kv);
+            const int t = warp - 9;
+            const uint64_t desc_q = smem_desc_k128(s_q + t * kTile), desc_k = smem_desc_k128(s_kv), desc_v = smem_desc_n128(s_kv);
+            const uint32_t at_s = tmem + t * 128, at_o = tmem + 256 + t * 128;
             bool ok = true;
             int s = 0;
-            uint32_t round = 0, p_round[2] = {0, 0}, q_round[2] = {0, 0};
-            auto step = [&](int& stage, uint32_t& r) { if (++stage == ST) { stage = 0; r ^= 1u; } };
-            auto logits = [&](int t, int stage) {                   // S_t = Q_t K^T
-    #pragma unroll
-                for (int k = 0; k < D / 16; ++k)                    // 32 bytes further along the swizzled row, 16 KB to the other half
-                    tc_mma_f16(tmem + t * 128, desc_q + ((t * kTile + (k >> 2) * 16384 + (k & 3) * 32) >> 4),
-                               desc_k + ((stage * kTile + (k >> 2) * 16384 + (k & 3) * 32) >> 4), idesc_s, k != 0);
-            };
+            uint32_t round = 0, p_round = 0, q_round = 0;
             for (uint32_t n = 0; ok; ++n) {
                 if (!(ok = warp_wait(&i_full[n & 1], (n >> 1) & 1, &s_dead))) break;
-                const int jb = s_item[n & 1].jb, end[2] = {s_item[n & 1].end[0], s_item[n & 1].end[1]};
+                const int jb = s_item[n & 1].jb, end = s_item[n & 1].end[t], je = max(s_item[n & 1].end[0], s_item[n & 1].end[1]);
                 const bool last = s_item[n & 1].tokens < 0;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&i_empty[n & 1]);
                 if (last) break;
-                const int je = max(end[0], end[1]);
-                if (je <= jb) continue;
-                for (int j = jb - 1; ok && j < je; ++j) {           // results of block j, logits of block j + 1
-                    const int sv = s;
+                for (int j = jb - 1; ok && j < je; ++j) {       // results of block j, logits of block j + 1
+                    const bool results = j >= jb && j < end, next = j + 1 < end;
+                    int sv = s, sk = s;
+                    uint32_t rv = round, rk = round;
                     if (j >= jb) {
-                        if (!(ok = warp_wait(&full[s], round, &s_dead))) break;
-                        step(s, round);
+                        if (++s == ST) { s = 0; round ^= 1u; }
+                        sk = s;
+                        rk = round;
                     }
-                    const int sk = s;
-                    if (j + 1 < je) {
-                        if (!(ok = warp_wait(&full[s], round, &s_dead))) break;
-                        step(s, round);
+                    if (j + 1 < je && ++s == ST) { s = 0; round ^= 1u; }
+                    if (j >= jb && !(ok = warp_wait(&full[sv], rv, &s_dead))) break;
+                    if (j + 1 < je && !(ok = warp_wait(&full[sk], rk, &s_dead))) break;
+                    if (next && j < jb) {
+                        if (!(ok = warp_wait(&q_full[t], q_round, &s_dead))) break;
+                        q_round ^= 1u;
                     }
-    #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        if (j >= jb && j < end[t]) {
-                            if (!(ok = warp_wait(&p_full[t], p_round[t], &s_dead))) break;
-                            p_round[t] ^= 1u;
-                            tc_fence_after();
-                            if (elect_one()) {
-    #pragma unroll
-                                for (int k = 0; k < kKeys / 16; ++k)
-                                    tc_mma_f16_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, desc_v + ((sv * kTile + k * 2048) >> 4), idesc_o,
-                                                  j > jb || k != 0);
-                                if (j + 1 == end[t]) tc_commit(&o_full[t]);
-                            }
+                    if (results) {
+                        if (!(ok = warp_wait(&p_full[2 * t], p_round, &s_dead))) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < kKeys / 32; ++k)
+                                tc_mma_f16_ts(at_o, at_s + k * 8, desc_v + ((sv * kTile + k * 2048) >> 4), idesc_o, j > jb || k != 0);
                         }
-                        if (j + 1 < end[t]) {
-                            if (j < jb) {
-                                if (!(ok = warp_wait(&q_full[t], q_round[t], &s_dead))) break;
-                                q_round[t] ^= 1u;
-                            }
-                            tc_fence_after();
-                            if (elect_one()) {                      // (behind the product that reads the weights in the same columns)
-                                logits(t, sk);
-                                tc_commit(&s_full[t]);
-                                if (j + 2 == end[t]) tc_commit(&q_empty[t]);
-                            }
-                        }
+                        __syncwarp();
+                        if (!(ok = warp_wait(&p_full[2 * t + 1], p_round, &s_dead))) break;
+                        p_round ^= 1u;
                     }
-                    if (!ok) break;
+                    tc_fence_after();
                     if (elect_one()) {
+                        if (results) {
+#pragma unroll
+                            for (int k = kKeys / 32; k < kKeys / 16; ++k)
+                                tc_mma_f16_ts(at_o, at_s + k * 8, desc_v + ((sv * kTile + k * 2048) >> 4), idesc_o, true);
+                            if (!next) tc_commit(&o_full[t]);
+                        }
+                        if (next) {                             // (behind the product that reads the weights in the same columns)
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k)    // 32 bytes further along the swizzled row, 16 KB to the other half
+                                tc_mma_f16(at_s, desc_q + (((k >> 2) * 16384 + (k & 3) * 32) >> 4),
+                                           desc_k + ((sk * kTile + (k >> 2) * 16384 + (k & 3) * 32) >> 4), idesc_s, k != 0);
+                            tc_commit(&s_full[t]);
+                            if (j + 2 == end) tc_commit(&q_empty[t]);
+                        }
                         if (j >= jb) tc_commit(&empty[sv]);
                         if (j + 1 < je) tc_commit(&empty[sk]);
                     }
+                    __syncwarp();
                 }
             }
-            if (!ok) {                            // products in flight end before the CTA leaves
+            if (!ok) {                        // products in flight end before the CTA leaves
                 __syncwarp();
-                if (elect_one()) tc_commit(drain);
-                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(drain, 0); ++polls) {}
+                if (elect_one()) tc_commit(&drain[t]);
+                for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(&drain[t], 0); ++polls) {}
             }
         }
     } else {
@@ -378,37 +421,51 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
         const int t = warp >> 2, row = threadIdx.x & 127;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t at_s = tmem + t * 128 + lanes, at_o = tmem + 256 + t * 128 + lanes;
-        const int token = t * p.tokens + row / p.g, head = row % p.g;
-        const bool in_tile = row < p.g * p.tokens;
-        uint32_t s_round = 0, o_round = 0, slot = 0;            // `slot`: places of the ring that items before this one took
+        const int token = row < p.g * p.tokens ? t * p.tokens + row / p.g : 1 << 30;         // of the item; far behind it: no row of the tile
+        uint32_t s_round = 0, o_round = 0, t_round = 0, slot = 0;               // `slot`: places of the ring that items before this one took
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
             if (!(ok = warp_wait(&i_full[n & 1], (n >> 1) & 1, &s_dead))) break;
-            const PromptItem it = s_item[n & 1];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&i_empty[n & 1]);
+            const PromptItem& it = s_item[n & 1];               // (stays there until the end of the item)
             if (it.tokens < 0) break;
-            const int jb = it.jb, end = t == 0 ? it.end[0] : it.end[1];
+            const int jb = it.jb, end = it.end[t];
             const uint32_t first_slot = slot;
             slot += 2 * max(max(it.end[0], it.end[1]) - jb, 0);
-            if (t * p.tokens >= it.tokens) continue;            // no such tile
+            if (t * p.tokens >= it.tokens) {                    // no such tile
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&i_empty[n & 1]);
+                continue;
+            }
             const int sees = it.sees + token;                   // this row's keys are the first `sees`
             const int all_see = it.sees + t * p.tokens;         // those that every row of the tile sees
+            const int common = min(it.end[0], it.end[1]);         // blocks before this one are both tiles'
             float ref = -INFINITY, sum = 0.0f;
             for (int j = jb; j < end; ++j) {
                 if (!(ok = warp_wait(&s_full[t], s_round, &s_dead))) break;
                 s_round ^= 1u;
                 tc_fence_after();
                 float x[4][32];
+                tmem_ld32(at_s, x[0]);
+                tmem_ld32(at_s + 32, x[1]);
+                tmem_ld_wait(x[0]);
+                tmem_ld_wait(x[1]);
+                tmem_ld32(at_s + 64, x[2]);
+                tmem_ld32(at_s + 96, x[3]);
+                float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_ld32(at_s + q * 32, x[q]);
+                for (int i = 0; i < 32; ++i) m[i & 3] = max3(m[i & 3], x[i >> 4][(2 * i) & 31], x[i >> 4][((2 * i) & 31) + 1]);
+                tmem_ld_wait(x[2]);
+                tmem_ld_wait(x[3]);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_ld_wait(x[q]);
+                for (int i = 32; i < 64; ++i) m[i & 3] = max3(m[i & 3], x[i >> 4][(2 * i) & 31], x[i >> 4][((2 * i) & 31) + 1]);
                 const bool edge = (j + 1) * kKeys > all_see;
                 if (edge) {
                     const int lim = sees - j * kKeys;
 #pragma unroll
                     for (int i = 0; i < 128; ++i) x[i >> 5][i & 31] = i < lim ? x[i >> 5][i & 31] : -INFINITY;
+                    m[0] = m[1] = m[2] = m[3] = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) m[i & 3] = max3(m[i & 3], x[i >> 4][(2 * i) & 31], x[i >> 4][((2 * i) & 31) + 1]);
                     // A weight of 0 does not hide an infinity or NaN in V from the product: such elements become 0 in shared memory
                     // and are added to the rows that see them at the end.
                     const uint32_t place = first_slot + 2 * (j - jb) + 1;
@@ -432,9 +489,12 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                     }
                     __syncwarp();
                 }
-                float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int i = 0; i < 128; ++i) m[i & 3] = fmaxf(m[i & 3], x[i >> 5][i & 31]);
+                auto half_ready = [&](int h) {
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[2 * t + h]);
+                };
                 const float top = __fmul_rn(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), p.c);
                 const bool renew = top > ref + (kBias + kSlack);
                 float keep = 1.0f;
@@ -454,26 +514,30 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                         tmem_st16(at_o + q * 16, o);
                     }
                 }
-                const float neg = ref == -INFINITY ? 0.0f : -ref;
-                float l[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t r[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int e = h * 64 + 2 * i;
-                        const float a = ex2(__fmaf_rn(x[e >> 5][e & 31], p.c, neg)), b = ex2(__fmaf_rn(x[e >> 5][(e & 31) + 1], p.c, neg));
-                        l[i & 1] += a;
-                        l[2 + (i & 1)] += b;
-                        r[i] = pack16x2<DT>(a, b);
-                    }
-                    tmem_st32(at_s + h * 32, r);
+                // The tiles take turns at their exponentials, so that one's stand beside the other's products: at random they meet, and
+                // the unit for exponentials is full for both and then idle for both (1 x 8192 tokens: 1069 us).
+                if (j < common && (t == 1 || j > jb)) {
+                    if (!(ok = warp_wait(&turn[t], t_round, &s_dead))) break;
+                    t_round ^= 1u;
                 }
-                sum += (l[0] + l[1]) + (l[2] + l[3]);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[t]);
+                const float neg = ref == -INFINITY ? 0.0f : -ref;
+                const uint64_t neg2 = both(neg, neg), c2 = both(p.c, p.c);
+                uint64_t l[2] = {0, 0};
+                // Weights of 32 keys at a time, to where their logits stood.  A half is handed over behind the next quarter's exponentials, so that
+                // their unit does not wait for the stores; the turn goes to the other tile before the last quarter's.
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (q == 3 && lane == 0 && j < common && (t == 0 || j + 1 < common)) mbar_arrive(&turn[t ^ 1]);
+                    uint32_t r[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        r[i] = weights<DT>(x[q][2 * i], x[q][2 * i + 1], c2, neg2, l[i & 1]);
+                    if (q == 2) half_ready(0);
+                    tmem_st16(at_s + q * 16, r);
+                }
+                half_ready(1);
+                const float2 l2 = apart(add2(l[0], l[1]));
+                sum += l2.x + l2.y;
             }
             if (!ok) break;
             const bool any = end > jb;
@@ -483,9 +547,9 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                 tc_fence_after();
             }
             // ---- results of this row
-            const bool mine = in_tile && token < it.tokens;
+            const bool mine = token < it.tokens;
             const bool poison = s_poison != 0u;
-            const int64_t place = (static_cast<int64_t>(it.q0) + token) * p.Hq + it.head0 + head;
+            const int64_t place = (static_cast<int64_t>(it.q0) + token) * p.Hq + it.head0 + row % p.g;
             const float inv = sum == 0.0f ? 0.0f : __frcp_rn(sum);
             const int from = max(jb, max(it.sees, 0) / kKeys) * kKeys, to = min(sees, end * kKeys);     // keys whose V may have been emptied
             const int64_t rows = static_cast<int64_t>(p.Tq) * p.Hq;
@@ -532,6 +596,7 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
             }
             tc_fence_before();
             __syncwarp();
+            if (lane == 0) mbar_arrive(&i_empty[n & 1]);
         }
     }
     tc_fence_before();
