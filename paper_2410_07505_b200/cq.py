@@ -572,7 +572,7 @@ def _raw(device: int) -> int:
 
 
 _DT16 = {torch.float16: CQ_F16, torch.bfloat16: CQ_BF16}
-_F32, _E4M3, _I32, _I64 = torch.float32, torch.float8_e4m3fn, torch.int32, torch.int64
+_F32, _F64, _E4M3, _I32, _I64 = torch.float32, torch.float64, torch.float8_e4m3fn, torch.int32, torch.int64
 
 
 def _matrix16(X: torch.Tensor):
@@ -850,22 +850,22 @@ def kv_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, lens
 
 
 # ----------------------------------------------------------------------------- prompts
-def _heads16(x: torch.Tensor, tokens, heads, head_dim, dtype, dev: int, what: str):
-    """Strides of tokens and heads of a 16-bit CUDA tensor [tokens, heads, head_dim] (None: any)."""
-    shape = x.shape
-    if x.dtype != dtype or len(shape) != 3 or x.get_device() != dev or any(n is not None and n != m for n, m in zip((tokens, heads, head_dim), shape)):
-        raise ValueError(f"{what} must be {dtype} [{tokens or 'tokens'}, {heads or 'heads'}, {head_dim}] on cuda:{dev}")
-    token, head, inner = x.stride()
-    if inner != 1 and x.numel() > 0:
+def _heads16(x: torch.Tensor, shape, dtype, dev: int, what: str):
+    """Strides of a 16-bit CUDA tensor [tokens, heads, head_dim] of that shape (with contiguous head elements)."""
+    if x.shape != shape or x.dtype != dtype or x.get_device() != dev:
+        raise ValueError(f"{what} must be {dtype} {list(shape)} on cuda:{dev}")
+    strides = x.stride()
+    if strides[2] != 1 and x.numel() > 0:
         raise ValueError(f"{what}: head elements must be contiguous")
-    return token, head
+    return strides
 
 
-def _starts(starts: torch.Tensor, B, dev: int, what: str) -> int:
-    if starts.dtype != _I32 or starts.dim() != 1 or starts.shape[0] < 1 or not starts.is_contiguous() or starts.get_device() != dev \
-            or (B is not None and starts.shape[0] != B + 1):
-        raise ValueError(f"{what} must be a contiguous int32 vector of {'sequences' if B is None else B} + 1 on cuda:{dev}")
-    return starts.shape[0] - 1
+def _starts(starts: torch.Tensor, n, dev: int, what: str) -> int:
+    shape = starts.shape
+    if starts.dtype != _I32 or len(shape) != 1 or shape[0] < 1 or (n is not None and shape[0] != n) or starts.get_device() != dev \
+            or not starts.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 vector of {'sequences + 1' if n is None else n} on cuda:{dev}")
+    return shape[0]
 
 
 def prompt_attention_workspace_bytes(sequences: int, queries: int, keys: int, query_heads: int, heads: int, head_dim: int) -> int:
@@ -881,19 +881,21 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts
     Sequence b's queries are the rows q_starts[b] .. q_starts[b + 1] (int32 [B + 1]), its keys those of k_starts (default: the same); the
     queries are its last tokens.  `scale` multiplies the logits (default 1 / sqrt(D)); `lse` float32 [Tq, Hq] receives the
     logarithm of the softmax's sum.  Rows outside the sequences are not written."""
-    dt, dev = _DT16.get(q.dtype), q.get_device()
-    if dt is None or q.dim() != 3 or dev < 0:
+    dtype, dev, shape = q.dtype, q.get_device(), q.shape
+    dt = _DT16.get(dtype)
+    if dt is None or len(shape) != 3 or dev < 0:
         raise TypeError("q must be a float16 / bfloat16 CUDA tensor [tokens, heads, head_dim]")
-    Tq, Hq, D = shape = q.shape
-    qs = _heads16(q, Tq, Hq, D, q.dtype, dev, "q")
-    ks = _heads16(k, None, None, D, q.dtype, dev, "k")
-    Tk, H, _ = k.shape
-    vs = _heads16(v, Tk, H, D, q.dtype, dev, "v")
-    B = _starts(q_starts, None, dev, "q_starts")
+    Tq, Hq, D = shape
+    kv = k.shape
+    if len(kv) != 3 or kv[2] != D:
+        raise ValueError(f"k must be {dtype} [tokens, heads, {D}] on cuda:{dev}")
+    qs, ks, vs = _heads16(q, shape, dtype, dev, "q"), _heads16(k, kv, dtype, dev, "k"), _heads16(v, kv, dtype, dev, "v")
+    Tk, H, _ = kv
+    n = _starts(q_starts, None, dev, "q_starts")
     if k_starts is None:
         k_starts = q_starts
-    else:
-        _starts(k_starts, B, dev, "k_starts")
+    elif k_starts is not q_starts:
+        _starts(k_starts, n, dev, "k_starts")
     if out is None:
         out = q.new_empty(shape)
     elif out.shape != shape or out.dtype != q.dtype or out.get_device() != dev or not out.is_contiguous():
@@ -902,11 +904,12 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts
         raise ValueError("lse must be a contiguous float32 [Tq, Hq] tensor")
     L = _lib or lib()
     if workspace is None:
-        need = L.cq_prompt_attention_workspace_bytes(B, Tq, Tk, Hq, H, D)
+        need = L.cq_prompt_attention_workspace_bytes(n - 1, Tq, Tk, Hq, H, D)
         workspace = q.new_empty(need, dtype=torch.uint8) if need else None
-    ws = (0, 0) if workspace is None else _workspace_of(workspace, dev)
-    st = L.cq_prompt_attention(q.data_ptr(), *qs, k.data_ptr(), *ks, v.data_ptr(), *vs, dt, B, Tq, Tk, Hq, H, D, q_starts.data_ptr(),
-                               k_starts.data_ptr(), D ** -0.5 if scale is None else float(scale), out.data_ptr(), _addr(lse), *ws, _raw(dev))
+    at, size = (0, 0) if workspace is None else _workspace_of(workspace, dev)
+    st = L.cq_prompt_attention(q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], dt, n - 1, Tq, Tk, Hq, H, D,
+                               q_starts.data_ptr(), k_starts.data_ptr(), D ** -0.5 if scale is None else float(scale), out.data_ptr(),
+                               0 if lse is None else lse.data_ptr(), at, size, _raw(dev))
     if st:
         raise CQError(st, "cq_prompt_attention")
     return out
@@ -925,30 +928,38 @@ def norm_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, freq:
     positions int64 [T], freq float64 [R / 2] (radians a position): the first R channels of a head are rotated, channel i with i + R / 2
     or, with `neighbours`, 2 i with 2 i + 1.  Weights [D] of q's dtype (default: ones); `eps` = None leaves the norms out.
     `out` = a pair of tensors to fill, which may be (q, k) themselves."""
-    dt, dev = _DT16.get(q.dtype), q.get_device()
-    if dt is None or q.dim() != 3 or dev < 0:
+    dtype, dev, shape, kv = q.dtype, q.get_device(), q.shape, k.shape
+    dt = _DT16.get(dtype)
+    if dt is None or len(shape) != 3 or dev < 0:
         raise TypeError("q must be a float16 / bfloat16 CUDA tensor [tokens, heads, head_dim]")
-    T, Hq, D = q.shape
-    qs, ks = _heads16(q, T, Hq, D, q.dtype, dev, "q"), _heads16(k, T, None, D, q.dtype, dev, "k")
-    H = k.shape[1]
-    if positions.dtype != _I64 or positions.shape != (T,) or not positions.is_contiguous() or positions.get_device() != dev:
+    T, Hq, D = shape
+    if len(kv) != 3 or kv[0] != T or kv[2] != D:
+        raise ValueError(f"k must be {dtype} [{T}, heads, {D}] on cuda:{dev}")
+    qs, ks = _heads16(q, shape, dtype, dev, "q"), _heads16(k, kv, dtype, dev, "k")
+    if positions.dtype != _I64 or positions.shape != (T,) or positions.get_device() != dev or not positions.is_contiguous():
         raise ValueError(f"positions must be a contiguous int64 vector of {T} on cuda:{dev}")
-    if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or freq.get_device() != dev:
+    pairs = freq.shape
+    if freq.dtype != _F64 or len(pairs) != 1 or freq.get_device() != dev or not freq.is_contiguous():
         raise ValueError(f"freq must be a contiguous float64 vector on cuda:{dev}")
     for w in (q_weight, k_weight):
-        if w is not None and (w.dtype != q.dtype or w.shape != (D,) or not w.is_contiguous() or w.get_device() != dev):
-            raise ValueError(f"weights must be contiguous {q.dtype} vectors of {D} on cuda:{dev}")
-    if eps is None and (q_weight is not None or k_weight is not None):
-        raise ValueError("weights belong to the norms: eps is None")
-    if eps is not None and not eps >= 0.0:
+        if w is not None and (w.dtype != dtype or w.shape != (D,) or w.get_device() != dev or not w.is_contiguous()):
+            raise ValueError(f"weights must be contiguous {dtype} vectors of {D} on cuda:{dev}")
+    if eps is None:
+        if q_weight is not None or k_weight is not None:
+            raise ValueError("weights belong to the norms: eps is None")
+        eps = -1.0
+    elif not eps >= 0.0:
         raise ValueError("eps must not be below 0")
     if out is None:
-        out = q.new_empty((T, Hq, D)), q.new_empty((T, H, D))
-    q_out, k_out = out
-    qo, ko = _heads16(q_out, T, Hq, D, q.dtype, dev, "out[0]"), _heads16(k_out, T, H, D, q.dtype, dev, "out[1]")
-    st = (_lib or lib()).cq_norm_rotate(q.data_ptr(), *qs, Hq, k.data_ptr(), *ks, H, dt, T, D, 2 * freq.shape[0], int(neighbours),
-                                        positions.data_ptr(), freq.data_ptr(), _addr(q_weight), _addr(k_weight),
-                                        -1.0 if eps is None else float(eps), q_out.data_ptr(), *qo, k_out.data_ptr(), *ko, _raw(dev))
+        out = q_out, k_out = q.new_empty(shape), q.new_empty(kv)
+        qo, ko = (Hq * D, D), (kv[1] * D, D)
+    else:
+        q_out, k_out = out
+        qo, ko = _heads16(q_out, shape, dtype, dev, "out[0]"), _heads16(k_out, kv, dtype, dev, "out[1]")
+    st = (_lib or lib()).cq_norm_rotate(q.data_ptr(), qs[0], qs[1], Hq, k.data_ptr(), ks[0], ks[1], kv[1], dt, T, D, 2 * pairs[0], neighbours,
+                                        positions.data_ptr(), freq.data_ptr(), 0 if q_weight is None else q_weight.data_ptr(),
+                                        0 if k_weight is None else k_weight.data_ptr(), eps, q_out.data_ptr(), qo[0], qo[1],
+                                        k_out.data_ptr(), ko[0], ko[1], _raw(dev))
     if st:
         raise CQError(st, "cq_norm_rotate")
     return out
@@ -974,30 +985,33 @@ def adapter_add(y: torch.Tensor, x: torch.Tensor, adapters: Adapters, index: tor
     y is what the shared projection gave (float16, bfloat16 or float32), x has the adapters' dtype; `out` may be y itself."""
     T, K, ldx, dt, dev = _matrix16(x)
     A, B, scale = adapters
-    if A.dim() != 3 or B.dim() != 3 or A.shape[2] != K or A.shape[:2] != (B.shape[0], B.shape[2]):
+    a_shape, b_shape, dtype = A.shape, B.shape, x.dtype
+    if len(a_shape) != 3 or len(b_shape) != 3 or a_shape[2] != K or a_shape[0] != b_shape[0] or a_shape[1] != b_shape[2]:
         raise ValueError(f"adapters must be A [n, R, {K}] and B [n, out channels, R]")
-    n, R, _ = A.shape
-    N = B.shape[1]
-    for w in (A, B):
-        if w.dtype != x.dtype or w.get_device() != dev or not w.is_contiguous():
-            raise ValueError(f"adapters must be contiguous {x.dtype} tensors on cuda:{dev}")
+    n, N, R = b_shape
+    if A.dtype != dtype or B.dtype != dtype or A.get_device() != dev or B.get_device() != dev or not A.is_contiguous() or not B.is_contiguous():
+        raise ValueError(f"adapters must be contiguous {dtype} tensors on cuda:{dev}")
     if scale is not None and (scale.dtype != _F32 or scale.shape != (n,) or scale.get_device() != dev or not scale.is_contiguous()):
         raise ValueError(f"scale must be a contiguous float32 vector of {n} on cuda:{dev}")
     if index.dtype != _I32 or index.shape != (T,) or index.get_device() != dev or not index.is_contiguous():
         raise ValueError(f"index must be a contiguous int32 vector of {T} on cuda:{dev}")
-    ydt = _DT.get(y.dtype)
+    ydt, shape, strides = _DT.get(y.dtype), y.shape, y.stride()
     if ydt is None:
         raise TypeError("expected float16, bfloat16 or float32 results of the projection")
-    if y.shape != (T, N) or y.get_device() != dev or (y.stride(1) != 1 and N > 1 and T > 0):
+    if shape != (T, N) or y.get_device() != dev or (strides[1] != 1 and N > 1 and T > 0):
         raise ValueError(f"y must be [{T}, {N}] on cuda:{dev} with contiguous columns")
-    out, _, ldo = _product_out(out, T, N, y.dtype, x)
-    if out.data_ptr() == y.data_ptr() and out.stride() != y.stride() and T > 1:
-        raise ValueError("out begins where y does and has other strides")
+    if out is None:
+        out, ldo = y.new_empty(shape), N or 1
+    else:
+        out, _, ldo = _product_out(out, T, N, y.dtype, x)
+        if T > 1 and out.data_ptr() == y.data_ptr() and out.stride() != strides:
+            raise ValueError("out begins where y does and has other strides")
     L = _lib or lib()
     if workspace is None:
         workspace = x.new_empty(L.cq_adapter_add_workspace_bytes(T, R), dtype=torch.uint8)
-    st = L.cq_adapter_add(x.data_ptr(), dt, T, K, ldx, A.data_ptr(), B.data_ptr(), _addr(scale), n, R, N, index.data_ptr(), y.data_ptr(), ydt,
-                          y.stride(0) if T > 1 else max(N, 1), out.data_ptr(), ldo, *_workspace_of(workspace, dev), _raw(dev))
+    at, size = _workspace_of(workspace, dev)
+    st = L.cq_adapter_add(x.data_ptr(), dt, T, K, ldx, A.data_ptr(), B.data_ptr(), 0 if scale is None else scale.data_ptr(), n, R, N,
+                          index.data_ptr(), y.data_ptr(), ydt, strides[0] if T > 1 else N or 1, out.data_ptr(), ldo, at, size, _raw(dev))
     if st:
         raise CQError(st, "cq_adapter_add")
     return out
