@@ -3,10 +3,10 @@
 //   y_d = w_d x_d / sqrt(mean_d x_d^2 + eps)   (y = x without norms),   then for each pair (a, b) of the first R channels
 //   (a, b) -> (a cos f - b sin f, a sin f + b cos f),   f = position * freq[pair]
 //
-// Bound by HBM (2 bytes in, 2 out).  A row's channels lie eight to a lane, so that its mean is a few shuffles and a pair is either in
-// one lane (neighbours) or one shuffle away (halves).  The angles of a token are the same for all of its heads: a block forms those of
-// a few tokens at a time, as a fraction of a turn in 64 bits (position * freq passes 2^24 radians, where 32 bits hold no angle), and
-// each lane keeps its token's, times the weights: an element then costs a product, a multiply-add and the row's factor.
+// Bound by HBM (2 bytes in, 2 out).  A lane has sixteen channels of a row, both sides of eight pairs, so that a row's mean is a few shuffles
+// and the rotation none.  The angles of a token are the same for all of its heads: a block forms those of a few tokens at a time, as
+// a fraction of a turn in 64 bits (position * freq passes 2^24 radians, where 32 bits hold no angle), and each lane keeps its
+// token's, times the weights: an element then costs two products and the row's factor.
 #include "cq_serve.cuh"
 
 #include <algorithm>
@@ -44,168 +44,200 @@ __device__ __forceinline__ void angles(const RotateArgs& p, int64_t t0, float* s
     }
 }
 
-// the sum of a row's squares in 64 bits, on all W lanes
-template <int W, int DT>
-__device__ __noinline__ double row_squares(uint4 x) {
-    double sum = 0.0;
-    const uint32_t r[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 e = unpack16x2<DT>(r[i]);
-        sum += static_cast<double>(e.x) * e.x + static_cast<double>(e.y) * e.y;
-    }
-#pragma unroll
-    for (int off = W / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off, W);
-    return sum;
-}
 // 1 / sqrt(mean + eps)
 __device__ __noinline__ double wide_factor(double sum, int D, double eps) { return 1.0 / sqrt(sum / D + eps); }
 
-template <int DT>
-__device__ __forceinline__ void unpack8(const uint4& w, float (&v)[8]) {
-    const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+// A lane's channels as the two sides of its pairs: two pieces of eight, or (NEAR) every other one of sixteen.
+template <int DT, bool NEAR>
+__device__ __forceinline__ void sides(const uint4& x, const uint4& y, float (&a)[8], float (&b)[8]) {
+    const uint32_t r[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
         const float2 f = unpack16x2<DT>(r[i]);
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
+        if constexpr (NEAR) { a[i] = f.x; b[i] = f.y; }
+        else if (i < 4) { a[2 * i] = f.x; a[2 * i + 1] = f.y; }
+        else { b[2 * i - 8] = f.x; b[2 * i - 7] = f.y; }
     }
 }
 
-// W lanes for a row, eight channels each; rows in 16-byte accesses, R a multiple of 16.  The block's rows are `group` tokens x
+// A row whose squares fp32 cannot hold, or are all zero, in 64 bits: a lane's sixteen channels; nothing is written where out is null.
+// Called by whole warps.
+template <int W, int DT, bool NEAR>
+__device__ __noinline__ void wide_row(const uint16_t* w, const float* s_cos, const float* s_sin, uint4 x, uint4 y, int D, double eps,
+                                      bool rotated, int da, int db, uint16_t* out) {
+    float a[8], b[8], wa[8], wb[8];
+    sides<DT, NEAR>(x, y, a, b);
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += static_cast<double>(a[i]) * a[i] + static_cast<double>(b[i]) * b[i];
+#pragma unroll
+    for (int off = W / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off, W);
+    if (out == nullptr) return;
+    const double f = wide_factor(sum, D, eps);
+    uint4 wx = make_uint4(0, 0, 0, 0), wy = wx;
+    if (w != nullptr) {
+        wx = *reinterpret_cast<const uint4*>(w + da);
+        if (db < D) wy = *reinterpret_cast<const uint4*>(w + db);
+    }
+    sides<DT, NEAR>(wx, wy, wa, wb);
+    uint32_t o[8];
+    float va[8], vb[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const double c = rotated ? s_cos[i] : 1.0f, s = rotated ? s_sin[i] : 0.0f;
+        const double u = a[i] * f * (w != nullptr ? wa[i] : 1.0f), v = b[i] * f * (w != nullptr ? wb[i] : 1.0f);
+        va[i] = static_cast<float>(rotated ? u * c - v * s : u);
+        vb[i] = static_cast<float>(rotated ? u * s + v * c : v);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (NEAR) o[i] = pack16x2<DT>(va[i], vb[i]);
+        else o[i] = i < 4 ? pack16x2<DT>(va[(2 * i) & 7], va[(2 * i + 1) & 7]) : pack16x2<DT>(vb[(2 * i) & 7], vb[(2 * i + 1) & 7]);
+    }
+    *reinterpret_cast<uint4*>(out + da) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (db < D) *reinterpret_cast<uint4*>(out + db) = make_uint4(o[4], o[5], o[6], o[7]);
+}
+
+// W lanes for a row, sixteen channels each; rows in 16-byte accesses, R a multiple of 16.  The block's rows are `group` tokens x
 // kRows / group heads at a time.
 constexpr int kMaxGroup = 8;
 constexpr int kFastDim = 256;
 
 template <int W, int DT, bool NORM, bool NEAR>                 // NEAR: neighbours are pairs
-__global__ void __launch_bounds__(kRotateThreads, 3)
+__global__ void __launch_bounds__(kRotateThreads, NORM ? 2 : 3)
 k24_norm_rotate(const RotateArgs p) {
     constexpr int kRows = kRotateThreads / W;
-    constexpr int kAhead = 4;                                   // rows whose loads are issued together
+    constexpr int kAhead = 2;                                   // rows of a pass
     __shared__ float s_cos[2][kMaxGroup * kFastDim / 2], s_sin[2][kMaxGroup * kFastDim / 2];
     asm volatile("griddepcontrol.launch_dependents;");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x % W, row = threadIdx.x / W;
     const int token = row % p.group, first = row / p.group, step = kRows / p.group;
-    const int d0 = lane * 8;
-    const bool have = d0 < p.D;
-    const int half = p.R / 2;
-    const bool rotated = d0 < p.R, second = d0 >= half;
-    // the lane with the other channels of this one's pairs (halves), and the first of its angles
-    const int partner = NEAR || !rotated ? lane : second ? lane - half / 8 : lane + half / 8;
-    const int angle0 = NEAR ? d0 / 2 : second ? d0 - half : d0;
+    // the lane's two pieces of eight channels: of a rotated lane both sides of its pairs, else two neighbours of the rest
+    const bool rotated = lane < p.R / 16;
+    const int da = NEAR || !rotated ? lane * 16 : lane * 8, db = NEAR || !rotated ? lane * 16 + 8 : lane * 8 + p.R / 2;
+    const bool have_a = da < p.D, have_b = db < p.D;
     const int slice = blockIdx.x % p.slices;
     const int64_t stride = static_cast<int64_t>(gridDim.x / p.slices) * p.group;
     int buffer = 0;
     for (int64_t t0 = static_cast<int64_t>(blockIdx.x / p.slices) * p.group; t0 < p.T; t0 += stride, buffer ^= 1) {
         const int64_t t = t0 + token;
-        bool ready = false;
+        // this lane's heads of a side: first, first + step .. of those from `from` on; `passes` of kAhead each, of any lane
+        int from[2], rows[2], passes[2];
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-            const RotateSide& a = p.side[kv];
-            const int h0 = static_cast<int>(static_cast<int64_t>(a.heads) * slice / p.slices), h1 = static_cast<int>(static_cast<int64_t>(a.heads) * (slice + 1) / p.slices);
-            // this lane's heads: h0 + first, every `step`-th, `rows` of them; `most` of any lane of the block
-            const bool live = have && t < p.T;
-            const int rows = live && h1 - h0 > first ? (h1 - h0 - first + step - 1) / step : 0, most = (h1 - h0 + step - 1) / step;
-            const uint16_t* x_at = a.x + t * a.xt + (h0 + first) * a.xh + d0;
-            uint16_t* y_at = a.y + t * a.yt + (h0 + first) * a.yh + d0;
-            const int64_t x_step = step * a.xh, y_step = step * a.yh;
-            float c[8], s[8];                                   // y = (x c + partner s) factor
-            for (int done = 0; done < most || (kv == 0 && !ready); done += kAhead) {
-                uint4 x[kAhead];
+            const int64_t heads = p.side[kv].heads;
+            from[kv] = static_cast<int>(heads * slice / p.slices);
+            const int n = static_cast<int>(heads * (slice + 1) / p.slices) - from[kv];
+            rows[kv] = have_a && t < p.T && n > first ? (n - first + step - 1) / step : 0;
+            passes[kv] = (n + kAhead * step - 1) / (kAhead * step);
+        }
+        const int total = passes[0] + passes[1];
+        uint4 x[kAhead], y[kAhead];
+        auto load = [&](int pass) {                             // the lane's pieces of pass `pass`
+            const bool keys = pass >= passes[0];
+            const RotateSide& side = p.side[keys ? 1 : 0];
+            const int done = (keys ? pass - passes[0] : pass) * kAhead, have = pass < total ? (keys ? rows[1] : rows[0]) - done : 0;
+            const uint16_t* at = side.x + t * side.xt + (static_cast<int64_t>(keys ? from[1] : from[0]) + first + static_cast<int64_t>(done) * step) * side.xh;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                x[u] = y[u] = make_uint4(0, 0, 0, 0);
+                if (u < have) {
+                    x[u] = __ldcs(reinterpret_cast<const uint4*>(at + da));
+                    if (have_b) y[u] = __ldcs(reinterpret_cast<const uint4*>(at + db));
+                }
+                at += step * side.xh;
+            }
+        };
+        load(0);
+        angles(p, t0, s_cos[buffer], s_sin[buffer]);            // (behind the first loads)
+        __syncthreads();
+        float ca[8], cb[8], sa[8], sb[8];                       // a' = a ca - b sb,  b' = b cb + a sa
+        for (int pass = 0; pass < total; ++pass) {
+            const bool keys = pass >= passes[0];
+            const RotateSide& side = p.side[keys ? 1 : 0];
+            const int done = (keys ? pass - passes[0] : pass) * kAhead, have = (keys ? rows[1] : rows[0]) - done;
+            if (done == 0) {
+                uint4 wx = make_uint4(0, 0, 0, 0), wy = wx;
+                if (NORM && side.w != nullptr) {
+                    if (have_a) wx = *reinterpret_cast<const uint4*>(side.w + da);
+                    if (have_b) wy = *reinterpret_cast<const uint4*>(side.w + db);
+                }
+                sides<DT, NEAR>(wx, wy, ca, cb);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (!NORM || side.w == nullptr) ca[i] = cb[i] = 1.0f;
+                    const int at = token * (p.R / 2) + lane * 8 + i;
+                    const float c = rotated ? s_cos[buffer][at] : 1.0f, s = rotated ? s_sin[buffer][at] : 0.0f;
+                    sa[i] = s * ca[i];
+                    sb[i] = s * cb[i];
+                    ca[i] *= c;
+                    cb[i] *= c;
+                }
+            }
+            uint4 xn[kAhead], yn[kAhead];                       // this pass's: the next one's are on the way meanwhile
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) { xn[u] = x[u]; yn[u] = y[u]; }
+            load(pass + 1);
+            float f[kAhead];
+            uint32_t wide = 0;                                  // rows of these that want 64 bits
+            if constexpr (NORM) {
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
-                    x[u] = make_uint4(0, 0, 0, 0);
-                    if (done + u < rows) x[u] = __ldcs(reinterpret_cast<const uint4*>(x_at));
-                    x_at += x_step;
-                }
-                if (done == 0) {                                // (behind the first loads)
-                    if (!ready) {
-                        angles(p, t0, s_cos[buffer], s_sin[buffer]);
-                        __syncthreads();
-                        ready = true;
-                    }
-                    float w[8], wp[8];
-                    if (NORM && a.w != nullptr && have) {
-                        unpack8<DT>(*reinterpret_cast<const uint4*>(a.w + d0), w);
-                        unpack8<DT>(*reinterpret_cast<const uint4*>(a.w + partner * 8), wp);
-                    } else {
+                    float a[8], b[8];
+                    sides<DT, NEAR>(xn[u], yn[u], a, b);
+                    float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) w[i] = wp[i] = 1.0f;
-                    }
+                    for (int i = 0; i < 8; ++i) { s0 = __fmaf_rn(a[i], a[i], s0); s1 = __fmaf_rn(b[i], b[i], s1); }
+                    f[u] = s0 + s1;
+                }
+#pragma unroll
+                for (int off = W / 2; off > 0; off >>= 1)
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) f[u] += __shfl_xor_sync(0xFFFFFFFFu, f[u], off, W);
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    if (u < have && !(f[u] > 1e-25f && f[u] < 1e35f)) wide |= 1u << u;
+                    f[u] = rsqrtf(__fmaf_rn(f[u], 1.0f / static_cast<float>(p.D), static_cast<float>(p.eps)));
+                }
+            }
+            uint16_t* out = side.y + t * side.yt + (static_cast<int64_t>(keys ? from[1] : from[0]) + first + static_cast<int64_t>(done) * step) * side.yh;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                float a[8], b[8];
+                sides<DT, NEAR>(xn[u], yn[u], a, b);
+                if (rotated) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int at = token * half + angle0 + (NEAR ? i / 2 : i);
-                        const bool later = NEAR ? (i & 1) != 0 : second;
-                        const float other = NEAR ? w[i ^ 1] : wp[i];
-                        c[i] = rotated ? s_cos[buffer][at] * w[i] : w[i];
-                        s[i] = rotated ? (later ? s_sin[buffer][at] : -s_sin[buffer][at]) * other : 0.0f;
+                        const float v = __fmaf_rn(a[i], ca[i], -(b[i] * sb[i]));
+                        b[i] = __fmaf_rn(b[i], cb[i], a[i] * sa[i]);
+                        a[i] = v;
                     }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { a[i] *= ca[i]; b[i] *= cb[i]; }
                 }
-                float f[kAhead];
-                uint32_t moved = 0;                             // bits u, u + 4: row u is moved by 2^64, by 2^-64
                 if constexpr (NORM) {
 #pragma unroll
-                    for (int u = 0; u < kAhead; ++u) {
-                        float v[8];
-                        unpack8<DT>(x[u], v);
-                        f[u] = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) f[u] = __fmaf_rn(v[i], v[i], f[u]);
-                    }
-#pragma unroll
-                    for (int off = W / 2; off > 0; off >>= 1)
-#pragma unroll
-                        for (int u = 0; u < kAhead; ++u) f[u] += __shfl_xor_sync(0xFFFFFFFFu, f[u], off, W);
-#pragma unroll
-                    for (int u = 0; u < kAhead; ++u)
-                        if (done + u < rows && !(f[u] > 1e-25f && f[u] < 1e35f)) moved |= f[u] > 1.0f ? 16u << u : 1u << u;
-                    const bool any = __any_sync(0xFFFFFFFFu, moved != 0u);
-#pragma unroll
-                    for (int u = 0; u < kAhead; ++u) {
-                        const float mean = __fmaf_rn(f[u], 1.0f / static_cast<float>(p.D), static_cast<float>(p.eps));
-                        if (any) {                              // squares that fp32 cannot hold, or that are all zero: the sum in 64 bits
-                            const double wide = row_squares<W, DT>(x[u]);
-                            if (moved >> u & 0x11u) f[u] = static_cast<float>(wide_factor(wide, p.D, p.eps) * (moved >> u & 1u ? 0x1p-64 : 0x1p64));
-                            else f[u] = rsqrtf(mean);
-                        } else {
-                            f[u] = rsqrtf(mean);
-                        }
-                    }
+                    for (int i = 0; i < 8; ++i) { a[i] *= f[u]; b[i] *= f[u]; }
                 }
+                uint32_t o[8];
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    if (done + u >= most) break;                // the same for the whole block
-                    float v[8], o[8];
-                    unpack8<DT>(x[u], v);
-                    if constexpr (NEAR) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) o[i] = rotated ? v[i ^ 1] : 0.0f;      // (an infinity times a sine of 0)
-                    } else {
-                        uint4 xp;
-                        xp.x = __shfl_sync(0xFFFFFFFFu, x[u].x, partner, W);
-                        xp.y = __shfl_sync(0xFFFFFFFFu, x[u].y, partner, W);
-                        xp.z = __shfl_sync(0xFFFFFFFFu, x[u].z, partner, W);
-                        xp.w = __shfl_sync(0xFFFFFFFFu, x[u].w, partner, W);
-                        if (!rotated) xp = make_uint4(0, 0, 0, 0);
-                        unpack8<DT>(xp, o);
-                    }
-                    if (NORM && (moved >> u & 0x11u)) {
-                        const float move = moved >> u & 1u ? 0x1p64f : 0x1p-64f;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) { v[i] *= move; o[i] *= move; }
-                    }
-                    float y[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        y[i] = __fmaf_rn(v[i], c[i], o[i] * s[i]);
-                        if constexpr (NORM) y[i] *= f[u];
-                    }
-                    if (done + u < rows)
-                        *reinterpret_cast<uint4*>(y_at) =
-                            make_uint4(pack16x2<DT>(y[0], y[1]), pack16x2<DT>(y[2], y[3]), pack16x2<DT>(y[4], y[5]), pack16x2<DT>(y[6], y[7]));
-                    y_at += y_step;
+                for (int i = 0; i < 8; ++i) {
+                    if constexpr (NEAR) o[i] = pack16x2<DT>(a[i], b[i]);
+                    else o[i] = i < 4 ? pack16x2<DT>(a[(2 * i) & 7], a[(2 * i + 1) & 7]) : pack16x2<DT>(b[(2 * i) & 7], b[(2 * i + 1) & 7]);
                 }
+                if (u < have && !(NORM && (wide >> u & 1u))) {
+                    *reinterpret_cast<uint4*>(out + u * step * side.yh + da) = make_uint4(o[0], o[1], o[2], o[3]);
+                    if (have_b) *reinterpret_cast<uint4*>(out + u * step * side.yh + db) = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+            }
+            if (NORM && __any_sync(0xFFFFFFFFu, wide != 0u)) {
+                const int at = rotated ? token * (p.R / 2) + lane * 8 : 0;
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    wide_row<W, DT, NEAR>(side.w, s_cos[buffer] + at, s_sin[buffer] + at, xn[u], yn[u], p.D, p.eps, rotated, da, db,
+                                          wide >> u & 1u ? out + u * step * side.yh : nullptr);
             }
         }
     }
@@ -274,7 +306,7 @@ static int launch_rotate_rows(const RotateArgs& p, dim3 grid, cudaStream_t st) {
 
 template <int DT>
 static int launch_rotate(RotateArgs& p, bool fast, cudaStream_t st) {
-    const int W = p.D <= 64 ? 8 : p.D <= 128 ? 16 : 32;
+    const int W = p.D <= 64 ? 4 : p.D <= 128 ? 8 : 16;
     const int rows = fast ? kRotateThreads / W : kRotateThreads / 32;
     const int heads = std::max(p.side[0].heads, p.side[1].heads);
     // As many tokens at a time as leave all SMs some blocks; few tokens: a token's heads are shared out, a pass to a block.
@@ -286,9 +318,9 @@ static int launch_rotate(RotateArgs& p, bool fast, cudaStream_t st) {
     const int64_t blocks = std::min<int64_t>(groups, std::max(1, 48 * sm_count() / p.slices));
     const dim3 grid(static_cast<unsigned>(blocks * p.slices));
     if (!fast) return launch_ex(k24_norm_rotate_any<DT>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
+    if (W == 4) return launch_rotate_rows<4, DT>(p, grid, st);
     if (W == 8) return launch_rotate_rows<8, DT>(p, grid, st);
-    if (W == 16) return launch_rotate_rows<16, DT>(p, grid, st);
-    return launch_rotate_rows<32, DT>(p, grid, st);
+    return launch_rotate_rows<16, DT>(p, grid, st);
 }
 
 }  // namespace cq
