@@ -151,8 +151,9 @@ __device__ __forceinline__ int pairs_from(const Sequence& s, int tokens2, int x)
 }
 
 // The items in the order of their work, the longest first: all head groups of a pair of tiles side by side, the pairs of all
-// sequences by the number of their key blocks (found by bisection over that number).  Computed by a whole warp.
-__device__ __forceinline__ bool find_item(const PromptArgs& p, int64_t index, int total_pairs, int most_blocks, PromptItem& it) {
+// sequences by the number of their key blocks.  Computed by a whole warp; `level` holds a number of blocks that no later item passes
+// (at first more than any has): a CTA's items come in falling order, so that the next one's is found in a few steps from there.
+__device__ __forceinline__ bool find_item(const PromptArgs& p, int64_t index, int total_pairs, int& level, PromptItem& it) {
     const int lane = threadIdx.x & 31;
     const int per_pair = p.groups * p.splits;
     const int64_t rank64 = index / per_pair;
@@ -165,11 +166,16 @@ __device__ __forceinline__ bool find_item(const PromptArgs& p, int64_t index, in
         for (int b = lane; b < p.B; b += 32) n += pairs_from(sequence_at(p, b), tokens2, x);
         return __reduce_add_sync(0xFFFFFFFFu, n);
     };
-    int lo = 0, hi = most_blocks + 1;                           // count(lo) > rank, count(hi) <= rank
+    int lo = level, hi = level + 1;                             // in the end count(lo) > rank, count(hi) <= rank
+    for (int down = 1; lo > 0 && count(lo) <= rank; down *= 2) {
+        hi = lo;
+        lo = max(lo - down, 0);
+    }
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (count(mid) > rank) lo = mid; else hi = mid;
     }
+    level = lo;
     int skip = rank - count(hi);                                // of the pairs with exactly lo blocks
     Sequence seq{};
     int pair = -1;
@@ -280,14 +286,14 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");    // 128 x 72 + 256 x 216 = 384 x 168
         if (warp == 8) {
             // ---- items and loads
-            int total = 0, most = 0;
+            int total = 0, level = 0;                           // (at first the most blocks of a sequence)
             for (int b = lane; b < p.B; b += 32) {
                 const Sequence s = sequence_at(p, b);
                 total += pairs_from(s, 2 * p.tokens, 0);
-                if (s.lq > 0) most = max(most, (s.lk + kKeys - 1) / kKeys);
+                if (s.lq > 0) level = max(level, (s.lk + kKeys - 1) / kKeys);
             }
             total = __reduce_add_sync(0xFFFFFFFFu, total);
-            most = __reduce_max_sync(0xFFFFFFFFu, most);
+            level = __reduce_max_sync(0xFFFFFFFFu, level);
             bool ok = true;
             int s = 0;
             uint32_t round = 0, issued = 0, q_round[2] = {0, 0};
@@ -296,7 +302,7 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                 PromptItem it;
                 // in rounds of one item for each CTA, every other one in reverse, so that none gets the longest of each
                 const int64_t index = static_cast<int64_t>(n) * gridDim.x + ((n & 1u) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-                const bool have = find_item(p, index, total, most, it);
+                const bool have = find_item(p, index, total, level, it);
                 if (!have) it.tokens = -1;
                 if (!(ok = warp_wait(&i_empty[n & 1], ((n >> 1) & 1) ^ 1u, &s_dead))) break;
                 if (lane == 0) {

@@ -99,7 +99,7 @@ class AttentionLayer:
 
     def prompts(self, x: torch.Tensor, seqs, lengths, adapters=None) -> torch.Tensor:
         """Prompts of several sequences, packed: the first lengths[0] rows of x are that of sequence seqs[0], and so on;
-        `adapters`: which adapter each sequence has from now on (default: none)."""
+        `adapters`: which adapter each sequence has from now on (outside their range, as by default: none)."""
         seqs = [range(len(self._filled))[s] for s in seqs]
         adapters = [-1] * len(seqs) if adapters is None else list(adapters)
         if len(set(seqs)) != len(seqs) or not len(seqs) == len(lengths) == len(adapters) or sum(lengths) != x.shape[0]:

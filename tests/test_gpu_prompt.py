@@ -99,6 +99,12 @@ def test_packed_prompts(cq, dtype, D, lens):  # noqa: F811
     check(cq, *qkv(sum(lens), (8, 2, 2), D, dtype, len(lens)), lens)
 
 
+def test_more_sequences_than_a_warp_looks_at_at_once(cq):  # noqa: F811
+    lens = [(29 * i) % 41 for i in range(1500)]
+    lens[700], lens[1499] = 400, 0
+    check(cq, *qkv(sum(lens), (2, 1, 1), 64, "bf16", 8), lens)
+
+
 def test_more_items_than_ctas(cq):  # noqa: F811
     lens = [(37 * i) % 301 for i in range(40)]
     check(cq, *qkv(sum(lens), (16, 16, 16), 64, "f16", 3), lens)
