@@ -13,6 +13,7 @@
 #include "cq_adapter.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace cq {
 
@@ -450,13 +451,14 @@ __device__ __forceinline__ void add_rows(const AdapterArgs& p, const float* d, c
 // words between rows of h in shared memory: 8 more than a multiple of 32, so that the rows of a fragment lie in different banks
 template <int MT> __host__ __device__ constexpr int h_pitch() { return MT * 8 + (MT == 1 ? 0 : MT == 2 ? 24 : 8); }
 
-template <int MT, int DT, int YT>
+// SHARE: the block's tokens have their h in shared memory, else each warp takes it from L2.
+template <int MT, int DT, int YT, bool SHARE>
 __global__ void __launch_bounds__(kAdThreads, MT <= 2 ? 3 : 2)
 k26_adapter_out(const AdapterArgs p) {
     constexpr int kPitch = h_pitch<MT>();
     constexpr int kHeld = MT == 8 ? 32 : kWindow;               // tokens whose h is in shared memory at a time
     __shared__ uint8_t s_list[kAdThreads / 32][kWindow];
-    __shared__ __align__(16) uint32_t s_h[2][kHeld][kPitch];
+    __shared__ __align__(16) uint32_t s_h[2][SHARE ? kHeld : 1][kPitch];
     __shared__ float s_d[YT == CQ_F32 ? 1 : kAdThreads / 32][16 * 36];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
     uint8_t* list = s_list[warp];
@@ -497,7 +499,7 @@ k26_adapter_out(const AdapterArgs p) {
             asm volatile("griddepcontrol.wait;" ::: "memory");
             waited = true;
         }
-        const bool few = count <= 16;                           // then h comes from memory, else from shared memory
+        const bool few = !SHARE || count <= 16;
         for (int base = 0; base < count; base += kHeld) {
             const int held = min(kHeld, count - base), pieces = p.R / 8;         // 16 bytes each
             if (!few) {
@@ -603,16 +605,24 @@ static int launch_adapter(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     else rc = launch_ex(k25_adapter_in<MT, DT>, grid, kAdThreads, smem, st, grid.x, !tuning_no_pdl(), p);
     if (rc != CQ_OK) return rc;
     if (p.tiles) return launch_adapter_out_tiles(p, DT, y_dtype, st);
-    // two, four or eight warps to a block: the most with which there are two blocks an SM
+    // two, four or eight warps to a block: the most with which there are two blocks an SM (50 x 1003, rank 128: 41.5 us with two, 45.6 with eight)
     int warps = 8;
     while (warps > 2 && windows * adapters * ((p.N + 32 * warps - 1) / (32 * warps)) < 2 * sms) warps /= 2;
     const int64_t cols = (p.N + 32 * warps - 1) / (32 * warps);
     const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(adapters, 16 * sms / (windows * cols)));
     const dim3 grid2(static_cast<unsigned>(cols), static_cast<unsigned>(windows), static_cast<unsigned>(turns));
     const unsigned threads = 32u * warps;
-    if (y_dtype == CQ_F32) return launch_ex(k26_adapter_out<MT, DT, CQ_F32>, grid2, threads, 0, st, 1, !tuning_no_pdl(), p);
-    if (y_dtype == CQ_F16) return launch_ex(k26_adapter_out<MT, DT, CQ_F16>, grid2, threads, 0, st, 1, !tuning_no_pdl(), p);
-    return launch_ex(k26_adapter_out<MT, DT, CQ_BF16>, grid2, threads, 0, st, 1, !tuning_no_pdl(), p);
+    // Blocks that fill the SMs more than once share their tokens' h in shared memory (2223 x 17853, rank 64: 237 us, 298 without); with fewer
+    // that costs more than it saves (64 x 6144, rank 64: 20.2 us without, 24.0 with).
+    const bool share = windows * cols > 2 * sms;
+    auto launch = [&](auto y_type) {
+        constexpr int YT = decltype(y_type)::value;
+        return share ? launch_ex(k26_adapter_out<MT, DT, YT, true>, grid2, threads, 0, st, 1, !tuning_no_pdl(), p)
+                     : launch_ex(k26_adapter_out<MT, DT, YT, false>, grid2, threads, 0, st, 1, !tuning_no_pdl(), p);
+    };
+    if (y_dtype == CQ_F32) return launch(std::integral_constant<int, CQ_F32>());
+    if (y_dtype == CQ_F16) return launch(std::integral_constant<int, CQ_F16>());
+    return launch(std::integral_constant<int, CQ_BF16>());
 }
 
 template <int DT>

@@ -66,7 +66,7 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kTileTokens;
-    const int count = sort_tile(p, t0, s_sort, blockIdx.x == 0);
+    const int count = sort_tile(p, t0, s_sort, blockIdx.x == 0 && blockIdx.z == 0);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -74,13 +74,13 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
     const int rank = blockIdx.x, ranks = gridDim.x;
     const int kblocks = static_cast<int>((p.K + 63) / 64), kb0 = static_cast<int>(static_cast<int64_t>(kblocks) * rank / ranks),
               kb1 = static_cast<int>(static_cast<int64_t>(kblocks) * (rank + 1) / ranks);
-    const int per = kInCols / p.R, groups = (count + per - 1) / per;
+    const int per = kInCols / p.R, groups = (count + per - 1) / per, gr0 = blockIdx.z, turns = gridDim.z;      // this cluster's: gr0, gr0 + turns ..
     if (warp == 0) {
         int s = 0;
         uint32_t round = 0;
         int issued = 0;
         bool ok = true;
-        for (int gr = 0; ok && gr < groups; ++gr) {
+        for (int gr = gr0; ok && gr < groups; gr += turns) {
             const int n = min(per, count - gr * per);
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (!(ok = agreed_wait(&empty[s], round ^ 1u, &s_dead))) break;
@@ -104,10 +104,10 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
         int s = 0;
         uint32_t round = 0;
         bool ok = true;
-        for (int gr = 0; ok && gr < groups; ++gr) {
-            const int b = gr & 1, cols = (min(per, count - gr * per) * p.R + 15) & ~15;
+        for (int gr = gr0, n = 0; ok && gr < groups; gr += turns, ++n) {
+            const int b = n & 1, cols = (min(per, count - gr * per) * p.R + 15) & ~15;
             const uint32_t idesc = idesc_f16<DT>(128, cols, false);
-            if (!(ok = agreed_wait(&d_empty[b], ((gr >> 1) & 1) ^ 1u, &s_dead))) break;
+            if (!(ok = agreed_wait(&d_empty[b], ((n >> 1) & 1) ^ 1u, &s_dead))) break;
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (!(ok = agreed_wait(&full[s], round, &s_dead))) break;
                 tc_fence_after();
@@ -132,11 +132,11 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
         const uint32_t at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         float* h = s_h + token * (p.R + 1);
         bool ok = true;
-        for (int gr = 0; ok && gr < groups; ++gr) {
-            const int b = gr & 1, n = min(per, count - gr * per);
-            if (!(ok = agreed_wait(&d_full[b], (gr >> 1) & 1, &s_dead))) break;
+        for (int gr = gr0, n = 0; ok && gr < groups; gr += turns, ++n) {
+            const int b = n & 1, have = min(per, count - gr * per);
+            if (!(ok = agreed_wait(&d_full[b], (n >> 1) & 1, &s_dead))) break;
             tc_fence_after();
-            for (int i = 0; i < n; ++i) {
+            for (int i = 0; i < have; ++i) {
                 const bool here = mine == gr * per + i;
                 if (!__any_sync(0xFFFFFFFFu, here)) continue;
                 for (int c = 0; c < p.R; c += 8) {
@@ -162,7 +162,7 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
     __syncwarp();
     if (ranks > 1) cluster_barrier();
     for (int m = rank + warp * ranks; m < kTileTokens; m += ranks * (kInThreads / 32))
-        if (s_sort.idx[m] >= 0) finish_token<DT>(p, s_h + m * (p.R + 1), ranks, t0 + m, s_sort.idx[m]);
+        if (s_sort.idx[m] >= 0 && s_sort.slot[m] / per % turns == gr0) finish_token<DT>(p, s_h + m * (p.R + 1), ranks, t0 + m, s_sort.idx[m]);
     __syncwarp();
     if (ranks > 1) cluster_barrier();         // nobody leaves while its sums are being read
     if (tid == 0 && s_dead != 0u) atomicExch(&g_adapter_fault, 1u);
@@ -391,11 +391,12 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
 #pragma unroll
                     for (int q = 0; q < kCols / 32; ++q) tmem_ld_wait(v[q]);
                     if (mine == d) {
+                        uint4 w[8];                             // all at once: one latency instead of eight
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const uint4*>(y + ((c ^ (row & 7)) << 4));
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
-                            uint4* piece = reinterpret_cast<uint4*>(y + ((c ^ (row & 7)) << 4));
-                            const uint4 w = *piece;
-                            const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+                            const uint32_t r[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
                             uint32_t o[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
@@ -407,7 +408,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
                                     o[i] = pack16x2<YT>(__fmaf_rn(v[e >> 5][e & 31], f, b.x), __fmaf_rn(v[e >> 5][(e & 31) + 1], f, b.y));
                                 }
                             }
-                            *piece = make_uint4(o[0], o[1], o[2], o[3]);
+                            *reinterpret_cast<uint4*>(y + ((c ^ (row & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
                         }
                     }
                     __syncwarp();
@@ -469,6 +470,35 @@ static int launch_out_tiles(const AdapterArgs& p, cudaStream_t st) {
     return launch_ex(k28_adapter_out_tiles<HB, DT, YT>, dim3(grid), kOutThreads, smem, st, 1, !tuning_no_pdl(), high, low, b, y, out, p, group);
 }
 
+// Clusters of 2^i blocks that are resident at one time (asked once for a device and size of shared memory).
+constexpr int kMaxParts = 4;
+template <typename Kernel>
+static int resident_clusters(Kernel* kernel, int i, size_t smem) {
+    struct Known { int device; size_t smem; int n[kMaxParts]; };
+    static thread_local Known known[2] = {{-1, 0, {}}, {-1, 0, {}}};
+    int device = -1;
+    if (cudaGetDevice(&device) != cudaSuccess) return 0;
+    Known& k = known[smem == in_smem(kMaxRank) ? 1 : 0];
+    if (k.device != device || k.smem != smem) k = {device, smem, {}};
+    if (k.n[i] == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 1u << i;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.gridDim = dim3(1u << i, 1, 1);
+        cfg.blockDim = dim3(kInThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&k.n[i], kernel, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            k.n[i] = 0;
+        }
+    }
+    return k.n[i];
+}
+
 template <int DT>
 static int launch_in_tiles(const AdapterArgs& p, cudaStream_t st) {
     CUtensorMap x, a;
@@ -477,10 +507,22 @@ static int launch_in_tiles(const AdapterArgs& p, cudaStream_t st) {
     static thread_local LaunchMemo memo;
     const size_t smem = in_smem(p.R);
     if (resident_ctas(k27_adapter_in_tiles<DT>, kInThreads, smem, std::max(in_smem(64), in_smem(kMaxRank)), memo) < 1) return CQ_ERR_CUDA;
-    // as many parts of the contraction, four blocks of 64 each or more, as leave one block an SM
-    const int64_t tiles = (p.T + kTileTokens - 1) / kTileTokens;
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, (p.K + 63) / 64 / 4), sm_count() / tiles));
-    return launch_ex(k27_adapter_in_tiles<DT>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(tiles)), kInThreads, smem, st,
+    // The parts of the contraction, four blocks of 64 or more to each, with which tiles of few adapters end first, as those of prompts do; then, as
+    // far as there is room, several clusters a tile, which share out the groups of 128 / R adapters that it may have (a tile with fewer
+    // leaves the others idle).
+    const int64_t tiles = (p.T + kTileTokens - 1) / kTileTokens, per = kInCols / p.R, blocks = (p.K + 63) / 64;
+    const int64_t groups = (std::min<int64_t>(p.n, kTileTokens) + per - 1) / per;
+    int64_t parts = 1, turns = 1, least = INT64_MAX;
+    for (int i = kMaxParts - 1; i >= 0; --i) {
+        const int64_t n = int64_t(1) << i, room = resident_clusters(k27_adapter_in_tiles<DT>, i, smem);
+        if (room < 1) return CQ_ERR_CUDA;
+        const int64_t length = (tiles + room - 1) / room * ((blocks + n - 1) / n);
+        if ((n > 1 && blocks < 4 * n) || length >= least) continue;
+        least = length;
+        parts = n;
+        turns = std::max<int64_t>(1, std::min(groups, room / tiles));
+    }
+    return launch_ex(k27_adapter_in_tiles<DT>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(tiles), static_cast<unsigned>(turns)), kInThreads, smem, st,
                      static_cast<unsigned>(parts), !tuning_no_pdl(), x, a, p, in_stages(p.R));
 }
 int launch_adapter_in_tiles(const AdapterArgs& p, int dtype, cudaStream_t st) {

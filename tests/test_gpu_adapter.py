@@ -100,6 +100,14 @@ def test_many_tokens(cq, T, K, N, n, R):  # noqa: F811
     check(cq, y.float(), x, ad, some_index(T, n, R, "runs"))
 
 
+@pytest.mark.parametrize("T,n", ((128, 1), (128, 128), (300, 90), (1200, 33)))
+def test_clusters_that_share_out_a_tiles_adapters(cq, T, n):  # noqa: F811
+    for R in (8, 16, 64):
+        y, x = tokens(T, 2056, 264, "f16", n + R)
+        for kind in ("turns", "one"):
+            check(cq, y, x, adapters(cq, n, 2056, 264, R, "f16", R), some_index(T, n, n, kind))
+
+
 def test_long_contractions_and_wide_results(cq):  # noqa: F811
     for T, K, N, R in ((3, 8192, 6000, 16), (90, 8200, 2048, 64), (150, 8192, 2048, 128)):
         y, x = tokens(T, K, N, "bf16", T)
