@@ -102,12 +102,12 @@ __device__ __noinline__ void wide_row(const uint16_t* w, const float* s_cos, con
 // kRows / group heads at a time.
 constexpr int kMaxGroup = 8;
 constexpr int kFastDim = 256;
+constexpr int kAhead = 2;                                      // rows of a lane in a pass
 
 template <int W, int DT, bool NORM, bool NEAR>                 // NEAR: neighbours are pairs
 __global__ void __launch_bounds__(kRotateThreads, NORM ? 2 : 3)
 k24_norm_rotate(const RotateArgs p) {
     constexpr int kRows = kRotateThreads / W;
-    constexpr int kAhead = 2;                                   // rows of a pass
     __shared__ float s_cos[2][kMaxGroup * kFastDim / 2], s_sin[2][kMaxGroup * kFastDim / 2];
     asm volatile("griddepcontrol.launch_dependents;");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -309,13 +309,16 @@ static int launch_rotate(RotateArgs& p, bool fast, cudaStream_t st) {
     const int W = p.D <= 64 ? 4 : p.D <= 128 ? 8 : 16;
     const int rows = fast ? kRotateThreads / W : kRotateThreads / 32;
     const int heads = std::max(p.side[0].heads, p.side[1].heads);
-    // As many tokens at a time as leave all SMs some blocks; few tokens: a token's heads are shared out, a pass to a block.
+    // Persistent blocks.  As many tokens at a time as leave an SM one group of them (two without norms, whose groups take less): 500 tokens x 72
+    // heads of 128 with norms 8.1 us, two groups 11.9, one token at a time 11.9; 777 x 80 of 64 without norms 6.7, one group 7.7.  Few tokens:
+    // a token's heads are shared out, a pass or more to a block, while all blocks are resident.
+    const int64_t resident = (!fast ? 6 : p.norm ? 2 : 3) * sm_count();
     p.group = 1;
-    while (fast && p.group < kMaxGroup && p.T / (2 * p.group) >= 2 * sm_count()) p.group *= 2;
+    while (fast && p.group < kMaxGroup && p.T / (2 * p.group) >= (p.norm ? 1 : 2) * sm_count()) p.group *= 2;
     const int64_t groups = (p.T + p.group - 1) / p.group;
-    const int64_t most = std::max(1, (heads + rows - 1) / rows);
-    p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 6 * sm_count() / groups)));
-    const int64_t blocks = std::min<int64_t>(groups, std::max(1, 48 * sm_count() / p.slices));
+    const int64_t most = std::max(1, (heads + rows - 1) / rows / (fast ? kAhead : 1));
+    p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, resident / groups)));
+    const int64_t blocks = std::min<int64_t>(groups, resident / p.slices);
     const dim3 grid(static_cast<unsigned>(blocks * p.slices));
     if (!fast) return launch_ex(k24_norm_rotate_any<DT>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
     if (W == 4) return launch_rotate_rows<4, DT>(p, grid, st);
