@@ -424,7 +424,7 @@ int cq_adapter_add(const void* X, int dtype, int64_t T, int64_t K, int64_t ldx, 
                    int64_t R, int64_t N, const int* index, const void* y, int y_dtype, int64_t ldy, void* out, int64_t ldo,
                    void* workspace, size_t workspace_bytes, void* stream);
 
-/* Health check of the product and the attentions, as cq_stage_fault is of the quantizers: 1 if a bounded wait in one of their
+/* Health check of the product, the attentions and the adapters, as cq_stage_fault is of the quantizers: 1 if a bounded wait in one of their
  * kernels ever gave up on the current device.  Synchronises the device. */
 int cq_serve_fault(unsigned int* fault_host);
 

@@ -1018,7 +1018,8 @@ def adapter_add(y: torch.Tensor, x: torch.Tensor, adapters: Adapters, index: tor
 
 
 def serve_fault() -> int:
-    """1 if a bounded wait of fp8_matmul, fp8_linear, kv_attention or prompt_attention ever gave up on the current device, else 0."""
+    """1 if a bounded wait of fp8_matmul, fp8_linear, kv_attention, prompt_attention or adapter_add ever gave up on the current
+    device, else 0."""
     flag = C.c_uint(0)
     _check(lib().cq_serve_fault(C.byref(flag)), "cq_serve_fault")
     return int(flag.value)

@@ -7,6 +7,9 @@
 //        is split over a cluster and joined through distributed shared memory in rank order
 //   k28  out = y + B h: persistent over 128 x 256-byte tiles of y; those stream through a ring in shared memory in which the
 //        epilogue adds the product to the rows that have the adapter at hand.  Bound by HBM (y in, out out)
+// Measured (operands not in L2): 4096 x 8192 x 28672, rank 64, both 112 us (556 MB, 5.0 TB/s of 6.6 of a copy), k28 by itself 83 us (485 MB, 5.8 TB/s).  A tile of
+// many adapters is bound by the round of signals for each: 1024 x 8192 x 8192 with 55 of 64 adapters in every tile, rank 16, 190 us, 0.45 us an
+// adapter and tile of columns in k28, of which neither its rows of B nor its epilogue are more than 15 %.
 #include "cq_adapter.cuh"
 
 #include <algorithm>
@@ -438,7 +441,8 @@ int adapter_stage_fault(unsigned int* fault_host) {
     return cudaMemcpyFromSymbol(fault_host, g_adapter_fault, sizeof(unsigned int)) == cudaSuccess ? CQ_OK : CQ_ERR_CUDA;
 }
 
-// A tile of fewer than 128 tokens is mostly empty, and what a tensor map cannot hold goes the other way too.
+// A tile of fewer than 128 tokens is mostly empty (40 tokens on 8 adapters x 4096 x 6144, rank 16: 18.0 us, 9.9 in windows; 128 x 8192 x 8192 on 64 adapters
+// 48.8 us, 89 in windows; on one 16.5, 18.1), and what a tensor map cannot hold goes the other way too.
 constexpr int64_t kMapMost = (int64_t(1) << 31) - 1024;
 bool adapter_in_tiles(const AdapterArgs& p) {
     return p.T >= kTileTokens && p.K >= 64 && p.n >= 1 && p.vec_k == 8 && 2 * p.K < kMapMost && static_cast<int64_t>(p.n) * p.R < kMapMost &&

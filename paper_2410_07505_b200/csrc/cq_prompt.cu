@@ -17,9 +17,9 @@
 // exponentials 62 %.  Everything the softmax issues delays the products as well: a product costs its warp some 30 issue slots, which it shares
 // with two softmax warps.  Tried and dropped: logits in two buffers of 64 keys (products of 64 columns are bound by shared memory, 970 us),
 // two threads to a row (1220 us), a share of the exponentials by polynomial (895 us).
-// Measured (GPU alone, operands not in L2): 1 x 8192 tokens, 64 / 8 heads of 128, bf16 889 us (1240 TFLOP/s; 1090 in a long run, which the power limit
-// sets); 12 packed prompts up to 2060 tokens, 64 / 8 heads, fp16 350 us; 1000 tokens behind 19011, 32 heads of 64 260 us (bound by exponentials:
-// 139 us at one a lane and clock); 1000 tokens, 32 / 8 heads 28.6 us.
+// Measured (GPU alone, operands not in L2): 1 x 8192 tokens, 64 / 8 heads of 128, bf16 869 us (1265 TFLOP/s; 1090 in a long run, which the power limit
+// sets); 12 packed prompts up to 2060 tokens, 64 / 8 heads, fp16 338 us; 1000 tokens behind 19011, 32 heads of 64 257 us (bound by exponentials:
+// 139 us at one a lane and clock); 1000 tokens, 32 / 8 heads 26.7 us.
 #include "cq_serve.cuh"
 
 #include <algorithm>
@@ -675,7 +675,7 @@ int prompt_stage_fault(unsigned int* fault_host) {
 
 // Query heads of a key head that share a tile: the largest divisor of G up to 16 whose tiles have at least 120 of 128 rows.
 // (All rows of a tile read the same keys, so heads side by side make the tile's tokens few: less of the diagonal is computed in vain,
-// and short sequences leave fewer rows empty.)
+// and short sequences leave fewer rows empty: 12 prompts up to 100 tokens, 32 / 8 heads of 128 17.4 us, 25.9 with a head a tile; 8192 tokens 469, 474.)
 static int heads_of_tile(int G) {
     for (int g = G < 16 ? G : 16; g > 1; --g)
         if (G % g == 0 && g * (kTileRows / g) >= 120) return g;
@@ -690,7 +690,8 @@ static PromptPlan prompt_plan(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int
     r.tokens = kTileRows / r.g;
     r.groups = static_cast<int>(Hq / r.g);
     r.items = (Tq / (2 * r.tokens) + std::min(B, Tq)) * r.groups;        // at most
-    // Items for less than half of the SMs: the keys of each are split, four blocks or more to a part.
+    // Items for less than half of the SMs: the keys of each are split, four blocks or more to a part (100 tokens behind 19000, 8 heads of 128: 36 us
+    // with the join, 238 in one part; behind 1000, 16 heads: 22.7, 30.0).
     int64_t splits = r.items > 0 ? sm_count() / r.items : 1;
     splits = std::min(splits, Tk / std::max<int64_t>(B, 1) / (4 * kKeys));
     r.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(splits, kMaxSplits)));
