@@ -193,7 +193,117 @@ __device__ __forceinline__ OutItem out_items(const AdapterArgs& p, int width, in
     return {items * at / groups + blockIdx.x % group, items * (at + 1) / groups, group, cols};
 }
 
-template <int HB, int DT, int YT>
+// y + f v, rounded once, for half a row of a tile in shared memory
+template <int YT, int Q>
+__device__ __forceinline__ void add_to_row(uint8_t* y, int row, const float (&v)[Q][32], float f) {
+    uint4 w[8];                                                 // all at once: one latency instead of eight
+#pragma unroll
+    for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const uint4*>(y + ((c ^ (row & 7)) << 4));
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const uint32_t r[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (YT == CQ_F32) {
+                o[i] = __float_as_uint(__fmaf_rn(v[0][4 * c + i], f, __uint_as_float(r[i])));
+            } else {
+                const float2 b = unpack16x2<YT>(r[i]);
+                const int e = 8 * c + 2 * i;
+                o[i] = pack16x2<YT>(__fmaf_rn(v[e >> 5][e & 31], f, b.x), __fmaf_rn(v[e >> 5][(e & 31) + 1], f, b.y));
+            }
+        }
+        *reinterpret_cast<uint4*>(y + ((c ^ (row & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+// Rows of y (and out) that begin anywhere, which no tensor map takes: a warp has sixteen rows of a tile, 64 words of a row in two registers a lane.
+// A row that begins in the middle of a word is moved by half a word on its way into shared memory and out of it; its last element, in a
+// word of its own, is in lane `row` of `edge`.
+struct LooseRows { uint32_t w[16][2]; uint32_t edge; };
+
+template <int YT>
+__device__ __forceinline__ int begins_odd(const void* base, int64_t at) {
+    return YT == CQ_F32 ? 0 : static_cast<int>((reinterpret_cast<uintptr_t>(base) >> 1) + at) & 1;
+}
+template <int YT>
+__device__ __forceinline__ void fetch_rows(const AdapterArgs& p, int64_t t0, int64_t col, LooseRows& v) {
+    constexpr int kPer = YT == CQ_F32 ? 1 : 2, kElem = 4 / kPer, CT = out_cols<YT>();
+    const int lane = threadIdx.x & 31, left = static_cast<int>(min(p.N - col, static_cast<int64_t>(CT)));
+    const uint8_t* y = static_cast<const uint8_t*>(p.y);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int64_t at = (t0 + i) * p.ldy + col;
+        const int odd = begins_odd<YT>(y, at);
+        const uint32_t* words = reinterpret_cast<const uint32_t*>(y + (at - odd) * kElem);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int q = lane + 32 * h;
+            v.w[i][h] = t0 + i < p.T && kPer * q - odd < left ? __ldcg(words + q) : 0u;      // (a word that holds an element of the tile)
+        }
+    }
+    v.edge = 0;
+    if constexpr (YT != CQ_F32) {
+        const int64_t at = (t0 + lane) * p.ldy + col;
+        if (lane < 16 && t0 + lane < p.T && left == CT && begins_odd<YT>(y, at) != 0) v.edge = __ldcg(reinterpret_cast<const uint16_t*>(y) + at + CT - 1);
+    }
+}
+__device__ __forceinline__ uint32_t* loose_word(uint8_t* tile, int row, int h) {
+    const int lane = threadIdx.x & 31;
+    return reinterpret_cast<uint32_t*>(tile + h * kXTile + row * 128 + (((lane >> 2) ^ (row & 7)) << 4)) + (lane & 3);
+}
+template <int YT>
+__device__ __forceinline__ void rows_to_tile(const AdapterArgs& p, int64_t t0, int64_t col, const LooseRows& v, uint8_t* tile, int row0) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        uint32_t a = v.w[i][0], b = v.w[i][1];
+        if (begins_odd<YT>(p.y, (t0 + i) * p.ldy + col) != 0) {                 // (the same for the whole warp)
+            uint32_t next_a = __shfl_down_sync(0xFFFFFFFFu, a, 1), next_b = __shfl_down_sync(0xFFFFFFFFu, b, 1);
+            const uint32_t first_b = __shfl_sync(0xFFFFFFFFu, b, 0), edge = __shfl_sync(0xFFFFFFFFu, v.edge, i);
+            if (lane == 31) { next_a = first_b; next_b = edge; }
+            a = __funnelshift_r(a, next_a, 16);
+            b = __funnelshift_r(b, next_b, 16);
+        }
+        *loose_word(tile, row0 + i, 0) = a;
+        *loose_word(tile, row0 + i, 1) = b;
+    }
+}
+template <int YT>
+__device__ __forceinline__ void tile_to_rows(const AdapterArgs& p, int64_t t0, int64_t col, uint8_t* tile, int row0) {
+    constexpr int kPer = YT == CQ_F32 ? 1 : 2, kElem = 4 / kPer, CT = out_cols<YT>();
+    const int lane = threadIdx.x & 31, left = static_cast<int>(min(p.N - col, static_cast<int64_t>(CT)));
+    uint8_t* out = static_cast<uint8_t*>(p.out);
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+        if (t0 + i >= p.T) break;
+        const int64_t at = (t0 + i) * p.ldo + col;
+        const int odd = begins_odd<YT>(out, at);
+        uint32_t w[2] = {*loose_word(tile, row0 + i, 0), *loose_word(tile, row0 + i, 1)};
+        if (odd != 0) {
+            if (lane == 31 && left == CT) reinterpret_cast<uint16_t*>(out)[at + CT - 1] = static_cast<uint16_t>(w[1] >> 16);
+            uint32_t before_a = __shfl_up_sync(0xFFFFFFFFu, w[0], 1), before_b = __shfl_up_sync(0xFFFFFFFFu, w[1], 1);
+            const uint32_t last_a = __shfl_sync(0xFFFFFFFFu, w[0], 31);
+            if (lane == 0) before_b = last_a;
+            w[0] = __funnelshift_r(before_a, w[0], 16);
+            w[1] = __funnelshift_r(before_b, w[1], 16);
+        }
+        uint32_t* words = reinterpret_cast<uint32_t*>(out + (at - odd) * kElem);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int q = lane + 32 * h, e = kPer * q - odd;    // the word's first element
+            if (e >= 0 && e + kPer <= left) {
+                words[q] = w[h];
+            } else if constexpr (kPer == 2) {
+                uint16_t* halves = reinterpret_cast<uint16_t*>(words + q);
+                if (e >= 0 && e < left) halves[0] = static_cast<uint16_t>(w[h]);
+                if (e + 1 >= 0 && e + 1 < left) halves[1] = static_cast<uint16_t>(w[h] >> 16);
+            }
+        }
+    }
+}
+
+template <int HB, int DT, int YT, bool LOOSE>                  // LOOSE: rows of y and out begin anywhere
 __global__ void __launch_bounds__(kOutThreads, 1)
 k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_constant__ CUtensorMap mapLow, const __grid_constant__ CUtensorMap mapB,
                       const __grid_constant__ CUtensorMap mapY, const __grid_constant__ CUtensorMap mapOut, const AdapterArgs p, int group) {
@@ -233,8 +343,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
         prefetch_map(&mapHigh);
         prefetch_map(&mapLow);
         prefetch_map(&mapB);
-        prefetch_map(&mapY);
-        prefetch_map(&mapOut);
+        if (!LOOSE) { prefetch_map(&mapY); prefetch_map(&mapOut); }
     }
     if (warp == 1) tmem_alloc(&s_tmem, kOutBuffers * CT);
     tc_fence_before();
@@ -254,14 +363,16 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
             const int64_t tl = it / work.cols;
             const int col = static_cast<int>(it - tl * work.cols) * CT;
             const int32_t t0 = static_cast<int32_t>(tl) * kTileTokens;
-            if (!(ok = agreed_wait(&y_empty[ys], y_round ^ 1u, &s_dead))) break;
-            if (elect_one()) {
-                mbar_expect_tx(&y_full[ys], static_cast<uint32_t>(kYTile));
-                tile_load(s_y + ys * kYTile, &mapY, col * (YT == CQ_F32 ? 4 : 2), t0, &y_full[ys]);
-                tile_load(s_y + ys * kYTile + kXTile, &mapY, col * (YT == CQ_F32 ? 4 : 2) + 128, t0, &y_full[ys]);
+            if constexpr (!LOOSE) {
+                if (!(ok = agreed_wait(&y_empty[ys], y_round ^ 1u, &s_dead))) break;
+                if (elect_one()) {
+                    mbar_expect_tx(&y_full[ys], static_cast<uint32_t>(kYTile));
+                    tile_load(s_y + ys * kYTile, &mapY, col * (YT == CQ_F32 ? 4 : 2), t0, &y_full[ys]);
+                    tile_load(s_y + ys * kYTile + kXTile, &mapY, col * (YT == CQ_F32 ? 4 : 2) + 128, t0, &y_full[ys]);
+                }
+                y_issued = min(y_issued + 1, SY);
+                if (++ys == SY) { ys = 0; y_round ^= 1u; }
             }
-            y_issued = min(y_issued + 1, SY);
-            if (++ys == SY) { ys = 0; y_round ^= 1u; }
             if (tl != tile) {
                 tile = tl;
                 info = p.info + tl * kTileInfo;
@@ -344,7 +455,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
             if (elect_one()) tc_commit(drain);
             for (uint32_t polls = 0; polls < (1u << 21) && !mbar_try(drain, 0); ++polls) {}
         }
-    } else if (warp == 2) {
+    } else if (warp == 2 && !LOOSE) {
         int ys = 0;
         uint32_t y_round = 0;
         bool ok = true;
@@ -373,7 +484,20 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
         float f = 0.0f;
         int64_t tile = -1;
         bool ok = true;
-        for (int64_t it = work.first; ok && it < work.end; it += work.step) {
+        // LOOSE: these warps bring the rows of y themselves, those of the next item while this one is worked on; all eight meet at barriers on
+        // either side of the additions, also after a wait that gave up.
+        LooseRows rows;
+        const int row0 = (warp - 4) * 16;
+        auto place = [&](int64_t it, int64_t& t, int64_t& col) {
+            t = it / work.cols * kTileTokens + row0;
+            col = it % work.cols * CT;
+        };
+        int64_t t_in = 0, col_in = 0;
+        if constexpr (LOOSE) {
+            place(work.first, t_in, col_in);
+            if (work.first < work.end) fetch_rows<YT>(p, t_in, col_in, rows);
+        }
+        for (int64_t it = work.first; (ok || LOOSE) && it < work.end; it += work.step) {
             const int64_t tl = it / work.cols;
             if (tl != tile) {
                 tile = tl;
@@ -382,9 +506,19 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
                 mine = t < p.T ? __ldcg(p.slot + t) : -1;
                 f = mine >= 0 ? __ldcg(p.factor + t) : 0.0f;
             }
-            if (!(ok = agreed_wait(&y_full[ys], y_round, &s_dead))) break;
+            const int64_t t_out = t_in, col_out = col_in;
+            if constexpr (LOOSE) {
+                rows_to_tile<YT>(p, t_in, col_in, rows, s_y, row0);
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (it + work.step < work.end) {
+                    place(it + work.step, t_in, col_in);
+                    fetch_rows<YT>(p, t_in, col_in, rows);
+                }
+            } else {
+                if (!(ok = agreed_wait(&y_full[ys], y_round, &s_dead))) break;
+            }
             uint8_t* y = s_y + ys * kYTile + half * kXTile + row * 128;
-            for (int d = 0; d < count; ++d) {
+            for (int d = 0; ok && d < count; ++d) {
                 if (!(ok = agreed_wait(&d_full[db], d_round, &s_dead))) break;
                 tc_fence_after();
                 if (__any_sync(0xFFFFFFFFu, mine == d)) {
@@ -394,25 +528,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
 #pragma unroll
                     for (int q = 0; q < kCols / 32; ++q) tmem_ld_wait(v[q]);
                     if (mine == d) {
-                        uint4 w[8];                             // all at once: one latency instead of eight
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) w[c] = *reinterpret_cast<const uint4*>(y + ((c ^ (row & 7)) << 4));
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            const uint32_t r[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
-                            uint32_t o[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if constexpr (YT == CQ_F32) {
-                                    o[i] = __float_as_uint(__fmaf_rn(v[0][4 * c + i], f, __uint_as_float(r[i])));
-                                } else {
-                                    const float2 b = unpack16x2<YT>(r[i]);
-                                    const int e = 8 * c + 2 * i;
-                                    o[i] = pack16x2<YT>(__fmaf_rn(v[e >> 5][e & 31], f, b.x), __fmaf_rn(v[e >> 5][(e & 31) + 1], f, b.y));
-                                }
-                            }
-                            *reinterpret_cast<uint4*>(y + ((c ^ (row & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-                        }
+                        add_to_row<YT>(y, row, v, f);
                     }
                     __syncwarp();
                 }
@@ -421,11 +537,17 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
                 if (lane == 0) mbar_arrive(&d_empty[db]);
                 if (++db == kOutBuffers) { db = 0; d_round ^= 1u; }
             }
-            if (!ok) break;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&o_full[ys]);
-            if (++ys == SY) { ys = 0; y_round ^= 1u; }
+            if constexpr (LOOSE) {
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                tile_to_rows<YT>(p, t_out, col_out, s_y, row0);
+                __syncwarp();
+            } else {
+                if (!ok) break;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&o_full[ys]);
+                if (++ys == SY) { ys = 0; y_round ^= 1u; }
+            }
         }
     }
     tc_fence_before();
@@ -450,28 +572,28 @@ bool adapter_in_tiles(const AdapterArgs& p) {
 }
 bool adapter_out_tiles(const AdapterArgs& p, int y_dtype) {
     const int64_t elem = y_dtype == CQ_F32 ? 4 : 2;
-    return p.T >= kTileTokens && p.n >= 1 && p.vec_n == 16 / elem && elem * p.N < kMapMost && p.n * p.N < kMapMost && p.ldy < (int64_t(1) << 37) &&
-           p.ldo < (int64_t(1) << 37);
+    return p.T >= kTileTokens && p.n >= 1 && elem * p.N < kMapMost && p.n * p.N < kMapMost && p.ldy < (int64_t(1) << 37) && p.ldo < (int64_t(1) << 37);
 }
 
-template <int HB, int DT, int YT>
+template <int HB, int DT, int YT, bool LOOSE>
 static int launch_out_tiles(const AdapterArgs& p, cudaStream_t st) {
     constexpr int64_t elem = YT == CQ_F32 ? 4 : 2;
     CUtensorMap high, low, b, y, out;
     const auto sw = CU_TENSOR_MAP_SWIZZLE_128B;
     if (!make_byte_map(&high, p.high, 2 * p.R, p.T, 2 * p.R, 128, kTileTokens, sw) || !make_byte_map(&low, p.low, 2 * p.R, p.T, 2 * p.R, 128, kTileTokens, sw) ||
-        !make_byte_map(&b, p.B, 2 * p.R, p.n * p.N, 2 * p.R, 128, out_cols<YT>(), sw) ||
-        !make_byte_map(&y, p.y, elem * p.N, p.T, elem * p.ldy, 128, kTileTokens, sw) ||
-        !make_byte_map(&out, p.out, elem * p.N, p.T, elem * p.ldo, 128, kTileTokens, sw)) return CQ_ERR_CUDA;
+        !make_byte_map(&b, p.B, 2 * p.R, p.n * p.N, 2 * p.R, 128, out_cols<YT>(), sw)) return CQ_ERR_CUDA;
+    if constexpr (LOOSE) y = out = b;         // (not used)
+    else if (!make_byte_map(&y, p.y, elem * p.N, p.T, elem * p.ldy, 128, kTileTokens, sw) ||
+             !make_byte_map(&out, p.out, elem * p.N, p.T, elem * p.ldo, 128, kTileTokens, sw)) return CQ_ERR_CUDA;
     static thread_local LaunchMemo memo;
     constexpr size_t smem = out_smem<HB, YT>();
-    if (resident_ctas(k28_adapter_out_tiles<HB, DT, YT>, kOutThreads, smem, smem, memo) < 1) return CQ_ERR_CUDA;
+    if (resident_ctas(k28_adapter_out_tiles<HB, DT, YT, LOOSE>, kOutThreads, smem, smem, memo) < 1) return CQ_ERR_CUDA;
     const int64_t items = (p.T + kTileTokens - 1) / kTileTokens * ((p.N + out_cols<YT>() - 1) / out_cols<YT>());
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>(items, sm_count()));
     // blocks in groups that take neighbouring columns at one time, so that rows of y pass through memory in long pieces: 4096 x 28672
     // 131 us with every block on a run of its own, 127 in groups of 4, 105 of 37 (a quarter of the SMs), 109 of 74, 114 of 148
     const int group = grid >= 16 && grid % 4 == 0 ? grid / 4 : 1;
-    return launch_ex(k28_adapter_out_tiles<HB, DT, YT>, dim3(grid), kOutThreads, smem, st, 1, !tuning_no_pdl(), high, low, b, y, out, p, group);
+    return launch_ex(k28_adapter_out_tiles<HB, DT, YT, LOOSE>, dim3(grid), kOutThreads, smem, st, 1, !tuning_no_pdl(), high, low, b, y, out, p, group);
 }
 
 // Clusters of 2^i blocks that are resident at one time (asked once for a device and size of shared memory).
@@ -533,14 +655,18 @@ int launch_adapter_in_tiles(const AdapterArgs& p, int dtype, cudaStream_t st) {
     return dtype == CQ_F16 ? launch_in_tiles<CQ_F16>(p, st) : launch_in_tiles<CQ_BF16>(p, st);
 }
 
+template <int HB, int DT, int YT>
+static int launch_out_rows(const AdapterArgs& p, cudaStream_t st) {
+    return p.vec_n == (YT == CQ_F32 ? 4 : 8) ? launch_out_tiles<HB, DT, YT, false>(p, st) : launch_out_tiles<HB, DT, YT, true>(p, st);
+}
+template <int HB, int DT>
+static int launch_out_type(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
+    if (y_dtype == CQ_F32) return launch_out_rows<HB, DT, CQ_F32>(p, st);
+    return y_dtype == CQ_F16 ? launch_out_rows<HB, DT, CQ_F16>(p, st) : launch_out_rows<HB, DT, CQ_BF16>(p, st);
+}
 template <int DT>
 static int launch_out_rank(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
-    if (p.R <= 64) {
-        if (y_dtype == CQ_F32) return launch_out_tiles<1, DT, CQ_F32>(p, st);
-        return y_dtype == CQ_F16 ? launch_out_tiles<1, DT, CQ_F16>(p, st) : launch_out_tiles<1, DT, CQ_BF16>(p, st);
-    }
-    if (y_dtype == CQ_F32) return launch_out_tiles<2, DT, CQ_F32>(p, st);
-    return y_dtype == CQ_F16 ? launch_out_tiles<2, DT, CQ_F16>(p, st) : launch_out_tiles<2, DT, CQ_BF16>(p, st);
+    return p.R <= 64 ? launch_out_type<1, DT>(p, y_dtype, st) : launch_out_type<2, DT>(p, y_dtype, st);
 }
 int launch_adapter_out_tiles(const AdapterArgs& p, int dtype, int y_dtype, cudaStream_t st) {
     return dtype == CQ_F16 ? launch_out_rank<CQ_F16>(p, y_dtype, st) : launch_out_rank<CQ_BF16>(p, y_dtype, st);

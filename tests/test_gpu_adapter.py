@@ -108,6 +108,28 @@ def test_clusters_that_share_out_a_tiles_adapters(cq, T, n):  # noqa: F811
             check(cq, y, x, adapters(cq, n, 2056, 264, R, "f16", R), some_index(T, n, n, kind))
 
 
+@pytest.mark.parametrize("dtype", ("bf16", "f16", "f32"))
+@pytest.mark.parametrize("N", (1, 127, 128, 129, 255, 258, 1003, 20011))
+def test_many_tokens_whose_rows_begin_anywhere(cq, N, dtype):  # noqa: F811
+    """Rows at every place of a word, ends inside tiles, in place, and results that begin elsewhere than y."""
+    T, K, n = 300, 72, 5
+    y, x = tokens(T, K, N, "bf16", N)
+    y = y.to({"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[dtype])
+    ad, index = adapters(cq, n, K, N, 16, "bf16", N), some_index(T, n, N, "mixed")
+    check(cq, y, x, ad, index)
+    for first, pitch in ((0, N + 1), (1, N + 2), (3, N + 4)):
+        room = torch.full((T, pitch + 3), 7.0, dtype=y.dtype, device="cuda")
+        room[:, first:first + N] = y
+        here = room[:, first:first + N]
+        check(cq, here, x, ad, index, out=torch.empty(T, N, dtype=y.dtype, device="cuda"))
+        check(cq, y, x, ad, index, out=here)
+        room[:, first:first + N] = y
+        want = cq.adapter_add(y, x, ad, index)
+        cq.adapter_add(here, x, ad, index, out=here)
+        assert torch.equal(here, want)
+        assert bool((room[:, :first] == 7).all()) and bool((room[:, first + N:] == 7).all())
+
+
 def test_long_contractions_and_wide_results(cq):  # noqa: F811
     for T, K, N, R in ((3, 8192, 6000, 16), (90, 8200, 2048, 64), (150, 8192, 2048, 128)):
         y, x = tokens(T, K, N, "bf16", T)
