@@ -9,8 +9,8 @@
 // long as both operands agree, so a lane's piece fills its places of two (one) products.
 //
 // Measured (GPU alone, operands not in L2), rank 16: one token x 4096 x 6144 7.2 and then 9.1 us for both; 64 tokens on 57 adapters x 8192 x 8192 14.4 and
-// 20.6 us, 33 MB.  What bounds them is latency: the index, the first pieces, the cluster's join, then h.  Rows that begin in the middle of
-// words (777 x 2060 x 1003): 12.6 and 31.5 us.
+// 20.6 us, 33 MB.  What bounds them is latency: the index, the first pieces, the cluster's join, then h.  777 x 2060, rows on 8 bytes:
+// 12.5 us.
 //
 // h is fp32 until it is written: as two 16-bit halves (h 2^-e = high + low, e from the token's largest |h|), so that the second
 // product, on 16-bit operands, sees 16 bits of it or more, and fp16 neither overflows nor loses small tokens.
@@ -616,7 +616,7 @@ static int launch_adapter(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     const int64_t turns = std::max<int64_t>(1, std::min<int64_t>(adapters, 16 * sms / (windows * cols)));
     const dim3 grid2(static_cast<unsigned>(cols), static_cast<unsigned>(windows), static_cast<unsigned>(turns));
     const unsigned threads = 32u * warps;
-    // Blocks that fill the SMs more than once share their tokens' h in shared memory (2223 x 17853, rank 64: 237 us, 298 without); with fewer
+    // Blocks that fill the SMs more than once share their tokens' h in shared memory (64 x 100000, rank 64: 43 us, 62 without); with fewer
     // that costs more than it saves (64 x 6144, rank 64: 20.2 us without, 24.0 with).
     const bool share = windows * cols > 2 * sms;
     auto launch = [&](auto y_type) {

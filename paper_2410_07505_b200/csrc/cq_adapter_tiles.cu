@@ -6,7 +6,8 @@
 //   k27  h = A x: a tile's x against the rows of up to 128 / R adapters side by side, so that x is read once for them; the contraction
 //        is split over a cluster and joined through distributed shared memory in rank order
 //   k28  out = y + B h: persistent over 128 x 256-byte tiles of y; those stream through a ring in shared memory in which the
-//        epilogue adds the product to the rows that have the adapter at hand.  Bound by HBM (y in, out out)
+//        epilogue adds the product to the rows that have the adapter at hand.  Bound by HBM (y in, out out).  Rows that no tensor map takes
+//        are brought and taken away by the warps of the epilogue, bound by their instructions: 2223 x 17853, rank 64, 86 us, 35 of 17856 columns
 // Measured (operands not in L2): 4096 x 8192 x 28672, rank 64, both 112 us (556 MB, 5.0 TB/s of 6.6 of a copy), k28 by itself 83 us (485 MB, 5.8 TB/s).  A tile of
 // many adapters is bound by the round of signals for each: 1024 x 8192 x 8192 with 55 of 64 adapters in every tile, rank 16, 190 us, 0.45 us an
 // adapter and tile of columns in k28, of which neither its rows of B nor its epilogue are more than 15 %.
@@ -231,6 +232,17 @@ __device__ __forceinline__ void fetch_rows(const AdapterArgs& p, int64_t t0, int
     constexpr int kPer = YT == CQ_F32 ? 1 : 2, kElem = 4 / kPer, CT = out_cols<YT>();
     const int lane = threadIdx.x & 31, left = static_cast<int>(min(p.N - col, static_cast<int64_t>(CT)));
     const uint8_t* y = static_cast<const uint8_t*>(p.y);
+    if (left == CT && t0 + 16 <= p.T) {       // all there: a load and an addition for each word
+        const uint8_t* at = y + (t0 * p.ldy + col) * kElem + 4 * lane;
+        const int64_t pitch = p.ldy * kElem;
+        const int first = begins_odd<YT>(y, t0 * p.ldy + col), turns = begins_odd<YT>(nullptr, p.ldy);
+#pragma unroll
+        for (int i = 0; i < 16; ++i, at += pitch) {
+            const uint32_t* word = reinterpret_cast<const uint32_t*>(YT == CQ_F32 ? at : at - 2 * ((first + i * turns) & 1));
+            v.w[i][0] = __ldcg(word);
+            v.w[i][1] = __ldcg(word + 32);
+        }
+    } else
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int64_t at = (t0 + i) * p.ldy + col;
@@ -254,11 +266,11 @@ __device__ __forceinline__ uint32_t* loose_word(uint8_t* tile, int row, int h) {
 }
 template <int YT>
 __device__ __forceinline__ void rows_to_tile(const AdapterArgs& p, int64_t t0, int64_t col, const LooseRows& v, uint8_t* tile, int row0) {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, first = begins_odd<YT>(p.y, t0 * p.ldy + col), turns = begins_odd<YT>(nullptr, p.ldy);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         uint32_t a = v.w[i][0], b = v.w[i][1];
-        if (begins_odd<YT>(p.y, (t0 + i) * p.ldy + col) != 0) {                 // (the same for the whole warp)
+        if (((first + i * turns) & 1) != 0) { // (the same for the whole warp)
             uint32_t next_a = __shfl_down_sync(0xFFFFFFFFu, a, 1), next_b = __shfl_down_sync(0xFFFFFFFFu, b, 1);
             const uint32_t first_b = __shfl_sync(0xFFFFFFFFu, b, 0), edge = __shfl_sync(0xFFFFFFFFu, v.edge, i);
             if (lane == 31) { next_a = first_b; next_b = edge; }
@@ -274,7 +286,31 @@ __device__ __forceinline__ void tile_to_rows(const AdapterArgs& p, int64_t t0, i
     constexpr int kPer = YT == CQ_F32 ? 1 : 2, kElem = 4 / kPer, CT = out_cols<YT>();
     const int lane = threadIdx.x & 31, left = static_cast<int>(min(p.N - col, static_cast<int64_t>(CT)));
     uint8_t* out = static_cast<uint8_t*>(p.out);
-#pragma unroll 4
+    if (left == CT && t0 + 16 <= p.T) {
+        uint8_t* at = out + (t0 * p.ldo + col) * kElem + 4 * lane;
+        const int64_t pitch = p.ldo * kElem;
+        const int first = begins_odd<YT>(out, t0 * p.ldo + col), turns = begins_odd<YT>(nullptr, p.ldo);
+#pragma unroll
+        for (int i = 0; i < 16; ++i, at += pitch) {
+            uint32_t a = *loose_word(tile, row0 + i, 0), b = *loose_word(tile, row0 + i, 1);
+            if (YT != CQ_F32 && ((first + i * turns) & 1) != 0) {
+                uint16_t* halves = reinterpret_cast<uint16_t*>(at);
+                uint32_t before_a = __shfl_up_sync(0xFFFFFFFFu, a, 1), before_b = __shfl_up_sync(0xFFFFFFFFu, b, 1);
+                const uint32_t last_a = __shfl_sync(0xFFFFFFFFu, a, 31);
+                if (lane == 0) before_b = last_a;
+                uint32_t* words = reinterpret_cast<uint32_t*>(at - 2);
+                if (lane == 0) halves[0] = static_cast<uint16_t>(a);
+                else words[0] = __funnelshift_r(before_a, a, 16);
+                words[32] = __funnelshift_r(before_b, b, 16);
+                if (lane == 31) halves[65] = static_cast<uint16_t>(b >> 16);    // (of element 62 on: the 127th)
+            } else {
+                reinterpret_cast<uint32_t*>(at)[0] = a;
+                reinterpret_cast<uint32_t*>(at)[32] = b;
+            }
+        }
+        return;
+    }
+#pragma unroll 1
     for (int i = 0; i < 16; ++i) {
         if (t0 + i >= p.T) break;
         const int64_t at = (t0 + i) * p.ldo + col;
@@ -571,8 +607,10 @@ bool adapter_in_tiles(const AdapterArgs& p) {
            p.ldx < (int64_t(1) << 38);
 }
 bool adapter_out_tiles(const AdapterArgs& p, int y_dtype) {
-    const int64_t elem = y_dtype == CQ_F32 ? 4 : 2;
-    return p.T >= kTileTokens && p.n >= 1 && elem * p.N < kMapMost && p.n * p.N < kMapMost && p.ldy < (int64_t(1) << 37) && p.ldo < (int64_t(1) << 37);
+    // Rows that begin anywhere want two tiles of tokens to win (300 x 17853, rank 16: 37.2 us, 38.5 in windows; 130 tokens 30.2, 24.3; 2223, rank 64:
+    // 107, 256).
+    const int64_t elem = y_dtype == CQ_F32 ? 4 : 2, least = p.vec_n == 16 / elem ? kTileTokens : 2 * kTileTokens;
+    return p.T >= least && p.n >= 1 && elem * p.N < kMapMost && p.n * p.N < kMapMost && p.ldy < (int64_t(1) << 37) && p.ldo < (int64_t(1) << 37);
 }
 
 template <int HB, int DT, int YT, bool LOOSE>
