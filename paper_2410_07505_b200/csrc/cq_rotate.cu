@@ -9,7 +9,7 @@
 // token's, times the weights: an element then costs two products and the row's factor.  A block's next rows are on the way while these are
 // worked on; the issue slots are 59 % busy, the rest waits at the angles' phase of each group of tokens.
 // Measured (GPU alone, operands not in L2): 8192 tokens x 72 heads of 128 with norms, bf16 61.5 us (4.9 TB/s of 6.6 of a copy); 777 x 80 of 64 without
-// norms 6.8 us; one token 5.5 us.  Rows that begin anywhere, through shared memory: the first 272 us.
+// norms 6.8 us; one token 5.5 us.  Rows that begin anywhere, through shared memory: the first 269 us.
 #include "cq_serve.cuh"
 
 #include <algorithm>
@@ -312,16 +312,16 @@ static int launch_rotate(RotateArgs& p, bool fast, cudaStream_t st) {
     const int W = p.D <= 64 ? 4 : p.D <= 128 ? 8 : 16;
     const int rows = fast ? kRotateThreads / W : kRotateThreads / 32;
     const int heads = std::max(p.side[0].heads, p.side[1].heads);
-    // Persistent blocks.  As many tokens at a time as leave an SM one group of them (two without norms, whose groups take less): 500 tokens x 72
-    // heads of 128 with norms 8.1 us, two groups 11.9, one token at a time 11.9; 777 x 80 of 64 without norms 6.7, one group 7.7.  Few tokens:
-    // a token's heads are shared out, a pass or more to a block, while all blocks are resident.
+    // Persistent blocks (where a warp has a row, eight times as many: 8192 tokens 269 us, 351).  As many tokens at a time as leave an SM one group
+    // of them (two without norms, whose groups take less): 500 tokens x 72 heads of 128 with norms 8.1 us, two groups 11.9; 777 x 80 of 64 without
+    // norms 6.7, one group 7.7.  Few tokens: a token's heads are shared out, a pass or more to a block, while all blocks are resident.
     const int64_t resident = (!fast ? 6 : p.norm ? 2 : 3) * sm_count();
     p.group = 1;
     while (fast && p.group < kMaxGroup && p.T / (2 * p.group) >= (p.norm ? 1 : 2) * sm_count()) p.group *= 2;
     const int64_t groups = (p.T + p.group - 1) / p.group;
     const int64_t most = std::max(1, (heads + rows - 1) / rows / (fast ? kAhead : 1));
     p.slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, resident / groups)));
-    const int64_t blocks = std::min<int64_t>(groups, resident / p.slices);
+    const int64_t blocks = std::min<int64_t>(groups, (fast ? resident : 8 * resident) / p.slices);
     const dim3 grid(static_cast<unsigned>(blocks * p.slices));
     if (!fast) return launch_ex(k24_norm_rotate_any<DT>, grid, kRotateThreads, 0, st, 1, !tuning_no_pdl(), p);
     if (W == 4) return launch_rotate_rows<4, DT>(p, grid, st);
