@@ -68,12 +68,12 @@ k27_adapter_in_tiles(const __grid_constant__ CUtensorMap mapX, const __grid_cons
     }
     if (warp == 1) tmem_alloc(&s_tmem, 2 * kInCols);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;");
     const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kTileTokens;
     const int count = sort_tile(p, t0, s_sort, blockIdx.x == 0 && blockIdx.z == 0);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;");  // (behind the allocation: see tmem_alloc)
     const uint32_t tmem = s_tmem;
     const int rank = blockIdx.x, ranks = gridDim.x;
     const int kblocks = static_cast<int>((p.K + 63) / 64), kb0 = static_cast<int>(static_cast<int64_t>(kblocks) * rank / ranks),
@@ -365,7 +365,6 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
     static_assert((3 * SY + 2 * SB + 2 * kOutBuffers + 3) * 8 + 8 <= 512, "barriers");
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
 
-    asm volatile("griddepcontrol.launch_dependents;");
     if (tid == 0) {
         if ((smem_u32(smem) & 1023u) != 0u) atomicExch(&g_adapter_fault, 1u);      // cannot be: see above
         for (int i = 0; i < SY; ++i) { mbar_init(&y_full[i], 1); mbar_init(&y_empty[i], 1); mbar_init(&o_full[i], 8); }
@@ -385,6 +384,7 @@ k28_adapter_out_tiles(const __grid_constant__ CUtensorMap mapHigh, const __grid_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;");  // (behind the allocation: see tmem_alloc)
     const uint32_t tmem = s_tmem;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const OutItem work = out_items(p, CT, group);

@@ -109,7 +109,6 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     static_assert((2 * ST + 2 * TB) * 8 + 8 <= 256, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-    asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x == 0) {
         if ((smem_u32(smem) & 1023u) != 0u) atomicExch(&g_fp8_fault, 1u);      // cannot be: see above
         for (int i = 0; i < ST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 8); }
@@ -123,6 +122,7 @@ k12_product(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CU
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;");  // (behind the allocation: see tmem_alloc)
     const uint32_t tmem = s_tmem;
     const int64_t ntotal = static_cast<int64_t>(p.mtiles) * p.ntiles;
     const int rank = SPLIT ? blockIdx.x & 1 : 0;
@@ -362,7 +362,6 @@ k13_product_few(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     const int kb1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (rank + 1) / p.split);
     const int count = kb1 - kb0;
 
-    asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x == 0) {
         for (int i = 0; i < kSt; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], EW); }
         for (int i = 0; i < kFewBuffers; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], EW); }
@@ -373,6 +372,7 @@ k13_product_few(const __grid_constant__ CUtensorMap mapA, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;");  // (behind the allocation: see tmem_alloc)
     const uint32_t tmem = s_tmem;
 
     float acc[kCols];

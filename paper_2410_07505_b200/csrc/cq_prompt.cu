@@ -271,7 +271,6 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
     static_assert((2 * ST + 20) * 8 + 2 * sizeof(PromptItem) + 12 <= 512, "barriers");
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
-    asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x == 0) {
         if ((smem_u32(smem) & 1023u) != 0u) atomicExch(&g_prompt_fault, 1u);      // cannot be: see above
         for (int i = 0; i < ST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 2); }
@@ -292,6 +291,7 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
+    asm volatile("griddepcontrol.launch_dependents;");  // (behind the allocation: see tmem_alloc)
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if (warp >= 8) {

@@ -94,6 +94,8 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
 }
 
 // ---- device: tensor memory and 5th-generation products ---------------------------------------------
+// Waits, without a limit, until the SM has that many columns free.  So a kernel says launch_dependents only behind the barrier that follows its
+// allocation: a dependent that found room beside a block without columns could take them and wait for that block's end for good.
 __device__ __forceinline__ void tmem_alloc(uint32_t* where_smem, uint32_t columns) {      // a whole warp
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(where_smem)), "r"(columns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
