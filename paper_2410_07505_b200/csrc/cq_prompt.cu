@@ -4,9 +4,10 @@
 // j <= Lk - Lq + i; G = Hq / H query heads share a key/value head:
 //   out[i] = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(c q_i . k_j - ref_i),   c = softmax_scale log2(e)
 // in one pass over the keys.  ref_i is the largest c q_i . k_j so far, renewed only when a block exceeds it by 2^kSlack, so
-// that the running result is hardly ever rescaled.  Sums and references are fp32; p is rounded once to the inputs' 16 bits,
-// as an operand of the second product (kind::f16 takes both operands in one type), in fp16 with 2^kBias in front so that small
-// weights keep their bits.
+// that the running result is hardly ever rescaled.  (Beyond 2^20 the last bit of a logit in base 2 is worth more than a weight may be
+// off by: there it is rounded before ref_i, one of them, is taken from it, so that the largest has the exponent that it should have.)
+// Sums and references are fp32; p is rounded once to the inputs' 16 bits, as an operand of the second product (kind::f16 takes both
+// operands in one type), in fp16 with 2^kBias in front so that small weights keep their bits.
 //
 // A persistent CTA takes pairs of tiles of 128 rows (tokens x query heads of one key head) over blocks of 128 keys, longest first.  Q, K
 // and V come by TMA; the logits S = Q K^T of either tile stand in tensor memory (128 columns), the weights take their place (64), the
@@ -33,6 +34,7 @@ constexpr int kPromptThreads = 384;           // warps 0..3, 4..7: softmax of th
 constexpr int kTileRows = 128;                // rows of a tile: tokens x the query heads that go together
 constexpr int kKeys = 128;                    // keys of a block
 constexpr float kSlack = 8.0f;
+constexpr float kFarLogit = 1048576.0f;       // 2^20: up to here c x - ref, formed in one rounding, is off by 2^-4 at most
 constexpr int kMaxSplits = 16;
 template <int DT> __host__ __device__ constexpr float prompt_bias() { return DT == CQ_F16 ? 7.0f : 0.0f; }   // 2^(7 + 8) < 65504
 
@@ -457,7 +459,10 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
             const int sees = it.sees + token;                   // this row's keys are the first `sees`
             const int all_see = it.sees + t * p.tokens;         // those that every row of the tile sees
             const int common = min(it.end[0], it.end[1]);         // blocks before this one are both tiles'
-            float ref = -INFINITY, sum = 0.0f;
+            // Weights are 2^(c x - ref).  Of a row whose reference came to lie beyond kFarLogit it is `far` (-infinity: there is none; kBias would
+            // be lost in it) and ref -infinity, so that every block of the row asks for a new one and the far from 0 cost the others nothing.
+            // (Rows of no token, whose logits are whatever lay in memory, ask for none.)
+            float ref = token < 1 << 30 ? -INFINITY : INFINITY, far = -INFINITY, sum = 0.0f;
             for (int j = jb; j < end; ++j) {
                 if (!(ok = warp_wait(&s_full[t], s_round, &s_dead))) break;
                 s_round ^= 1u;
@@ -515,15 +520,23 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                 };
                 const float top = __fmul_rn(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), p.c);
                 const bool renew = top > ref + (kBias + kSlack);
-                float keep = 1.0f;
-                if (renew) {
-                    keep = ex2(ref - (top - kBias));
-                    ref = top - kBias;
-                    sum *= keep;
-                }
-                if (j > jb && __any_sync(0xFFFFFFFFu, renew)) {
+                if (__any_sync(0xFFFFFFFFu, renew)) {
+                    float keep = 1.0f;
+                    if (renew && fabsf(top) < kFarLogit && far == -INFINITY) {
+                        keep = ex2(ref - (top - kBias));
+                        ref = top - kBias;
+                    } else if (renew) {
+                        if (far == -INFINITY || top - far > kSlack) {
+                            keep = ex2(far == -INFINITY ? ref - top + kBias : far - top);
+                            far = top;                          // (infinite too: infinity less infinity is NaN, in one rounding it would be 0)
+                            ref = -INFINITY;
+                        }
+                        const float back = __frcp_rn(p.c);      // the exponent in two roundings, over c
 #pragma unroll
-                    for (int q = 0; q < D / 16; ++q) {
+                        for (int i = 0; i < 128; ++i) x[i >> 5][i & 31] = (__fmul_rn(x[i >> 5][i & 31], p.c) - far + kBias) * back;
+                    }
+                    sum *= keep;
+                    for (int q = 0; q < (j > jb ? D / 16 : 0); ++q) {
                         float o[16];
                         tmem_ld16(at_o + q * 16, o);
                         tmem_ld_wait(o);
@@ -569,6 +582,9 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
             const bool poison = s_poison != 0u;
             const int64_t place = (static_cast<int64_t>(it.q0) + token) * p.Hq + it.head0 + row % p.g;
             const float inv = sum == 0.0f ? 0.0f : __frcp_rn(sum);
+            // what is said of the row besides its result is in units of 2^ref, of a far one too
+            const float unit = far == -INFINITY ? 1.0f : 1.0f / static_cast<float>(1 << static_cast<int>(kBias));
+            if (far != -INFINITY) ref = far;
             const int from = max(jb, max(it.sees, 0) / kKeys) * kKeys, to = min(sees, end * kKeys);     // keys whose V may have been emptied
             const int64_t rows = static_cast<int64_t>(p.Tq) * p.Hq;
             float* part = p.part + (it.part * rows + place) * D;
@@ -595,7 +611,7 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                 if (p.splits > 1) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        reinterpret_cast<float4*>(part + q * 32)[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        reinterpret_cast<float4*>(part + q * 32)[i] = make_float4(o[4 * i] * unit, o[4 * i + 1] * unit, o[4 * i + 2] * unit, o[4 * i + 3] * unit);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -608,9 +624,9 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
             }
             if (mine) {
                 if (p.splits > 1)
-                    *reinterpret_cast<float2*>(p.part + p.splits * rows * D + (it.part * rows + place) * 2) = make_float2(ref, sum);
+                    *reinterpret_cast<float2*>(p.part + p.splits * rows * D + (it.part * rows + place) * 2) = make_float2(ref, sum * unit);
                 else if (p.lse != nullptr)
-                    p.lse[place] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.69314718f;
+                    p.lse[place] = sum == 0.0f ? -INFINITY : (ref + log2f(sum * unit)) * 0.69314718f;
             }
             tc_fence_before();
             __syncwarp();
