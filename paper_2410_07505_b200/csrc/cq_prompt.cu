@@ -135,10 +135,11 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
 }
 
 // ---- which item is the i-th ---------------------------------------------------------------------------------
+// (Ordinary loads: the kernel before this one, which may have written the starts, can still run when this one begins.)
 struct Sequence { int q0, k0, lq, lk; };
 __device__ __forceinline__ Sequence sequence_at(const PromptArgs& p, int b) {
-    const int q0 = min(max(__ldg(p.q_starts + b), 0), p.Tq), q1 = min(max(__ldg(p.q_starts + b + 1), q0), p.Tq);
-    const int k0 = min(max(__ldg(p.k_starts + b), 0), p.Tk), k1 = min(max(__ldg(p.k_starts + b + 1), k0), p.Tk);
+    const int q0 = min(max(p.q_starts[b], 0), p.Tq), q1 = min(max(p.q_starts[b + 1], q0), p.Tq);
+    const int k0 = min(max(p.k_starts[b], 0), p.Tk), k1 = min(max(p.k_starts[b + 1], k0), p.Tk);
     return {q0, k0, q1 - q0, k1 - k0};
 }
 // Pairs of tiles of the sequence that need at least x blocks of keys.  Later pairs need more, the i-th
@@ -649,8 +650,8 @@ k23_prompt_join(const PromptArgs p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const int64_t rows = static_cast<int64_t>(p.Tq) * p.Hq;
-    const int64_t first = static_cast<int64_t>(min(max(__ldg(p.q_starts), 0), p.Tq)) * p.Hq;
-    const int64_t stop = static_cast<int64_t>(min(max(__ldg(p.q_starts + p.B), 0), p.Tq)) * p.Hq;
+    const int64_t first = static_cast<int64_t>(min(max(p.q_starts[0], 0), p.Tq)) * p.Hq;
+    const int64_t stop = static_cast<int64_t>(min(max(p.q_starts[p.B], 0), p.Tq)) * p.Hq;
     const float2* stats = reinterpret_cast<const float2*>(p.part + p.splits * rows * D);
     for (int64_t row = first + static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5); row < stop; row += static_cast<int64_t>(gridDim.x) * 8) {
         float2 st = make_float2(-INFINITY, 0.0f);
