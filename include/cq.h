@@ -387,6 +387,13 @@ int cq_prompt_attention(const void* Q, int64_t q_token_stride, int64_t q_head_st
                         int64_t k_head_stride, const void* V, int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t B,
                         int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D, const int* q_starts, const int* k_starts,
                         double softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+/* The same with finer weights: each meets the values as two numbers of the dtype, the second what the first leaves of it (off by 2^-16 of
+ * itself in bfloat16; in float16 by 2^-22, and 2^-32 of its row's largest), so that beside the result's rounding little is left but that
+ * of fp32 sums.  The product with the values is done twice.  Workspace: the same. */
+int cq_prompt_attention_fine(const void* Q, int64_t q_token_stride, int64_t q_head_stride, const void* K, int64_t k_token_stride,
+                             int64_t k_head_stride, const void* V, int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t B,
+                             int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D, const int* q_starts, const int* k_starts,
+                             double softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Norms of queries and keys for each head and their rotation by position.  For each token t and head, over its D channels:

@@ -28,7 +28,7 @@ EXPORTS = (
     "cq_vector_max", "cq_quantize_act_given",
     "cq_fp8_quantize_act", "cq_fp8_quantize_weight", "cq_fp8_matmul", "cq_fp8_linear_workspace_bytes", "cq_fp8_linear",
     "cq_kv_write", "cq_kv_read", "cq_kv_attention_workspace_bytes", "cq_kv_attention", "cq_serve_fault",
-    "cq_prompt_attention_workspace_bytes", "cq_prompt_attention", "cq_norm_rotate", "cq_adapter_add_workspace_bytes", "cq_adapter_add",
+    "cq_prompt_attention_workspace_bytes", "cq_prompt_attention", "cq_prompt_attention_fine", "cq_norm_rotate", "cq_adapter_add_workspace_bytes", "cq_adapter_add",
 )
 _SIZES = ("cq_workspace_bytes", "cq_host_scratch_bytes", "cq_fp8_linear_workspace_bytes", "cq_kv_attention_workspace_bytes",
           "cq_prompt_attention_workspace_bytes", "cq_adapter_add_workspace_bytes")
@@ -96,6 +96,7 @@ def lib() -> C.CDLL:
         L.cq_prompt_attention_workspace_bytes.argtypes = [i64] * 6
         L.cq_prompt_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, ci, i64, i64, i64, i64, i64, i64, vp, vp, dbl, vp, vp,
                                           vp, sz, vp]
+        L.cq_prompt_attention_fine.argtypes = L.cq_prompt_attention.argtypes
         L.cq_norm_rotate.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, ci, i64, i64, i64, ci, vp, vp, vp, vp, dbl, vp, i64, i64, vp, i64,
                                      i64, vp]
         L.cq_adapter_add_workspace_bytes.restype = sz
@@ -874,13 +875,14 @@ def prompt_attention_workspace_bytes(sequences: int, queries: int, keys: int, qu
 
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: torch.Tensor, k_starts: torch.Tensor | None = None, *,
                      scale: float | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-                     workspace: torch.Tensor | None = None) -> torch.Tensor:
+                     workspace: torch.Tensor | None = None, fine: bool = False) -> torch.Tensor:
     """Causal attention over packed prompts, q [Tq, Hq, D], k and v [Tk, H, D] (float16 / bfloat16; strides of tokens and heads
     multiples of 8).
 
     Sequence b's queries are the rows q_starts[b] .. q_starts[b + 1] (int32 [B + 1]), its keys those of k_starts (default: the same); the
     queries are its last tokens.  `scale` multiplies the logits (default 1 / sqrt(D)); `lse` float32 [Tq, Hq] receives the
-    logarithm of the softmax's sum.  Rows outside the sequences are not written."""
+    logarithm of the softmax's sum.  Rows outside the sequences are not written.  The softmax's weights are rounded to q's dtype before they
+    meet the values; `fine` keeps what that leaves of them too, for a second product (`cq_prompt_attention_fine`)."""
     dtype, dev, shape = q.dtype, q.get_device(), q.shape
     dt = _DT16.get(dtype)
     if dt is None or len(shape) != 3 or dev < 0:
@@ -907,11 +909,12 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts
         need = L.cq_prompt_attention_workspace_bytes(n - 1, Tq, Tk, Hq, H, D)
         workspace = q.new_empty(need, dtype=torch.uint8) if need else None
     at, size = (0, 0) if workspace is None else _workspace_of(workspace, dev)
-    st = L.cq_prompt_attention(q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], dt, n - 1, Tq, Tk, Hq, H, D,
-                               q_starts.data_ptr(), k_starts.data_ptr(), D ** -0.5 if scale is None else float(scale), out.data_ptr(),
-                               0 if lse is None else lse.data_ptr(), at, size, _raw(dev))
+    call = L.cq_prompt_attention_fine if fine else L.cq_prompt_attention
+    st = call(q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], dt, n - 1, Tq, Tk, Hq, H, D, q_starts.data_ptr(),
+              k_starts.data_ptr(), D ** -0.5 if scale is None else float(scale), out.data_ptr(), 0 if lse is None else lse.data_ptr(), at, size,
+              _raw(dev))
     if st:
-        raise CQError(st, "cq_prompt_attention")
+        raise CQError(st, "cq_prompt_attention_fine" if fine else "cq_prompt_attention")
     return out
 
 

@@ -7,7 +7,9 @@
 // that the running result is hardly ever rescaled.  (Beyond 2^20 the last bit of a logit in base 2 is worth more than a weight may be
 // off by: there it is rounded before ref_i, one of them, is taken from it, so that the largest has the exponent that it should have.)
 // Sums and references are fp32; p is rounded once to the inputs' 16 bits, as an operand of the second product (kind::f16 takes both
-// operands in one type), in fp16 with 2^kBias in front so that small weights keep their bits.
+// operands in one type), in fp16 with 2^kBias in front so that small weights keep their bits.  That adds about half of the result's own
+// rounding to its error (against 64 bits 0.0021 for 0.0016 in bf16, 0.00025 for 0.0002 in fp16).  FINE, the caller's choice, hands over what
+// the rounding leaves as well, in the other half of the logits' columns, for a second product: the error is the result's rounding again.
 //
 // A persistent CTA takes pairs of tiles of 128 rows (tokens x query heads of one key head) over blocks of 128 keys, longest first.  Q, K
 // and V come by TMA; the logits S = Q K^T of either tile stand in tensor memory (128 columns), the weights take their place (64), the
@@ -20,11 +22,12 @@
 // two threads to a row (1220 us), a share of the exponentials by polynomial (895 us).
 // Measured (GPU alone, operands not in L2): 1 x 8192 tokens, 64 / 8 heads of 128, bf16 869 us (1265 TFLOP/s; 1090 in a long run, which the power limit
 // sets); 12 packed prompts up to 2060 tokens, 64 / 8 heads, fp16 338 us; 1000 tokens behind 19011, 32 heads of 64 257 us (bound by exponentials:
-// 139 us at one a lane and clock); 1000 tokens, 32 / 8 heads 26.7 us.
+// 139 us at one a lane and clock); 1000 tokens, 32 / 8 heads 26.7 us.  FINE: 1132, 412, 306, 34.7 us (products 256 cycles longer on the chain).
 #include "cq_serve.cuh"
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 namespace cq {
 
@@ -119,12 +122,17 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
     return __all_sync(0xFFFFFFFFu, role_wait(bar, parity, dead)) != 0;
 }
 
-// Two weights 2^(c x - ref), added to a pair of sums and rounded to a pair.
-template <int DT>
-__device__ __forceinline__ uint32_t weights(float x0, float x1, uint64_t c, uint64_t neg, uint64_t& sums) {
+// Two weights 2^(c x - ref), added to a pair of sums and rounded to a pair; FINE: what that leaves of them, rounded too.
+template <int DT, bool FINE>
+__device__ __forceinline__ uint32_t weights(float x0, float x1, uint64_t c, uint64_t neg, uint64_t& sums, uint32_t& rest) {
     const float2 u = apart(fma2(both(x0, x1), c, neg)), p = make_float2(ex2(u.x), ex2(u.y));
     sums = add2(sums, both(p.x, p.y));
-    return pack16x2<DT>(p.x, p.y);
+    const uint32_t r = pack16x2<DT>(p.x, p.y);
+    if constexpr (FINE) {
+        const float2 v = unpack16x2<DT>(r);
+        rest = pack16x2<DT>(p.x - v.x, p.y - v.y);
+    }
+    return r;
 }
 
 // nonzero bit 15 or 31 where a 16-bit element is an infinity or NaN
@@ -245,7 +253,7 @@ __device__ __forceinline__ bool find_item(const PromptArgs& p, int64_t index, in
 }
 
 // ---- the kernel ------------------------------------------------------------------------------------------------
-template <int D, int DT>
+template <int D, int DT, bool FINE>                            // FINE: weights as two 16-bit numbers each
 __global__ void __launch_bounds__(kPromptThreads, 1)
 k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
            const PromptArgs p) {
@@ -403,6 +411,11 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
 #pragma unroll
                             for (int k = 0; k < kKeys / 32; ++k)
                                 tc_mma_f16_ts(at_o, at_s + k * 8, desc_v + ((sv * kTile + k * 2048) >> 4), idesc_o, j > jb || k != 0);
+                            if constexpr (FINE) {
+#pragma unroll
+                                for (int k = 0; k < kKeys / 32; ++k)
+                                    tc_mma_f16_ts(at_o, at_s + kKeys / 2 + k * 8, desc_v + ((sv * kTile + k * 2048) >> 4), idesc_o, true);
+                            }
                         }
                         __syncwarp();
                         if (!(ok = warp_wait(&p_full[2 * t + 1], p_round, &s_dead))) break;
@@ -414,6 +427,11 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
 #pragma unroll
                             for (int k = kKeys / 32; k < kKeys / 16; ++k)
                                 tc_mma_f16_ts(at_o, at_s + k * 8, desc_v + ((sv * kTile + k * 2048) >> 4), idesc_o, true);
+                            if constexpr (FINE) {
+#pragma unroll
+                                for (int k = kKeys / 32; k < kKeys / 16; ++k)
+                                    tc_mma_f16_ts(at_o, at_s + kKeys / 2 + k * 8, desc_v + ((sv * kTile + k * 2048) >> 4), idesc_o, true);
+                            }
                             if (!next) tc_commit(&o_full[t]);
                         }
                         if (next) {                             // (behind the product that reads the weights in the same columns)
@@ -560,12 +578,13 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     if (q == 3 && lane == 0 && j < common && (t == 0 || j + 1 < common)) mbar_arrive(&turn[t ^ 1]);
-                    uint32_t r[16];
+                    uint32_t r[16], rest[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        r[i] = weights<DT>(x[q][2 * i], x[q][2 * i + 1], c2, neg2, l[i & 1]);
+                        r[i] = weights<DT, FINE>(x[q][2 * i], x[q][2 * i + 1], c2, neg2, l[i & 1], rest[i]);
                     if (q == 2) half_ready(0);
                     tmem_st16(at_s + q * 16, r);
+                    if constexpr (FINE) tmem_st16(at_s + kKeys / 2 + q * 16, rest);
                 }
                 half_ready(1);
                 const float2 l2 = apart(add2(l[0], l[1]));
@@ -742,12 +761,12 @@ static bool make_head_map(CUtensorMap* map, const void* base, int64_t D, int64_t
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int DT>
+template <int D, int DT, bool FINE>
 static int launch_prompt(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PromptArgs& p, int64_t items, cudaStream_t st) {
     static thread_local LaunchMemo memo;
-    if (resident_ctas(k22_prompt<D, DT>, kPromptThreads, prompt_smem<D>(), prompt_smem<D>(), memo) < 1) return CQ_ERR_CUDA;
+    if (resident_ctas(k22_prompt<D, DT, FINE>, kPromptThreads, prompt_smem<D>(), prompt_smem<D>(), memo) < 1) return CQ_ERR_CUDA;
     const int64_t grid = std::min<int64_t>(items, sm_count());
-    const int rc = launch_ex(k22_prompt<D, DT>, dim3(static_cast<unsigned>(grid)), kPromptThreads, prompt_smem<D>(), st, 1, !tuning_no_pdl(), q, k, v, p);
+    const int rc = launch_ex(k22_prompt<D, DT, FINE>, dim3(static_cast<unsigned>(grid)), kPromptThreads, prompt_smem<D>(), st, 1, !tuning_no_pdl(), q, k, v, p);
     if (rc != CQ_OK || p.splits == 1) return rc;
     const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(p.Tq) * p.Hq + 7) / 8, 8 * sm_count());
     return launch_ex(k23_prompt_join<D, DT>, dim3(static_cast<unsigned>(blocks)), 256, 0, st, 1, !tuning_no_pdl(), p);
@@ -769,22 +788,10 @@ static int check_strides(const void* X, int64_t tokens, int64_t heads, int64_t t
     return CQ_OK;
 }
 
-}  // namespace cq
-
-extern "C" {
-
-size_t cq_prompt_attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D) {
-    using namespace cq;
-    if (!prompt_shape_ok(B, Tq, Tk, Hq, H, D)) return 0;
-    const PromptPlan plan = prompt_plan(B, Tq, Tk, Hq, H);
-    return plan.splits == 1 ? 0 : sizeof(float) * plan.splits * static_cast<size_t>(Tq) * Hq * (D + 2);
-}
-
-int cq_prompt_attention(const void* Q, int64_t q_token_stride, int64_t q_head_stride, const void* K, int64_t k_token_stride,
-                        int64_t k_head_stride, const void* V, int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t B,
-                        int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D, const int* q_starts, const int* k_starts,
-                        double softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
-    using namespace cq;
+static int prompt_attention(bool fine, const void* Q, int64_t q_token_stride, int64_t q_head_stride, const void* K, int64_t k_token_stride,
+                            int64_t k_head_stride, const void* V, int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t B,
+                            int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D, const int* q_starts, const int* k_starts,
+                            double softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     if (!prompt_shape_ok(B, Tq, Tk, Hq, H, D)) return CQ_ERR_SHAPE;
     if (dtype != CQ_F16 && dtype != CQ_BF16) return CQ_ERR_DTYPE;
     if (!(softmax_scale >= 0x1p-100 && softmax_scale <= 1e30)) return CQ_ERR_ALPHA;
@@ -815,8 +822,39 @@ int cq_prompt_attention(const void* Q, int64_t q_token_stride, int64_t q_head_st
         !make_head_map(&mapV, v, D, Tk > 0 ? H : 1, keys, used_stride(Tk > 0 ? H : 1, v_head_stride, D), used_stride(keys, v_token_stride, H * D), 1, kKeys))
         return CQ_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (D == 128) return dtype == CQ_F16 ? launch_prompt<128, CQ_F16>(mapQ, mapK, mapV, p, plan.items, st) : launch_prompt<128, CQ_BF16>(mapQ, mapK, mapV, p, plan.items, st);
-    return dtype == CQ_F16 ? launch_prompt<64, CQ_F16>(mapQ, mapK, mapV, p, plan.items, st) : launch_prompt<64, CQ_BF16>(mapQ, mapK, mapV, p, plan.items, st);
+    auto launch = [&](auto width) {
+        constexpr int W = decltype(width)::value;
+        if (fine) return dtype == CQ_F16 ? launch_prompt<W, CQ_F16, true>(mapQ, mapK, mapV, p, plan.items, st) : launch_prompt<W, CQ_BF16, true>(mapQ, mapK, mapV, p, plan.items, st);
+        return dtype == CQ_F16 ? launch_prompt<W, CQ_F16, false>(mapQ, mapK, mapV, p, plan.items, st) : launch_prompt<W, CQ_BF16, false>(mapQ, mapK, mapV, p, plan.items, st);
+    };
+    return D == 128 ? launch(std::integral_constant<int, 128>()) : launch(std::integral_constant<int, 64>());
+}
+
+}  // namespace cq
+
+extern "C" {
+
+size_t cq_prompt_attention_workspace_bytes(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D) {
+    using namespace cq;
+    if (!prompt_shape_ok(B, Tq, Tk, Hq, H, D)) return 0;
+    const PromptPlan plan = prompt_plan(B, Tq, Tk, Hq, H);
+    return plan.splits == 1 ? 0 : sizeof(float) * plan.splits * static_cast<size_t>(Tq) * Hq * (D + 2);
+}
+
+int cq_prompt_attention(const void* Q, int64_t q_token_stride, int64_t q_head_stride, const void* K, int64_t k_token_stride,
+                        int64_t k_head_stride, const void* V, int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t B,
+                        int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D, const int* q_starts, const int* k_starts,
+                        double softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    return cq::prompt_attention(false, Q, q_token_stride, q_head_stride, K, k_token_stride, k_head_stride, V, v_token_stride, v_head_stride, dtype, B, Tq, Tk,
+                                Hq, H, D, q_starts, k_starts, softmax_scale, out, lse, workspace, workspace_bytes, stream);
+}
+
+int cq_prompt_attention_fine(const void* Q, int64_t q_token_stride, int64_t q_head_stride, const void* K, int64_t k_token_stride,
+                             int64_t k_head_stride, const void* V, int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t B,
+                             int64_t Tq, int64_t Tk, int64_t Hq, int64_t H, int64_t D, const int* q_starts, const int* k_starts,
+                             double softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    return cq::prompt_attention(true, Q, q_token_stride, q_head_stride, K, k_token_stride, k_head_stride, V, v_token_stride, v_head_stride, dtype, B, Tq, Tk,
+                                Hq, H, D, q_starts, k_starts, softmax_scale, out, lse, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -25,12 +25,13 @@ class AttentionLayer:
     def __init__(self, w_qkv: torch.Tensor, w_out: torch.Tensor, heads: int, kv_heads: int, *, sequences: int, longest: int,
                  bits: int = 8, page_size: int = 64, alpha: float = 0.15, freq: torch.Tensor | None = None, eps: float | None = None,
                  q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, neighbours: bool = False,
-                 qkv_adapters=None, out_adapters=None):
+                 qkv_adapters=None, out_adapters=None, fine_prompts: bool = True):
         """w_qkv [(heads + 2 kv_heads) * D, hidden], w_out [hidden, heads * D], both 16-bit on the GPU.
         A sequence has room for `longest` tokens, rounded up to whole pages.
 
         `freq` (float64, `cq.rotation_freq`) turns the rotation on, `eps` the norms, with the weights if they are given; the adapters
-        (`cq.Adapters` of either projection) are chosen for each prompt."""
+        (`cq.Adapters` of either projection) are chosen for each prompt.  `fine_prompts` = False lets a prompt's attention round its weights to
+        16 bits (the faster `cq.prompt_attention`)."""
         self.heads, self.kv_heads, self.alpha, self.bits, self.page_size = heads, kv_heads, alpha, bits, page_size
         self.head_dim = w_out.shape[1] // heads
         self.w_qkv, self.w_out = cq.fp8_quantize_weight(w_qkv), cq.fp8_quantize_weight(w_out)
@@ -50,7 +51,7 @@ class AttentionLayer:
             if freq is None:                                            # norms alone: no channel is rotated
                 freq = torch.empty(0, dtype=torch.float64, device=dev)
             self._turn = (freq, q_weight, k_weight, eps, neighbours)
-        self.qkv_adapters, self.out_adapters = qkv_adapters, out_adapters
+        self.qkv_adapters, self.out_adapters, self.fine_prompts = qkv_adapters, out_adapters, fine_prompts
         self.adapter = torch.full((sequences,), -1, dtype=torch.int32, device=dev)      # of each sequence; below 0: none
 
     def _project(self, x: torch.Tensor, w, adapters, adapter: torch.Tensor) -> torch.Tensor:
@@ -71,7 +72,7 @@ class AttentionLayer:
         if q.is_cuda:
             ends = [sum(lengths[:i]) for i in range(len(lengths) + 1)]
             starts = torch.cat([torch.full((1,), n, dtype=torch.int32, device=q.device) for n in ends])      # (no copy from the host)
-            return cq.prompt_attention(q, k, v, starts)
+            return cq.prompt_attention(q, k, v, starts, fine=self.fine_prompts)
         G, outs = self.heads // self.kv_heads, []                       # on the host, in elementary operations
         for q, k, v in zip(q.split(lengths), k.split(lengths), v.split(lengths)):
             T = q.shape[0]
