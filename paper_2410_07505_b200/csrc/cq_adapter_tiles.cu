@@ -41,8 +41,11 @@ constexpr int kInCols = 128;                  // rows of A (of several adapters)
 constexpr int kInMaxStages = 5;
 constexpr size_t kXTile = size_t(kTileTokens) * 128, kATile = size_t(kInCols) * 128;
 
-static int in_stages(int R) { return R <= 64 ? kInMaxStages : 4; }
-static size_t in_smem(int R) { return 1024 + in_stages(R) * (kXTile + kATile) + size_t(kTileTokens) * (R + 1) * 4; }
+constexpr int in_stages(int R) { return R <= 64 ? kInMaxStages : 4; }
+constexpr size_t in_smem(int R) { return 1024 + in_stages(R) * (kXTile + kATile) + size_t(kTileTokens) * (R + 1) * 4; }
+// Every rank is launched with this much, which leaves no room for a second block either way: what the runtime says of the kernel is then
+// asked once, whatever the ranks of a layer's adapters are.
+constexpr size_t kInSmem = in_smem(64) > in_smem(kMaxRank) ? in_smem(64) : in_smem(kMaxRank);
 
 template <int DT>
 __global__ void __launch_bounds__(kInThreads, 1)
@@ -634,16 +637,15 @@ static int launch_out_tiles(const AdapterArgs& p, cudaStream_t st) {
     return launch_ex(k28_adapter_out_tiles<HB, DT, YT, LOOSE>, dim3(grid), kOutThreads, smem, st, 1, !tuning_no_pdl(), high, low, b, y, out, p, group);
 }
 
-// Clusters of 2^i blocks that are resident at one time (asked once for a device and size of shared memory).
+// Clusters of 2^i blocks that are resident at one time (asked once for a device).
 constexpr int kMaxParts = 4;
 template <typename Kernel>
-static int resident_clusters(Kernel* kernel, int i, size_t smem) {
-    struct Known { int device; size_t smem; int n[kMaxParts]; };
-    static thread_local Known known[2] = {{-1, 0, {}}, {-1, 0, {}}};
+static int resident_clusters(Kernel* kernel, int i) {
+    struct Known { int device; int n[kMaxParts]; };
+    static thread_local Known k = {-1, {}};
     int device = -1;
     if (cudaGetDevice(&device) != cudaSuccess) return 0;
-    Known& k = known[smem == in_smem(kMaxRank) ? 1 : 0];
-    if (k.device != device || k.smem != smem) k = {device, smem, {}};
+    if (k.device != device) k = {device, {}};
     if (k.n[i] == 0) {
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr;
@@ -652,7 +654,7 @@ static int resident_clusters(Kernel* kernel, int i, size_t smem) {
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
         cfg.gridDim = dim3(1u << i, 1, 1);
         cfg.blockDim = dim3(kInThreads);
-        cfg.dynamicSmemBytes = smem;
+        cfg.dynamicSmemBytes = kInSmem;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
         if (cudaOccupancyMaxActiveClusters(&k.n[i], kernel, &cfg) != cudaSuccess) {
@@ -669,8 +671,7 @@ static int launch_in_tiles(const AdapterArgs& p, cudaStream_t st) {
     if (!make_byte_map(&x, p.x, 2 * p.K, p.T, 2 * p.ldx, 128, kTileTokens, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_byte_map(&a, p.A, 2 * p.K, static_cast<uint64_t>(p.n) * p.R, 2 * p.K, 128, p.R, CU_TENSOR_MAP_SWIZZLE_128B)) return CQ_ERR_CUDA;
     static thread_local LaunchMemo memo;
-    const size_t smem = in_smem(p.R);
-    if (resident_ctas(k27_adapter_in_tiles<DT>, kInThreads, smem, std::max(in_smem(64), in_smem(kMaxRank)), memo) < 1) return CQ_ERR_CUDA;
+    if (resident_ctas(k27_adapter_in_tiles<DT>, kInThreads, kInSmem, kInSmem, memo) < 1) return CQ_ERR_CUDA;
     // The parts of the contraction, four blocks of 64 or more to each, with which tiles of few adapters end first, as those of prompts do; then, as
     // far as there is room, several clusters a tile, which share out the groups of 128 / R adapters that it may have (a tile with fewer
     // leaves the others idle).
@@ -678,7 +679,7 @@ static int launch_in_tiles(const AdapterArgs& p, cudaStream_t st) {
     const int64_t groups = (std::min<int64_t>(p.n, kTileTokens) + per - 1) / per;
     int64_t parts = 1, turns = 1, least = INT64_MAX;
     for (int i = kMaxParts - 1; i >= 0; --i) {
-        const int64_t n = int64_t(1) << i, room = resident_clusters(k27_adapter_in_tiles<DT>, i, smem);
+        const int64_t n = int64_t(1) << i, room = resident_clusters(k27_adapter_in_tiles<DT>, i);
         if (room < 1) return CQ_ERR_CUDA;
         const int64_t length = (tiles + room - 1) / room * ((blocks + n - 1) / n);
         if ((n > 1 && blocks < 4 * n) || length >= least) continue;
@@ -686,7 +687,7 @@ static int launch_in_tiles(const AdapterArgs& p, cudaStream_t st) {
         parts = n;
         turns = std::max<int64_t>(1, std::min(groups, room / tiles));
     }
-    return launch_ex(k27_adapter_in_tiles<DT>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(tiles), static_cast<unsigned>(turns)), kInThreads, smem, st,
+    return launch_ex(k27_adapter_in_tiles<DT>, dim3(static_cast<unsigned>(parts), static_cast<unsigned>(tiles), static_cast<unsigned>(turns)), kInThreads, kInSmem, st,
                      static_cast<unsigned>(parts), !tuning_no_pdl(), x, a, p, in_stages(p.R));
 }
 int launch_adapter_in_tiles(const AdapterArgs& p, int dtype, cudaStream_t st) {
