@@ -209,6 +209,10 @@ k24_norm_rotate(const RotateArgs p) {
             for (int u = 0; u < kAhead; ++u) {
                 float a[8], b[8];
                 sides<DT, NEAR>(xn[u], yn[u], a, b);
+                if constexpr (NORM) {                           // (first: an element times its weight may leave fp32's range, its norm times that does not)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { a[i] *= f[u]; b[i] *= f[u]; }
+                }
                 if (rotated) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -219,10 +223,6 @@ k24_norm_rotate(const RotateArgs p) {
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) { a[i] *= ca[i]; b[i] *= cb[i]; }
-                }
-                if constexpr (NORM) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) { a[i] *= f[u]; b[i] *= f[u]; }
                 }
                 uint32_t o[8];
 #pragma unroll
