@@ -374,8 +374,9 @@ int cq_kv_attention(const void* Q, int dtype, int64_t q_batch_stride, int64_t q_
  *   out      dense [Tq][Hq][D] of that dtype, 16-byte aligned;  lse  float [Tq][Hq], the logarithm of the softmax's sum; nullable
  * A query that sees no key gets zeros (lse: -infinity).  Rows of out and lse before q_starts[0] and from q_starts[B] on are not written.
  * Keys and values that a query does not see have no effect on its result, infinities and NaN included; an infinity or NaN in a value
- * that it sees makes that channel of its result one (or the other), one in a key its whole row NaN, but for logits of -infinity,
- * which count as not seen.  Logits and sums are fp32 (a logit beyond its range, times log2(e), is infinite); each weight, relative to a
+ * that it sees makes that channel of its result one (or the other), one in a key its whole row NaN, but for logits of -infinity:
+ * such a key has no weight, and a query that sees no other gets zeros (an infinity or NaN in the value of such a key may still make its channel
+ * one for a query that does).  Logits and sums are fp32 (a logit beyond its range, times log2(e), is infinite); each weight, relative to a
  * reference of its row at most 2^8 below the largest so far, is rounded once to the dtype before it meets the values (fp16: after a factor
  * of 2^7).  Logits beyond 2^20 are rounded to fp32 before the reference is taken from them: equal ones have equal weights.
  * softmax_scale lies in [2^-100, 1e30] (CQ_ERR_ALPHA otherwise).  Equal calls give equal bits.

@@ -620,7 +620,7 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = 0.0f;
                 }
-                if (poison && mine)
+                if (poison && mine && sum != 0.0f)              // (0: nothing has weight, the row is zeros)
                     for (int j = from; j < to; ++j) {
                         const uint16_t* v = p.v + (static_cast<int64_t>(it.k0) + j) * p.vt + it.kv * p.vh + q * 32;
 #pragma unroll
