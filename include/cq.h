@@ -350,6 +350,7 @@ int cq_kv_read(const void* k_codes, const void* v_codes, const float* k_scale, c
  * head with an infinity or NaN that it sees makes its result NaN.  Queries times channel factors and probabilities times value
  * scales enter the products as fp16, for CQ_F16 as two such numbers each: an element of the one is off by at most 2^-11 (2^-22) of
  * itself plus 2^-35 of its row's largest, one of the other by 2^-11 (2^-22) of itself plus 2^-29 of its row's largest.
+ * Logits beyond 2^20 are rounded to fp32 before the reference is taken from them: equal ones have equal probabilities.
  * A query that sees no token gets zeros (lse: -infinity).  Tokens of a page number outside the cache are not
  * seen; lens beyond table_width * page_size are cut to it, below 0 they count as 0.  Whatever lies in slots behind a
  * sequence's end has no effect.  softmax_scale lies above 0 (CQ_ERR_ALPHA otherwise).  The result does not depend on what other

@@ -36,6 +36,9 @@
 // 0 times an infinite va is none).  One unit for all rows of a warp, above the largest va, took 2 to 7 % less time (4 x 100003 INT4,
 // 16 rows a head: 114 against 118 us), but lost rows beside a large value that they do not see or give no weight: with 1e30 behind
 // it, a value of 100 read as 0.  Less room above the reference (2^5) makes rows ask more often: 124 us.
+// Beyond 2^20 the last bit of a logit is worth more than a probability may be off by: there logits are rounded before the reference is taken
+// from them.  Such a row has the reference of one that has seen nothing, so that it asks at every token, and its own one in shared memory:
+// the rows near 0, and the path that they take, are as they would be without it.
 #include "cq_adapter.cuh"
 #include "cq_kv.cuh"
 
@@ -50,6 +53,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLeastFac = 1.17549435e-38f;    // 2^-126
 constexpr float kNoRef = -3.402823466e38f;      // the reference of a row that has seen nothing
+constexpr float kFarLogit = 1048576.0f;         // references beyond 2^20 are kept apart (see above)
 constexpr float kMostProb = 1024.0f;            // a probability may be so many times the reference's,
 constexpr float kMostUnits = 61440.0f;          // and a probability times va be so many of its row's units (fp16 ends at 65504);
 constexpr int kPlace = 5;                       // new units put the row's largest between 2^4 and 2^5 of them
@@ -440,10 +444,12 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
             ref[nt][0] = ref[nt][1] = kNoRef;
             l[nt][0] = l[nt][1] = 0.0f;
             unit[nt][0] = unit[nt][1] = 1.0f;
+            if (g8 < 2) s_m[warp][nt * 8 + 2 * r4 + g8] = -INFINITY;            // (references far from 0, until the warps are joined)
 #pragma unroll
             for (int t = 0; t < MT; ++t) o[nt][t][0] = o[nt][t][1] = o[nt][t][2] = o[nt][t][3] = 0.0f;
         }
 
+        __syncwarp();
         for (int n = 0; n < n_units; ++n) {
             if (!dead && !role_wait(&full[stage], round, &s_dead)) {
                 dead = true;                                   // nothing is computed from here on
@@ -576,18 +582,33 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                         for (int e = 0; e < 2; ++e) {
                             const unsigned ask = (asks >> (4 * nt + 2 * e)) & 3u;
                             // whole numbers, so that no bits are lost; `held`: what the row's results are held under, with the new reference
-                            const float next = (ask & 2u) != 0u ? ceilf(top[nt][e]) : ref[nt][e], fall = ref[nt][e] - next;
+                            float* const kept = &s_m[warp][nt * 8 + 2 * r4 + e];
+                            const float was = *kept, base = was == -INFINITY ? ref[nt][e] : was;
+                            const float next = (ask & 2u) != 0u && (was == -INFINITY || !(top[nt][e] - was <= 10.0f)) ? ceilf(top[nt][e]) : base, fall = base - next;
+                            const bool far = next != kNoRef && fabsf(next) >= kFarLogit;
+                            float above = heavy[nt][e] - next;
+                            if (__any_sync(0xFFFFFFFFu, far)) {
+                                float h = -INFINITY;
+#pragma unroll
+                                for (int k = 0; k < 2; ++k)
+                                    if (x[nt][e][k] != -INFINITY) h = fmaxf(h, __fmul_rn(x[nt][e][k], fac[nt][e]) - next + lv[k]);
+                                h = over_tokens(h);
+                                if (far) above = h;
+                            }
+                            __syncwarp();
+                            if (g8 == 0) *kept = far ? next : -INFINITY;
+                            __syncwarp();
                             const int had = static_cast<int>(__float_as_uint(unit[nt][e]) >> 23) - 127;
-                            const float held = static_cast<float>(kPlace - had) + fall, need = floorf(heavy[nt][e] - next) + 1.0f;
+                            const float held = static_cast<float>(kPlace - had) + fall, need = floorf(above) + 1.0f;
                             const int now = ask != 0u ? static_cast<int>(fminf(fmaxf(kPlace - fmaxf(held, need), -116.0f), 110.0f)) : had;
                             const float keep = ex2(fall + static_cast<float>(now - had));
                             unit[nt][e] = pow2i(now);
                             finest = fmaxf(finest, unit[nt][e]);
-                            ref[nt][e] = next;
+                            ref[nt][e] = far ? kNoRef : next;
                             l[nt][e] *= ex2(fall);
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
-                                pr[nt][e][k] = ex2(__fmaf_rn(x[nt][e][k], fac[nt][e], -next));
+                                pr[nt][e][k] = ex2(far ? __fmul_rn(x[nt][e][k], fac[nt][e]) - next : __fmaf_rn(x[nt][e][k], fac[nt][e], -next));
                                 pv[nt][e][k] = x[nt][e][k] == -INFINITY ? 0.0f : pr[nt][e][k] * va[k] * unit[nt][e];
                             }
 #pragma unroll
@@ -682,7 +703,10 @@ k16_kv_attend(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ 
                 l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], 4);
                 l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], 8);
                 l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], 16);
+                const float far = s_m[warp][nt * 8 + 2 * r4 + e];
+                if (far != -INFINITY) ref[nt][e] = far;
                 if (l[nt][e] == 0.0f) ref[nt][e] = -INFINITY;   // has seen nothing
+                __syncwarp();
                 if (g8 == 0) {
                     s_m[warp][nt * 8 + 2 * r4 + e] = ref[nt][e];
                     s_l[warp][nt * 8 + 2 * r4 + e] = l[nt][e];
