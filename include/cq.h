@@ -426,7 +426,8 @@ int cq_norm_rotate(const void* Q, int64_t q_token_stride, int64_t q_head_stride,
  * R is a multiple of 8 up to 128 (pad with zeros), T up to 4194240.  16-byte aligned rows of X and A (of y and out) with K (N) a multiple of 8: fast.
  * A_a X[t] is summed in fp32 and enters the second product as two 16-bit halves relative to the token's largest: off by 2^-16 of itself
  * and 2^-24 of that (fp16; bf16 2^-17 of itself).  The result is fp32 and rounded once.  A token's result depends on no other token's values; its last
- * bits may depend on how many of the 64 neighbouring tokens share its adapter.  Equal calls give equal bits.
+ * bits may depend on T, on which of its neighbours share its adapter, and on the layout (strides, alignment): they choose how the contraction is cut
+ * and added.  So a token's bits can change when a batch grows around it.  Equal calls give equal bits.
  * workspace: device, 256-byte aligned, >= cq_adapter_add_workspace_bytes(T, R); contents undefined after.
  */
 size_t cq_adapter_add_workspace_bytes(int64_t T, int64_t R);

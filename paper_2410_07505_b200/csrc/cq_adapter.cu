@@ -456,6 +456,8 @@ __device__ __forceinline__ void add_rows(const AdapterArgs& p, const float* d, c
 template <int MT> __host__ __device__ constexpr int h_pitch() { return MT * 8 + (MT == 1 ? 0 : MT == 2 ? 24 : 8); }
 
 // SHARE: the block's tokens have their h in shared memory, else each warp takes it from L2.
+// Three blocks an SM for ranks up to 32, although that spills 16 to 100 bytes: 64 x 8192 x 8192 on 64 adapters 20.6 us, 23.6 with two blocks and no
+// spills, 100 x 4096 x 11008 on 40 65.4, 69.2; against it 100 x 2060 x 1003 on 3, rows of y on 2 bytes, 18.8, 17.0.  Ranks above spill 32 to 72.
 template <int MT, int DT, int YT, bool SHARE>
 __global__ void __launch_bounds__(kAdThreads, MT <= 2 ? 3 : 2)
 k26_adapter_out(const AdapterArgs p) {
@@ -595,7 +597,9 @@ static int launch_adapter(const AdapterArgs& p, int y_dtype, cudaStream_t st) {
     const int64_t adapters = std::min<int64_t>(kWindow, std::min<int64_t>(p.n, p.T));
     if (windows > 65535) return CQ_ERR_SHAPE;
     // Parts of the contraction of 512 or more, up to a portable cluster and while the windows' blocks fit twice an SM (one token x 4096: 7.2 us, 11.8
-    // in one part); a block for each adapter of a window while they all fit.
+    // in one part); a block for each adapter of a window up to four an SM, twice as many as are resident: most windows have fewer adapters
+    // than they might, and a block that finds none ends at once (64 tokens on 64 adapters x 8192 x 8192, rank 16: 14.4 us and 20.6 for the second kernel;
+    // 28.2 and 26.4 with two an SM; 100 x 4096 x 11008 on 40: 28.9 and 65.4, 27.3 and 68.8).
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(8, p.K / 512), 2 * sms / windows));
     const int64_t slots = std::max<int64_t>(1, std::min<int64_t>(adapters, 4 * sms / (windows * parts)));
     static thread_local LaunchMemo memo;

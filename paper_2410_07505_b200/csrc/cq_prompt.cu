@@ -164,7 +164,7 @@ __device__ __forceinline__ int pairs_from(const Sequence& s, int tokens2, int x)
 // The items in the order of their work, the longest first: all head groups of a pair of tiles side by side, the pairs of all
 // sequences by the number of their key blocks.  Computed by a whole warp.  A CTA's items come in falling order: the next one is looked for
 // from where the last one was found, and all sequences are counted only where the number of blocks changes (1500 sequences of 64
-// tokens, 32 / 8 heads: 451 us; 2247 where they were counted for every item).
+// tokens, 32 / 8 heads: 410 us of 64 channels, 550 of 128; about 2200 where they were counted for every item).
 struct ItemSearch {
     int level, above, upto;                   // pairs with more than `level` blocks, with `level` or more (at first none has as many)
     int b0, before;                           // a group of 32 sequences, and the pairs with `level` blocks of the sequences before it
@@ -726,8 +726,10 @@ static PromptPlan prompt_plan(int64_t B, int64_t Tq, int64_t Tk, int64_t Hq, int
     r.tokens = kTileRows / r.g;
     r.groups = static_cast<int>(Hq / r.g);
     r.items = (Tq / (2 * r.tokens) + std::min(B, Tq)) * r.groups;        // at most
-    // Items for less than half of the SMs: the keys of each are split, four blocks or more to a part (100 tokens behind 19000, 8 heads of 128: 36 us
-    // with the join, 238 in one part; behind 1000, 16 heads: 22.7, 30.0).
+    // Items for at most half of the SMs: the keys of each are split, four blocks or more to a part (100 tokens behind 19000, 8 heads of 128: 36 us
+    // with the join, 238 in one part; behind 1000, 16 heads: 22.7, 30.0).  More items stay whole: two parts of each of 128 on 148 SMs are two
+    // rounds and a join (1000 tokens behind 19011, 32 heads of 64: 257 us, 245 whole; 32 / 8 of 128 301, 274; 900 behind 3100 87, 66); of 96 they
+    // gain only where keys are very many (640 tokens behind 19360, 32 heads of 64: 200, 250; behind 3360 61, 58).
     int64_t splits = r.items > 0 ? sm_count() / r.items : 1;
     splits = std::min(splits, Tk / std::max<int64_t>(B, 1) / (4 * kKeys));
     r.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(splits, kMaxSplits)));
