@@ -555,6 +555,7 @@ k22_prompt(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                         for (int i = 0; i < 128; ++i) x[i >> 5][i & 31] = (__fmul_rn(x[i >> 5][i & 31], p.c) - far + kBias) * back;
                     }
                     sum *= keep;
+                    __syncwarp();                               // (the accesses to tensor memory below are the whole warp's)
                     for (int q = 0; q < (j > jb ? D / 16 : 0); ++q) {
                         float o[16];
                         tmem_ld16(at_o + q * 16, o);
